@@ -400,6 +400,72 @@ onecomp_status onecomp_jointq_refine(const void* W, onecomp_dtype w_dtype, int64
                                      void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t onecomp_jointq_workspace_bytes(int64_t d_out, int64_t d_in, int group_size);
 
+/* ---- The block around the linear layers --------------------------------------------------------------------------
+ * What runs between a block's linear layers: it produces the activations X that the Gram accumulation takes (calibration
+ * passes through the preceding layers, Sec. 2.5) and, with its gradients, tunes what stays in floating point beside
+ * quantized weights (block-wise compensation: gradients clipped to a global norm).
+ */
+
+/* A tensor of packed tokens, [token, head, dim]: strides in elements, dim dense.  Slices of one projection's output, and
+ * [head, token, dim] layouts, are given by their strides.  The base address, token_stride and head_stride are multiples of
+ * 16 bytes; token_stride is at most 2^22. */
+typedef struct {
+    void* data;
+    int64_t token_stride;
+    int64_t head_stride;
+} onecomp_heads;
+
+/* Sequences packed one behind the other.  Sequence i has the queries cu_q[i] .. cu_q[i + 1] - 1 and keys from cu_k[i] on, up to
+ * cu_k[i + 1] - 1, or len_k[i] of them (a cache with room behind the sequence).  cu_q[0] = cu_k[0] = 0, non-decreasing.
+ *   causal   query i of a sequence of a queries and b keys sees the keys 0 .. i + b - a (its own token is the last); without
+ *            it, all b.  A query that sees no key has output 0, log-sum-exp -inf and gradient 0.
+ *   max_q, max_k   the longest sequence's lengths.  They choose between launch shapes and say nothing about the results:
+ *            lengths are read from the arrays, cut to the tensors' rows.
+ * Rows behind the last sequence are padding: outputs and gradients there are set to 0 (log-sum-exps to -inf). */
+typedef struct {
+    onecomp_dtype dtype;       /* of q, k, v, out and their gradients */
+    int n_heads, n_kv_heads;   /* n_heads is a multiple of n_kv_heads: head h shares keys and values h / (n_heads / n_kv_heads) */
+    int head_dim;              /* up to 128, a multiple of 8 (bf16) or 4 (fp32) */
+    int n_seqs;
+    int causal;
+    float scale;               /* > 0, finite */
+    int64_t total_q, total_k;  /* rows of q and of k */
+    int64_t max_q, max_k;
+    const int32_t* cu_q;       /* device, n_seqs + 1 */
+    const int32_t* cu_k;       /* device, n_seqs + 1 */
+    const int32_t* len_k;      /* device, n_seqs, or NULL */
+} onecomp_attention_shape;
+
+/*
+ * out_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i . k_j, lse_i = log sum_j exp(s_ij) over the keys that
+ * query i sees: attention over whole prompts, over chunks behind a cache, and of one new token per sequence.  One pass over
+ * the keys with running maximum and sum in fp32; bf16 products are exact and added in fp32, the probabilities are rounded to
+ * bf16 for their product with v, fp32 inputs are multiplied in fp32.  What lies behind a query's last key never reaches its
+ * result, NaN and infinities included.
+ *   out        [total_q, n_heads, head_dim]
+ *   lse        device fp32 [n_heads, total_q], or NULL (it is wanted for onecomp_attention_backward)
+ *   workspace  >= onecomp_attention_workspace_bytes(shape) bytes, 256-byte aligned (0 bytes: may be NULL).  Where there are few
+ *              rows the keys are split between workgroups, whose sums meet there, in an order that depends on the sizes alone.
+ */
+onecomp_status onecomp_attention_forward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
+                                         const onecomp_heads* v, const onecomp_heads* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, void* hip_stream);
+size_t onecomp_attention_workspace_bytes(const onecomp_attention_shape* shape);
+
+/*
+ * Gradients of onecomp_attention_forward from that of its output, d_out, with out and lse as it left them:
+ *   dv_j = sum_i p_ij d_out_i,  ds_ij = p_ij (d_out_i . v_j - d_out_i . out_i),
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+ * dk and dv summed over the heads of a group.  dq, dk and dv are overwritten (rows of k and v that no query sees get 0).
+ * Sums in fp32, bf16 factors of the products as in the forward call, no atomics: the same inputs give the same bits.
+ *   workspace  >= onecomp_attention_backward_workspace_bytes(shape), 256-byte aligned.
+ */
+onecomp_status onecomp_attention_backward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
+                                          const onecomp_heads* v, const onecomp_heads* out, const float* lse,
+                                          const onecomp_heads* d_out, const onecomp_heads* dq, const onecomp_heads* dk,
+                                          const onecomp_heads* dv, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t onecomp_attention_backward_workspace_bytes(const onecomp_attention_shape* shape);
+
 /* Static, NUL-terminated description of a status code. */
 /*
  * Measurement aid, no part of the method: launches a register-only loop of independent MFMAs (no LDS, no memory

@@ -10,6 +10,8 @@ from .binding import (  # noqa: F401
     load_library,
     onecomp_accumulate_describe,
     onecomp_accumulate_workspace_bytes,
+    onecomp_attention_backward,
+    onecomp_attention_forward,
     onecomp_crossgram_accumulate,
     onecomp_factor_workspace_bytes,
     onecomp_hessian_accumulate,

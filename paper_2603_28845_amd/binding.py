@@ -49,11 +49,28 @@ EXPORTED_SYMBOLS = (
     "onecomp_rtn_sensitivity_static",
     "onecomp_jointq_refine",
     "onecomp_jointq_workspace_bytes",
+    "onecomp_attention_forward",
+    "onecomp_attention_workspace_bytes",
+    "onecomp_attention_backward",
+    "onecomp_attention_backward_workspace_bytes",
     "onecomp_status_string",
     "onecomp_version",
 )
 
 _lib = None
+
+
+class Heads(ctypes.Structure):
+    """onecomp_heads"""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class AttentionShape(ctypes.Structure):
+    """onecomp_attention_shape"""
+    _fields_ = [("dtype", ctypes.c_int), ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("n_seqs", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("total_q", ctypes.c_int64),
+                ("total_k", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_k", ctypes.c_int64), ("cu_q", ctypes.c_void_p),
+                ("cu_k", ctypes.c_void_p), ("len_k", ctypes.c_void_p)]
 
 
 class OnecompError(RuntimeError):
@@ -116,6 +133,15 @@ def load_library() -> ctypes.CDLL:
     lib.onecomp_jointq_refine.restype = i32
     lib.onecomp_jointq_workspace_bytes.argtypes = [i64, i64, i32]
     lib.onecomp_jointq_workspace_bytes.restype = sz
+    shape, heads = ctypes.POINTER(AttentionShape), ctypes.POINTER(Heads)
+    lib.onecomp_attention_forward.argtypes = [shape, heads, heads, heads, heads, vp, vp, sz, vp]
+    lib.onecomp_attention_forward.restype = i32
+    lib.onecomp_attention_workspace_bytes.argtypes = [shape]
+    lib.onecomp_attention_workspace_bytes.restype = sz
+    lib.onecomp_attention_backward.argtypes = [shape, heads, heads, heads, heads, vp, heads, heads, heads, heads, vp, sz, vp]
+    lib.onecomp_attention_backward.restype = i32
+    lib.onecomp_attention_backward_workspace_bytes.argtypes = [shape]
+    lib.onecomp_attention_backward_workspace_bytes.restype = sz
     lib.onecomp_status_string.argtypes = [i32]
     lib.onecomp_status_string.restype = ctypes.c_char_p
     lib.onecomp_version.argtypes = []
@@ -421,3 +447,91 @@ def onecomp_jointq_refine(W: torch.Tensor, H: torch.Tensor, Q_codes: torch.Tenso
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_jointq_refine")
     return {"Q_codes": Q_codes, "scales": scales, "W_hat": W_hat, "objective": objective, "n_moves": n_moves}
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor, shape: Optional[tuple] = None) -> Heads:
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be [tokens, heads, dim]" + (f", here {list(shape)}" if shape is not None else ""))
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on {like.device}")
+    if t.numel() > 0 and t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"rows of {name} must be dense")
+    token = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return Heads(t.data_ptr(), token, t.stride(1) if t.shape[1] > 1 else t.shape[2])
+
+
+def _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k) -> AttentionShape:
+    _dev(q, "q", contiguous=False)
+    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
+        raise ValueError("shapes: q [tokens, heads, dim], k and v [tokens, key heads, dim]")
+    for t, name in ((cu_q, "cu_q"), (cu_k, "cu_k"), (len_k, "len_k")):
+        if t is not None:
+            _dev(t, name, torch.int32)
+            if t.device != q.device:
+                raise ValueError(f"{name} must live on {q.device}")
+    n = cu_q.numel() - 1
+    if n < 0 or cu_k.numel() != n + 1 or (len_k is not None and len_k.numel() != n):
+        raise ValueError("cu_q and cu_k hold one start per sequence and the end, len_k one length per sequence")
+    return AttentionShape(_dtype_code(q), q.shape[1], k.shape[1], q.shape[2], n, int(bool(causal)),
+                          q.shape[2] ** -0.5 if scale is None else float(scale), q.shape[0], k.shape[0], int(max_q), int(max_k),
+                          cu_q.data_ptr(), cu_k.data_ptr(), len_k.data_ptr() if len_k is not None else None)
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[ctypes.c_void_p, int, Optional[torch.Tensor]]:
+    """Address, size and owner of a call's workspace; allocated here where the caller brought none."""
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return ctypes.c_void_p(0), 0, None
+    return _dev(workspace, "workspace", torch.uint8), workspace.numel(), workspace
+
+
+def onecomp_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
+                              max_q: int, max_k: int, causal: bool = True, scale: Optional[float] = None,
+                              len_k: Optional[torch.Tensor] = None, want_lse: bool = True, out: Optional[torch.Tensor] = None,
+                              lse: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Attention of packed sequences.  q: [total_q, heads, dim], k, v: [total_k, key heads, dim] bf16/fp32 (any strides with
+    dense rows); cu_q, cu_k: int32 starts of the sequences and the end; len_k: int32 keys of each, where its room in k holds
+    more; scale: 1 / sqrt(dim) unless given.  Returns (out [total_q, heads, dim], lse [heads, total_q] fp32 or None)."""
+    lib = load_library()
+    s = _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    if lse is not None and tuple(lse.shape) != (q.shape[1], q.shape[0]):
+        raise ValueError("lse must be [heads, total_q]")
+    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_attention_workspace_bytes(ctypes.byref(s))), q.device)
+    rc = lib.onecomp_attention_forward(ctypes.byref(s), ctypes.byref(_heads(q, "q", q)), ctypes.byref(_heads(k, "k", q)),
+                                       ctypes.byref(_heads(v, "v", q, tuple(k.shape))),
+                                       ctypes.byref(_heads(out, "out", q, tuple(q.shape))),
+                                       _dev(lse, "lse", torch.float32) if lse is not None else _ptr(None), ws, ws_bytes, _stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_attention_forward")
+    return out, lse
+
+
+def onecomp_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                               lse: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor, max_q: int, max_k: int,
+                               causal: bool = True, scale: Optional[float] = None, len_k: Optional[torch.Tensor] = None,
+                               dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                               dv: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Returns (dq, dk, dv) from the gradient of the forward call's output and from what that call took and returned."""
+    lib = load_library()
+    s = _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    if tuple(lse.shape) != (q.shape[1], q.shape[0]):
+        raise ValueError("lse must be [heads, total_q]")
+    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_attention_backward_workspace_bytes(ctypes.byref(s))), q.device)
+    rows = [ctypes.byref(_heads(t, name, q, tuple(like.shape))) for t, name, like in
+            ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q), (d_out, "d_out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
+    rc = lib.onecomp_attention_backward(ctypes.byref(s), *rows[:4], _dev(lse, "lse", torch.float32), *rows[4:], ws, ws_bytes, _stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_attention_backward")
+    return dq, dk, dv

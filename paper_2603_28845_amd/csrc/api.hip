@@ -1,5 +1,7 @@
 // extern "C" boundary: argument checks, then dispatch to the kernel launchers.  See include/onecomp.h.
 #include "common.hpp"
+#include "attention.hpp"
+#include <cmath>
 #include <dlfcn.h>
 #include <cstdlib>
 
@@ -40,6 +42,51 @@ struct ApiRange {
     ApiRange(const ApiRange&) = delete;
     ApiRange& operator=(const ApiRange&) = delete;
 };
+
+// ONECOMP_OK if a shape can be worked on; what its arrays hold is the kernels' business
+onecomp_status check_attention(const onecomp_attention_shape* s) {
+    if (!s) return ONECOMP_ERR_INVALID_ARG;
+    if (s->dtype != ONECOMP_F32 && s->dtype != ONECOMP_BF16) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->n_heads <= 0 || s->n_kv_heads <= 0 || s->head_dim <= 0 || s->n_seqs < 0 || s->n_heads % s->n_kv_heads != 0)
+        return ONECOMP_ERR_INVALID_ARG;
+    if (s->head_dim > 128 || s->head_dim % (s->dtype == ONECOMP_BF16 ? 8 : 4) != 0 || s->n_heads > (1 << 16)) return ONECOMP_ERR_UNSUPPORTED;
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return ONECOMP_ERR_INVALID_ARG;
+    const int64_t most = (int64_t(1) << 31) - 4096;
+    if (s->total_q < 0 || s->total_k < 0 || s->max_q < 0 || s->max_k < 0 || s->total_q > most || s->total_k > most || s->n_seqs > (1 << 24))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (!s->cu_q || !s->cu_k) return ONECOMP_ERR_INVALID_ARG;
+    return ONECOMP_OK;
+}
+
+bool check_heads(const onecomp_attention_shape* s, const onecomp_heads* h, int64_t rows) {
+    if (!h) return false;
+    if (rows == 0) return true;
+    const int64_t esz = s->dtype == ONECOMP_BF16 ? 2 : 4;
+    return h->data && aligned(h->data, 16) && h->token_stride >= s->head_dim && h->token_stride <= (1 << 22) && h->head_stride >= 0 &&
+           h->head_stride <= (int64_t(1) << 40) && (h->token_stride * esz) % 16 == 0 && (h->head_stride * esz) % 16 == 0;
+}
+
+attn::View view(const onecomp_heads* h) { return attn::View{h->data, h->token_stride, h->head_stride}; }
+
+attn::Params attention_params(const onecomp_attention_shape* s) {
+    attn::Params P{};
+    P.cu_q = s->cu_q;
+    P.cu_k = s->cu_k;
+    P.len_k = s->len_k;
+    P.total_q = s->total_q;
+    P.total_k = s->total_k;
+    P.n_seqs = s->n_seqs;
+    P.heads = s->n_heads;
+    P.kv_heads = s->n_kv_heads;
+    P.group = s->n_heads / s->n_kv_heads;
+    P.dim = s->head_dim;
+    P.causal = s->causal != 0;
+    P.scale = s->scale;
+    P.c = s->scale * attn::LOG2E;
+    P.max_q = s->max_q;
+    P.max_k = s->max_k;
+    return P;
+}
 }  // namespace
 
 #define ONECOMP_API __attribute__((visibility("default")))
@@ -292,6 +339,63 @@ ONECOMP_API onecomp_status onecomp_mfma_rate_probe(int kind, int waves_per_simd,
     const ApiRange range("onecomp_mfma_rate_probe");
     return mfma_rate_probe(kind, waves_per_simd, random_operands, iters, sink, flops_out,
                            static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_attention_workspace_bytes(const onecomp_attention_shape* shape) {
+    if (check_attention(shape) != ONECOMP_OK) return 0;
+    return attn::forward_workspace_bytes(attention_params(shape));
+}
+
+ONECOMP_API onecomp_status onecomp_attention_forward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
+                                                     const onecomp_heads* v, const onecomp_heads* out, float* lse, void* workspace,
+                                                     size_t workspace_bytes, void* hip_stream) {
+    const ApiRange range("onecomp_attention_forward");
+    if (const onecomp_status st = check_attention(shape)) return st;
+    if (!check_heads(shape, q, shape->total_q) || !check_heads(shape, out, shape->total_q) || !check_heads(shape, k, shape->total_k) ||
+        !check_heads(shape, v, shape->total_k) || !aligned(lse, 4))
+        return ONECOMP_ERR_INVALID_ARG;
+    attn::Params P = attention_params(shape);
+    const size_t need = attn::forward_workspace_bytes(P);
+    if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
+    if (P.total_q == 0) return ONECOMP_OK;
+    P.q = view(q);
+    P.k = view(k);
+    P.v = view(v);
+    P.o = view(out);
+    P.lse = lse;
+    P.part = static_cast<float*>(workspace);
+    return attn::forward_run(shape->dtype, P, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_attention_backward_workspace_bytes(const onecomp_attention_shape* shape) {
+    if (check_attention(shape) != ONECOMP_OK) return 0;
+    return attn::backward_workspace_bytes(attention_params(shape));
+}
+
+ONECOMP_API onecomp_status onecomp_attention_backward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
+                                                      const onecomp_heads* v, const onecomp_heads* out, const float* lse,
+                                                      const onecomp_heads* d_out, const onecomp_heads* dq, const onecomp_heads* dk,
+                                                      const onecomp_heads* dv, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const ApiRange range("onecomp_attention_backward");
+    if (const onecomp_status st = check_attention(shape)) return st;
+    if (!check_heads(shape, q, shape->total_q) || !check_heads(shape, out, shape->total_q) || !check_heads(shape, d_out, shape->total_q) ||
+        !check_heads(shape, dq, shape->total_q) || !check_heads(shape, k, shape->total_k) || !check_heads(shape, v, shape->total_k) ||
+        !check_heads(shape, dk, shape->total_k) || !check_heads(shape, dv, shape->total_k) || (!lse && shape->total_q) || !aligned(lse, 4))
+        return ONECOMP_ERR_INVALID_ARG;
+    attn::Params P = attention_params(shape);
+    const size_t need = attn::backward_workspace_bytes(P);
+    if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
+    P.q = view(q);
+    P.k = view(k);
+    P.v = view(v);
+    P.o = view(out);
+    P.d_o = view(d_out);
+    P.dq = view(dq);
+    P.dk = view(dk);
+    P.dv = view(dv);
+    P.lse = const_cast<float*>(lse);
+    P.aux = static_cast<float*>(workspace);
+    return attn::backward_run(shape->dtype, P, static_cast<hipStream_t>(hip_stream));
 }
 
 ONECOMP_API const char* onecomp_status_string(onecomp_status status) {

@@ -1,0 +1,368 @@
+// Shared device code of the attention kernels: which sequence and tile a workgroup has, tiles on their way to LDS, and the
+// two products that every kernel is made of.
+//
+// All scores live in registers in the layout of a 32 x 32 MFMA accumulator: lane l holds column l % 32 and the rows
+// 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15.  The sum over the rows that follows (probabilities times values, and its
+// likes in the gradients) takes these registers as its right operand as they are: a product's inner index may run in any
+// order, so the left operand is read from LDS in the order 0..3, 8..11 (lanes 0..31) and 4..7, 12..15 (lanes 32..63) and no
+// score ever moves between lanes.
+#pragma once
+#include "common.hpp"
+
+namespace onecomp {
+namespace attn {
+
+// One tensor of packed rows: [token, head, dim], the last dense.
+struct View {
+    const void* p;
+    int64_t token, head;   // strides in elements
+};
+
+struct Params {
+    View q, k, v, o;       // o: output of the forward call, input of the gradients
+    View d_o, dq, dk, dv;
+    float* lse;            // [heads, total_q], may be null in the forward call
+    float* aux;            // scratch of the gradients: [2, heads, total_q], log-sum-exps in powers of two and d_out . out
+    float* part;           // scratch of the split forward call
+    const int32_t *cu_q, *cu_k, *len_k;
+    int64_t total_q, total_k;
+    int n_seqs, heads, kv_heads, group, dim, causal;
+    int splits, run;       // few rows: runs of keys and the keys of a run; splits = 0: whole prompts
+    int64_t max_q, max_k;
+    float scale, c;        // c = scale log2(e): probabilities are powers of two
+};
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// ---- element types ------------------------------------------------------------------------------------------------------
+// DT: head dimension in units of 32, rounded up (columns behind the head dimension are zeros in LDS).
+struct Bf16 {
+    typedef uint16_t T;
+    static constexpr int PER_CHUNK = 8;          // elements of a 16-byte chunk
+    typedef bf16x8 Row;                          // a chunk as an operand whose inner index is the head dimension
+    typedef bf16x8 Score;                        // eight score registers as a right operand
+    static __device__ __forceinline__ Score pack(const float* s) {
+        bf16x8 r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = static_cast<__bf16>(s[i]);
+        return r;
+    }
+    static __device__ __forceinline__ float16v mma(Row a, Row b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float to_float(T x) { return __uint_as_float(uint32_t(x) << 16); }
+};
+struct F32 {
+    typedef float T;
+    static constexpr int PER_CHUNK = 4;
+    typedef float4v Row;
+    struct Score { float s[8]; };
+    static __device__ __forceinline__ Score pack(const float* s) {
+        Score r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.s[i] = s[i];
+        return r;
+    }
+    static __device__ __forceinline__ float16v mma(Row a, Row b, float16v c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ float to_float(T x) { return x; }
+};
+
+// A tile of ROWS rows in LDS.  Rows are PITCH bytes, a power of two; the 16-byte chunk c of row r lies at c ^ swizzle(r), so
+// that the 32 rows of one chunk, and the four rows of a transposed read, spread over the banks.
+template <class E, int DT>
+struct Tile {
+    static constexpr int ESZ = int(sizeof(typename E::T));
+    static constexpr int PITCH = (DT == 3 ? 128 : 32 * DT) * ESZ;
+    static constexpr int CHUNKS = PITCH / 16;                     // of a row
+    static constexpr int STEPS = 32 * DT * ESZ / 32;              // pairs of chunks that hold data: inner steps of a row product
+    static __device__ __forceinline__ int swizzle(int r) {
+        if (CHUNKS >= 16) return ((r & 7) << 1) | ((r >> 3) & 1);
+        if (CHUNKS == 8) return ((r & 3) << 1) | ((r >> 2) & 1);
+        return ((r & 1) << 1) | ((r >> 1) & 1);
+    }
+    static constexpr int bytes(int rows) { return rows * PITCH; }
+};
+
+// What one thread needs to bring its part of ROWS rows from memory to LDS, WAVES waves sharing the work.
+template <class E, int DT, int ROWS, int WAVES>
+struct Loader {
+    typedef attn::Tile<E, DT> T;
+    static constexpr int LOADS = T::bytes(ROWS) / 1024;           // wave-wide loads of 64 chunks
+    static constexpr int MINE = (LOADS + WAVES - 1) / WAVES;
+    uint32_t off[MINE];
+    uint32_t row_bytes, dim_bytes;
+    __device__ __forceinline__ void init(int wave, int lane, int64_t token_stride, int dim) {
+        row_bytes = uint32_t(token_stride) * T::ESZ;
+        dim_bytes = uint32_t(dim) * T::ESZ;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int at = (wave + i * WAVES) * 64 + lane, r = at / T::CHUNKS;
+            const uint32_t chunk = uint32_t((at % T::CHUNKS) ^ T::swizzle(r)) * 16u;
+            off[i] = chunk < dim_bytes ? uint32_t(r) * row_bytes + chunk : LDS_DMA_OOB;
+        }
+    }
+    // first: address of the tile's first row (wave-uniform); rows behind `valid` and columns behind the head dimension
+    // become zeros, whatever lies there
+    __device__ __forceinline__ void load(uint32_t lds, const char* first, int valid, int wave) const {
+        valid = valid < 0 ? 0 : valid > ROWS ? ROWS : valid;
+        const uint32_t range = valid == 0 ? 0u : uint32_t(valid - 1) * row_bytes + dim_bytes;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, int(range), 0x00020000);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i)
+            if (LOADS % WAVES == 0 || wave + i * WAVES < LOADS) lds_load16(lds + uint32_t(wave + i * WAVES) * 1024u, off[i], rsrc);
+    }
+};
+
+// Reads of a tile by one lane, as left operands.
+template <class E, int DT>
+struct Reader {
+    typedef attn::Tile<E, DT> T;
+    int row, tr;                                                  // byte offsets of this lane in a tile
+    __device__ __forceinline__ void init(int lane) {
+        const int half = lane >> 5, r = lane & 31;
+        row = r * T::PITCH + ((half ^ T::swizzle(r)) << 4);
+        if (sizeof(typename E::T) == 2) {
+            // transposed: inside 16 lanes, lane 4 k + c points at four columns of row k and lane i receives column i of rows 0..3
+            const int k = ((lane & 15) >> 2) + 4 * half;
+            tr = k * T::PITCH + (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ T::swizzle(k)) << 4) + (lane & 1) * 8;
+        } else {
+            tr = 4 * half * T::PITCH + ((((lane & 31) >> 2) ^ T::swizzle(4 * half)) << 4) + (lane & 3) * 4;
+        }
+    }
+    // rows 32 block .. + 31, inner step s: chunk 2 s (lanes 0..31) and 2 s + 1
+    __device__ __forceinline__ typename E::Row rows(const char* tile, int block, int s) const {
+        return *reinterpret_cast<const typename E::Row*>(tile + block * 32 * T::PITCH + (row ^ (s << 5)));
+    }
+};
+
+// acc[col][.] += sum over the 16 rows from 16 step of tile[row][32 n + m] p[row]: m is the accumulator's row, p the
+// probabilities of these rows
+template <int DT>
+__device__ __forceinline__ float16v mma_t(const Reader<Bf16, DT>& rd, const char* tile, int step, int n, const Bf16::Score& p, float16v acc) {
+    typedef Tile<Bf16, DT> T;
+    const char* a = tile + step * 16 * T::PITCH;
+    // rows 8 further on: the swizzle's lowest bit for rows of 256 bytes, none otherwise
+    const int far = T::CHUNKS >= 16 ? 16 : 0;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + (rd.tr ^ (n << 6))));
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 8 * T::PITCH + (rd.tr ^ (n << 6) ^ far)));
+    return Bf16::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), p, acc);
+}
+template <int DT>
+__device__ __forceinline__ float16v mma_t(const Reader<F32, DT>& rd, const char* tile, int step, int n, const F32::Score& p, float16v acc) {
+    typedef Tile<F32, DT> T;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = step * 16 + (i >> 2) * 8 + (i & 3);          // and r + 4 in lanes 32..63
+        const int sw = T::swizzle(r) << 4;                         // swizzle(r + 4) = swizzle(r) ^ swizzle(4) for r % 8 < 4
+        const float a = *reinterpret_cast<const float*>(tile + r * T::PITCH + (rd.tr ^ sw ^ (n << 7)));
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.s[i], acc, 0, 0, 0);
+    }
+    return acc;
+}
+
+// ---- sequences ----------------------------------------------------------------------------------------------------------
+struct Seq {
+    int64_t q0, k0;        // first rows
+    int nq, nk;            // lengths
+    int room;              // rows of k that belong to the sequence, nk of them in use
+    int shift;             // query i sees keys 0 .. i + shift (causal)
+};
+
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// Rows from `first` on that belong to sequence i.  Behind the last sequence comes one of all rows that are left: padding,
+// whose queries see no keys and whose keys no query sees.
+__device__ __forceinline__ int rows_of(const int32_t* cu, int64_t total, int n_seqs, int i, int64_t& first) {
+    first = clamp64(cu[i], 0, total);
+    return int((i < n_seqs ? clamp64(cu[i + 1], first, total) : total) - first);
+}
+
+// Sequence i; what the arrays say is cut to the tensors' rows.  Wave-uniform.
+__device__ __forceinline__ Seq sequence(const Params& P, int i) {
+    Seq s;
+    int64_t q0, k0;
+    s.nq = __builtin_amdgcn_readfirstlane(rows_of(P.cu_q, P.total_q, P.n_seqs, i, q0));
+    int nk = rows_of(P.cu_k, P.total_k, P.n_seqs, i, k0);
+    s.room = __builtin_amdgcn_readfirstlane(nk);
+    if (i == P.n_seqs) nk = 0;
+    else if (P.len_k) nk = int(clamp64(P.len_k[i], 0, nk));
+    s.nk = __builtin_amdgcn_readfirstlane(nk);
+    s.q0 = __builtin_amdgcn_readfirstlane(int(q0));
+    s.k0 = __builtin_amdgcn_readfirstlane(int(k0));
+    s.shift = s.nk - s.nq;
+    return s;
+}
+
+// The t-th tile of `size` rows of all sequences: false if there are fewer.  `mul` rows stand for each row of cu (heads of a
+// group that are packed into rows).  Of up to 63 sequences the tiles come by their number x in the sequence, the largest
+// first and at the same x by sequence: x + 1 tiles of keys lie before a causal prompt's tile x, so that long work starts
+// early and the last workgroups are short (32 x 2048 tokens: see the forward kernel).  Of more, one sequence after the other,
+// each from its largest x down: counting by number would read the array many times.  Every lane of a wave takes part and
+// gets the same answer.
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int64_t total, int n_seqs, int mul, int size, int t, int& seq, int& x, int& tiles) {
+    const int lane = threadIdx.x & 63;
+    int done = 0;
+    for (int base = 0; base <= n_seqs; base += 64) {
+        int count = 0;
+        int64_t first;
+        if (base + lane <= n_seqs) count = int((int64_t(rows_of(cu, total, n_seqs, base + lane, first)) * mul + size - 1) / size);
+        int mine = count;                                         // tiles of this lane's sequence among those looked at
+        if (n_seqs < 64) {
+            int lo = 0, hi = count;                               // the largest x of which t + 1 tiles are at least x
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) hi = max(hi, __shfl_xor(hi, o, 64));
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                int n = max(0, count - mid);
+#pragma unroll
+                for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+                if (n > t) lo = mid; else hi = mid;
+            }
+            int n = max(0, count - lo - 1);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+            done = n;                                             // tiles with a larger number
+            mine = count > lo ? 1 : 0;
+            x = __builtin_amdgcn_readfirstlane(lo);
+        }
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += v;
+        }
+        const unsigned long long past = __ballot(done + upto > t);
+        if (past) {
+            const int who = __ffsll(past) - 1;
+            seq = __builtin_amdgcn_readfirstlane(base + who);
+            tiles = __builtin_amdgcn_readfirstlane(__shfl(count, who, 64));
+            if (n_seqs >= 64) x = tiles - 1 - __builtin_amdgcn_readfirstlane(t - done - __shfl(upto - mine, who, 64));
+            return x >= 0 && x < tiles;                           // sums of starts that make no sense may have wrapped
+        }
+        done += __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
+    }
+    return false;
+}
+
+// Head of the i-th of `heads` workgroups that have the same rows.  Workgroups go round the eight XCDs one by one; the heads
+// of a group, which read the same keys and values, come 8 apart where there are 8 groups, and so share an L2.
+__device__ __forceinline__ int head_at(const Params& P, int i) { return (i % P.kv_heads) * P.group + i / P.kv_heads; }
+
+template <class E>
+__device__ __forceinline__ const char* at(const View& v, int64_t row, int head) {
+    return reinterpret_cast<const char*>(v.p) + (row * v.token + int64_t(head) * v.head) * int64_t(sizeof(typename E::T));
+}
+
+// the other half's value of the same column
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+__device__ __forceinline__ float16v zero16() {
+    float16v z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    return z;
+}
+
+// rows of an accumulator that a lane holds: row(r) = 8 (r / 4) + 4 half + r % 4
+__device__ __forceinline__ int acc_row(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
+
+// acc (32 columns of the head dimension from 32 n, in rows; one token per lane) times f, to row[..] of a tensor, cut at dim
+template <class E>
+__device__ __forceinline__ void store_column(char* row, const float16v& acc, float f, int n, int dim, int half) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int d = 32 * n + 8 * g + 4 * half;
+        if (d < dim) {
+            if (sizeof(typename E::T) == 2) {
+                short4v x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(short, static_cast<__bf16>(acc[4 * g + i] * f));
+                *reinterpret_cast<short4v*>(row + d * 2) = x;
+            } else {
+                float4v x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = acc[4 * g + i] * f;
+                *reinterpret_cast<float4v*>(row + d * 4) = x;
+            }
+        }
+    }
+}
+
+// A token's row as right operands (lane: token l % 32)
+template <class E, int DT>
+struct Operand {
+    static constexpr int STEPS = Tile<E, DT>::STEPS;
+    typename E::Row x[STEPS];
+    // straight from memory; zeros where the token is not there
+    __device__ __forceinline__ void load(const char* row, bool there, int dim, int half) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            typename E::Row z;
+#pragma unroll
+            for (int i = 0; i < E::PER_CHUNK; ++i) z[i] = 0;
+            x[s] = z;
+            if (there && (2 * s + half) * E::PER_CHUNK < dim) x[s] = *reinterpret_cast<const typename E::Row*>(row + (2 * s + half) * 16);
+        }
+    }
+};
+
+// ---- results that are not finite ------------------------------------------------------------------------------------------
+// A score that a query must not see has probability 0, but 0 times a value that is infinite or no number is no number.  Tiles
+// behind a sequence's end hold zeros, so this can only come from later tokens of the query's own prompt.  The kernels look at
+// their sums once, at the end, and where one is not finite they form it again here, term by term, over the seen pairs alone:
+// nothing in the ordinary case, and slow where numbers have broken down already.
+template <class E>
+__device__ __forceinline__ float dot_rows(const char* a, const char* b, int dim) {
+    float x = 0.f;
+    for (int d = 0; d < dim; ++d)
+        x = fmaf(E::to_float(reinterpret_cast<const typename E::T*>(a)[d]), E::to_float(reinterpret_cast<const typename E::T*>(b)[d]), x);
+    return x;
+}
+
+// sum[e] += f v[lane + 64 e] for the lanes' columns of one row
+template <class E>
+__device__ __forceinline__ void add_row(float (&sum)[2], float f, const char* row, int dim, int lane) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (lane + 64 * e < dim) sum[e] = fmaf(f, E::to_float(reinterpret_cast<const typename E::T*>(row)[lane + 64 * e]), sum[e]);
+}
+
+template <class E>
+__device__ __forceinline__ void put(char* row, int d, float x) {
+    if (sizeof(typename E::T) == 2) reinterpret_cast<__bf16*>(row)[d] = static_cast<__bf16>(x);
+    else reinterpret_cast<float*>(row)[d] = x;
+}
+
+// true in the lanes whose column of the accumulators holds an entry that is not finite
+template <int DT>
+__device__ __forceinline__ bool not_finite(const float16v (&acc)[DT]) {
+    float x = 0.f;
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x = fmaf(acc[n][r], 0.f, x);
+    return !(x + other_half(x) == 0.f);
+}
+
+// sum_j 2^(c s_j - base) v_j over keys begin .. end - 1 of a row
+template <class E>
+__device__ __forceinline__ void careful_values(float (&sum)[2], const Params& P, const Seq& S, int64_t q_row, int head, int begin, int end, float base, int lane) {
+    const int kv = head / P.group;
+    sum[0] = sum[1] = 0.f;
+    for (int j0 = begin; j0 < end; j0 += 64) {
+        float p = 0.f;
+        if (j0 + lane < end) p = __builtin_amdgcn_exp2f(fmaf(dot_rows<E>(at<E>(P.q, q_row, head), at<E>(P.k, S.k0 + j0 + lane, kv), P.dim), P.c, -base));
+        for (int t = 0; t < 64 && j0 + t < end; ++t) add_row<E>(sum, __shfl(p, t, 64), at<E>(P.v, S.k0 + j0 + t, kv), P.dim, lane);
+    }
+}
+
+size_t forward_workspace_bytes(const Params& P);
+size_t backward_workspace_bytes(const Params& P);
+onecomp_status forward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);
+onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);
+
+}  // namespace attn
+}  // namespace onecomp

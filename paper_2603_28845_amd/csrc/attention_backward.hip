@@ -1,0 +1,315 @@
+// Gradients of the attention of packed sequences, in two kernels: one with the queries in lanes (dq, and the per-query numbers
+// that both need), one with the keys in lanes (dk and dv).  Each forms the scores and the probabilities' gradients anew, seven
+// products where the definition has five, and in return no sum of one workgroup depends on another's: no atomics, no partial
+// gradients in memory.
+#include "attention.hpp"
+
+namespace onecomp {
+namespace attn {
+namespace {
+
+template <class E>
+constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1;            // blocks of 32 rows in a tile
+
+// One pair's probability and its gradient, from memory.
+struct Pair {
+    float p, ds;
+};
+template <class E>
+__device__ __forceinline__ Pair score_grad(const Params& P, int64_t q_row, int head, int64_t k_row, float lse, float delta) {
+    const int kv = head / P.group;
+    const float s = dot_rows<E>(at<E>(P.q, q_row, head), at<E>(P.k, k_row, kv), P.dim);
+    const float dp = dot_rows<E>(at<E>(P.d_o, q_row, head), at<E>(P.v, k_row, kv), P.dim);
+    const float p = __builtin_amdgcn_exp2f(fmaf(s, P.c, -lse));
+    return {p, p * (dp - delta)};
+}
+
+// dq_i = scale sum_j ds_ij k_j for WAVES x 32 queries of one head.  Also leaves lse log2(e) and delta_i = d_out_i . out_i in
+// scratch for the other kernel.
+template <class E, int DT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void grad_q_kernel(const Params P) {
+    constexpr int KEYS = 32 * KB<E>;
+    typedef Tile<E, DT> T;
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = head_at(P, int(blockIdx.x) % P.heads), kv = head / P.group;
+    int i, tile, tiles;
+    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.heads, i, tile, tiles)) return;
+    const Seq S = sequence(P, i);
+    const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
+    const bool there = query < S.nq;
+    const int last_q = min(first + WAVES * 32, S.nq) - 1, last_mine = min(mine + 31, S.nq - 1);
+    const int end = P.causal ? max(0, min(S.nk, last_q + 1 + S.shift)) : S.nk;
+    const int end_mine = mine >= S.nq ? 0 : P.causal ? max(0, min(S.nk, last_mine + 1 + S.shift)) : S.nk;
+    const int end_all = P.causal ? min(S.nk, mine + 1 + S.shift) : S.nk;
+    const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
+
+    Loader<E, DT, KEYS, WAVES> lk, lv;
+    lk.init(wave, lane, P.k.token, P.dim);
+    lv.init(wave, lane, P.v.token, P.dim);
+    constexpr int SIZE = T::bytes(KEYS);
+    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds));
+    auto bring = [&](int j, int buf) {
+        lk.load(base + uint32_t(buf) * 2 * SIZE, at<E>(P.k, S.k0 + j, kv), end - j, wave);
+        lv.load(base + uint32_t(buf) * 2 * SIZE + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
+    };
+    if (end > 0) bring(0, 0);
+
+    Operand<E, DT> q, d;
+    q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
+    d.load(at<E>(P.d_o, S.q0 + query, head), there, P.dim, half);
+    float delta = 0.f, lse = 0.f;
+    {
+        Operand<E, DT> o;
+        o.load(at<E>(P.o, S.q0 + query, head), there, P.dim, half);
+#pragma unroll
+        for (int s = 0; s < T::STEPS; ++s)
+#pragma unroll
+            for (int e = 0; e < E::PER_CHUNK; ++e) delta = fmaf(float(o.x[s][e]), float(d.x[s][e]), delta);
+        delta += other_half(delta);
+        if (there) {
+            const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
+            lse = P.lse[at_q] * LOG2E;
+            if (half == 0) {
+                P.aux[at_q] = lse;
+                P.aux[int64_t(P.heads) * P.total_q + at_q] = delta;
+            }
+        }
+    }
+    Reader<E, DT> rd;
+    rd.init(lane);
+    float16v dq[DT];
+#pragma unroll
+    for (int n = 0; n < DT; ++n) dq[n] = zero16();
+
+    for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        __syncthreads();
+        if (j + KEYS < end) bring(j + KEYS, buf ^ 1);
+        if (j >= end_mine) continue;
+        const char *kt = lds + buf * 2 * SIZE, *vt = kt + SIZE;
+        const bool all_seen = j + KEYS <= end_all;
+#pragma unroll
+        for (int b = 0; b < KB<E>; ++b) {
+            float16v s = zero16(), dp = zero16();
+#pragma unroll
+            for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(kt, b, x), q.x[x], s);
+#pragma unroll
+            for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(vt, b, x), d.x[x], dp);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse)) * (dp[r] - delta);
+            if (!all_seen) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j + 32 * b + acc_row(r, half) > last) s[r] = 0.f;
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float x[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) x[r] = s[8 * t + r];
+                const typename E::Score ds = E::pack(x);
+#pragma unroll
+                for (int n = 0; n < DT; ++n) dq[n] = mma_t<DT>(rd, kt, 2 * b + t, n, ds, dq[n]);
+            }
+        }
+    }
+    const bool broken = there && lse == lse && delta == delta && not_finite(dq);
+    if (there && !broken) {
+        char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
+#pragma unroll
+        for (int n = 0; n < DT; ++n) store_column<E>(row, dq[n], P.scale, n, P.dim, half);
+    }
+    for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
+        const int r = __ffs(rows) - 1, keys = __shfl(last, r, 64) + 1;
+        const float lse_r = __shfl(lse, r, 64), delta_r = __shfl(delta, r, 64);
+        const int64_t token = S.q0 + mine + r;
+        float sum[2] = {0.f, 0.f};
+        for (int j0 = 0; j0 < keys; j0 += 64) {
+            float ds = 0.f;
+            if (j0 + lane < keys)
+                ds = score_grad<E>(P, token, head, S.k0 + j0 + lane, lse_r, delta_r).ds;
+            for (int t = 0; t < 64 && j0 + t < keys; ++t) add_row<E>(sum, __shfl(ds, t, 64), at<E>(P.k, S.k0 + j0 + t, kv), P.dim, lane);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (lane + 64 * e < P.dim) put<E>(const_cast<char*>(at<E>(P.dq, token, head)), lane + 64 * e, sum[e] * P.scale);
+    }
+}
+
+// dv_j = sum_i p_ij d_out_i and dk_j = scale sum_i ds_ij q_i over the queries of all heads of a group, for WAVES x 32 keys.
+template <class E, int DT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void grad_kv_kernel(const Params P) {
+    constexpr int ROWS = 32 * KB<E>;
+    typedef Tile<E, DT> T;
+    constexpr int SIZE = T::bytes(ROWS), BUF = 2 * SIZE + 512;    // queries, d_out, 64 log-sum-exps, 64 deltas
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv = int(blockIdx.x) % P.kv_heads;
+    int i, tile, tiles;
+    if (!find_tile(P.cu_k, P.total_k, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.kv_heads, i, tile, tiles)) return;
+    tile = tiles - 1 - tile;                                      // a causal prompt's first keys are seen by all that follow
+    const Seq S = sequence(P, i);
+    const int first = tile * WAVES * 32, mine = first + wave * 32, key = mine + col;
+    // queries that see any key of the workgroup, of this wave: from `begin` on; from `all` on they see all of the wave's
+    const int begin = first >= S.nk ? S.nq : P.causal ? min(S.nq, max(0, first - S.shift)) / ROWS * ROWS : 0;
+    const int begin_mine = mine >= S.nk ? S.nq : P.causal ? max(0, mine - S.shift) : 0;
+    const int all = P.causal ? mine + 31 - S.shift : 0;
+    const int steps = begin < S.nq ? (S.nq - begin + ROWS - 1) / ROWS : 0, total = steps * P.group;
+
+    Loader<E, DT, ROWS, WAVES> lq, ld;
+    lq.init(wave, lane, P.q.token, P.dim);
+    ld.init(wave, lane, P.d_o.token, P.dim);
+    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds));
+    auto bring = [&](int head, int r, int buf) {
+        const uint32_t to = base + uint32_t(buf) * BUF;
+        lq.load(to, at<E>(P.q, S.q0 + r, head), S.nq - r, wave);
+        ld.load(to + SIZE, at<E>(P.d_o, S.q0 + r, head), S.nq - r, wave);
+        if (wave < 2) {                                           // numbers of rows that are not there: zeros
+            const float* from = P.aux + (int64_t(wave) * P.heads + head) * P.total_q + S.q0 + r;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, min(S.nq - r, ROWS) * 4, 0x00020000);
+            lds_load4(to + 2 * SIZE + uint32_t(wave) * 256u, uint32_t(lane) * 4u, rsrc);
+        }
+    };
+    const int head0 = kv * P.group;
+    if (total > 0) bring(head0, begin, 0);
+
+    Operand<E, DT> k, v;
+    k.load(at<E>(P.k, S.k0 + key, kv), key < S.nk, P.dim, half);
+    v.load(at<E>(P.v, S.k0 + key, kv), key < S.nk, P.dim, half);
+    Reader<E, DT> rd;
+    rd.init(lane);
+    float16v dk[DT], dv[DT];
+#pragma unroll
+    for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
+
+    int head = head0, r0 = begin;
+    for (int step = 0, buf = 0; step < total; ++step, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        __syncthreads();
+        int next_head = head, next = r0 + ROWS;
+        if (next >= S.nq) { next = begin; ++next_head; }
+        if (step + 1 < total) bring(next_head, next, buf ^ 1);
+        if (r0 + ROWS > begin_mine) {
+            const char *qt = lds + buf * BUF, *dt = qt + SIZE;
+            const bool all_seen = r0 >= all;
+#pragma unroll
+            for (int b = 0; b < KB<E>; ++b) {
+                float16v s = zero16(), dp = zero16();
+#pragma unroll
+                for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(qt, b, x), k.x[x], s);
+#pragma unroll
+                for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(dt, b, x), v.x[x], dp);
+                const float* num = reinterpret_cast<const float*>(dt + SIZE) + 32 * b + 4 * half;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4v lse = *reinterpret_cast<const float4v*>(num + 8 * g), delta = *reinterpret_cast<const float4v*>(num + 64 + 8 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 4 * g + e;
+                        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse[e]));
+                        dp[r] = s[r] * (dp[r] - delta[e]);
+                    }
+                }
+                if (!all_seen) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (r0 + 32 * b + acc_row(r, half) + S.shift < key) s[r] = dp[r] = 0.f;
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    float x[8], y[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) { x[r] = s[8 * t + r]; y[r] = dp[8 * t + r]; }
+                    const typename E::Score p = E::pack(x), ds = E::pack(y);
+#pragma unroll
+                    for (int n = 0; n < DT; ++n) dv[n] = mma_t<DT>(rd, dt, 2 * b + t, n, p, dv[n]);
+#pragma unroll
+                    for (int n = 0; n < DT; ++n) dk[n] = mma_t<DT>(rd, qt, 2 * b + t, n, ds, dk[n]);
+                }
+            }
+        }
+        head = next_head;
+        r0 = next;
+    }
+    if (key >= S.nk) {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
+    }
+    const bool broken = not_finite(dk) || not_finite(dv);
+    if (key < S.room && !broken) {
+        char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
+        char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+            store_column<E>(row_k, dk[n], P.scale, n, P.dim, half);
+            store_column<E>(row_v, dv[n], 1.f, n, P.dim, half);
+        }
+    }
+    for (unsigned cols = unsigned(__ballot(broken)); cols; cols &= cols - 1) {
+        const int j = mine + __ffs(cols) - 1, from = P.causal ? max(0, j - S.shift) : 0;
+        float sum_k[2] = {0.f, 0.f}, sum_v[2] = {0.f, 0.f};
+        for (int h = head0; h < head0 + P.group; ++h)
+            for (int i0 = from; i0 < S.nq; i0 += 64) {
+                Pair x = {0.f, 0.f};
+                if (i0 + lane < S.nq) {
+                    const int64_t at_q = int64_t(h) * P.total_q + S.q0 + i0 + lane;
+                    x = score_grad<E>(P, S.q0 + i0 + lane, h, S.k0 + j, P.aux[at_q], P.aux[int64_t(P.heads) * P.total_q + at_q]);
+                }
+                for (int t = 0; t < 64 && i0 + t < S.nq; ++t) {
+                    add_row<E>(sum_v, __shfl(x.p, t, 64), at<E>(P.d_o, S.q0 + i0 + t, h), P.dim, lane);
+                    add_row<E>(sum_k, __shfl(x.ds, t, 64), at<E>(P.q, S.q0 + i0 + t, h), P.dim, lane);
+                }
+            }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (lane + 64 * e < P.dim) {
+                put<E>(const_cast<char*>(at<E>(P.dk, S.k0 + j, kv)), lane + 64 * e, sum_k[e] * P.scale);
+                put<E>(const_cast<char*>(at<E>(P.dv, S.k0 + j, kv)), lane + 64 * e, sum_v[e]);
+            }
+    }
+}
+
+template <class E, int DT, int WQ, int WK>
+onecomp_status launch_backward(const Params& P, hipStream_t stream) {
+    typedef Tile<E, DT> T;
+    constexpr int LDS_Q = 4 * T::bytes(32 * KB<E>), LDS_K = LDS_Q + 1024;
+    static std::atomic<uint64_t> done_q{0}, done_k{0};
+    onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(grad_q_kernel<E, DT, WQ>), LDS_Q, done_q);
+    if (st != ONECOMP_OK) return st;
+    st = allow_dynamic_lds(reinterpret_cast<const void*>(grad_kv_kernel<E, DT, WK>), LDS_K, done_k);
+    if (st != ONECOMP_OK) return st;
+    const int64_t grid_q = (P.total_q / (WQ * 32) + P.n_seqs + 1) * P.heads, grid_k = (P.total_k / (WK * 32) + P.n_seqs + 1) * P.kv_heads;
+    if (grid_q > 0x7fffffff || grid_k > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
+    if (P.total_q > 0) {
+        grad_q_kernel<E, DT, WQ><<<dim3(unsigned(grid_q)), dim3(WQ * 64), LDS_Q, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    if (P.total_k > 0) {
+        grad_kv_kernel<E, DT, WK><<<dim3(unsigned(grid_k)), dim3(WK * 64), LDS_K, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    return ONECOMP_OK;
+}
+
+}  // namespace
+
+size_t backward_workspace_bytes(const Params& P) { return align_up(size_t(P.total_q) * P.heads * 8, 256); }
+
+onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream) {
+    const int dt = (P.dim + 31) / 32;
+    if (dtype == ONECOMP_BF16)
+        return dt == 1   ? launch_backward<Bf16, 1, 8, 8>(P, stream)
+               : dt == 2 ? launch_backward<Bf16, 2, 8, 8>(P, stream)
+               : dt == 3 ? launch_backward<Bf16, 3, 8, 8>(P, stream)
+                         : launch_backward<Bf16, 4, 8, 8>(P, stream);
+    return dt == 1   ? launch_backward<F32, 1, 4, 4>(P, stream)
+           : dt == 2 ? launch_backward<F32, 2, 4, 4>(P, stream)
+           : dt == 3 ? launch_backward<F32, 3, 4, 4>(P, stream)
+                     : launch_backward<F32, 4, 4, 4>(P, stream);
+}
+
+}  // namespace attn
+}  // namespace onecomp

@@ -1,0 +1,390 @@
+// Attention of packed sequences, forward: o_i = sum_j exp(s_ij - lse_i) v_j, s_ij = scale q_i . k_j.
+#include "attention.hpp"
+
+namespace onecomp {
+namespace attn {
+namespace {
+
+// One pass over the keys of 32 queries (one per lane pair): the running maximum and sum of the softmax, and the weighted sum
+// of the values, all fp32.
+template <class E, int DT>
+struct Rows32 {
+    float16v o[DT];        // values' columns in rows, query in the lane
+    float m, l;            // maximum (powers of two) and this half's part of the sum
+
+    __device__ __forceinline__ void init() {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) o[n] = zero16();
+        m = NEG_INF;
+        l = 0.f;
+    }
+
+    // KB blocks of 32 keys in LDS.  last: the last key (counted from the tile's first) that this lane's query sees; all_seen:
+    // every lane sees all of them (wave-uniform).
+    template <int KB>
+    __device__ __forceinline__ void tile(const Reader<E, DT>& rd, const char* kt, const char* vt, const Operand<E, DT>& q, float c, bool all_seen, int last, int half) {
+        float16v s[KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            s[b] = zero16();
+#pragma unroll
+            for (int i = 0; i < Tile<E, DT>::STEPS; ++i) s[b] = E::mma(rd.rows(kt, b, i), q.x[i], s[b]);
+        }
+        if (!all_seen) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * b + acc_row(r, half) > last) s[b][r] = NEG_INF;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = fmaxf(top, other_half(top)) * c;
+        // The sums keep the maximum they began with until a score passes it by 2^8: the probabilities' rounding is relative
+        // and their sum has room for that, and the many products with the new scale fall away.
+        if (__any(top > m + 8.f)) {
+            const float to = fmaxf(m, top), base = to == NEG_INF ? 0.f : to;
+            const float f = __builtin_amdgcn_exp2f(m - base);
+            l *= f;
+#pragma unroll
+            for (int n = 0; n < DT; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[n][r] *= f;
+            m = to;
+        }
+        const float base = m == NEG_INF ? 0.f : m;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -base));
+            float add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int r = 0; r < 16; ++r) add[r & 3] += s[b][r];
+            l += (add[0] + add[1]) + (add[2] + add[3]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float x[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) x[r] = s[b][8 * t + r];
+                const typename E::Score p = E::pack(x);
+#pragma unroll
+                for (int n = 0; n < DT; ++n) o[n] = mma_t<DT>(rd, vt, 2 * b + t, n, p, o[n]);
+            }
+        }
+    }
+};
+
+// ---- whole prompts ------------------------------------------------------------------------------------------------------
+// A workgroup has WAVES x 32 queries of one head and walks through the keys in tiles that all waves share.
+template <class E, int DT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void forward_kernel(const Params P) {
+    constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1, KEYS = 32 * KB;
+    typedef Tile<E, DT> T;
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = head_at(P, int(blockIdx.x) % P.heads);
+    int i, tile, tiles;
+    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.heads, i, tile, tiles)) return;
+    const Seq S = sequence(P, i);
+    const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
+    const bool there = query < S.nq;
+    const int kv = head / P.group;
+
+    // keys that any query of the workgroup, this wave, this lane sees: 0 .. end - 1
+    const int last_q = min(first + WAVES * 32, S.nq) - 1, last_mine = min(mine + 31, S.nq - 1);
+    const int end = P.causal ? max(0, min(S.nk, last_q + 1 + S.shift)) : S.nk;
+    const int end_mine = mine >= S.nq ? 0 : P.causal ? max(0, min(S.nk, last_mine + 1 + S.shift)) : S.nk;
+    const int end_all = P.causal ? min(S.nk, mine + 1 + S.shift) : S.nk;      // keys that every query of the wave sees
+    const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
+
+    Operand<E, DT> q;
+    q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
+
+    Loader<E, DT, KEYS, WAVES> lk, lv;
+    lk.init(wave, lane, P.k.token, P.dim);
+    lv.init(wave, lane, P.v.token, P.dim);
+    Reader<E, DT> rd;
+    rd.init(lane);
+    Rows32<E, DT> acc;
+    acc.init();
+
+    constexpr int SIZE = T::bytes(KEYS);
+    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds));
+    auto bring = [&](int j, int buf) {
+        lk.load(base + uint32_t(buf) * 2 * SIZE, at<E>(P.k, S.k0 + j, kv), end - j, wave);
+        lv.load(base + uint32_t(buf) * 2 * SIZE + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
+    };
+    if (end > 0) bring(0, 0);
+    for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        __syncthreads();
+        if (j + KEYS < end) bring(j + KEYS, buf ^ 1);
+        if (j < end_mine)
+            acc.template tile<KB>(rd, lds + buf * 2 * SIZE, lds + buf * 2 * SIZE + SIZE, q, P.c, j + KEYS <= end_all, last - j, half);
+    }
+    const float l = acc.l + other_half(acc.l), f = l == 0.f ? 0.f : 1.f / l;
+    const bool broken = there && l == l && not_finite(acc.o);
+    if (there && !broken) {
+        char* row = const_cast<char*>(at<E>(P.o, S.q0 + query, head));
+#pragma unroll
+        for (int n = 0; n < DT; ++n) store_column<E>(row, acc.o[n], f, n, P.dim, half);
+    }
+    if (there && P.lse && half == 0)
+        P.lse[int64_t(head) * P.total_q + S.q0 + query] = l == 0.f ? NEG_INF : (acc.m + __builtin_amdgcn_logf(l)) * LN2;
+    for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
+        const int r = __ffs(rows) - 1;
+        const float m = __shfl(acc.m, r, 64), g = __shfl(f, r, 64);
+        const int64_t token = S.q0 + mine + r;
+        float sum[2];
+        careful_values<E>(sum, P, S, token, head, 0, __shfl(last, r, 64) + 1, m == NEG_INF ? 0.f : m, lane);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (lane + 64 * e < P.dim) put<E>(const_cast<char*>(at<E>(P.o, token, head)), lane + 64 * e, sum[e] * g);
+    }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------
+// One or a few new tokens per sequence: the rows of a group's heads lie side by side in the 32 columns (row = query x group +
+// head), so that keys and values are read once for all of them, and the keys are the work that is shared out: a workgroup has
+// a run of them, its waves take tiles of 32 in turn, each through LDS of its own.  Nothing is multiplied that could be the
+// bound; it is bytes in flight, one tile of each wave at a time.
+template <class E, int DT>
+struct Few {
+    typedef attn::Tile<E, DT> T;
+    static constexpr int SIZE = T::bytes(32);
+    static constexpr int WAVES = 4 * SIZE * 4 <= 128 * 1024 ? 4 : 2;   // two tiles of keys and of values per wave
+    static constexpr int LDS = 4 * SIZE * WAVES;
+    static constexpr int COLS = 32 * DT;                               // of a partial sum's row
+    static_assert(LDS >= WAVES * DT * 4096 + WAVES * 256, "the waves' sums meet in the same memory");
+};
+
+// Keys of one workgroup: runs of `run` or, where the host knew of fewer keys than there are, as many as cover them all.
+__device__ __forceinline__ int run_of(const Params& P, int nk) { return max(P.run, (nk + P.splits * 128 - 1) / (P.splits * 128) * 128); }
+
+template <class E, int DT>
+__global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(const Params P) {
+    typedef Few<E, DT> F;
+    extern __shared__ __align__(1024) char lds[];
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv = int(blockIdx.x) % P.kv_heads, split = int(blockIdx.y);
+    int i, tile, tiles;
+    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, P.group, 32, int(blockIdx.x) / P.kv_heads, i, tile, tiles)) return;
+    const Seq S = sequence(P, i);
+    const int row = tile * 32 + col, query = row / P.group, head = kv * P.group + row % P.group;
+    const bool there = query < S.nq;
+    const int last_q = min((tile * 32 + 31) / P.group, S.nq - 1), first_q = tile * 32 / P.group;
+    const int seen = P.causal ? max(0, min(S.nk, last_q + 1 + S.shift)) : S.nk;
+    const int run = run_of(P, S.nk), begin = split * run, end = min(seen, begin + run);
+    const int end_all = P.causal ? min(S.nk, first_q + 1 + S.shift) : S.nk;
+    const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
+
+    Rows32<E, DT> acc;
+    acc.init();
+    if (begin < end) {
+        Operand<E, DT> q;
+        q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
+        Loader<E, DT, 32, 1> lk, lv;
+        lk.init(0, lane, P.k.token, P.dim);
+        lv.init(0, lane, P.v.token, P.dim);
+        Reader<E, DT> rd;
+        rd.init(lane);
+        char* own = lds + wave * 4 * F::SIZE;
+        const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds)) + uint32_t(wave) * 4 * F::SIZE;
+        auto bring = [&](int j, int buf) {
+            lk.load(base + uint32_t(buf) * 2 * F::SIZE, at<E>(P.k, S.k0 + j, kv), end - j, 0);
+            lv.load(base + uint32_t(buf) * 2 * F::SIZE + F::SIZE, at<E>(P.v, S.k0 + j, kv), end - j, 0);
+        };
+        constexpr int STEP = 32 * F::WAVES, LOADS = 2 * Loader<E, DT, 32, 1>::LOADS;
+        int j = begin + wave * 32, buf = 0;
+        if (j < end) bring(j, 0);
+        for (; j < end; j += STEP, buf ^= 1) {
+            // the other tile is free: this wave has read it into registers, and no other reads it
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (j + STEP < end) {
+                bring(j + STEP, buf ^ 1);
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS));
+            } else {
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            }
+            asm volatile("" ::: "memory");
+            acc.template tile<1>(rd, own + buf * 2 * F::SIZE, own + buf * 2 * F::SIZE + F::SIZE, q, P.c, j + 32 <= end_all, last - j, half);
+        }
+    }
+
+    // the waves' sums meet: their maxima and sums, then 32 columns of the values by each wave
+    float l = acc.l + other_half(acc.l);
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(lds);
+    float* tops = sums + F::WAVES * DT * 1024;
+    if (half == 0) {
+        tops[wave * 64 + col] = acc.m;
+        tops[wave * 64 + 32 + col] = l;
+    }
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[((wave * DT + n) * 16 + r) * 64 + lane] = acc.o[n][r];
+    __syncthreads();
+    float top = NEG_INF, f[F::WAVES];
+#pragma unroll
+    for (int w = 0; w < F::WAVES; ++w) top = fmaxf(top, tops[w * 64 + col]);
+    const float zero = top == NEG_INF ? 0.f : top;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < F::WAVES; ++w) {
+        const float m = tops[w * 64 + col];
+        f[w] = __builtin_amdgcn_exp2f(m - zero);
+        l = fmaf(f[w], tops[w * 64 + 32 + col], l);
+    }
+    const int64_t at_row = int64_t(head) * P.total_q + S.q0 + query, rows = int64_t(P.heads) * P.total_q;
+    const bool whole = P.splits == 1;
+    const float out = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    for (int n = wave; n < DT; n += F::WAVES) {
+        float16v o = zero16();
+#pragma unroll
+        for (int w = 0; w < F::WAVES; ++w)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[r] = fmaf(f[w], sums[((w * DT + n) * 16 + r) * 64 + lane], o[r]);
+        float16v one[1] = {o};
+        const bool broken = there && l == l && not_finite(one);
+        if (there && !broken) {
+            if (whole) {
+                store_column<E>(const_cast<char*>(at<E>(P.o, S.q0 + query, head)), o, out, n, P.dim, half);
+            } else {
+                char* to = reinterpret_cast<char*>(P.part + 2 * P.splits * rows + (split * rows + at_row) * F::COLS);
+                store_column<F32>(to, o, 1.f, n, F::COLS, half);
+            }
+        }
+        for (unsigned bad = unsigned(__ballot(broken)); bad; bad &= bad - 1) {
+            const int r = __ffs(bad) - 1;
+            const int64_t token = S.q0 + __shfl(query, r, 64);
+            const int h = __shfl(head, r, 64);
+            const float m = __shfl(zero, r, 64), g = __shfl(out, r, 64);
+            float sum[2];
+            careful_values<E>(sum, P, S, token, h, begin, min(end, __shfl(last, r, 64) + 1), m, lane);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int d = lane + 64 * e;
+                if (d / 32 != n) continue;
+                if (whole && d < P.dim) put<E>(const_cast<char*>(at<E>(P.o, token, h)), d, sum[e] * g);
+                if (!whole) P.part[2 * P.splits * rows + (split * rows + int64_t(h) * P.total_q + token) * F::COLS + d] = sum[e];
+            }
+        }
+    }
+    if (there && wave == 0 && half == 0) {
+        if (!whole) {
+            P.part[2 * (split * rows + at_row)] = top;
+            P.part[2 * (split * rows + at_row) + 1] = l;
+        } else if (P.lse) {
+            P.lse[at_row] = l == 0.f ? NEG_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+        }
+    }
+}
+
+// The runs' sums of one row meet, in their order: one wave per row, a lane per two columns.
+template <class E, int DT>
+__global__ __launch_bounds__(256) void join_kernel(const Params P) {
+    constexpr int COLS = 32 * DT;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = int64_t(P.heads) * P.total_q, row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int head = int(row / P.total_q);
+    const int64_t token = row - int64_t(head) * P.total_q;
+    float top = NEG_INF;
+    for (int s = lane; s < P.splits; s += 64) top = fmaxf(top, P.part[2 * (s * rows + row)]);
+    top = wave_max(top);
+    const float zero = top == NEG_INF ? 0.f : top;
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    const float* sums = P.part + 2 * P.splits * rows;
+    for (int s = 0; s < P.splits; ++s) {
+        const float m = P.part[2 * (s * rows + row)], n = P.part[2 * (s * rows + row) + 1];
+        if (n == 0.f) continue;                                   // a run behind the row's keys: nothing was written for it but this
+        const float f = __builtin_amdgcn_exp2f(m - zero);
+        l = fmaf(f, n, l);
+        const float* from = sums + (s * rows + row) * COLS;
+        if (lane < COLS) o0 = fmaf(f, from[lane], o0);
+        if (DT > 2 && lane + 64 < COLS) o1 = fmaf(f, from[lane + 64], o1);
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    char* to = const_cast<char*>(at<E>(P.o, token, head));
+    if (lane < P.dim) put<E>(to, lane, o0 * f);
+    if (lane + 64 < P.dim) put<E>(to, lane + 64, o1 * f);
+    if (P.lse && lane == 0) P.lse[row] = l == 0.f ? NEG_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+template <class E, int DT, int WAVES>
+onecomp_status launch_forward(const Params& P, hipStream_t stream) {
+    constexpr int KEYS = sizeof(typename E::T) == 2 ? 64 : 32;
+    constexpr int LDS = 4 * Tile<E, DT>::bytes(KEYS);
+    static std::atomic<uint64_t> done{0};
+    const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(forward_kernel<E, DT, WAVES>), LDS, done);
+    if (st != ONECOMP_OK) return st;
+    const int64_t tiles = P.total_q / (WAVES * 32) + P.n_seqs + 1;    // no less than the sequences' tiles together
+    const int64_t grid = tiles * P.heads;
+    if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
+    forward_kernel<E, DT, WAVES><<<dim3(unsigned(grid)), dim3(WAVES * 64), LDS, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
+}
+
+template <class E, int DT>
+onecomp_status launch_few(const Params& P, hipStream_t stream) {
+    typedef Few<E, DT> F;
+    static std::atomic<uint64_t> done{0};
+    const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(few_rows_kernel<E, DT>), F::LDS, done);
+    if (st != ONECOMP_OK) return st;
+    const int64_t grid = (P.total_q * P.group / 32 + P.n_seqs + 1) * P.kv_heads, rows = P.total_q * P.heads;
+    if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
+    few_rows_kernel<E, DT><<<dim3(unsigned(grid), unsigned(P.splits)), dim3(F::WAVES * 64), F::LDS, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    if (P.splits > 1) {
+        join_kernel<E, DT><<<dim3(unsigned((rows + 3) / 4)), dim3(256), 0, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    return ONECOMP_OK;
+}
+
+// How the keys are shared out where there are few rows; splits = 0: whole prompts.
+void plan(Params& P) {
+    P.splits = P.run = 0;
+    if (P.max_q * P.group > 64) return;
+    // runs of keys: enough of them to keep four workgroups per CU busy, none shorter than 256
+    const int64_t all = P.total_k * P.kv_heads;
+    int64_t run = align_up(size_t(ceil_div(all, 1024)), 128);
+    run = run < 256 ? 256 : run;
+    int64_t splits = ceil_div(P.max_k, run);
+    P.splits = int(splits < 1 ? 1 : splits > 256 ? 256 : splits);
+    P.run = int(run > (1 << 30) ? (1 << 30) : run);
+}
+
+template <class E, int DT>
+onecomp_status forward(const Params& P, hipStream_t stream) {
+    return P.splits ? launch_few<E, DT>(P, stream) : launch_forward<E, DT, 8>(P, stream);
+}
+
+}  // namespace
+
+size_t forward_workspace_bytes(const Params& in) {
+    Params P = in;
+    plan(P);
+    if (P.splits < 2) return 0;
+    const size_t cols = size_t(P.dim + 31) / 32 * 32;
+    return align_up(size_t(P.splits) * size_t(P.total_q) * P.heads * (2 + cols) * 4, 256);
+}
+
+onecomp_status forward_run(onecomp_dtype dtype, const Params& in, hipStream_t stream) {
+    Params P = in;
+    plan(P);
+    const int dt = (P.dim + 31) / 32;
+    if (dtype == ONECOMP_BF16)
+        return dt == 1 ? forward<Bf16, 1>(P, stream) : dt == 2 ? forward<Bf16, 2>(P, stream) : dt == 3 ? forward<Bf16, 3>(P, stream) : forward<Bf16, 4>(P, stream);
+    return dt == 1 ? forward<F32, 1>(P, stream) : dt == 2 ? forward<F32, 2>(P, stream) : dt == 3 ? forward<F32, 3>(P, stream) : forward<F32, 4>(P, stream);
+}
+
+}  // namespace attn
+}  // namespace onecomp

@@ -61,6 +61,11 @@ __device__ __forceinline__ void lds_load16(uint32_t lds_byte_addr, uint32_t voff
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :: "s"(lds_byte_addr), "v"(voffset), "s"(rsrc) : "memory", "m0");
 }
+// The same with 4 bytes per lane, to lds_byte_addr + 4 l.
+__device__ __forceinline__ void lds_load4(uint32_t lds_byte_addr, uint32_t voffset, __amdgpu_buffer_rsrc_t rsrc) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :: "s"(lds_byte_addr), "v"(voffset), "s"(rsrc) : "memory", "m0");
+}
 // a buffer offset that is out of range for every descriptor used here
 constexpr uint32_t LDS_DMA_OOB = 0xFFFFFFF0u;
 // s_waitcnt immediate that waits until at most n (< 64) vector memory loads are outstanding and for nothing else
