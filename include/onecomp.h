@@ -466,6 +466,91 @@ onecomp_status onecomp_attention_backward(const onecomp_attention_shape* shape, 
                                           const onecomp_heads* dv, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t onecomp_attention_backward_workspace_bytes(const onecomp_attention_shape* shape);
 
+/* Rows of one tensor: stride in elements between them, entries of a row dense. */
+typedef struct {
+    void* data;
+    int64_t row_stride;
+} onecomp_rows;
+
+typedef enum {
+    ONECOMP_NORM_RMS = 0,      /* x / sqrt(mean(x^2) + eps), times a weight */
+    ONECOMP_NORM_LAYER = 1     /* (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps), times a weight, plus a bias */
+} onecomp_norm;
+
+typedef enum {
+    ONECOMP_GATE_NONE = 0,
+    ONECOMP_GATE_CHANNEL = 1,  /* one factor per channel (w_dtype), the same for all rows */
+    ONECOMP_GATE_ROWS = 2      /* one factor per entry (dtype), as from a gating branch */
+} onecomp_gate;
+
+/* The norms of a block, fused with its gate and residual.  h is the residual stream, y the block's output:
+ *   u = y, or norm(y) with post_weight and post_bias where post_norm is set (the norm behind the block)
+ *   h' = residual_scale h + gate u
+ *   n = norm(h') with weight and bias (the norm in front of the next block: the X of its first linear layers)
+ * Without y (NULL) h' is h, and n = norm(h). */
+typedef struct {
+    onecomp_dtype dtype;       /* of h, y, h', n, a gate per entry, and their gradients */
+    onecomp_dtype w_dtype;     /* of weights, biases, a gate per channel, and their gradients */
+    onecomp_norm kind;
+    onecomp_gate gate_kind;
+    int post_norm;
+    int64_t rows, width;       /* width up to 32768 */
+    float residual_scale;
+    float eps;                 /* >= 0 */
+} onecomp_norm_shape;
+
+/*
+ * Forward.  Arithmetic in fp32 on each entry, rounded once where it is stored (n follows from h' before it is rounded).
+ *   weight, bias, post_weight, post_bias   [width] of w_dtype, NULL: 1 and 0.  post_*: only with post_norm; biases: layer norms only.
+ *   gate    onecomp_rows (row_stride unused for one factor per channel), NULL with ONECOMP_GATE_NONE
+ *   h_out   NULL if not wanted; may be h itself (same stride).  Only with y.
+ *   n       NULL if not wanted; not h_out, not h.
+ * Any address and stride of whole elements will do; whole 16 bytes are best.
+ */
+onecomp_status onecomp_block_norm_forward(const onecomp_norm_shape* shape, const onecomp_rows* h, const onecomp_rows* y, const void* weight,
+                                          const void* bias, const void* post_weight, const void* post_bias, const onecomp_rows* gate,
+                                          const onecomp_rows* h_out, const onecomp_rows* n, void* hip_stream);
+
+/* Gradients that the backward call is asked for: NULL where one is not wanted.  dweight .. dpost_bias and dgate_channel: [width]
+ * of w_dtype, sums over all rows in fp32 in an order that the sizes alone decide, overwritten. */
+typedef struct {
+    const onecomp_rows *dh, *dy, *dgate;
+    void *dweight, *dbias, *dpost_weight, *dpost_bias, *dgate_channel;
+} onecomp_norm_gradients;
+
+/*
+ * Gradients of the forward call from those of n (dn) and of h' (dh_out; what comes back along the residual), either of them NULL
+ * if there is none.  h is h' as the forward call left it (h itself without y).  With G the gradient of h':
+ *   dh = residual_scale G, dgate = G u, du = gate G, dy = du or that of the norm behind the block.
+ * dh may be dh_out, dy may be dn (same strides).
+ *   workspace  >= onecomp_block_norm_workspace_bytes(shape), 256-byte aligned.
+ */
+onecomp_status onecomp_block_norm_backward(const onecomp_norm_shape* shape, const onecomp_rows* dn, const onecomp_rows* dh_out,
+                                           const onecomp_rows* h, const onecomp_rows* y, const void* weight, const void* post_weight,
+                                           const void* post_bias, const onecomp_rows* gate, const onecomp_norm_gradients* out,
+                                           void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t onecomp_block_norm_workspace_bytes(const onecomp_norm_shape* shape);
+
+/* One gradient: numel dense entries; out may be grad itself. */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t numel;
+    onecomp_dtype dtype;
+} onecomp_gradient;
+
+/*
+ * norm = sqrt(sum of all squares) and out = grad min(1, max_norm / (norm + 1e-6)) for n gradients together.  Squares are added in
+ * 64 bits in an order that the sizes alone decide.  A norm that is not finite scales by what the formula gives (0, or NaN).
+ *   grads      host array of n, read before the call returns; addresses aligned to their type
+ *   max_norm   >= 0; infinity: nothing is clipped
+ *   norm       device fp32, or NULL
+ *   workspace  >= onecomp_clip_workspace_bytes(), 256-byte aligned
+ */
+onecomp_status onecomp_clip_gradients(const onecomp_gradient* grads, int n, float max_norm, float* norm, void* workspace,
+                                      size_t workspace_bytes, void* hip_stream);
+size_t onecomp_clip_workspace_bytes(void);
+
 /* Static, NUL-terminated description of a status code. */
 /*
  * Measurement aid, no part of the method: launches a register-only loop of independent MFMAs (no LDS, no memory

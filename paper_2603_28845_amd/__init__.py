@@ -12,6 +12,9 @@ from .binding import (  # noqa: F401
     onecomp_accumulate_workspace_bytes,
     onecomp_attention_backward,
     onecomp_attention_forward,
+    onecomp_block_norm_backward,
+    onecomp_block_norm_forward,
+    onecomp_clip_gradients,
     onecomp_crossgram_accumulate,
     onecomp_factor_workspace_bytes,
     onecomp_hessian_accumulate,

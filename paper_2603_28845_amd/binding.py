@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch  # imported before the library so that both share one HIP runtime
 
@@ -53,6 +53,11 @@ EXPORTED_SYMBOLS = (
     "onecomp_attention_workspace_bytes",
     "onecomp_attention_backward",
     "onecomp_attention_backward_workspace_bytes",
+    "onecomp_block_norm_forward",
+    "onecomp_block_norm_backward",
+    "onecomp_block_norm_workspace_bytes",
+    "onecomp_clip_gradients",
+    "onecomp_clip_workspace_bytes",
     "onecomp_status_string",
     "onecomp_version",
 )
@@ -71,6 +76,30 @@ class AttentionShape(ctypes.Structure):
                 ("n_seqs", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("total_q", ctypes.c_int64),
                 ("total_k", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_k", ctypes.c_int64), ("cu_q", ctypes.c_void_p),
                 ("cu_k", ctypes.c_void_p), ("len_k", ctypes.c_void_p)]
+
+
+class Rows(ctypes.Structure):
+    """onecomp_rows"""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class NormShape(ctypes.Structure):
+    """onecomp_norm_shape"""
+    _fields_ = [("dtype", ctypes.c_int), ("w_dtype", ctypes.c_int), ("kind", ctypes.c_int), ("gate_kind", ctypes.c_int),
+                ("post_norm", ctypes.c_int), ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("residual_scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
+class NormGradients(ctypes.Structure):
+    """onecomp_norm_gradients"""
+    _fields_ = [("dh", ctypes.POINTER(Rows)), ("dy", ctypes.POINTER(Rows)), ("dgate", ctypes.POINTER(Rows)), ("dweight", ctypes.c_void_p),
+                ("dbias", ctypes.c_void_p), ("dpost_weight", ctypes.c_void_p), ("dpost_bias", ctypes.c_void_p),
+                ("dgate_channel", ctypes.c_void_p)]
+
+
+class Gradient(ctypes.Structure):
+    """onecomp_gradient"""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int)]
 
 
 class OnecompError(RuntimeError):
@@ -142,6 +171,18 @@ def load_library() -> ctypes.CDLL:
     lib.onecomp_attention_backward.restype = i32
     lib.onecomp_attention_backward_workspace_bytes.argtypes = [shape]
     lib.onecomp_attention_backward_workspace_bytes.restype = sz
+    rows = ctypes.POINTER(Rows)
+    lib.onecomp_block_norm_forward.argtypes = [ctypes.POINTER(NormShape), rows, rows, vp, vp, vp, vp, rows, rows, rows, vp]
+    lib.onecomp_block_norm_forward.restype = i32
+    lib.onecomp_block_norm_backward.argtypes = [ctypes.POINTER(NormShape), rows, rows, rows, rows, vp, vp, vp, rows,
+                                                ctypes.POINTER(NormGradients), vp, sz, vp]
+    lib.onecomp_block_norm_backward.restype = i32
+    lib.onecomp_block_norm_workspace_bytes.argtypes = [ctypes.POINTER(NormShape)]
+    lib.onecomp_block_norm_workspace_bytes.restype = sz
+    lib.onecomp_clip_gradients.argtypes = [ctypes.POINTER(Gradient), i32, f32, vp, vp, sz, vp]
+    lib.onecomp_clip_gradients.restype = i32
+    lib.onecomp_clip_workspace_bytes.argtypes = []
+    lib.onecomp_clip_workspace_bytes.restype = sz
     lib.onecomp_status_string.argtypes = [i32]
     lib.onecomp_status_string.restype = ctypes.c_char_p
     lib.onecomp_version.argtypes = []
@@ -535,3 +576,146 @@ def onecomp_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Te
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_attention_backward")
     return dq, dk, dv
+
+
+_NORMS = {"rms": 0, "layer": 1}
+_GATES = {"none": 0, "channel": 1, "rows": 2}
+
+
+def _row_view(t: Optional[torch.Tensor], name: str, like: torch.Tensor):
+    """onecomp_rows of a [rows, width] tensor (None stays None)."""
+    if t is None:
+        return None
+    if t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name} must be [rows, width], here {list(like.shape)}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on {like.device}")
+    if t.numel() > 0 and t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError(f"rows of {name} must be dense")
+    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _param(t: Optional[torch.Tensor], name: str, like: torch.Tensor, dtype: torch.dtype) -> ctypes.c_void_p:
+    if t is None:
+        return ctypes.c_void_p(0)
+    if t.numel() != like.shape[1]:
+        raise ValueError(f"{name} must have {like.shape[1]} entries")
+    if t.device != like.device:
+        raise ValueError(f"{name} must live on {like.device}")
+    return _dev(t, name, dtype)
+
+
+def _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm):
+    """(shape, dtype of the parameters, gate as rows or None); params: dict of the weights and biases."""
+    _dev(h, "h", contiguous=False)
+    if h.dim() != 2:
+        raise ValueError("h must be [rows, width]")
+    if kind not in _NORMS:
+        raise ValueError("kind must be 'rms' or 'layer'")
+    channel = gate is not None and gate.dim() == 1
+    given = [t for t in list(params.values()) + ([gate] if channel else []) if t is not None]
+    w_dtype = given[0].dtype if given else h.dtype
+    gate_kind = "none" if gate is None else "channel" if channel else "rows"
+    if post_norm is None:
+        post_norm = params["post_weight"] is not None or params["post_bias"] is not None
+    shape = NormShape(_dtype_code(h), ONECOMP_BF16 if w_dtype == torch.bfloat16 else ONECOMP_F32, _NORMS[kind], _GATES[gate_kind], int(bool(post_norm)),
+                      h.shape[0], h.shape[1], float(residual_scale), float(eps))
+    if channel:
+        gate_rows = Rows(_param(gate, "gate", h, w_dtype).value, 0)
+    else:
+        gate_rows = _row_view(gate, "gate", h)
+    return shape, w_dtype, gate_rows
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def onecomp_block_norm_forward(h: torch.Tensor, y: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                               bias: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None,
+                               post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                               residual_scale: float = 1.0, eps: float = 1e-6, kind: str = "rms", post_norm: Optional[bool] = None,
+                               want_n: bool = True, h_out: Optional[torch.Tensor] = None,
+                               n: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """h' = residual_scale h + gate u with u = y, or norm(y) (post_norm: whether; by default where post_weight or post_bias is
+    given), and n = norm(h').  h, y: [rows, width] bf16/fp32 (rows may be strided); weights, biases: [width] of one dtype; gate:
+    [width] of that dtype or [rows, width].  Without y h' is h.  Returns (h', n); h_out may be h."""
+    lib = load_library()
+    params = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
+    shape, w_dtype, gate_rows = _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm)
+    if y is None:
+        if h_out is not None:
+            raise ValueError("h_out goes with y: without it h' is h")
+    elif h_out is None:
+        h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    if n is None and want_n:
+        n = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    views = [_row_view(t, name, h) for t, name in ((h, "h"), (y, "y"), (h_out, "h_out"), (n, "n"))]
+    rc = lib.onecomp_block_norm_forward(ctypes.byref(shape), _ref(views[0]), _ref(views[1]),
+                                        *(_param(t, name, h, w_dtype) for name, t in params.items()), _ref(gate_rows), _ref(views[2]),
+                                        _ref(views[3]), _stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_block_norm_forward")
+    return (h if y is None else h_out), n
+
+
+def onecomp_block_norm_backward(dn: Optional[torch.Tensor], dh_out: Optional[torch.Tensor], h: torch.Tensor,
+                                y: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                                bias: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None,
+                                post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                                residual_scale: float = 1.0, eps: float = 1e-6, kind: str = "rms", post_norm: Optional[bool] = None,
+                                out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """Gradients of onecomp_block_norm_forward from those of n and of h' (either None if there is none); h is the h' that it
+    returned.  Returns dict(h, y, weight, bias, post_weight, post_bias, gate), None for what was not given; out: optional dict of
+    preallocated tensors of these names."""
+    lib = load_library()
+    params = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
+    shape, w_dtype, gate_rows = _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm)
+    given = dict(params, h=h, y=y, gate=gate)
+    res = {name: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) if out is None else out.get(name)
+           for name, t in given.items()}
+    if dn is None:
+        res["weight"] = res["bias"] = None
+    channel = gate is not None and gate.dim() == 1
+    views = {name: _row_view(t, name, h) for name, t in (("dn", dn), ("dh_out", dh_out), ("h", h), ("y", y), ("dh", res["h"]),
+                                                         ("dy", res["y"]), ("dgate", None if channel else res["gate"]))}
+    grads = NormGradients(*(ctypes.pointer(views[name]) if views[name] is not None else None for name in ("dh", "dy", "dgate")),
+                          *(_param(res[name], "gradient of " + name, h, w_dtype) for name in params),
+                          _param(res["gate"] if channel else None, "gradient of gate", h, w_dtype))
+    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_block_norm_workspace_bytes(ctypes.byref(shape))), h.device)
+    rc = lib.onecomp_block_norm_backward(ctypes.byref(shape), _ref(views["dn"]), _ref(views["dh_out"]), _ref(views["h"]), _ref(views["y"]),
+                                         *(_param(params[name], name, h, w_dtype) for name in ("weight", "post_weight", "post_bias")),
+                                         _ref(gate_rows), ctypes.byref(grads), ws, ws_bytes, _stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_block_norm_backward")
+    return res
+
+
+def onecomp_clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+                           norm: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None) -> Tuple[Sequence[torch.Tensor], torch.Tensor]:
+    """Scales the gradients (dense fp32/bf16 tensors, in any mixture) by min(1, max_norm / (norm + 1e-6)), norm that of all of them
+    together: into `out`, or in place.  Returns (out or grads, norm as a device fp32 scalar)."""
+    lib = load_library()
+    to = grads if out is None else out
+    if len(to) != len(grads):
+        raise ValueError("out must have one tensor per gradient")
+    if not grads and norm is None:
+        raise ValueError("no gradients: pass norm, so that it is known where it belongs")
+    device = norm.device if norm is not None else grads[0].device
+    table = (Gradient * max(1, len(grads)))()
+    for i, (g, o) in enumerate(zip(grads, to)):
+        if o is not g and (o.dtype != g.dtype or o.numel() != g.numel()):
+            raise ValueError(f"out {i} must have the dtype and size of its gradient")
+        if g.device != device or o.device != device:
+            raise ValueError(f"gradient {i} must live on {device}")
+        table[i] = Gradient(_dev(g, f"gradient {i}").value, _dev(o, f"out {i}").value, g.numel(), _dtype_code(g))
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=device)
+    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_clip_workspace_bytes()), device)
+    rc = lib.onecomp_clip_gradients(table, len(grads), float(max_norm), _dev(norm, "norm", torch.float32), ws, ws_bytes, _stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_clip_gradients")
+    return to, norm

@@ -11,7 +11,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libonecomp.so")
 SOURCES = ["api.hip", "gram.hip", "factor.hip", "residue.hip", "sweep.hip", "qep.hip", "sensitivity.hip", "jointq.hip", "probe.hip",
-           "attention_forward.hip", "attention_backward.hip"]
+           "attention_forward.hip", "attention_backward.hip", "norm.hip", "clip.hip"]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,6 +1,7 @@
 // extern "C" boundary: argument checks, then dispatch to the kernel launchers.  See include/onecomp.h.
 #include "common.hpp"
 #include "attention.hpp"
+#include "block.hpp"
 #include <cmath>
 #include <dlfcn.h>
 #include <cstdlib>
@@ -64,6 +65,62 @@ bool check_heads(const onecomp_attention_shape* s, const onecomp_heads* h, int64
     const int64_t esz = s->dtype == ONECOMP_BF16 ? 2 : 4;
     return h->data && aligned(h->data, 16) && h->token_stride >= s->head_dim && h->token_stride <= (1 << 22) && h->head_stride >= 0 &&
            h->head_stride <= (int64_t(1) << 40) && (h->token_stride * esz) % 16 == 0 && (h->head_stride * esz) % 16 == 0;
+}
+
+onecomp_status check_norm(const onecomp_norm_shape* s) {
+    if (!s) return ONECOMP_ERR_INVALID_ARG;
+    if ((s->dtype != ONECOMP_F32 && s->dtype != ONECOMP_BF16) || (s->w_dtype != ONECOMP_F32 && s->w_dtype != ONECOMP_BF16)) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->kind != ONECOMP_NORM_RMS && s->kind != ONECOMP_NORM_LAYER) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->gate_kind != ONECOMP_GATE_NONE && s->gate_kind != ONECOMP_GATE_CHANNEL && s->gate_kind != ONECOMP_GATE_ROWS) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->rows < 0 || s->width <= 0 || s->rows > (int64_t(1) << 31) - 4096 || !(s->eps >= 0.f) || !std::isfinite(s->eps) || !std::isfinite(s->residual_scale))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (s->width > 32768) return ONECOMP_ERR_UNSUPPORTED;
+    return ONECOMP_OK;
+}
+
+// rows of the shape (NULL: fine, nothing is there)
+bool check_rows(const onecomp_norm_shape* s, const onecomp_rows* r) {
+    if (!r) return true;
+    if (s->rows == 0) return true;
+    return r->data && aligned(r->data, s->dtype == ONECOMP_BF16 ? 2 : 4) && r->row_stride >= s->width && r->row_stride <= (int64_t(1) << 31);
+}
+bool check_param(const onecomp_norm_shape* s, const void* p) { return aligned(p, s->w_dtype == ONECOMP_BF16 ? 2 : 4); }
+
+block::Rows rows_of(const onecomp_rows* r) { return r ? block::Rows{r->data, r->row_stride} : block::Rows{nullptr, 0}; }
+
+block::Params norm_params(const onecomp_norm_shape* s) {
+    block::Params P{};
+    P.rows = s->rows;
+    P.width = int(s->width);
+    P.layer = s->kind == ONECOMP_NORM_LAYER;
+    P.post = s->post_norm != 0;
+    P.gate_rows = s->gate_kind == ONECOMP_GATE_ROWS;
+    P.w_bf16 = s->w_dtype == ONECOMP_BF16;
+    P.scale = s->residual_scale;
+    P.eps = s->eps;
+    return P;
+}
+
+// what both directions have in common
+onecomp_status norm_arguments(const onecomp_norm_shape* s, block::Params& P, const onecomp_rows* h, const onecomp_rows* y, const void* weight, const void* bias,
+                              const void* post_weight, const void* post_bias, const onecomp_rows* gate) {
+    if (!h || !check_rows(s, h) || !check_rows(s, y)) return ONECOMP_ERR_INVALID_ARG;
+    if (!check_param(s, weight) || !check_param(s, bias) || !check_param(s, post_weight) || !check_param(s, post_bias)) return ONECOMP_ERR_INVALID_ARG;
+    if ((!y && (s->post_norm || s->gate_kind != ONECOMP_GATE_NONE)) || (!s->post_norm && (post_weight || post_bias))) return ONECOMP_ERR_INVALID_ARG;
+    if (s->kind == ONECOMP_NORM_RMS && (bias || post_bias)) return ONECOMP_ERR_INVALID_ARG;
+    if ((s->gate_kind != ONECOMP_GATE_NONE) != (gate != nullptr)) return ONECOMP_ERR_INVALID_ARG;
+    if (s->gate_kind == ONECOMP_GATE_ROWS && !check_rows(s, gate)) return ONECOMP_ERR_INVALID_ARG;
+    if (s->gate_kind == ONECOMP_GATE_CHANNEL && (!gate->data || !check_param(s, gate->data))) return ONECOMP_ERR_INVALID_ARG;
+    P = norm_params(s);
+    P.h = rows_of(h);
+    P.y = rows_of(y);
+    P.gate = rows_of(gate);
+    P.weight = weight;
+    P.bias = bias;
+    P.post_weight = post_weight;
+    P.post_bias = post_bias;
+    if (!y) P.scale = 1.f;                                        // h' is h
+    return ONECOMP_OK;
 }
 
 attn::View view(const onecomp_heads* h) { return attn::View{h->data, h->token_stride, h->head_stride}; }
@@ -396,6 +453,78 @@ ONECOMP_API onecomp_status onecomp_attention_backward(const onecomp_attention_sh
     P.lse = const_cast<float*>(lse);
     P.aux = static_cast<float*>(workspace);
     return attn::backward_run(shape->dtype, P, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API onecomp_status onecomp_block_norm_forward(const onecomp_norm_shape* shape, const onecomp_rows* h, const onecomp_rows* y,
+                                                      const void* weight, const void* bias, const void* post_weight, const void* post_bias,
+                                                      const onecomp_rows* gate, const onecomp_rows* h_out, const onecomp_rows* n,
+                                                      void* hip_stream) {
+    const ApiRange range("onecomp_block_norm_forward");
+    if (const onecomp_status st = check_norm(shape)) return st;
+    block::Params P;
+    if (const onecomp_status st = norm_arguments(shape, P, h, y, weight, bias, post_weight, post_bias, gate)) return st;
+    if (!check_rows(shape, h_out) || !check_rows(shape, n) || (!h_out && !n) || (h_out && !y)) return ONECOMP_ERR_INVALID_ARG;
+    if (shape->rows == 0) return ONECOMP_OK;
+    if (n && (n->data == h->data || (h_out && n->data == h_out->data))) return ONECOMP_ERR_INVALID_ARG;
+    P.h_out = rows_of(h_out);
+    P.n = rows_of(n);
+    return block::norm_run(shape->dtype, P, false, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_block_norm_workspace_bytes(const onecomp_norm_shape* shape) {
+    if (check_norm(shape) != ONECOMP_OK) return 0;
+    const bool layer = shape->kind == ONECOMP_NORM_LAYER;
+    const int wanted = 1 | (layer ? 2 : 0) | (shape->post_norm ? 4 | (layer ? 8 : 0) : 0) | (shape->gate_kind == ONECOMP_GATE_CHANNEL ? 16 : 0);
+    return block::gradient_workspace_bytes(shape->rows, shape->width, wanted);
+}
+
+ONECOMP_API onecomp_status onecomp_block_norm_backward(const onecomp_norm_shape* shape, const onecomp_rows* dn, const onecomp_rows* dh_out,
+                                                       const onecomp_rows* h, const onecomp_rows* y, const void* weight,
+                                                       const void* post_weight, const void* post_bias, const onecomp_rows* gate,
+                                                       const onecomp_norm_gradients* out, void* workspace, size_t workspace_bytes,
+                                                       void* hip_stream) {
+    const ApiRange range("onecomp_block_norm_backward");
+    if (const onecomp_status st = check_norm(shape)) return st;
+    block::Params P;
+    if (const onecomp_status st = norm_arguments(shape, P, h, y, weight, nullptr, post_weight, post_bias, gate)) return st;
+    if (!out || (!dn && !dh_out) || !check_rows(shape, dn) || !check_rows(shape, dh_out)) return ONECOMP_ERR_INVALID_ARG;
+    if (!check_rows(shape, out->dh) || !check_rows(shape, out->dy) || !check_rows(shape, out->dgate)) return ONECOMP_ERR_INVALID_ARG;
+    const bool layer = shape->kind == ONECOMP_NORM_LAYER;
+    if ((out->dy && !y) || (out->dgate && shape->gate_kind != ONECOMP_GATE_ROWS) || (out->dgate_channel && shape->gate_kind != ONECOMP_GATE_CHANNEL) ||
+        ((out->dweight || out->dbias) && !dn) || ((out->dpost_weight || out->dpost_bias) && !shape->post_norm) || ((out->dbias || out->dpost_bias) && !layer))
+        return ONECOMP_ERR_INVALID_ARG;
+    void* const params[5] = {out->dweight, out->dbias, out->dpost_weight, out->dpost_bias, out->dgate_channel};
+    for (int i = 0; i < 5; ++i) {
+        if (!check_param(shape, params[i])) return ONECOMP_ERR_INVALID_ARG;
+        P.d_param[i] = params[i];
+        P.wanted |= params[i] ? 1 << i : 0;
+    }
+    if (P.wanted && (!workspace || !aligned(workspace, 256) || workspace_bytes < onecomp_block_norm_workspace_bytes(shape))) return ONECOMP_ERR_WORKSPACE;
+    if (shape->rows == 0 && !P.wanted) return ONECOMP_OK;
+    P.part = static_cast<float*>(workspace);
+    P.dn = rows_of(dn);
+    P.dh_out = rows_of(dh_out);
+    P.dh = rows_of(out->dh);
+    P.dy = rows_of(out->dy);
+    P.dgate = rows_of(out->dgate);
+    return block::norm_run(shape->dtype, P, true, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_clip_workspace_bytes(void) { return block::clip_workspace_bytes(); }
+
+ONECOMP_API onecomp_status onecomp_clip_gradients(const onecomp_gradient* grads, int n, float max_norm, float* norm, void* workspace,
+                                                  size_t workspace_bytes, void* hip_stream) {
+    const ApiRange range("onecomp_clip_gradients");
+    if (n < 0 || (n > 0 && !grads) || !(max_norm >= 0.f) || !aligned(norm, 4)) return ONECOMP_ERR_INVALID_ARG;
+    for (int i = 0; i < n; ++i) {
+        const onecomp_gradient& g = grads[i];
+        if (g.dtype != ONECOMP_F32 && g.dtype != ONECOMP_BF16) return ONECOMP_ERR_UNSUPPORTED;
+        const size_t esz = g.dtype == ONECOMP_BF16 ? 2 : 4;
+        if (g.numel < 0 || g.numel > (int64_t(1) << 40) || (g.numel > 0 && (!g.grad || !g.out || !aligned(g.grad, esz) || !aligned(g.out, esz))))
+            return ONECOMP_ERR_INVALID_ARG;
+    }
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < block::clip_workspace_bytes()) return ONECOMP_ERR_WORKSPACE;
+    return block::clip_run(grads, n, max_norm, norm, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 ONECOMP_API const char* onecomp_status_string(onecomp_status status) {

@@ -1,0 +1,385 @@
+// The norms around a block, fused with its gate and residual: h' = r h + g u, n = norm(h'), u = y or norm(y), and their
+// gradients.  Every tensor is read once and written once; rows stay in registers between the sums that a norm needs.
+#include "block.hpp"
+
+namespace onecomp {
+namespace block {
+namespace {
+
+// G threads have a row: thread t of them the values VEC (t + G v) .. + VEC - 1, v < NV; 16 bytes of T each.
+template <class T_, int NV, int G>
+struct Part {
+    typedef T_ T;
+    static constexpr int VEC = 16 / int(sizeof(T)), E = VEC * NV;
+    static __device__ __forceinline__ int col(int t, int v) { return VEC * (t + G * v); }
+    // zeros behind the width
+    static __device__ __forceinline__ void load(float (&x)[E], const Rows& r, int64_t row, int width, int t, bool there) {
+        const T* p = static_cast<const T*>(r.p) + row * r.stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col(t, v);
+            float y[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) y[i] = 0.f;
+            if (there && c + VEC <= width) {
+                load_vector(y, p + c);
+            } else if (there && c < width) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (c + i < width) y[i] = load_one(p + c + i);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[v * VEC + i] = y[i];
+        }
+    }
+    static __device__ __forceinline__ void store(const Rows& r, int64_t row, int width, int t, bool there, const float (&x)[E]) {
+        T* p = static_cast<T*>(r.p) + row * r.stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col(t, v);
+            float y[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) y[i] = x[v * VEC + i];
+            if (there && c + VEC <= width) {
+                store_vector(p + c, y);
+            } else if (there && c < width) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (c + i < width) store_one(p + c + i, y[i]);
+            }
+        }
+    }
+    // this thread's entries of a parameter, in either type
+    template <class W>
+    static __device__ __forceinline__ void parameter(float (&x)[E], const W* p, int width, int t) {
+        constexpr int N = 16 / int(sizeof(W));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col(t, v);
+            if (c + VEC <= width) {
+                if (VEC >= N) {
+#pragma unroll
+                    for (int i = 0; i < VEC / N; ++i) {
+                        float y[N];
+                        load_vector(y, p + c + N * i);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[v * VEC + (N * i + e) % VEC] = y[e];
+                    }
+                } else {                                          // fp32 rows with bf16 parameters: half a vector of these
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) x[v * VEC + i] = load_one(p + c + i);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) x[v * VEC + i] = c + i < width ? load_one(p + c + i) : 0.f;
+            }
+        }
+    }
+    static __device__ __forceinline__ void parameter(float (&x)[E], const void* p, bool bf16, int width, int t) {
+        if (bf16) parameter(x, static_cast<const uint16_t*>(p), width, t);
+        else parameter(x, static_cast<const float*>(p), width, t);
+    }
+};
+
+// Sums of K numbers over the G threads of each group of a workgroup.  `slot` alternates between two places in LDS, so that one
+// barrier a sum is enough.  Every thread of the workgroup takes part.
+template <int K, int G, int THREADS>
+__device__ __forceinline__ void group_sum(float (&x)[K], float* lds, int& slot) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) x[k] += __shfl_xor(x[k], o, 64);
+    if (G > 64) {
+        constexpr int WAVES = THREADS / 64, EACH = G / 64;
+        float* to = lds + slot * 4 * WAVES;
+        slot ^= 1;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) to[k * WAVES + wave] = x[k];
+        }
+        __syncthreads();
+        const int first = wave / EACH * EACH;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            x[k] = 0.f;
+#pragma unroll
+            for (int w = 0; w < EACH; ++w) x[k] += to[k * WAVES + first + w];
+        }
+    }
+}
+
+// x to (x - mean) / size in place: size^2 = mean of squares + eps; the mean for layer norms only
+template <class Pt, int G, int THREADS>
+__device__ __forceinline__ float normalise(float (&x)[Pt::E], bool layer, int width, float eps, int t, float* lds, int& slot) {
+    const float inv_width = 1.f / float(width);
+    if (layer) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int e = 0; e < Pt::E; ++e) s[0] += x[e];
+        group_sum<1, G, THREADS>(s, lds, slot);
+        const float mean = s[0] * inv_width;
+#pragma unroll
+        for (int e = 0; e < Pt::E; ++e) x[e] = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? x[e] - mean : 0.f;
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < Pt::E; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+    group_sum<1, G, THREADS>(s, lds, slot);
+    const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, eps));
+#pragma unroll
+    for (int e = 0; e < Pt::E; ++e) x[e] *= inv;
+    return inv;
+}
+
+// x = x w + b
+template <class Pt>
+__device__ __forceinline__ void affine(float (&x)[Pt::E], const void* w, const void* b, bool w_bf16, int width, int t) {
+    float p[Pt::E];
+    if (w) {
+        Pt::parameter(p, w, w_bf16, width, t);
+#pragma unroll
+        for (int e = 0; e < Pt::E; ++e) x[e] *= p[e];
+    }
+    if (b) {
+        Pt::parameter(p, b, w_bf16, width, t);
+#pragma unroll
+        for (int e = 0; e < Pt::E; ++e) x[e] += p[e];
+    }
+}
+
+template <class T, int NV, int G>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params P) {
+    constexpr int THREADS = G < 256 ? 256 : G;
+    typedef Part<T, NV, G> Pt;
+    __shared__ float lds[2 * 4 * (THREADS / 64)];
+    int slot = 0;
+    const int t = threadIdx.x % G;
+    const int64_t row = int64_t(blockIdx.x) * (THREADS / G) + threadIdx.x / G;
+    const bool there = row < P.rows;
+    const int width = P.width;
+    float x[Pt::E];
+    if (P.y.p) {
+        float u[Pt::E];
+        Pt::load(u, P.y, row, width, t, there);
+        Pt::load(x, P.h, row, width, t, there);
+        if (P.post) {
+            normalise<Pt, G, THREADS>(u, P.layer, width, P.eps, t, lds, slot);
+            affine<Pt>(u, P.post_weight, P.post_bias, P.w_bf16, width, t);
+        }
+        if (P.gate.p) {
+            float g[Pt::E];
+            if (P.gate_rows) Pt::load(g, P.gate, row, width, t, there);
+            else Pt::parameter(g, P.gate.p, P.w_bf16, width, t);
+#pragma unroll
+            for (int e = 0; e < Pt::E; ++e) u[e] *= g[e];
+        }
+#pragma unroll
+        for (int e = 0; e < Pt::E; ++e) x[e] = fmaf(P.scale, x[e], u[e]);
+        if (P.h_out.p) Pt::store(P.h_out, row, width, t, there, x);
+    } else {
+        Pt::load(x, P.h, row, width, t, there);
+    }
+    if (!P.n.p) return;
+    normalise<Pt, G, THREADS>(x, P.layer, width, P.eps, t, lds, slot);
+    affine<Pt>(x, P.weight, P.bias, P.w_bf16, width, t);
+    Pt::store(P.n, row, width, t, there, x);
+}
+
+// d to the gradient of the rows in front of a norm: inv (d - x mean(d x) - mean(d)), x the normalised row; the last for layer
+// norms only
+template <class Pt, int G, int THREADS>
+__device__ __forceinline__ void norm_gradient(float (&d)[Pt::E], const float (&x)[Pt::E], float inv, bool layer, int width, int t, float* lds, int& slot) {
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < Pt::E; ++e) {
+        s[0] = fmaf(d[e], x[e], s[0]);
+        s[1] += d[e];
+    }
+    group_sum<2, G, THREADS>(s, lds, slot);
+    const float along = s[0] / float(width), mean = layer ? s[1] / float(width) : 0.f;
+#pragma unroll
+    for (int e = 0; e < Pt::E; ++e) d[e] = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? inv * (d[e] - mean - x[e] * along) : 0.f;
+}
+
+// A workgroup takes rows in turn (as many at a time as it has groups of G threads) and keeps the parameters' gradients, sums
+// over rows, in registers until its last row; then its groups' sums meet in LDS and go to scratch, one row per workgroup.
+template <class T, int NV, int G, bool LAYER>
+__global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
+    constexpr int THREADS = 1024, GROUPS = THREADS / G;
+    typedef Part<T, NV, G> Pt;
+    constexpr int E = Pt::E;
+    __shared__ float lds[2 * 4 * (THREADS / 64)];
+    __shared__ float meet[GROUPS > 1 ? THREADS * E : 1];
+    int slot = 0;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    const int width = P.width;
+    float sums[5][E];     // weight, bias, post_weight, post_bias, gate
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[i][e] = 0.f;
+    for (int64_t first = int64_t(blockIdx.x) * GROUPS; first < P.rows; first += int64_t(gridDim.x) * GROUPS) {
+        const int64_t row = first + group;
+        const bool there = row < P.rows;
+        float d[E];       // the gradient of h'
+        Pt::load(d, P.dh_out, row, width, t, there && P.dh_out.p);
+        if (P.dn.p) {
+            float x[E], dn[E], w[E];
+            Pt::load(x, P.h, row, width, t, there);
+            Pt::load(dn, P.dn, row, width, t, there);
+            const float inv = normalise<Pt, G, THREADS>(x, LAYER, width, P.eps, t, lds, slot);
+            if (P.weight) Pt::parameter(w, P.weight, P.w_bf16, width, t);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                sums[0][e] = fmaf(dn[e], x[e], sums[0][e]);
+                if (LAYER) sums[1][e] += dn[e];
+                if (P.weight) dn[e] *= w[e];
+            }
+            norm_gradient<Pt, G, THREADS>(dn, x, inv, LAYER, width, t, lds, slot);
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] += dn[e];
+        }
+        {
+            float dh[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) dh[e] = P.scale * d[e];
+            if (P.dh.p) Pt::store(P.dh, row, width, t, there, dh);
+        }
+        if (!P.y.p) continue;
+        float x[E], u[E], inv = 0.f;
+        Pt::load(x, P.y, row, width, t, there);
+        if (P.post) inv = normalise<Pt, G, THREADS>(x, LAYER, width, P.eps, t, lds, slot);
+        if (P.gate.p) {
+            float g[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) u[e] = x[e];
+            if (P.post) affine<Pt>(u, P.post_weight, P.post_bias, P.w_bf16, width, t);
+#pragma unroll
+            for (int e = 0; e < E; ++e) u[e] *= d[e];
+            if (P.gate_rows) {
+                if (P.dgate.p) Pt::store(P.dgate, row, width, t, there, u);
+                Pt::load(g, P.gate, row, width, t, there);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) sums[4][e] += u[e];
+                Pt::parameter(g, P.gate.p, P.w_bf16, width, t);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] *= g[e];
+        }
+        if (P.post) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                sums[2][e] = fmaf(d[e], x[e], sums[2][e]);
+                if (LAYER) sums[3][e] += d[e];
+            }
+            if (P.post_weight) affine<Pt>(d, P.post_weight, nullptr, P.w_bf16, width, t);
+            norm_gradient<Pt, G, THREADS>(d, x, inv, LAYER, width, t, lds, slot);
+        }
+        if (P.dy.p) Pt::store(P.dy, row, width, t, there, d);
+    }
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        if (!(P.wanted >> i & 1)) continue;
+        float* to = P.part + (int64_t(__popc(P.wanted & ((1 << i) - 1))) * gridDim.x + blockIdx.x) * width;
+        if (GROUPS == 1) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int c = Pt::col(t, e / Pt::VEC) + e % Pt::VEC;
+                if (c < width) to[c] = sums[i][e];
+            }
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e) meet[(group * E + e) * G + t] = sums[i][e];
+            __syncthreads();
+            for (int at = threadIdx.x; at < E * G; at += THREADS) {
+                float s = 0.f;
+                for (int g = 0; g < GROUPS; ++g) s += meet[g * E * G + at];
+                const int e = at / G, c = Pt::col(at % G, e / Pt::VEC) + e % Pt::VEC;
+                if (c < width) to[c] = s;
+            }
+        }
+    }
+}
+
+// Sums over the workgroups of the kernel above: 64 columns of one parameter per workgroup, 16 waves with every sixteenth row.
+__global__ __launch_bounds__(1024) void columns_kernel(const Params P, const int n_parts) {
+    __shared__ float meet[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
+    const float* from = P.part + int64_t(blockIdx.y) * n_parts * P.width;
+    float s = 0.f;
+    if (c < P.width)
+        for (int r = wave; r < n_parts; r += 16) s += from[int64_t(r) * P.width + c];
+    meet[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= P.width) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += meet[w][lane];
+    int which = 0;
+    for (int left = int(blockIdx.y); which < 5; ++which)
+        if ((P.wanted >> which & 1) && left-- == 0) break;
+    if (P.w_bf16) static_cast<__bf16*>(P.d_param[which])[c] = static_cast<__bf16>(s);
+    else static_cast<float*>(P.d_param[which])[c] = s;
+}
+
+int gradient_workgroups(int64_t rows, int groups) {
+    const int cus = device_cus();
+    const int64_t all = ceil_div(rows, groups);
+    const int64_t most = cus > 0 ? cus : 256;
+    return int(all < 1 ? 1 : all < most ? all : most);            // one even without rows: the sums are 0
+}
+
+template <class T, int NV, int G>
+onecomp_status launch(const Params& P, bool gradient, hipStream_t stream) {
+    if (!gradient) {
+        constexpr int THREADS = G < 256 ? 256 : G;
+        const int64_t grid = ceil_div(P.rows, THREADS / G);
+        if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
+        forward_kernel<T, NV, G><<<dim3(unsigned(grid)), dim3(THREADS), 0, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+        return ONECOMP_OK;
+    }
+    const int grid = gradient_workgroups(P.rows, 1024 / G);
+    if (P.layer) gradient_kernel<T, NV, G, true><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
+    else gradient_kernel<T, NV, G, false><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    if (const int n = __builtin_popcount(P.wanted)) {
+        columns_kernel<<<dim3(unsigned((P.width + 63) / 64), unsigned(n)), dim3(1024), 0, stream>>>(P, grid);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    return ONECOMP_OK;
+}
+
+// As few threads as hold a row with 16 bytes each: sums cross the fewest waves, and registers stay free for the parameters'
+// sums.  Rows over 8192 (bf16) or 4096 (fp32) take more per thread.
+template <class T>
+onecomp_status run(const Params& P, bool gradient, hipStream_t s) {
+    constexpr int V = 16 / int(sizeof(T));
+    const int w = P.width;
+    if (w <= 64 * V) return launch<T, 1, 64>(P, gradient, s);
+    if (w <= 256 * V) return launch<T, 1, 256>(P, gradient, s);
+    if (w <= 512 * V) return launch<T, 1, 512>(P, gradient, s);
+    if (w <= 1024 * V) return launch<T, 1, 1024>(P, gradient, s);
+    if (w <= 2048 * V) return launch<T, 2, 1024>(P, gradient, s);
+    if constexpr (V == 4) {
+        if (w > 4096 * V) return launch<T, 8, 1024>(P, gradient, s);
+    }
+    return launch<T, 4, 1024>(P, gradient, s);
+}
+
+}  // namespace
+
+size_t gradient_workspace_bytes(int64_t rows, int64_t width, int wanted) {
+    const int64_t most = rows < 1 ? 1 : rows < 1024 ? rows : 1024;               // no device has more workgroups of these at a time
+    return align_up(size_t(most) * size_t(width) * size_t(__builtin_popcount(unsigned(wanted))) * 4, 256);
+}
+
+onecomp_status norm_run(onecomp_dtype dtype, const Params& P, bool gradient, hipStream_t stream) {
+    return dtype == ONECOMP_BF16 ? run<uint16_t>(P, gradient, stream) : run<float>(P, gradient, stream);
+}
+
+}  // namespace block
+}  // namespace onecomp

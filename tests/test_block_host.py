@@ -92,3 +92,107 @@ def test_attention_binding_checks():
     cu = torch.tensor([0, 4], dtype=torch.int32)
     with pytest.raises(ValueError):
         og.onecomp_attention_forward(q, k, k, cu, cu, 4, 4)        # not on the GPU
+
+
+def _norm_shape(**kw):
+    s = dict(dtype=1, w_dtype=1, kind=0, gate_kind=0, post_norm=0, rows=10, width=64, residual_scale=1.0, eps=1e-6)
+    s.update(kw)
+    return binding.NormShape(**s)
+
+
+def _rows(data=P, stride=64):
+    return ctypes.byref(binding.Rows(data, stride))
+
+
+Q = P + 0x10000     # another buffer
+
+
+def _norm(lib, h=0, y=None, weight=P, bias=None, pw=None, pb=None, gate=None, h_out=None, n=0, **kw):
+    """h, n: given unless None"""
+    return lib.onecomp_block_norm_forward(ctypes.byref(_norm_shape(**kw)), _rows() if h == 0 else h, y, weight, bias, pw, pb, gate, h_out,
+                                          _rows(Q) if n == 0 else n, NULL)
+
+
+def test_norm_refusals(lib):
+    assert _norm(lib, dtype=3) == UNSUPPORTED
+    assert _norm(lib, w_dtype=3) == UNSUPPORTED
+    assert _norm(lib, kind=2) == UNSUPPORTED
+    assert _norm(lib, gate_kind=3) == UNSUPPORTED
+    assert _norm(lib, width=32769) == UNSUPPORTED
+    assert _norm(lib, width=0) == INVALID
+    assert _norm(lib, rows=-1) == INVALID
+    for eps in (-1.0, float("nan"), float("inf")):
+        assert _norm(lib, eps=eps) == INVALID
+    assert _norm(lib, residual_scale=float("nan")) == INVALID
+    assert _norm(lib, h=None) == INVALID
+    assert _norm(lib, h=_rows(None)) == INVALID
+    assert _norm(lib, h=_rows(stride=63)) == INVALID                # rows overlap
+    assert _norm(lib, h=_rows(P + 1)) == INVALID                    # not even an element's address
+    assert _norm(lib, weight=P + 1) == INVALID
+    assert _norm(lib, n=None) == INVALID                            # nothing to do
+    assert _norm(lib, n=_rows(P)) == INVALID                        # n over h
+    assert _norm(lib, h_out=_rows()) == INVALID                     # without y, h' is h
+    assert _norm(lib, bias=P) == INVALID                            # rms norms have none
+    assert _norm(lib, post_norm=1) == INVALID                       # without y
+    assert _norm(lib, y=_rows(), pw=P) == INVALID                   # without post_norm
+    assert _norm(lib, y=_rows(), gate_kind=1) == INVALID            # no gate
+    assert _norm(lib, y=_rows(), gate=_rows()) == INVALID           # a gate that no kind announces
+    assert _norm(lib, y=_rows(), gate_kind=2, gate=_rows(stride=3)) == INVALID
+    assert _norm(lib, y=_rows(), h_out=_rows(Q)) == INVALID         # n over h'
+    assert _norm(lib, rows=0) == OK
+
+
+def _norm_back(lib, dn=0, dh_out=0, h=0, y=None, weight=P, pw=None, gate=None, out=0, ws=P, ws_bytes=BIG, grads=None, **kw):
+    g = binding.NormGradients(*(grads or [ctypes.pointer(binding.Rows(P, 64)), None, None, P, None, None, None, None]))
+    pick = lambda x: _rows() if x == 0 else x  # noqa: E731
+    return lib.onecomp_block_norm_backward(ctypes.byref(_norm_shape(**kw)), pick(dn), pick(dh_out), pick(h), y, weight, pw, None, gate,
+                                           ctypes.byref(g) if out == 0 else out, ws, ws_bytes, NULL)
+
+
+def test_norm_gradient_refusals(lib):
+    r = ctypes.pointer(binding.Rows(P, 64))
+    assert _norm_back(lib, dtype=3) == UNSUPPORTED
+    assert _norm_back(lib, h=None) == INVALID
+    assert _norm_back(lib, dn=None, dh_out=None) == INVALID
+    assert _norm_back(lib, out=None) == INVALID
+    assert _norm_back(lib, dn=None) == INVALID                      # the weight's gradient without that of n
+    assert _norm_back(lib, grads=[r, r, None, None, None, None, None, None]) == INVALID      # dy without y
+    assert _norm_back(lib, grads=[r, None, r, None, None, None, None, None]) == INVALID      # a gate's without a gate
+    assert _norm_back(lib, grads=[r, None, None, None, None, None, None, P]) == INVALID
+    assert _norm_back(lib, grads=[r, None, None, None, P, None, None, None]) == INVALID      # a bias of an rms norm
+    assert _norm_back(lib, grads=[r, None, None, None, None, P, None, None]) == INVALID      # no norm behind the block
+    assert _norm_back(lib, ws=None) == WORKSPACE
+    assert _norm_back(lib, ws_bytes=ctypes.c_size_t(64)) == WORKSPACE
+    assert lib.onecomp_block_norm_workspace_bytes(ctypes.byref(_norm_shape())) >= 10 * 64 * 4
+    assert lib.onecomp_block_norm_workspace_bytes(ctypes.byref(_norm_shape(width=0))) == 0
+
+
+def test_clip_refusals(lib):
+    def call(grad=P, out=P, numel=10, dtype=1, n=1, max_norm=1.0, norm=P, ws=P, ws_bytes=BIG, table=True):
+        g = (binding.Gradient * 1)(binding.Gradient(grad, out, numel, dtype))
+        return lib.onecomp_clip_gradients(g if table else None, n, max_norm, norm, ws, ws_bytes, NULL)
+
+    assert call(dtype=2) == UNSUPPORTED
+    assert call(grad=None) == INVALID
+    assert call(out=None) == INVALID
+    assert call(grad=P + 1) == INVALID
+    assert call(dtype=0, out=P + 2) == INVALID
+    assert call(numel=-1) == INVALID
+    assert call(n=-1) == INVALID
+    assert call(table=False) == INVALID
+    assert call(max_norm=-1.0) == INVALID
+    assert call(max_norm=float("nan")) == INVALID
+    assert call(norm=P + 2) == INVALID
+    assert call(ws=None) == WORKSPACE
+    assert call(ws_bytes=ctypes.c_size_t(lib.onecomp_clip_workspace_bytes() - 1)) == WORKSPACE
+
+
+def test_binding_checks():
+    x = torch.zeros(4, 8)
+    for call in (lambda: og.onecomp_block_norm_forward(x), lambda: og.onecomp_block_norm_backward(x, x, x), lambda: og.onecomp_clip_gradients([x], 1.0)):
+        with pytest.raises(ValueError):
+            call()                                                  # not on the GPU
+    with pytest.raises(ValueError):
+        og.onecomp_clip_gradients([x], 1.0, out=[])
+    with pytest.raises(ValueError):
+        og.onecomp_clip_gradients([], 1.0)
