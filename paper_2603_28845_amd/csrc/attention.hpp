@@ -138,17 +138,23 @@ struct Reader {
     }
 };
 
-// acc[col][.] += sum over the 16 rows from 16 step of tile[row][32 n + m] p[row]: m is the accumulator's row, p the
-// probabilities of these rows
+// Left operand of the sum over 16 rows from 16 step on: columns 32 n .. + 31 of the tile, transposed.
 template <int DT>
-__device__ __forceinline__ float16v mma_t(const Reader<Bf16, DT>& rd, const char* tile, int step, int n, const Bf16::Score& p, float16v acc) {
+__device__ __forceinline__ bf16x8 columns(const Reader<Bf16, DT>& rd, const char* tile, int step, int n) {
     typedef Tile<Bf16, DT> T;
     const char* a = tile + step * 16 * T::PITCH;
     // rows 8 further on: the swizzle's lowest bit for rows of 256 bytes, none otherwise
     const int far = T::CHUNKS >= 16 ? 16 : 0;
     const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + (rd.tr ^ (n << 6))));
     const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 8 * T::PITCH + (rd.tr ^ (n << 6) ^ far)));
-    return Bf16::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), p, acc);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// acc[col][.] += sum over the 16 rows from 16 step of tile[row][32 n + m] p[row]: m is the accumulator's row, p the
+// probabilities of these rows
+template <int DT>
+__device__ __forceinline__ float16v mma_t(const Reader<Bf16, DT>& rd, const char* tile, int step, int n, const Bf16::Score& p, float16v acc) {
+    return Bf16::mma(columns<DT>(rd, tile, step, n), p, acc);
 }
 template <int DT>
 __device__ __forceinline__ float16v mma_t(const Reader<F32, DT>& rd, const char* tile, int step, int n, const F32::Score& p, float16v acc) {

@@ -197,6 +197,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
             const bool all_seen = r0 >= all;
 #pragma unroll
             for (int b = 0; b < KB<E>; ++b) {
+                asm volatile("" : "+v"(rd.row), "+v"(rd.tr));
                 float16v s = zero16(), dp = zero16();
 #pragma unroll
                 for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(qt, b, x), k.x[x], s);
@@ -301,10 +302,10 @@ size_t backward_workspace_bytes(const Params& P) { return align_up(size_t(P.tota
 onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream) {
     const int dt = (P.dim + 31) / 32;
     if (dtype == ONECOMP_BF16)
-        return dt == 1   ? launch_backward<Bf16, 1, 8, 8>(P, stream)
-               : dt == 2 ? launch_backward<Bf16, 2, 8, 8>(P, stream)
-               : dt == 3 ? launch_backward<Bf16, 3, 8, 8>(P, stream)
-                         : launch_backward<Bf16, 4, 8, 8>(P, stream);
+        return dt == 1   ? launch_backward<Bf16, 1, 4, 4>(P, stream)
+               : dt == 2 ? launch_backward<Bf16, 2, 4, 4>(P, stream)
+               : dt == 3 ? launch_backward<Bf16, 3, 4, 4>(P, stream)
+                         : launch_backward<Bf16, 4, 4, 4>(P, stream);
     return dt == 1   ? launch_backward<F32, 1, 4, 4>(P, stream)
            : dt == 2 ? launch_backward<F32, 2, 4, 4>(P, stream)
            : dt == 3 ? launch_backward<F32, 3, 4, 4>(P, stream)

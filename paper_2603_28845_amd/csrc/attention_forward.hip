@@ -19,29 +19,106 @@ struct Rows32 {
         l = 0.f;
     }
 
-    // KB blocks of 32 keys in LDS.  last: the last key (counted from the tile's first) that this lane's query sees; all_seen:
-    // every lane sees all of them (wave-uniform).
+    // Scores of KB blocks of 32 keys in LDS.
     template <int KB>
-    __device__ __forceinline__ void tile(const Reader<E, DT>& rd, const char* kt, const char* vt, const Operand<E, DT>& q, float c, bool all_seen, int last, int half) {
-        float16v s[KB];
+    static __device__ __forceinline__ void scores(float16v (&s)[KB], const Reader<E, DT>& rd, const char* kt, const Operand<E, DT>& q) {
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            s[b] = zero16();
+        for (int b = 0; b < KB; ++b) s[b] = zero16();
 #pragma unroll
-            for (int i = 0; i < Tile<E, DT>::STEPS; ++i) s[b] = E::mma(rd.rows(kt, b, i), q.x[i], s[b]);
+        for (int i = 0; i < Tile<E, DT>::STEPS; ++i)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) s[b] = E::mma(rd.rows(kt, b, i), q.x[i], s[b]);
+    }
+
+    // values() of one tile and scores() of the next in one stream of instructions, each product with its share of the
+    // exponentials beside it and its operand read some products ahead:
+    //   half of the next scores   | exponentials of the first 32 keys
+    //   the other half, in turn with the products of these 32 | exponentials of the second 32
+    //   products of the second 32 | maximum of the next scores, which it returns
+    // The compiler on its own reads each operand right before its product and so waits for LDS every time.
+    __device__ __forceinline__ float step(float16v (&s)[2], float16v (&next)[2], const Reader<E, DT>& rd, const char* kt, const char* vt,
+                                          const Operand<E, DT>& q, float c) {
+        static_assert(sizeof(typename E::T) == 2, "bf16");
+        constexpr int N = 4 * DT, A = N / 2;                      // products of each kind, half of them
+        constexpr int AHEAD = 4, AHEAD_V = A < 3 ? A : 3;         // operands read ahead
+        const float base = m == NEG_INF ? 0.f : m;
+        typename E::Row a[AHEAD], v[AHEAD_V];
+        typename E::Score p[4];
+        float add[4] = {l, 0.f, 0.f, 0.f}, top = NEG_INF;
+        auto read_q = [&](int i) { if (i < N) a[i % AHEAD] = rd.rows(kt, i & 1, i >> 1); };
+        auto read_v = [&](int i) { if (i < N) v[i % AHEAD_V] = columns<DT>(rd, vt, i / DT, i % DT); };
+        auto score = [&](int i) {
+            next[i & 1] = E::mma(a[i % AHEAD], q.x[i >> 1], i < 2 ? zero16() : next[i & 1]);
+            read_q(i + AHEAD);
+        };
+        auto value = [&](int i) {
+            o[i % DT] = E::mma(v[i % AHEAD_V], p[i / DT], o[i % DT]);
+            read_v(i + AHEAD_V);
+        };
+        // exponentials of block b that belong to slot i of n
+        auto exponentials = [&](int b, int i, int n) {
+#pragma unroll
+            for (int r = 16 * i / n; r < 16 * (i + 1) / n; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -base));
+                add[r & 3] += s[b][r];
+                asm volatile("" : "+v"(add[r & 3]));              // here, not where the sum is used: 32 registers less
+                if (r % 8 == 7) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = s[b][r - 7 + e];
+                    p[2 * b + r / 8] = E::pack(x);
+                }
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) read_q(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            score(i);
+            if (i >= A - AHEAD_V) read_v(i - (A - AHEAD_V));
+            exponentials(0, i, A);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (!all_seen) {
 #pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (32 * b + acc_row(r, half) > last) s[b][r] = NEG_INF;
+        for (int i = 0; i < A; ++i) {
+            score(A + i);
+            exponentials(1, 2 * i, N);
+            __builtin_amdgcn_sched_barrier(0);
+            value(i);
+            exponentials(1, 2 * i + 1, N);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        float top = s[0][0];
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            value(A + i);
+#pragma unroll
+            for (int r = 32 * i / A; r < 32 * (i + 1) / A; ++r) top = fmaxf(top, next[r >> 4][r & 15]);
+            asm volatile("" : "+v"(top));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l = (add[0] + add[1]) + (add[2] + add[3]);
+        return top;
+    }
+
+    // Takes unseen keys out and returns the largest score of this half's keys.  last: the last key, counted from the tile's first,
+    // that this lane's query sees.
+    template <int KB>
+    static __device__ __forceinline__ float mask(float16v (&s)[KB], int last, int half) {
+        float top = NEG_INF;
+        asm volatile("");                                         // a branch around this stays one: 64 selections per tile otherwise
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+            for (int r = 0; r < 16; ++r) {
+                if (32 * b + acc_row(r, half) > last) s[b][r] = NEG_INF;
+                top = fmaxf(top, s[b][r]);
+            }
+        return top;
+    }
+
+    // Moves the maximum; top: the largest score of this half's keys.
+    __device__ __forceinline__ void settle(float top, float c) {
         top = fmaxf(top, other_half(top)) * c;
         // The sums keep the maximum they began with until a score passes it by 2^8: the probabilities' rounding is relative
         // and their sum has room for that, and the many products with the new scale fall away.
@@ -55,14 +132,19 @@ struct Rows32 {
                 for (int r = 0; r < 16; ++r) o[n][r] *= f;
             m = to;
         }
+    }
+
+    // Probabilities and their sums with the values.
+    template <int KB>
+    __device__ __forceinline__ void values(float16v (&s)[KB], const Reader<E, DT>& rd, const char* vt, float c) {
         const float base = m == NEG_INF ? 0.f : m;
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -base));
-            float add[4] = {0.f, 0.f, 0.f, 0.f};
+            float add[4] = {s[b][0], s[b][1], s[b][2], s[b][3]};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) add[r & 3] += s[b][r];
+            for (int r = 4; r < 16; ++r) add[r & 3] += s[b][r];
             l += (add[0] + add[1]) + (add[2] + add[3]);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -112,20 +194,63 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     Rows32<E, DT> acc;
     acc.init();
 
+    // Tile t's scores are formed while tile t - 1 goes through exponentials and values, so that a wave has products for the
+    // matrix pipe and arithmetic for the vector pipe at the same time.  LDS: two tiles of keys, two of values.
     constexpr int SIZE = T::bytes(KEYS);
     const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds));
-    auto bring = [&](int j, int buf) {
-        lk.load(base + uint32_t(buf) * 2 * SIZE, at<E>(P.k, S.k0 + j, kv), end - j, wave);
-        lv.load(base + uint32_t(buf) * 2 * SIZE + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
+    const int n = (end + KEYS - 1) / KEYS, n_mine = (end_mine + KEYS - 1) / KEYS;
+    auto bring_k = [&](int t) {
+        if (t < n) lk.load(base + uint32_t(t & 1) * SIZE, at<E>(P.k, S.k0 + t * KEYS, kv), end - t * KEYS, wave);
     };
-    if (end > 0) bring(0, 0);
-    for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
+    auto bring_v = [&](int t) {
+        if (t < n) lv.load(base + uint32_t(2 + (t & 1)) * SIZE, at<E>(P.v, S.k0 + t * KEYS, kv), end - t * KEYS, wave);
+    };
+    auto next = [&](int t) {                                      // keys t + 1 and values t are there, keys t and values t - 1 done with
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
         __syncthreads();
-        if (j + KEYS < end) bring(j + KEYS, buf ^ 1);
-        if (j < end_mine)
-            acc.template tile<KB>(rd, lds + buf * 2 * SIZE, lds + buf * 2 * SIZE + SIZE, q, P.c, j + KEYS <= end_all, last - j, half);
+        bring_k(t + 2);
+        bring_v(t + 1);
+    };
+    auto step = [&](float16v(&s)[KB], float16v(&s_next)[KB], int t) {
+        next(t);
+        const char *kt = lds + ((t + 1) & 1) * SIZE, *vt = lds + (2 + (t & 1)) * SIZE;
+        float top;
+        if constexpr (KB == 2) {
+            top = acc.step(s, s_next, rd, kt, vt, q, P.c);
+            if ((t + 2) * KEYS > end_all) top = acc.mask(s_next, last - (t + 1) * KEYS, half);
+        } else {
+            acc.template scores<KB>(s_next, rd, kt, q);
+            acc.template values<KB>(s, rd, vt, P.c);
+            top = acc.mask(s_next, last - (t + 1) * KEYS, half);
+        }
+        acc.settle(top, P.c);
+    };
+    bring_k(0);
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+    __syncthreads();
+    bring_v(0);
+    bring_k(1);
+    int t = 0;
+    if (n_mine > 0) {
+        float16v s0[KB], s1[KB];
+        acc.template scores<KB>(s0, rd, lds, q);
+        acc.settle(acc.mask(s0, last, half), P.c);
+        for (; t + 2 < n_mine; t += 2) {
+            step(s0, s1, t);
+            step(s1, s0, t + 1);
+        }
+        if (t + 1 < n_mine) {
+            step(s0, s1, t);
+            next(t + 1);
+            acc.template values<KB>(s1, rd, lds + (2 + ((t + 1) & 1)) * SIZE, P.c);
+            t += 2;
+        } else {
+            next(t);
+            acc.template values<KB>(s0, rd, lds + (2 + (t & 1)) * SIZE, P.c);
+            t += 1;
+        }
     }
+    for (; t < n; ++t) next(t);
     const float l = acc.l + other_half(acc.l), f = l == 0.f ? 0.f : 1.f / l;
     const bool broken = there && l == l && not_finite(acc.o);
     if (there && !broken) {
@@ -212,7 +337,10 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
                 __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
             }
             asm volatile("" ::: "memory");
-            acc.template tile<1>(rd, own + buf * 2 * F::SIZE, own + buf * 2 * F::SIZE + F::SIZE, q, P.c, j + 32 <= end_all, last - j, half);
+            float16v s[1];
+            acc.template scores<1>(s, rd, own + buf * 2 * F::SIZE, q);
+            acc.settle(acc.mask(s, last - j, half), P.c);
+            acc.template values<1>(s, rd, own + buf * 2 * F::SIZE + F::SIZE, P.c);
         }
     }
 
@@ -364,7 +492,7 @@ void plan(Params& P) {
 
 template <class E, int DT>
 onecomp_status forward(const Params& P, hipStream_t stream) {
-    return P.splits ? launch_few<E, DT>(P, stream) : launch_forward<E, DT, 8>(P, stream);
+    return P.splits ? launch_few<E, DT>(P, stream) : launch_forward<E, DT, 4>(P, stream);
 }
 
 }  // namespace
