@@ -181,74 +181,79 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { 
 
 // Rows from `first` on that belong to sequence i.  Behind the last sequence comes one of all rows that are left: padding,
 // whose queries see no keys and whose keys no query sees.
-__device__ __forceinline__ int rows_of(const int32_t* cu, int64_t total, int n_seqs, int i, int64_t& first) {
-    first = clamp64(cu[i], 0, total);
-    return int((i < n_seqs ? clamp64(cu[i + 1], first, total) : total) - first);
+__device__ __forceinline__ int rows_of(const int32_t* cu, int64_t total, int n_seqs, int i, int& first) {
+    const int64_t at = clamp64(cu[i], 0, total);
+    first = int(at);
+    return int((i < n_seqs ? clamp64(cu[i + 1], at, total) : total) - at);
 }
 
-// Sequence i; what the arrays say is cut to the tensors' rows.  Wave-uniform.
-__device__ __forceinline__ Seq sequence(const Params& P, int i) {
-    Seq s;
-    int64_t q0, k0;
-    s.nq = __builtin_amdgcn_readfirstlane(rows_of(P.cu_q, P.total_q, P.n_seqs, i, q0));
-    int nk = rows_of(P.cu_k, P.total_k, P.n_seqs, i, k0);
-    s.room = __builtin_amdgcn_readfirstlane(nk);
-    if (i == P.n_seqs) nk = 0;
-    else if (P.len_k) nk = int(clamp64(P.len_k[i], 0, nk));
-    s.nk = __builtin_amdgcn_readfirstlane(nk);
-    s.q0 = __builtin_amdgcn_readfirstlane(int(q0));
-    s.k0 = __builtin_amdgcn_readfirstlane(int(k0));
-    s.shift = s.nk - s.nq;
-    return s;
+// Sums over the lanes up to each, and the largest of all lanes; in the vector pipe, with the last lane's value for the whole
+// wave.  (Through LDS, as shuffles go, the search below took 3 us of each workgroup's start.)
+__device__ __forceinline__ int scan_add(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int wave_add(int x) { return __builtin_amdgcn_readlane(scan_add(x), 63); }
+__device__ __forceinline__ int wave_max(int x) {
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
 }
 
-// The t-th tile of `size` rows of all sequences: false if there are fewer.  `mul` rows stand for each row of cu (heads of a
-// group that are packed into rows).  Of up to 63 sequences the tiles come by their number x in the sequence, the largest
-// first and at the same x by sequence: x + 1 tiles of keys lie before a causal prompt's tile x, so that long work starts
-// early and the last workgroups are short (32 x 2048 tokens: see the forward kernel).  Of more, one sequence after the other,
-// each from its largest x down: counting by number would read the array many times.  Every lane of a wave takes part and
-// gets the same answer.
-__device__ __forceinline__ bool find_tile(const int32_t* cu, int64_t total, int n_seqs, int mul, int size, int t, int& seq, int& x, int& tiles) {
+// The t-th tile of `size` rows of all sequences, queries or (KEYS) keys with the room behind them: its sequence, its number x
+// there and how many the sequence has; false if there are fewer.  `mul` rows stand for each row (heads of a group that are
+// packed into rows).  What the arrays say is cut to the tensors' rows.  Of up to 63 sequences the tiles come by their number
+// x, the largest first and at the same x by sequence: x + 1 tiles of keys lie before a causal prompt's tile x, so that long
+// work starts early and the last workgroups are short.  Of more, one sequence after the other, each from its largest x down:
+// counting by number would read the arrays many times.  Every lane of a wave takes part and gets the same answer.
+template <bool KEYS>
+__device__ __forceinline__ bool find_tile(const Params& P, int mul, int size, int t, Seq& S, int& x, int& tiles) {
     const int lane = threadIdx.x & 63;
     int done = 0;
-    for (int base = 0; base <= n_seqs; base += 64) {
-        int count = 0;
-        int64_t first;
-        if (base + lane <= n_seqs) count = int((int64_t(rows_of(cu, total, n_seqs, base + lane, first)) * mul + size - 1) / size);
+    for (int base = 0; base <= P.n_seqs; base += 64) {
+        int q0 = 0, k0 = 0, nq = 0, nk = 0, room = 0, count = 0;
+        const int i = base + lane;
+        if (i <= P.n_seqs) {
+            nq = rows_of(P.cu_q, P.total_q, P.n_seqs, i, q0);
+            room = rows_of(P.cu_k, P.total_k, P.n_seqs, i, k0);
+            nk = i == P.n_seqs ? 0 : P.len_k ? int(clamp64(P.len_k[i], 0, room)) : room;
+            count = int((int64_t(KEYS ? room : nq) * mul + size - 1) / size);
+        }
         int mine = count;                                         // tiles of this lane's sequence among those looked at
-        if (n_seqs < 64) {
-            int lo = 0, hi = count;                               // the largest x of which t + 1 tiles are at least x
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) hi = max(hi, __shfl_xor(hi, o, 64));
+        if (P.n_seqs < 64) {
+            int lo = 0, hi = wave_max(count);                     // lo: the largest x of which t + 1 tiles are at least x
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                int n = max(0, count - mid);
-#pragma unroll
-                for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-                if (n > t) lo = mid; else hi = mid;
+                if (wave_add(max(0, count - mid)) > t) lo = mid; else hi = mid;
             }
-            int n = max(0, count - lo - 1);
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-            done = n;                                             // tiles with a larger number
+            done = wave_add(max(0, count - lo - 1));              // tiles with a larger number
             mine = count > lo ? 1 : 0;
-            x = __builtin_amdgcn_readfirstlane(lo);
+            x = lo;
         }
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += v;
-        }
+        const int upto = scan_add(mine);
         const unsigned long long past = __ballot(done + upto > t);
         if (past) {
             const int who = __ffsll(past) - 1;
-            seq = __builtin_amdgcn_readfirstlane(base + who);
-            tiles = __builtin_amdgcn_readfirstlane(__shfl(count, who, 64));
-            if (n_seqs >= 64) x = tiles - 1 - __builtin_amdgcn_readfirstlane(t - done - __shfl(upto - mine, who, 64));
+            tiles = __builtin_amdgcn_readlane(count, who);
+            if (P.n_seqs >= 64) x = tiles - 1 - (t - done - __builtin_amdgcn_readlane(upto - mine, who));
+            S.q0 = __builtin_amdgcn_readlane(q0, who);
+            S.k0 = __builtin_amdgcn_readlane(k0, who);
+            S.nq = __builtin_amdgcn_readlane(nq, who);
+            S.nk = __builtin_amdgcn_readlane(nk, who);
+            S.room = __builtin_amdgcn_readlane(room, who);
+            S.shift = S.nk - S.nq;
             return x >= 0 && x < tiles;                           // sums of starts that make no sense may have wrapped
         }
-        done += __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
+        done += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }

@@ -34,9 +34,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = head_at(P, int(blockIdx.x) % P.heads), kv = head / P.group;
-    int i, tile, tiles;
-    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.heads, i, tile, tiles)) return;
-    const Seq S = sequence(P, i);
+    int tile, tiles;
+    Seq S;
+    if (!find_tile<false>(P, 1, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
     const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
     const bool there = query < S.nq;
     const int last_q = min(first + WAVES * 32, S.nq) - 1, last_mine = min(mine + 31, S.nq - 1);
@@ -148,10 +148,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kv = int(blockIdx.x) % P.kv_heads;
-    int i, tile, tiles;
-    if (!find_tile(P.cu_k, P.total_k, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.kv_heads, i, tile, tiles)) return;
+    int tile, tiles;
+    Seq S;
+    if (!find_tile<true>(P, 1, WAVES * 32, int(blockIdx.x) / P.kv_heads, S, tile, tiles)) return;
     tile = tiles - 1 - tile;                                      // a causal prompt's first keys are seen by all that follow
-    const Seq S = sequence(P, i);
     const int first = tile * WAVES * 32, mine = first + wave * 32, key = mine + col;
     // queries that see any key of the workgroup, of this wave: from `begin` on; from `all` on they see all of the wave's
     const int begin = first >= S.nk ? S.nq : P.causal ? min(S.nq, max(0, first - S.shift)) / ROWS * ROWS : 0;

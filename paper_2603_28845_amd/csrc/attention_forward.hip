@@ -169,9 +169,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = head_at(P, int(blockIdx.x) % P.heads);
-    int i, tile, tiles;
-    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, 1, WAVES * 32, int(blockIdx.x) / P.heads, i, tile, tiles)) return;
-    const Seq S = sequence(P, i);
+    int tile, tiles;
+    Seq S;
+    if (!find_tile<false>(P, 1, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
     const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
     const bool there = query < S.nq;
     const int kv = head / P.group;
@@ -226,10 +226,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         acc.settle(top, P.c);
     };
     bring_k(0);
-    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
-    __syncthreads();
     bring_v(0);
     bring_k(1);
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+    __syncthreads();
     int t = 0;
     if (n_mine > 0) {
         float16v s0[KB], s1[KB];
@@ -297,9 +297,9 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kv = int(blockIdx.x) % P.kv_heads, split = int(blockIdx.y);
-    int i, tile, tiles;
-    if (!find_tile(P.cu_q, P.total_q, P.n_seqs, P.group, 32, int(blockIdx.x) / P.kv_heads, i, tile, tiles)) return;
-    const Seq S = sequence(P, i);
+    int tile, tiles;
+    Seq S;
+    if (!find_tile<false>(P, P.group, 32, int(blockIdx.x) / P.kv_heads, S, tile, tiles)) return;
     const int row = tile * 32 + col, query = row / P.group, head = kv * P.group + row % P.group;
     const bool there = query < S.nq;
     const int last_q = min((tile * 32 + 31) / P.group, S.nq - 1), first_q = tile * 32 / P.group;
