@@ -22,7 +22,7 @@ struct Params {
     View q, k, v, o;       // o: output of the forward call, input of the gradients
     View d_o, dq, dk, dv;
     float* lse;            // [heads, total_q], may be null in the forward call
-    float* aux;            // scratch of the gradients: [2, heads, total_q], log-sum-exps in powers of two and d_out . out
+    float* aux;            // scratch of the gradients: [2, heads, total_q], -lse / scale and -d_out . out
     float* part;           // scratch of the split forward call
     const int32_t *cu_q, *cu_k, *len_k;
     int64_t total_q, total_k;
@@ -92,16 +92,21 @@ struct Loader {
     typedef attn::Tile<E, DT> T;
     static constexpr int LOADS = T::bytes(ROWS) / 1024;           // wave-wide loads of 64 chunks
     static constexpr int MINE = (LOADS + WAVES - 1) / WAVES;
-    uint32_t off[MINE];
+    static constexpr int STEP = WAVES * 1024 / T::PITCH;          // rows between two loads of a wave
+    // whole periods of the swizzle: the same columns again, one offset is enough
+    static constexpr bool SAME = STEP % 16 == 0;
+    // out of every range, and stays so with what is added to it (64 rows of 2^24 bytes)
+    static constexpr uint32_t NOWHERE = 0x80000000u;
+    uint32_t off[SAME ? 1 : MINE];
     uint32_t row_bytes, dim_bytes;
     __device__ __forceinline__ void init(int wave, int lane, int64_t token_stride, int dim) {
         row_bytes = uint32_t(token_stride) * T::ESZ;
         dim_bytes = uint32_t(dim) * T::ESZ;
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) {
+        for (int i = 0; i < (SAME ? 1 : MINE); ++i) {
             const int at = (wave + i * WAVES) * 64 + lane, r = at / T::CHUNKS;
             const uint32_t chunk = uint32_t((at % T::CHUNKS) ^ T::swizzle(r)) * 16u;
-            off[i] = chunk < dim_bytes ? uint32_t(r) * row_bytes + chunk : LDS_DMA_OOB;
+            off[i] = chunk < dim_bytes ? uint32_t(r) * row_bytes + chunk : NOWHERE;
         }
     }
     // first: address of the tile's first row (wave-uniform); rows behind `valid` and columns behind the head dimension
@@ -112,7 +117,8 @@ struct Loader {
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, int(range), 0x00020000);
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
-            if (LOADS % WAVES == 0 || wave + i * WAVES < LOADS) lds_load16(lds + uint32_t(wave + i * WAVES) * 1024u, off[i], rsrc);
+            if (LOADS % WAVES == 0 || wave + i * WAVES < LOADS)
+                lds_load16(lds + uint32_t(wave + i * WAVES) * 1024u, SAME ? off[0] + uint32_t(i * STEP) * row_bytes : off[i], rsrc);
     }
 };
 

@@ -16,16 +16,89 @@ struct Pair {
     float p, ds;
 };
 template <class E>
-__device__ __forceinline__ Pair score_grad(const Params& P, int64_t q_row, int head, int64_t k_row, float lse, float delta) {
+__device__ __forceinline__ Pair score_grad(const Params& P, int64_t q_row, int head, int64_t k_row, float minus_lse, float minus_delta) {
     const int kv = head / P.group;
     const float s = dot_rows<E>(at<E>(P.q, q_row, head), at<E>(P.k, k_row, kv), P.dim);
     const float dp = dot_rows<E>(at<E>(P.d_o, q_row, head), at<E>(P.v, k_row, kv), P.dim);
-    const float p = __builtin_amdgcn_exp2f(fmaf(s, P.c, -lse));
-    return {p, p * (dp - delta)};
+    const float p = __builtin_amdgcn_exp2f((s + minus_lse) * P.c);
+    return {p, p * (dp + minus_delta)};
 }
 
-// dq_i = scale sum_j ds_ij k_j for WAVES x 32 queries of one head.  Also leaves lse log2(e) and delta_i = d_out_i . out_i in
-// scratch for the other kernel.
+// Scores of unseen keys to -inf: their probabilities are 0.
+__device__ __forceinline__ void mask(float16v& s, int last, int half) {
+    asm volatile("");                                             // a branch around this stays one
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        if (acc_row(r, half) > last) s[r] = NEG_INF;
+}
+
+// A tile of 64 keys in one stream of instructions, products with their share of the arithmetic beside them and their operands
+// read from LDS some products ahead:
+//   scores and the probabilities' gradients of the first 32 keys
+//   the same of the second 32        | arithmetic of the first
+//   the first's products with k      | arithmetic of the second
+//   the second's products with k
+template <int DT>
+__device__ __forceinline__ void grad_q_tile(float16v (&dq)[DT], const Reader<Bf16, DT>& rd, const char* kt, const char* vt, const Operand<Bf16, DT>& q,
+                                            const Operand<Bf16, DT>& d, float c, float lse, float delta, bool all_seen, int last, int half) {
+    typedef Bf16 E;
+    constexpr int N = 4 * DT, AHEAD = 4, AHEAD_C = 3;             // products of one block with q and with d_out
+    float16v s[2], dp[2];
+    E::Row a[AHEAD], k[AHEAD_C];
+    E::Score ds[4];
+    auto read = [&](int i) {
+        if (i < 2 * N) a[i % AHEAD] = rd.rows(i & 1 ? vt : kt, i / N, (i % N) >> 1);
+    };
+    auto product = [&](int i) {
+        const int b = i / N, x = (i % N) >> 1;
+        if (i & 1) dp[b] = E::mma(a[i % AHEAD], d.x[x], x ? dp[b] : zero16());
+        else s[b] = E::mma(a[i % AHEAD], q.x[x], x ? s[b] : zero16());
+        read(i + AHEAD);
+    };
+    auto read_k = [&](int i) {
+        if (i < N) k[i % AHEAD_C] = columns<DT>(rd, kt, i / DT, i % DT);
+    };
+    auto arithmetic = [&](int b, int i, int n) {                  // entries of block b that belong to slot i of n
+#pragma unroll
+        for (int r = 16 * i / n; r < 16 * (i + 1) / n; ++r) {
+            s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -lse)) * (dp[b][r] - delta);
+            asm volatile("" : "+v"(s[b][r]));                     // here, not where the products need it
+            if (r % 8 == 7) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = s[b][r - 7 + e];
+                ds[2 * b + r / 8] = E::pack(x);
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        product(i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!all_seen) mask(s[0], last, half);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        product(N + i);
+        if (i >= N - AHEAD_C) read_k(i - (N - AHEAD_C));
+        arithmetic(0, i, N);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!all_seen) mask(s[1], last - 32, half);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        dq[i % DT] = E::mma(k[i % AHEAD_C], ds[i / DT], dq[i % DT]);
+        read_k(i + AHEAD_C);
+        if (i < N / 2) arithmetic(1, i, N / 2);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// dq_i = scale sum_j ds_ij k_j for WAVES x 32 queries of one head.  Also leaves in scratch what the other kernel's sums of
+// products begin with: -lse / scale for the scores and -delta_i = -d_out_i . out_i for the probabilities' gradients.
 template <class E, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void grad_q_kernel(const Params P) {
     constexpr int KEYS = 32 * KB<E>;
@@ -71,9 +144,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         if (there) {
             const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
             lse = P.lse[at_q] * LOG2E;
+            if (lse == NEG_INF) lse = -NEG_INF;                   // a query that sees nothing: all its probabilities are 0
             if (half == 0) {
-                P.aux[at_q] = lse;
-                P.aux[int64_t(P.heads) * P.total_q + at_q] = delta;
+                P.aux[at_q] = -lse / P.c;
+                P.aux[int64_t(P.heads) * P.total_q + at_q] = -delta;
             }
         }
     }
@@ -90,20 +164,17 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         if (j >= end_mine) continue;
         const char *kt = lds + buf * 2 * SIZE, *vt = kt + SIZE;
         const bool all_seen = j + KEYS <= end_all;
-#pragma unroll
-        for (int b = 0; b < KB<E>; ++b) {
+        if constexpr (KB<E> == 2) {
+            grad_q_tile<DT>(dq, rd, kt, vt, q, d, P.c, lse, delta, all_seen, last - j, half);
+        } else {
             float16v s = zero16(), dp = zero16();
 #pragma unroll
-            for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(kt, b, x), q.x[x], s);
+            for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(kt, 0, x), q.x[x], s);
 #pragma unroll
-            for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(vt, b, x), d.x[x], dp);
+            for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(vt, 0, x), d.x[x], dp);
+            if (!all_seen) mask(s, last - j, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse)) * (dp[r] - delta);
-            if (!all_seen) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j + 32 * b + acc_row(r, half) > last) s[r] = 0.f;
-            }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 float x[8];
@@ -111,7 +182,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
                 for (int r = 0; r < 8; ++r) x[r] = s[8 * t + r];
                 const typename E::Score ds = E::pack(x);
 #pragma unroll
-                for (int n = 0; n < DT; ++n) dq[n] = mma_t<DT>(rd, kt, 2 * b + t, n, ds, dq[n]);
+                for (int n = 0; n < DT; ++n) dq[n] = mma_t<DT>(rd, kt, t, n, ds, dq[n]);
             }
         }
     }
@@ -123,7 +194,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     }
     for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
         const int r = __ffs(rows) - 1, keys = __shfl(last, r, 64) + 1;
-        const float lse_r = __shfl(lse, r, 64), delta_r = __shfl(delta, r, 64);
+        const float lse_r = __shfl(-lse / P.c, r, 64), delta_r = __shfl(-delta, r, 64);
         const int64_t token = S.q0 + mine + r;
         float sum[2] = {0.f, 0.f};
         for (int j0 = 0; j0 < keys; j0 += 64) {
@@ -135,6 +206,100 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
 #pragma unroll
         for (int e = 0; e < 2; ++e)
             if (lane + 64 * e < P.dim) put<E>(const_cast<char*>(at<E>(P.dq, token, head)), lane + 64 * e, sum[e] * P.scale);
+    }
+}
+
+// A block of 32 queries: scores and the probabilities' gradients, then arithmetic of 8 rows at a time and their products with
+// d_out and with q.  numbers: what the rows' scores begin with, -lse / scale, and 64 further on what their probabilities'
+// gradients begin with, -delta; in an accumulator from the start they cost neither registers nor subtractions.  first: the
+// first row, counted from the block's, that sees this lane's key.  The keys' operands and sums fill three quarters of the registers: what can be had again
+// from a few instructions is not kept.
+template <class E, int DT>
+__device__ __forceinline__ void grad_kv_block(float16v (&dk)[DT], float16v (&dv)[DT], Reader<E, DT>& rd, const char* qt, const char* dt, const float* numbers,
+                                              const Operand<E, DT>& k, const Operand<E, DT>& v, float c, bool all_seen, int first, int half) {
+    typedef Tile<E, DT> T;
+    constexpr int N = 2 * T::STEPS, AHEAD = 2;
+    asm volatile("" : "+v"(rd.row), "+v"(rd.tr));                 // offsets anew, instead of 16 registers for them
+    float16v s, dp;
+    typename E::Row a[AHEAD];
+    auto read = [&](int i) {
+        if (i < N) a[i % AHEAD] = rd.rows(i & 1 ? dt : qt, 0, i >> 1);
+    };
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const float4v x = *reinterpret_cast<const float4v*>(numbers + 8 * g + 4 * half), y = *reinterpret_cast<const float4v*>(numbers + 64 + 8 * g + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s[4 * g + e] = x[e];
+            dp[4 * g + e] = y[e];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int x = i >> 1;
+        if (i & 1) dp = E::mma(a[i % AHEAD], v.x[x], dp);
+        else s = E::mma(a[i % AHEAD], k.x[x], s);
+        read(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!all_seen) {
+        asm volatile("");
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (acc_row(r, half) < first) s[r] = NEG_INF;
+    }
+    auto arithmetic = [&](int r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+        dp[r] *= s[r];
+        asm volatile("" : "+v"(s[r]), "+v"(dp[r]));
+    };
+    auto pack = [&](const float16v& from, int t) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from[8 * t + e];
+        return E::pack(x);
+    };
+#pragma unroll
+    for (int r = 0; r < 8; ++r) arithmetic(r);
+    if constexpr (sizeof(typename E::T) == 2) {
+        constexpr int M = 4 * DT;
+        typename E::Row u[AHEAD];
+        auto read_t = [&](int i) {
+            if (i < M) u[i % AHEAD] = columns<DT>(rd, (i / DT) & 1 ? qt : dt, i / (2 * DT), i % DT);
+        };
+        typename E::Score p = pack(s, 0), ds = pack(dp, 0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) read_t(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            if (i == M / 2) {
+                p = pack(s, 1);
+                ds = pack(dp, 1);
+            }
+            if ((i / DT) & 1) dk[i % DT] = E::mma(u[i % AHEAD], ds, dk[i % DT]);
+            else dv[i % DT] = E::mma(u[i % AHEAD], p, dv[i % DT]);
+            read_t(i + AHEAD);
+            if (i < M / 2) {
+#pragma unroll
+                for (int r = 8 + 16 * i / M; r < 8 + 16 * (i + 1) / M; ++r) arithmetic(r);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+#pragma unroll
+        for (int r = 8; r < 16; ++r) arithmetic(r);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const typename E::Score p = pack(s, t), ds = pack(dp, t);
+#pragma unroll
+            for (int n = 0; n < DT; ++n) dv[n] = mma_t<DT>(rd, dt, t, n, p, dv[n]);
+#pragma unroll
+            for (int n = 0; n < DT; ++n) dk[n] = mma_t<DT>(rd, qt, t, n, ds, dk[n]);
+        }
     }
 }
 
@@ -196,41 +361,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
             const char *qt = lds + buf * BUF, *dt = qt + SIZE;
             const bool all_seen = r0 >= all;
 #pragma unroll
-            for (int b = 0; b < KB<E>; ++b) {
-                asm volatile("" : "+v"(rd.row), "+v"(rd.tr));
-                float16v s = zero16(), dp = zero16();
-#pragma unroll
-                for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(qt, b, x), k.x[x], s);
-#pragma unroll
-                for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(dt, b, x), v.x[x], dp);
-                const float* num = reinterpret_cast<const float*>(dt + SIZE) + 32 * b + 4 * half;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4v lse = *reinterpret_cast<const float4v*>(num + 8 * g), delta = *reinterpret_cast<const float4v*>(num + 64 + 8 * g);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * g + e;
-                        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse[e]));
-                        dp[r] = s[r] * (dp[r] - delta[e]);
-                    }
-                }
-                if (!all_seen) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (r0 + 32 * b + acc_row(r, half) + S.shift < key) s[r] = dp[r] = 0.f;
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    float x[8], y[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) { x[r] = s[8 * t + r]; y[r] = dp[8 * t + r]; }
-                    const typename E::Score p = E::pack(x), ds = E::pack(y);
-#pragma unroll
-                    for (int n = 0; n < DT; ++n) dv[n] = mma_t<DT>(rd, dt, 2 * b + t, n, p, dv[n]);
-#pragma unroll
-                    for (int n = 0; n < DT; ++n) dk[n] = mma_t<DT>(rd, qt, 2 * b + t, n, ds, dk[n]);
-                }
-            }
+            for (int b = 0; b < KB<E>; ++b)
+                grad_kv_block<E, DT>(dk, dv, rd, qt + b * 32 * T::PITCH, dt + b * 32 * T::PITCH, reinterpret_cast<const float*>(qt + 2 * SIZE) + 32 * b, k, v, P.c,
+                                     all_seen, key - S.shift - r0 - 32 * b, half);
         }
         head = next_head;
         r0 = next;
