@@ -132,27 +132,55 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     Operand<E, DT> q, d;
     q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
     d.load(at<E>(P.d_o, S.q0 + query, head), there, P.dim, half);
-    float delta = 0.f, lse = 0.f;
-    {
+    Reader<E, DT> rd;
+    rd.init(lane);
+    const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
+    float delta = 0.f, lse = there ? P.lse[at_q] * LOG2E : 0.f;
+    if (lse == NEG_INF) lse = -NEG_INF;                           // a query that sees nothing: all its probabilities are 0
+    // delta from the output that was stored: with a few keys in a row its rounding to bf16 weighs as much as all others of the
+    // gradient together (short sequences: dq and dk 2.0 times as far off as a single rounding, 1.4 times otherwise).  Where a
+    // workgroup's rows see up to 256 keys, delta_i = sum_j p_ij (d_out_i . v_j) is added up in a pass of its own: one tile in
+    // 36 of a causal prompt of 2048.
+    if (sizeof(typename E::T) == 2 && end <= 256) {
+        for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            __syncthreads();
+            if (j + KEYS < end) bring(j + KEYS, buf ^ 1);
+            if (j >= end_mine) continue;
+#pragma unroll 1
+            for (int b = 0; b < KB<E>; ++b) {
+                const char *kt = lds + buf * 2 * SIZE + b * 32 * T::PITCH, *vt = kt + SIZE;
+                float16v s = zero16(), dp = zero16();
+#pragma unroll
+                for (int x = 0; x < T::STEPS; ++x) {
+                    s = E::mma(rd.rows(kt, 0, x), q.x[x], s);
+                    dp = E::mma(rd.rows(vt, 0, x), d.x[x], dp);
+                }
+                if (j + KEYS > end_all) mask(s, last - j - 32 * b, half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse));
+                    delta += p == 0.f ? 0.f : p * dp[r];          // values that are not seen may be no numbers
+                }
+            }
+        }
+        if (end > 0) {
+            __syncthreads();
+            bring(0, 0);
+        }
+    } else {
         Operand<E, DT> o;
         o.load(at<E>(P.o, S.q0 + query, head), there, P.dim, half);
 #pragma unroll
         for (int s = 0; s < T::STEPS; ++s)
 #pragma unroll
             for (int e = 0; e < E::PER_CHUNK; ++e) delta = fmaf(float(o.x[s][e]), float(d.x[s][e]), delta);
-        delta += other_half(delta);
-        if (there) {
-            const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
-            lse = P.lse[at_q] * LOG2E;
-            if (lse == NEG_INF) lse = -NEG_INF;                   // a query that sees nothing: all its probabilities are 0
-            if (half == 0) {
-                P.aux[at_q] = -lse / P.c;
-                P.aux[int64_t(P.heads) * P.total_q + at_q] = -delta;
-            }
-        }
     }
-    Reader<E, DT> rd;
-    rd.init(lane);
+    delta += other_half(delta);
+    if (there && half == 0) {
+        P.aux[at_q] = -lse / P.c;
+        P.aux[int64_t(P.heads) * P.total_q + at_q] = -delta;
+    }
     float16v dq[DT];
 #pragma unroll
     for (int n = 0; n < DT; ++n) dq[n] = zero16();
