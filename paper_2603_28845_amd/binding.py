@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+import threading
 from typing import Optional, Sequence, Tuple
 
 import torch  # imported before the library so that both share one HIP runtime
@@ -162,24 +164,22 @@ def load_library() -> ctypes.CDLL:
     lib.onecomp_jointq_refine.restype = i32
     lib.onecomp_jointq_workspace_bytes.argtypes = [i64, i64, i32]
     lib.onecomp_jointq_workspace_bytes.restype = sz
-    shape, heads = ctypes.POINTER(AttentionShape), ctypes.POINTER(Heads)
-    lib.onecomp_attention_forward.argtypes = [shape, heads, heads, heads, heads, vp, vp, sz, vp]
+    # structures go by address: an int, or ctypes.byref of the classes above
+    lib.onecomp_attention_forward.argtypes = [vp] * 7 + [sz, vp]
     lib.onecomp_attention_forward.restype = i32
-    lib.onecomp_attention_workspace_bytes.argtypes = [shape]
+    lib.onecomp_attention_workspace_bytes.argtypes = [vp]
     lib.onecomp_attention_workspace_bytes.restype = sz
-    lib.onecomp_attention_backward.argtypes = [shape, heads, heads, heads, heads, vp, heads, heads, heads, heads, vp, sz, vp]
+    lib.onecomp_attention_backward.argtypes = [vp] * 11 + [sz, vp]
     lib.onecomp_attention_backward.restype = i32
-    lib.onecomp_attention_backward_workspace_bytes.argtypes = [shape]
+    lib.onecomp_attention_backward_workspace_bytes.argtypes = [vp]
     lib.onecomp_attention_backward_workspace_bytes.restype = sz
-    rows = ctypes.POINTER(Rows)
-    lib.onecomp_block_norm_forward.argtypes = [ctypes.POINTER(NormShape), rows, rows, vp, vp, vp, vp, rows, rows, rows, vp]
+    lib.onecomp_block_norm_forward.argtypes = [vp] * 11
     lib.onecomp_block_norm_forward.restype = i32
-    lib.onecomp_block_norm_backward.argtypes = [ctypes.POINTER(NormShape), rows, rows, rows, rows, vp, vp, vp, rows,
-                                                ctypes.POINTER(NormGradients), vp, sz, vp]
+    lib.onecomp_block_norm_backward.argtypes = [vp] * 11 + [sz, vp]
     lib.onecomp_block_norm_backward.restype = i32
-    lib.onecomp_block_norm_workspace_bytes.argtypes = [ctypes.POINTER(NormShape)]
+    lib.onecomp_block_norm_workspace_bytes.argtypes = [vp]
     lib.onecomp_block_norm_workspace_bytes.restype = sz
-    lib.onecomp_clip_gradients.argtypes = [ctypes.POINTER(Gradient), i32, f32, vp, vp, sz, vp]
+    lib.onecomp_clip_gradients.argtypes = [vp, i32, f32, vp, vp, sz, vp]
     lib.onecomp_clip_gradients.restype = i32
     lib.onecomp_clip_workspace_bytes.argtypes = []
     lib.onecomp_clip_workspace_bytes.restype = sz
@@ -490,43 +490,88 @@ def onecomp_jointq_refine(W: torch.Tensor, H: torch.Tensor, Q_codes: torch.Tenso
     return {"Q_codes": Q_codes, "scales": scales, "W_hat": W_hat, "objective": objective, "n_moves": n_moves}
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor, shape: Optional[tuple] = None) -> Heads:
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be [tokens, heads, dim]" + (f", here {list(shape)}" if shape is not None else ""))
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} must live on {like.device}")
-    if t.numel() > 0 and t.stride(2) != 1 and t.shape[2] > 1:
+# ---- the block around the linear layers ----------------------------------------------------------------------------
+# These calls are made for single tokens too, where they take less time than ctypes needs to build a structure per tensor.
+# Their structures are packed into one buffer per thread (the library reads them before it returns) and go by address.
+_DTYPE_CODES = {torch.float32: ONECOMP_F32, torch.bfloat16: ONECOMP_BF16}
+_SHAPE = struct.Struct("iiiiiifqqqqPPP")          # onecomp_attention_shape
+_NORM_SHAPE = struct.Struct("iiiiiqqff")          # onecomp_norm_shape
+_GRAD_FIELDS = 4                                  # words of onecomp_gradient
+
+
+class _Buffer(threading.local):
+    def __init__(self):
+        self.data = ctypes.create_string_buffer(1024)
+        self.at = ctypes.addressof(self.data)
+
+
+_buffer = _Buffer()
+
+
+def _raw_stream() -> int:
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _head_fields(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, shape) -> Tuple[int, int, int]:
+    """(address, token stride, head stride) of a [tokens, heads, dim] tensor."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [tokens, heads, dim], here {list(shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}")
+    token, head, one = t.stride()
+    n, h, d = shape
+    if one != 1 and d > 1 and n > 0:
         raise ValueError(f"rows of {name} must be dense")
-    token = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-    return Heads(t.data_ptr(), token, t.stride(1) if t.shape[1] > 1 else t.shape[2])
+    return t.data_ptr(), token if n > 1 else max(token, h * d), head if h > 1 else d
 
 
-def _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k) -> AttentionShape:
-    _dev(q, "q", contiguous=False)
+def _index_address(t: Optional[torch.Tensor], name: str, device: int, n: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}")
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must have {n} entries (cu_q and cu_k: the starts of the sequences and the end)")
+    return t.data_ptr()
+
+
+def _attention_shape(q, k, cu_q, cu_k, max_q, max_k, causal, scale, len_k) -> int:
+    """Packs onecomp_attention_shape to the start of the buffer; returns the device."""
+    if not q.is_cuda:
+        raise ValueError("q must live on the GPU")
+    code = _DTYPE_CODES.get(q.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {q.dtype}: float32 or bfloat16 expected")
     if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
         raise ValueError("shapes: q [tokens, heads, dim], k and v [tokens, key heads, dim]")
-    for t, name in ((cu_q, "cu_q"), (cu_k, "cu_k"), (len_k, "len_k")):
-        if t is not None:
-            _dev(t, name, torch.int32)
-            if t.device != q.device:
-                raise ValueError(f"{name} must live on {q.device}")
-    n = cu_q.numel() - 1
-    if n < 0 or cu_k.numel() != n + 1 or (len_k is not None and len_k.numel() != n):
-        raise ValueError("cu_q and cu_k hold one start per sequence and the end, len_k one length per sequence")
-    return AttentionShape(_dtype_code(q), q.shape[1], k.shape[1], q.shape[2], n, int(bool(causal)),
-                          q.shape[2] ** -0.5 if scale is None else float(scale), q.shape[0], k.shape[0], int(max_q), int(max_k),
-                          cu_q.data_ptr(), cu_k.data_ptr(), len_k.data_ptr() if len_k is not None else None)
+    device, n = q.get_device(), cu_q.numel() - 1
+    if n < 0:
+        raise ValueError("cu_q and cu_k hold one start per sequence and the end")
+    tokens, heads, dim = q.shape
+    _SHAPE.pack_into(_buffer.data, 0, code, heads, k.shape[1], dim, n, 1 if causal else 0, dim ** -0.5 if scale is None else scale, tokens,
+                     k.shape[0], max_q, max_k, _index_address(cu_q, "cu_q", device, n + 1), _index_address(cu_k, "cu_k", device, n + 1),
+                     _index_address(len_k, "len_k", device, n))
+    return device
 
 
-def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[ctypes.c_void_p, int, Optional[torch.Tensor]]:
+def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[int, int, Optional[torch.Tensor]]:
     """Address, size and owner of a call's workspace; allocated here where the caller brought none."""
-    if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
     if workspace is None:
-        return ctypes.c_void_p(0), 0, None
-    return _dev(workspace, "workspace", torch.uint8), workspace.numel(), workspace
+        if need == 0:
+            return 0, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace.data_ptr(), need, workspace
+    return _dev(workspace, "workspace", torch.uint8).value or 0, workspace.numel(), workspace
+
+
+def _lse_address(lse: torch.Tensor, q: torch.Tensor) -> int:
+    if lse.dtype is not torch.float32 or lse.get_device() != q.get_device() or not lse.is_contiguous() or lse.shape != (q.shape[1], q.shape[0]):
+        raise ValueError("lse must be dense float32 [heads, total_q] on the GPU of q")
+    return lse.data_ptr()
 
 
 def onecomp_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
@@ -537,19 +582,20 @@ def onecomp_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     """Attention of packed sequences.  q: [total_q, heads, dim], k, v: [total_k, key heads, dim] bf16/fp32 (any strides with
     dense rows); cu_q, cu_k: int32 starts of the sequences and the end; len_k: int32 keys of each, where its room in k holds
     more; scale: 1 / sqrt(dim) unless given.  Returns (out [total_q, heads, dim], lse [heads, total_q] fp32 or None)."""
-    lib = load_library()
-    s = _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
+    lib = _lib or load_library()
+    device = _attention_shape(q, k, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
+    dtype, shape, k_shape = q.dtype, q.shape, k.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=dtype, device=q.device)
     if lse is None and want_lse:
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    if lse is not None and tuple(lse.shape) != (q.shape[1], q.shape[0]):
-        raise ValueError("lse must be [heads, total_q]")
-    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_attention_workspace_bytes(ctypes.byref(s))), q.device)
-    rc = lib.onecomp_attention_forward(ctypes.byref(s), ctypes.byref(_heads(q, "q", q)), ctypes.byref(_heads(k, "k", q)),
-                                       ctypes.byref(_heads(v, "v", q, tuple(k.shape))),
-                                       ctypes.byref(_heads(out, "out", q, tuple(q.shape))),
-                                       _dev(lse, "lse", torch.float32) if lse is not None else _ptr(None), ws, ws_bytes, _stream())
+        lse = torch.empty((shape[1], shape[0]), dtype=torch.float32, device=q.device)
+    at, base = _SHAPE.size, _buffer.at
+    struct.pack_into("Pqq" * 4, _buffer.data, at, *_head_fields(q, "q", dtype, device, shape), *_head_fields(k, "k", dtype, device, k_shape),
+                     *_head_fields(v, "v", dtype, device, k_shape), *_head_fields(out, "out", dtype, device, shape))
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_attention_workspace_bytes(base), q.device)
+    at += base
+    rc = lib.onecomp_attention_forward(base, at, at + 24, at + 48, at + 72, _lse_address(lse, q) if lse is not None else 0, ws, ws_bytes,
+                                       _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_attention_forward")
     return out, lse
@@ -562,75 +608,81 @@ def onecomp_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Te
                                dv: Optional[torch.Tensor] = None,
                                workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Returns (dq, dk, dv) from the gradient of the forward call's output and from what that call took and returned."""
-    lib = load_library()
-    s = _attention_shape(q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-    if tuple(lse.shape) != (q.shape[1], q.shape[0]):
-        raise ValueError("lse must be [heads, total_q]")
-    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_attention_backward_workspace_bytes(ctypes.byref(s))), q.device)
-    rows = [ctypes.byref(_heads(t, name, q, tuple(like.shape))) for t, name, like in
-            ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q), (d_out, "d_out", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
-    rc = lib.onecomp_attention_backward(ctypes.byref(s), *rows[:4], _dev(lse, "lse", torch.float32), *rows[4:], ws, ws_bytes, _stream())
+    lib = _lib or load_library()
+    device = _attention_shape(q, k, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
+    dtype, shape, k_shape, dev = q.dtype, q.shape, k.shape, q.device
+    dq = torch.empty(shape, dtype=dtype, device=dev) if dq is None else dq
+    dk = torch.empty(k_shape, dtype=dtype, device=dev) if dk is None else dk
+    dv = torch.empty(k_shape, dtype=dtype, device=dev) if dv is None else dv
+    at, base = _SHAPE.size, _buffer.at
+    struct.pack_into("Pqq" * 8, _buffer.data, at, *_head_fields(q, "q", dtype, device, shape), *_head_fields(k, "k", dtype, device, k_shape),
+                     *_head_fields(v, "v", dtype, device, k_shape), *_head_fields(out, "out", dtype, device, shape),
+                     *_head_fields(d_out, "d_out", dtype, device, shape), *_head_fields(dq, "dq", dtype, device, shape),
+                     *_head_fields(dk, "dk", dtype, device, k_shape), *_head_fields(dv, "dv", dtype, device, k_shape))
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_attention_backward_workspace_bytes(base), dev)
+    at += base
+    rc = lib.onecomp_attention_backward(base, at, at + 24, at + 48, at + 72, _lse_address(lse, q), at + 96, at + 120, at + 144, at + 168, ws,
+                                        ws_bytes, _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_attention_backward")
     return dq, dk, dv
 
 
 _NORMS = {"rms": 0, "layer": 1}
-_GATES = {"none": 0, "channel": 1, "rows": 2}
 
 
-def _row_view(t: Optional[torch.Tensor], name: str, like: torch.Tensor):
-    """onecomp_rows of a [rows, width] tensor (None stays None)."""
+def _row_fields(t: Optional[torch.Tensor], name: str, like: torch.Tensor) -> Tuple[int, int]:
+    """(address, row stride) of a [rows, width] tensor; zeros for None."""
     if t is None:
-        return None
-    if t.dim() != 2 or t.shape != like.shape:
+        return 0, 0
+    if t.shape != like.shape:
         raise ValueError(f"{name} must be [rows, width], here {list(like.shape)}")
-    if t.dtype != like.dtype:
+    if t.dtype is not like.dtype:
         raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} must live on {like.device}")
-    if t.numel() > 0 and t.stride(1) != 1 and t.shape[1] > 1:
+    row, one = t.stride()
+    rows, width = t.shape
+    if one != 1 and width > 1 and rows > 0:
         raise ValueError(f"rows of {name} must be dense")
-    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return t.data_ptr(), row if rows > 1 else width
 
 
-def _param(t: Optional[torch.Tensor], name: str, like: torch.Tensor, dtype: torch.dtype) -> ctypes.c_void_p:
+def _param_address(t: Optional[torch.Tensor], name: str, like: torch.Tensor, dtype: Optional[torch.dtype]) -> int:
     if t is None:
-        return ctypes.c_void_p(0)
-    if t.numel() != like.shape[1]:
-        raise ValueError(f"{name} must have {like.shape[1]} entries")
-    if t.device != like.device:
+        return 0
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 1 or t.shape[0] != like.shape[1] or not t.is_contiguous():
+        raise ValueError(f"{name} must have {like.shape[1]} dense entries")
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} must live on {like.device}")
-    return _dev(t, name, dtype)
+    return t.data_ptr()
 
 
-def _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm):
-    """(shape, dtype of the parameters, gate as rows or None); params: dict of the weights and biases."""
-    _dev(h, "h", contiguous=False)
+def _norm_shape(h, weight, bias, post_weight, post_bias, gate, residual_scale, eps, kind, post_norm):
+    """Packs onecomp_norm_shape to the start of the buffer; returns (dtype of the parameters, gate as (address, stride))."""
+    if not h.is_cuda:
+        raise ValueError("h must live on the GPU")
+    code = _DTYPE_CODES.get(h.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {h.dtype}: float32 or bfloat16 expected")
     if h.dim() != 2:
         raise ValueError("h must be [rows, width]")
     if kind not in _NORMS:
         raise ValueError("kind must be 'rms' or 'layer'")
     channel = gate is not None and gate.dim() == 1
-    given = [t for t in list(params.values()) + ([gate] if channel else []) if t is not None]
-    w_dtype = given[0].dtype if given else h.dtype
-    gate_kind = "none" if gate is None else "channel" if channel else "rows"
+    first = next((t for t in (weight, bias, post_weight, post_bias, gate if channel else None) if t is not None), h)
+    w_dtype = first.dtype
+    w_code = _DTYPE_CODES.get(w_dtype)
+    if w_code is None:
+        raise TypeError(f"unsupported dtype {w_dtype} of the parameters: float32 or bfloat16 expected")
     if post_norm is None:
-        post_norm = params["post_weight"] is not None or params["post_bias"] is not None
-    shape = NormShape(_dtype_code(h), ONECOMP_BF16 if w_dtype == torch.bfloat16 else ONECOMP_F32, _NORMS[kind], _GATES[gate_kind], int(bool(post_norm)),
-                      h.shape[0], h.shape[1], float(residual_scale), float(eps))
-    if channel:
-        gate_rows = Rows(_param(gate, "gate", h, w_dtype).value, 0)
-    else:
-        gate_rows = _row_view(gate, "gate", h)
-    return shape, w_dtype, gate_rows
-
-
-def _ref(struct):
-    return ctypes.byref(struct) if struct is not None else None
+        post_norm = post_weight is not None or post_bias is not None
+    rows, width = h.shape
+    _NORM_SHAPE.pack_into(_buffer.data, 0, code, w_code, _NORMS[kind], 0 if gate is None else 1 if channel else 2, 1 if post_norm else 0, rows, width,
+                          residual_scale, eps)
+    return w_dtype, (_param_address(gate, "gate", h, w_dtype), 0) if channel else _row_fields(gate, "gate", h)
 
 
 def onecomp_block_norm_forward(h: torch.Tensor, y: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
@@ -642,9 +694,8 @@ def onecomp_block_norm_forward(h: torch.Tensor, y: Optional[torch.Tensor] = None
     """h' = residual_scale h + gate u with u = y, or norm(y) (post_norm: whether; by default where post_weight or post_bias is
     given), and n = norm(h').  h, y: [rows, width] bf16/fp32 (rows may be strided); weights, biases: [width] of one dtype; gate:
     [width] of that dtype or [rows, width].  Without y h' is h.  Returns (h', n); h_out may be h."""
-    lib = load_library()
-    params = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
-    shape, w_dtype, gate_rows = _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm)
+    lib = _lib or load_library()
+    w_dtype, gate_fields = _norm_shape(h, weight, bias, post_weight, post_bias, gate, residual_scale, eps, kind, post_norm)
     if y is None:
         if h_out is not None:
             raise ValueError("h_out goes with y: without it h' is h")
@@ -652,10 +703,14 @@ def onecomp_block_norm_forward(h: torch.Tensor, y: Optional[torch.Tensor] = None
         h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
     if n is None and want_n:
         n = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-    views = [_row_view(t, name, h) for t, name in ((h, "h"), (y, "y"), (h_out, "h_out"), (n, "n"))]
-    rc = lib.onecomp_block_norm_forward(ctypes.byref(shape), _ref(views[0]), _ref(views[1]),
-                                        *(_param(t, name, h, w_dtype) for name, t in params.items()), _ref(gate_rows), _ref(views[2]),
-                                        _ref(views[3]), _stream())
+    at, base = _NORM_SHAPE.size, _buffer.at
+    struct.pack_into("Pq" * 5, _buffer.data, at, *_row_fields(h, "h", h), *_row_fields(y, "y", h), *gate_fields, *_row_fields(h_out, "h_out", h),
+                     *_row_fields(n, "n", h))
+    at += base
+    rc = lib.onecomp_block_norm_forward(base, at, at + 16 if y is not None else 0, _param_address(weight, "weight", h, w_dtype),
+                                        _param_address(bias, "bias", h, w_dtype), _param_address(post_weight, "post_weight", h, w_dtype),
+                                        _param_address(post_bias, "post_bias", h, w_dtype), at + 32 if gate is not None else 0,
+                                        at + 48 if h_out is not None else 0, at + 64 if n is not None else 0, _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_block_norm_forward")
     return (h if y is None else h_out), n
@@ -670,24 +725,35 @@ def onecomp_block_norm_backward(dn: Optional[torch.Tensor], dh_out: Optional[tor
     """Gradients of onecomp_block_norm_forward from those of n and of h' (either None if there is none); h is the h' that it
     returned.  Returns dict(h, y, weight, bias, post_weight, post_bias, gate), None for what was not given; out: optional dict of
     preallocated tensors of these names."""
-    lib = load_library()
-    params = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
-    shape, w_dtype, gate_rows = _norm_shape(h, y, params, gate, residual_scale, eps, kind, post_norm)
-    given = dict(params, h=h, y=y, gate=gate)
-    res = {name: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) if out is None else out.get(name)
-           for name, t in given.items()}
+    lib = _lib or load_library()
+    w_dtype, gate_fields = _norm_shape(h, weight, bias, post_weight, post_bias, gate, residual_scale, eps, kind, post_norm)
+    res = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias, "h": h, "y": y, "gate": gate}
+    if out is None:
+        for name, t in res.items():
+            if t is not None:
+                res[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    else:
+        for name, t in res.items():
+            if t is not None:
+                res[name] = out.get(name)
     if dn is None:
         res["weight"] = res["bias"] = None
+    d_gate = res["gate"]
     channel = gate is not None and gate.dim() == 1
-    views = {name: _row_view(t, name, h) for name, t in (("dn", dn), ("dh_out", dh_out), ("h", h), ("y", y), ("dh", res["h"]),
-                                                         ("dy", res["y"]), ("dgate", None if channel else res["gate"]))}
-    grads = NormGradients(*(ctypes.pointer(views[name]) if views[name] is not None else None for name in ("dh", "dy", "dgate")),
-                          *(_param(res[name], "gradient of " + name, h, w_dtype) for name in params),
-                          _param(res["gate"] if channel else None, "gradient of gate", h, w_dtype))
-    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_block_norm_workspace_bytes(ctypes.byref(shape))), h.device)
-    rc = lib.onecomp_block_norm_backward(ctypes.byref(shape), _ref(views["dn"]), _ref(views["dh_out"]), _ref(views["h"]), _ref(views["y"]),
-                                         *(_param(params[name], name, h, w_dtype) for name in ("weight", "post_weight", "post_bias")),
-                                         _ref(gate_rows), ctypes.byref(grads), ws, ws_bytes, _stream())
+    rows = (dn, dh_out, h, y, res["h"], res["y"], None if channel else d_gate)
+    fields = [x for t, name in zip(rows, ("dn", "dh_out", "h", "y", "gradient of h", "gradient of y", "gradient of gate")) for x in _row_fields(t, name, h)]
+    at, base = _NORM_SHAPE.size, _buffer.at
+    at += base
+    # behind the shape: seven tensors, the gate, onecomp_norm_gradients
+    struct.pack_into("Pq" * 8 + "8P", _buffer.data, at - base, *fields, *gate_fields,
+                     at + 64 if rows[4] is not None else 0, at + 80 if rows[5] is not None else 0, at + 96 if rows[6] is not None else 0,
+                     *(_param_address(res[name], "gradient of " + name, h, w_dtype) for name in ("weight", "bias", "post_weight", "post_bias")),
+                     _param_address(d_gate, "gradient of gate", h, w_dtype) if channel else 0)
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_block_norm_workspace_bytes(base), h.device)
+    rc = lib.onecomp_block_norm_backward(base, at if dn is not None else 0, at + 16 if dh_out is not None else 0, at + 32,
+                                         at + 48 if y is not None else 0, _param_address(weight, "weight", h, w_dtype),
+                                         _param_address(post_weight, "post_weight", h, w_dtype), _param_address(post_bias, "post_bias", h, w_dtype),
+                                         at + 112 if gate is not None else 0, at + 128, ws, ws_bytes, _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_block_norm_backward")
     return res
@@ -698,24 +764,29 @@ def onecomp_clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, out: 
                            workspace: Optional[torch.Tensor] = None) -> Tuple[Sequence[torch.Tensor], torch.Tensor]:
     """Scales the gradients (dense fp32/bf16 tensors, in any mixture) by min(1, max_norm / (norm + 1e-6)), norm that of all of them
     together: into `out`, or in place.  Returns (out or grads, norm as a device fp32 scalar)."""
-    lib = load_library()
-    to = grads if out is None else out
-    if len(to) != len(grads):
+    lib = _lib or load_library()
+    to, n = grads if out is None else out, len(grads)
+    if len(to) != n:
         raise ValueError("out must have one tensor per gradient")
-    if not grads and norm is None:
+    if n == 0 and norm is None:
         raise ValueError("no gradients: pass norm, so that it is known where it belongs")
-    device = norm.device if norm is not None else grads[0].device
-    table = (Gradient * max(1, len(grads)))()
-    for i, (g, o) in enumerate(zip(grads, to)):
-        if o is not g and (o.dtype != g.dtype or o.numel() != g.numel()):
-            raise ValueError(f"out {i} must have the dtype and size of its gradient")
-        if g.device != device or o.device != device:
-            raise ValueError(f"gradient {i} must live on {device}")
-        table[i] = Gradient(_dev(g, f"gradient {i}").value, _dev(o, f"out {i}").value, g.numel(), _dtype_code(g))
     if norm is None:
-        norm = torch.empty((), dtype=torch.float32, device=device)
-    ws, ws_bytes, _keep = _scratch(workspace, int(lib.onecomp_clip_workspace_bytes()), device)
-    rc = lib.onecomp_clip_gradients(table, len(grads), float(max_norm), _dev(norm, "norm", torch.float32), ws, ws_bytes, _stream())
+        norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+    norm_at = _dev(norm, "norm", torch.float32)
+    device = norm.get_device()
+    table = []
+    for g, o in zip(grads, to):
+        dtype, size, address = g.dtype, g.numel(), g.data_ptr()
+        if g.get_device() != device or not g.is_contiguous() or dtype not in _DTYPE_CODES:
+            raise ValueError(f"gradient {len(table) // _GRAD_FIELDS} must be dense float32 or bfloat16 on {norm.device}")
+        if o is g:
+            table += (address, address, size, _DTYPE_CODES[dtype])
+        else:
+            if o.dtype is not dtype or o.numel() != size or o.get_device() != device or not o.is_contiguous():
+                raise ValueError(f"out {len(table) // _GRAD_FIELDS} must be dense, of the dtype, size and device of its gradient")
+            table += (address, o.data_ptr(), size, _DTYPE_CODES[dtype])
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_clip_workspace_bytes(), norm.device)
+    rc = lib.onecomp_clip_gradients(struct.pack("q" * len(table), *table), n, max_norm, norm_at, ws, ws_bytes, _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_clip_gradients")
     return to, norm

@@ -187,6 +187,41 @@ def test_clip_refusals(lib):
     assert call(ws_bytes=ctypes.c_size_t(lib.onecomp_clip_workspace_bytes() - 1)) == WORKSPACE
 
 
+def test_packed_structures():
+    """The binding packs the structures by format: the same size and places as the header's."""
+    assert binding._SHAPE.size == ctypes.sizeof(binding.AttentionShape) and binding._NORM_SHAPE.size == ctypes.sizeof(binding.NormShape)
+    x = binding.AttentionShape.from_buffer_copy(binding._SHAPE.pack(1, 2, 3, 4, 5, 6, 0.5, 7, 8, 9, 10, 11, 12, 13))
+    assert [getattr(x, f) for f, _ in x._fields_] == [1, 2, 3, 4, 5, 6, 0.5, 7, 8, 9, 10, 11, 12, 13]
+    x = binding.NormShape.from_buffer_copy(binding._NORM_SHAPE.pack(1, 2, 3, 4, 5, 6, 7, 0.5, 0.25))
+    assert [getattr(x, f) for f, _ in x._fields_] == [1, 2, 3, 4, 5, 6, 7, 0.5, 0.25]
+    assert (ctypes.sizeof(binding.Heads), ctypes.sizeof(binding.Rows), ctypes.sizeof(binding.Gradient)) == (24, 16, 8 * binding._GRAD_FIELDS)
+
+
+def test_structures_against_the_compiler(tmp_path):
+    """Sizes and offsets of the header's structures as a C compiler lays them out."""
+    import shutil
+    import subprocess
+    gcc = shutil.which("gcc")
+    if gcc is None:
+        pytest.skip("no C compiler")
+    names = {"onecomp_heads": binding.Heads, "onecomp_attention_shape": binding.AttentionShape, "onecomp_rows": binding.Rows,
+             "onecomp_norm_shape": binding.NormShape, "onecomp_norm_gradients": binding.NormGradients, "onecomp_gradient": binding.Gradient}
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "onecomp.h"', "int main(void) {"]
+    for name, cls in names.items():
+        lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
+        lines += [f'printf("{name}.{f} %zu\\n", offsetof({name}, {f}));' for f, _ in cls._fields_]
+    src = tmp_path / "sizes.c"
+    src.write_text("\n".join(lines + ["return 0;", "}"]).replace("\\\\", "\\"))
+    import os
+    inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run([gcc, "-I", inc, str(src), "-o", str(tmp_path / "sizes")], check=True)
+    said = dict(l.split() for l in subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.splitlines())
+    for name, cls in names.items():
+        assert int(said[name]) == ctypes.sizeof(cls)
+        for f, _ in cls._fields_:
+            assert int(said[f"{name}.{f}"]) == getattr(cls, f).offset, f
+
+
 def test_binding_checks():
     x = torch.zeros(4, 8)
     for call in (lambda: og.onecomp_block_norm_forward(x), lambda: og.onecomp_block_norm_backward(x, x, x), lambda: og.onecomp_clip_gradients([x], 1.0)):
