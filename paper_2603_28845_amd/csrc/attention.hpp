@@ -215,14 +215,24 @@ __device__ __forceinline__ int wave_max(int x) {
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// The t-th tile of `size` rows of all sequences, queries or (KEYS) keys with the room behind them: its sequence, its number x
-// there and how many the sequence has; false if there are fewer.  `mul` rows stand for each row (heads of a group that are
-// packed into rows).  What the arrays say is cut to the tensors' rows.  Of up to 63 sequences the tiles come by their number
+// Few rows: keys of one piece of work.  Runs of P.run or, where the host knew of fewer keys than there are, as many as it
+// takes for P.splits runs to cover them all.
+__device__ __forceinline__ int run_of(const Params& P, int nk) { return max(P.run, (nk + P.splits * 128 - 1) / (P.splits * 128) * 128); }
+__device__ __forceinline__ int runs_of(const Params& P, int nk) {
+    const int run = run_of(P, nk);
+    return max(1, (nk + run - 1) / run);
+}
+
+// What is counted: tiles of `size` queries, tiles of `size` keys with the room behind them, or pieces of work of few rows
+// (blocks of 32 rows, of which every query has one per head of a group, times runs of keys).
+enum What { QUERIES, KEYS, PIECES };
+
+// The t-th of all sequences: its sequence, its number x there and how many the sequence has; false if there are fewer.  What the arrays say is cut to the tensors' rows.  Of up to 63 sequences the tiles come by their number
 // x, the largest first and at the same x by sequence: x + 1 tiles of keys lie before a causal prompt's tile x, so that long
 // work starts early and the last workgroups are short.  Of more, one sequence after the other, each from its largest x down:
 // counting by number would read the arrays many times.  Every lane of a wave takes part and gets the same answer.
-template <bool KEYS>
-__device__ __forceinline__ bool find_tile(const Params& P, int mul, int size, int t, Seq& S, int& x, int& tiles) {
+template <What WHAT>
+__device__ __forceinline__ bool find_tile(const Params& P, int size, int t, Seq& S, int& x, int& tiles) {
     const int lane = threadIdx.x & 63;
     int done = 0;
     for (int base = 0; base <= P.n_seqs; base += 64) {
@@ -232,7 +242,8 @@ __device__ __forceinline__ bool find_tile(const Params& P, int mul, int size, in
             nq = rows_of(P.cu_q, P.total_q, P.n_seqs, i, q0);
             room = rows_of(P.cu_k, P.total_k, P.n_seqs, i, k0);
             nk = i == P.n_seqs ? 0 : P.len_k ? int(clamp64(P.len_k[i], 0, room)) : room;
-            count = int((int64_t(KEYS ? room : nq) * mul + size - 1) / size);
+            if (WHAT == PIECES) count = int((int64_t(nq) * P.group + 31) / 32) * runs_of(P, nk);
+            else count = int((int64_t(WHAT == KEYS ? room : nq) + size - 1) / size);
         }
         int mine = count;                                         // tiles of this lane's sequence among those looked at
         if (P.n_seqs < 64) {

@@ -1,5 +1,6 @@
 // Attention of packed sequences, forward: o_i = sum_j exp(s_ij - lse_i) v_j, s_ij = scale q_i . k_j.
 #include "attention.hpp"
+#include <cmath>
 
 namespace onecomp {
 namespace attn {
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int head = head_at(P, int(blockIdx.x) % P.heads);
     int tile, tiles;
     Seq S;
-    if (!find_tile<false>(P, 1, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
+    if (!find_tile<QUERIES>(P, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
     const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
     const bool there = query < S.nq;
     const int kv = head / P.group;
@@ -275,20 +276,30 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
 // ---- few rows -----------------------------------------------------------------------------------------------------------
 // One or a few new tokens per sequence: the rows of a group's heads lie side by side in the 32 columns (row = query x group +
 // head), so that keys and values are read once for all of them, and the keys are the work that is shared out: a workgroup has
-// a run of them, its waves take tiles of 32 in turn, each through LDS of its own.  Nothing is multiplied that could be the
-// bound; it is bytes in flight, one tile of each wave at a time.
+// a run of them, its waves take tiles of 32 in turn, each through LDS of its own.  The products are no bound here; bytes in
+// flight are, one tile of each wave at a time, and what a workgroup takes to begin and end.
 template <class E, int DT>
 struct Few {
     typedef attn::Tile<E, DT> T;
     static constexpr int SIZE = T::bytes(32);
-    static constexpr int WAVES = 4 * SIZE * 4 <= 128 * 1024 ? 4 : 2;   // two tiles of keys and of values per wave
+    // two tiles of keys and of values per wave; 64 KB, so that one workgroup begins or ends beside another's work
+    static constexpr int WAVES = SIZE >= 16 * 1024 ? 1 : SIZE >= 8 * 1024 ? 2 : 4;
     static constexpr int LDS = 4 * SIZE * WAVES;
     static constexpr int COLS = 32 * DT;                               // of a partial sum's row
     static_assert(LDS >= WAVES * DT * 4096 + WAVES * 256, "the waves' sums meet in the same memory");
 };
 
-// Keys of one workgroup: runs of `run` or, where the host knew of fewer keys than there are, as many as cover them all.
-__device__ __forceinline__ int run_of(const Params& P, int nk) { return max(P.run, (nk + P.splits * 128 - 1) / (P.splits * 128) * 128); }
+// Scratch: runs of each row [rows], maximum and sum of each run [splits, rows, 2], its sums of values [splits, rows, COLS].
+struct Parts {
+    int32_t* runs;
+    float *tops, *sums;
+    __device__ __forceinline__ Parts(const Params& P) {
+        const int64_t rows = int64_t(P.heads) * P.total_q;
+        runs = reinterpret_cast<int32_t*>(P.part);
+        tops = P.part + (rows + 63) / 64 * 64;
+        sums = tops + 2 * P.splits * rows;
+    }
+};
 
 template <class E, int DT>
 __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(const Params P) {
@@ -296,15 +307,19 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     extern __shared__ __align__(1024) char lds[];
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kv = int(blockIdx.x) % P.kv_heads, split = int(blockIdx.y);
-    int tile, tiles;
+    const Parts parts(P);
+    // pieces of work in turn, whatever number of workgroups the host thought enough
+    for (int piece = blockIdx.x;; piece += gridDim.x) {
+    const int kv = piece % P.kv_heads;
+    int x, pieces;
     Seq S;
-    if (!find_tile<false>(P, P.group, 32, int(blockIdx.x) / P.kv_heads, S, tile, tiles)) return;
+    if (!find_tile<PIECES>(P, 0, piece / P.kv_heads, S, x, pieces)) return;
+    const int run = run_of(P, S.nk), runs = runs_of(P, S.nk), tile = x / runs, split = x % runs;
     const int row = tile * 32 + col, query = row / P.group, head = kv * P.group + row % P.group;
     const bool there = query < S.nq;
     const int last_q = min((tile * 32 + 31) / P.group, S.nq - 1), first_q = tile * 32 / P.group;
     const int seen = P.causal ? max(0, min(S.nk, last_q + 1 + S.shift)) : S.nk;
-    const int run = run_of(P, S.nk), begin = split * run, end = min(seen, begin + run);
+    const int begin = split * run, end = min(seen, begin + run);
     const int end_all = P.causal ? min(S.nk, first_q + 1 + S.shift) : S.nk;
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
 
@@ -384,7 +399,7 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
             if (whole) {
                 store_column<E>(const_cast<char*>(at<E>(P.o, S.q0 + query, head)), o, out, n, P.dim, half);
             } else {
-                char* to = reinterpret_cast<char*>(P.part + 2 * P.splits * rows + (split * rows + at_row) * F::COLS);
+                char* to = reinterpret_cast<char*>(parts.sums + (split * rows + at_row) * F::COLS);
                 store_column<F32>(to, o, 1.f, n, F::COLS, half);
             }
         }
@@ -400,17 +415,20 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
                 const int d = lane + 64 * e;
                 if (d / 32 != n) continue;
                 if (whole && d < P.dim) put<E>(const_cast<char*>(at<E>(P.o, token, h)), d, sum[e] * g);
-                if (!whole) P.part[2 * P.splits * rows + (split * rows + int64_t(h) * P.total_q + token) * F::COLS + d] = sum[e];
+                if (!whole) parts.sums[(split * rows + int64_t(h) * P.total_q + token) * F::COLS + d] = sum[e];
             }
         }
     }
     if (there && wave == 0 && half == 0) {
         if (!whole) {
-            P.part[2 * (split * rows + at_row)] = top;
-            P.part[2 * (split * rows + at_row) + 1] = l;
+            if (split == 0) parts.runs[at_row] = runs;
+            parts.tops[2 * (split * rows + at_row)] = top;
+            parts.tops[2 * (split * rows + at_row) + 1] = l;
         } else if (P.lse) {
             P.lse[at_row] = l == 0.f ? NEG_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
         }
+    }
+    __syncthreads();                                              // the next piece's tiles go where the sums met
     }
 }
 
@@ -423,20 +441,24 @@ __global__ __launch_bounds__(256) void join_kernel(const Params P) {
     if (row >= rows) return;
     const int head = int(row / P.total_q);
     const int64_t token = row - int64_t(head) * P.total_q;
+    const Parts parts(P);
+    const int runs = min(parts.runs[row], P.splits);
     float top = NEG_INF;
-    for (int s = lane; s < P.splits; s += 64) top = fmaxf(top, P.part[2 * (s * rows + row)]);
-    top = wave_max(top);
+    for (int s = lane; s < runs; s += 64) top = fmaxf(top, parts.tops[2 * (s * rows + row)]);
+    top = onecomp::wave_max(top);
     const float zero = top == NEG_INF ? 0.f : top;
     float l = 0.f, o0 = 0.f, o1 = 0.f;
-    const float* sums = P.part + 2 * P.splits * rows;
-    for (int s = 0; s < P.splits; ++s) {
-        const float m = P.part[2 * (s * rows + row)], n = P.part[2 * (s * rows + row) + 1];
-        if (n == 0.f) continue;                                   // a run behind the row's keys: nothing was written for it but this
+#pragma unroll 4
+    for (int s = 0; s < runs; ++s) {
+        const float m = parts.tops[2 * (s * rows + row)], n = parts.tops[2 * (s * rows + row) + 1];
+        const float* from = parts.sums + (s * rows + row) * COLS;
+        // a run behind the row's keys has no sums, only n = 0
+        const float x0 = lane < COLS ? from[lane] : 0.f, x1 = DT > 2 && lane + 64 < COLS ? from[lane + 64] : 0.f;
+        if (n == 0.f) continue;
         const float f = __builtin_amdgcn_exp2f(m - zero);
         l = fmaf(f, n, l);
-        const float* from = sums + (s * rows + row) * COLS;
-        if (lane < COLS) o0 = fmaf(f, from[lane], o0);
-        if (DT > 2 && lane + 64 < COLS) o1 = fmaf(f, from[lane + 64], o1);
+        o0 = fmaf(f, x0, o0);
+        o1 = fmaf(f, x1, o1);
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
     char* to = const_cast<char*>(at<E>(P.o, token, head));
@@ -460,15 +482,22 @@ onecomp_status launch_forward(const Params& P, hipStream_t stream) {
     return ONECOMP_OK;
 }
 
+// blocks of 32 rows (a group's heads of a query) for each head of keys, about
+int64_t row_blocks(const Params& P) {
+    const int64_t most = ceil_div(P.total_q * P.group, 32) + P.n_seqs, even = ceil_div(P.max_q * P.group, 32) * P.n_seqs;
+    return most < even || even < 1 ? most : even;
+}
+
 template <class E, int DT>
 onecomp_status launch_few(const Params& P, hipStream_t stream) {
     typedef Few<E, DT> F;
     static std::atomic<uint64_t> done{0};
     const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(few_rows_kernel<E, DT>), F::LDS, done);
     if (st != ONECOMP_OK) return st;
-    const int64_t grid = (P.total_q * P.group / 32 + P.n_seqs + 1) * P.kv_heads, rows = P.total_q * P.heads;
-    if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
-    few_rows_kernel<E, DT><<<dim3(unsigned(grid), unsigned(P.splits)), dim3(F::WAVES * 64), F::LDS, stream>>>(P);
+    const int64_t rows = P.total_q * P.heads;
+    int64_t grid = row_blocks(P) * (P.splits > 1 ? ceil_div(P.total_k, int64_t(P.run) * (P.n_seqs < 1 ? 1 : P.n_seqs)) + 1 : 1) * P.kv_heads;
+    grid = grid > 16384 ? 16384 : grid;                           // workgroups go on to further pieces
+    few_rows_kernel<E, DT><<<dim3(unsigned(grid)), dim3(F::WAVES * 64), F::LDS, stream>>>(P);
     ONECOMP_CHECK_LAUNCH();
     if (P.splits > 1) {
         join_kernel<E, DT><<<dim3(unsigned((rows + 3) / 4)), dim3(256), 0, stream>>>(P);
@@ -477,17 +506,22 @@ onecomp_status launch_few(const Params& P, hipStream_t stream) {
     return ONECOMP_OK;
 }
 
-// How the keys are shared out where there are few rows; splits = 0: whole prompts.
+// How the keys are shared out where there are few rows; splits = 0: whole prompts.  Estimates in microseconds from
+// measurements at 128 wide bf16 heads: 0.8 for 64 keys of a prompt's tile of 128 rows, two of them at a time on each CU, and
+// 0.6 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join.
 void plan(Params& P) {
     P.splits = P.run = 0;
-    if (P.max_q * P.group > 64) return;
-    // runs of keys: enough of them to keep four workgroups per CU busy, none shorter than 256
-    const int64_t all = P.total_k * P.kv_heads;
-    int64_t run = align_up(size_t(ceil_div(all, 1024)), 128);
-    run = run < 256 ? 256 : run;
-    int64_t splits = ceil_div(P.max_k, run);
+    const double tiles = double(P.heads) * (double(P.total_q) / 128 + P.n_seqs), blocks = double(row_blocks(P)) * P.kv_heads;
+    const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * 0.8 + 5;
+    const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * 0.6 + 12;
+    if (P.max_q * P.group > 32 && few > prompt) return;
+    // pieces of work for every CU to have a few, none shorter than 256 keys
+    const double each = double(P.total_k) / (P.n_seqs < 1 ? 1 : P.n_seqs);
+    double run = ceil(blocks * each / 1536 / 128) * 128;
+    run = run < 256 ? 256 : run > (1 << 30) ? (1 << 30) : run;
+    const int64_t splits = ceil_div(P.max_k, int64_t(run));
     P.splits = int(splits < 1 ? 1 : splits > 256 ? 256 : splits);
-    P.run = int(run > (1 << 30) ? (1 << 30) : run);
+    P.run = int(run);
 }
 
 template <class E, int DT>
@@ -502,7 +536,8 @@ size_t forward_workspace_bytes(const Params& in) {
     plan(P);
     if (P.splits < 2) return 0;
     const size_t cols = size_t(P.dim + 31) / 32 * 32;
-    return align_up(size_t(P.splits) * size_t(P.total_q) * P.heads * (2 + cols) * 4, 256);
+    const size_t rows = size_t(P.total_q) * P.heads;
+    return align_up((align_up(rows, 64) + P.splits * rows * (2 + cols)) * 4, 256);
 }
 
 onecomp_status forward_run(onecomp_dtype dtype, const Params& in, hipStream_t stream) {
