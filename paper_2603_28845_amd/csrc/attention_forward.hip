@@ -515,9 +515,10 @@ void plan(Params& P) {
     const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * 0.8 + 5;
     const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * 0.6 + 12;
     if (P.max_q * P.group > 32 && few > prompt) return;
-    // pieces of work for every CU to have a few, none shorter than 256 keys
+    // four pieces of work for each CU, none shorter than 256 keys: 32 requests of 100 to 16384 keys 100 us, with half as many again
+    // 106, with 768 in all 105
     const double each = double(P.total_k) / (P.n_seqs < 1 ? 1 : P.n_seqs);
-    double run = ceil(blocks * each / 1536 / 128) * 128;
+    double run = ceil(blocks * each / 1024 / 128) * 128;
     run = run < 256 ? 256 : run > (1 << 30) ? (1 << 30) : run;
     const int64_t splits = ceil_div(P.max_k, int64_t(run));
     P.splits = int(splits < 1 ? 1 : splits > 256 ? 256 : splits);

@@ -186,24 +186,30 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params
     Pt::store(P.n, row, width, t, there, x);
 }
 
-// d to the gradient of the rows in front of a norm: inv (d - x mean(d x) - mean(d)), x the normalised row; the last for layer
-// norms only
+// Subtracts the mean of x, and of y too if it goes through a norm, from their entries.
 template <class Pt, int G, int THREADS>
-__device__ __forceinline__ void norm_gradient(float (&d)[Pt::E], const float (&x)[Pt::E], float inv, bool layer, int width, int t, float* lds, int& slot) {
+__device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], bool both, int width, int t, float* lds, int& slot) {
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < Pt::E; ++e) {
-        s[0] = fmaf(d[e], x[e], s[0]);
-        s[1] += d[e];
+        s[0] += x[e];
+        s[1] += y[e];
     }
     group_sum<2, G, THREADS>(s, lds, slot);
-    const float along = s[0] / float(width), mean = layer ? s[1] / float(width) : 0.f;
+    const float mx = s[0] / float(width), my = both ? s[1] / float(width) : 0.f;
 #pragma unroll
-    for (int e = 0; e < Pt::E; ++e) d[e] = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? inv * (d[e] - mean - x[e] * along) : 0.f;
+    for (int e = 0; e < Pt::E; ++e) {
+        const bool in = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width;
+        x[e] = in ? x[e] - mx : 0.f;
+        y[e] = in ? y[e] - my : 0.f;
+    }
 }
 
 // A workgroup takes rows in turn (as many at a time as it has groups of G threads) and keeps the parameters' gradients, sums
 // over rows, in registers until its last row; then its groups' sums meet in LDS and go to scratch, one row per workgroup.
+// With x^ = x inv the normalised row, the gradient of the rows in front of a norm is inv (d - x^ mean(d x^) - mean(d)), the
+// last for layer norms only.  Both norms' squares and the first norm's means are added up in one go (mean(d x^) =
+// inv mean(d x)), the second norm's means in another; layer norms take one more for the means of the rows.
 template <class T, int NV, int G, bool LAYER>
 __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
@@ -214,6 +220,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     int slot = 0;
     const int t = threadIdx.x % G, group = threadIdx.x / G;
     const int width = P.width;
+    const float inv_width = 1.f / float(width);
     float sums[5][E];     // weight, bias, post_weight, post_bias, gate
 #pragma unroll
     for (int i = 0; i < 5; ++i)
@@ -222,47 +229,64 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     for (int64_t first = int64_t(blockIdx.x) * GROUPS; first < P.rows; first += int64_t(gridDim.x) * GROUPS) {
         const int64_t row = first + group;
         const bool there = row < P.rows;
-        float d[E];       // the gradient of h'
+        float x[E], y[E], dn[E], d[E];                            // h', the block's output, gradients of n and of h'
+        Pt::load(x, P.h, row, width, t, there && P.dn.p);
+        Pt::load(dn, P.dn, row, width, t, there && P.dn.p);
         Pt::load(d, P.dh_out, row, width, t, there && P.dh_out.p);
+        Pt::load(y, P.y, row, width, t, there && P.y.p);
+        if (LAYER) {
+            centre<Pt, G, THREADS>(x, y, P.post, width, t, lds, slot);
+        }
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, w[E];                  // x^2, dn w x, dn w, y^2
+        if (P.weight) {
+            Pt::parameter(w, P.weight, P.w_bf16, width, t);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = 1.f;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            s[0] = fmaf(x[e], x[e], s[0]);
+            s[1] = fmaf(dn[e] * w[e], x[e], s[1]);
+            if (LAYER) s[2] = fmaf(dn[e], w[e], s[2]);
+            s[3] = fmaf(y[e], y[e], s[3]);
+        }
+        group_sum<4, G, THREADS>(s, lds, slot);
+        const float inv_y = 1.f / sqrtf(fmaf(s[3], inv_width, P.eps));
         if (P.dn.p) {
-            float x[E], dn[E], w[E];
-            Pt::load(x, P.h, row, width, t, there);
-            Pt::load(dn, P.dn, row, width, t, there);
-            const float inv = normalise<Pt, G, THREADS>(x, LAYER, width, P.eps, t, lds, slot);
-            if (P.weight) Pt::parameter(w, P.weight, P.w_bf16, width, t);
+            const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)), along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                sums[0][e] = fmaf(dn[e], x[e], sums[0][e]);
+                const float hat = x[e] * inv;
+                sums[0][e] = fmaf(dn[e], hat, sums[0][e]);
                 if (LAYER) sums[1][e] += dn[e];
-                if (P.weight) dn[e] *= w[e];
+                d[e] += inv * (dn[e] * w[e] - mean - hat * along);
             }
-            norm_gradient<Pt, G, THREADS>(dn, x, inv, LAYER, width, t, lds, slot);
-#pragma unroll
-            for (int e = 0; e < E; ++e) d[e] += dn[e];
         }
-        {
+        if (P.dh.p) {
             float dh[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) dh[e] = P.scale * d[e];
-            if (P.dh.p) Pt::store(P.dh, row, width, t, there, dh);
+            Pt::store(P.dh, row, width, t, there, dh);
         }
         if (!P.y.p) continue;
-        float x[E], u[E], inv = 0.f;
-        Pt::load(x, P.y, row, width, t, there);
-        if (P.post) inv = normalise<Pt, G, THREADS>(x, LAYER, width, P.eps, t, lds, slot);
-        if (P.gate.p) {
-            float g[E];
+        if (P.post) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) u[e] = x[e];
+            for (int e = 0; e < E; ++e) y[e] *= inv_y;
+        }
+        if (P.gate.p) {
+            float u[E], g[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) u[e] = y[e];
             if (P.post) affine<Pt>(u, P.post_weight, P.post_bias, P.w_bf16, width, t);
 #pragma unroll
             for (int e = 0; e < E; ++e) u[e] *= d[e];
             if (P.gate_rows) {
-                if (P.dgate.p) Pt::store(P.dgate, row, width, t, there, u);
                 Pt::load(g, P.gate, row, width, t, there);
+                if (P.dgate.p) Pt::store(P.dgate, row, width, t, there, u);
             } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) sums[4][e] += u[e];
+                for (int e = 0; e < E; ++e) sums[4][e] += there ? u[e] : 0.f;
                 Pt::parameter(g, P.gate.p, P.w_bf16, width, t);
             }
 #pragma unroll
@@ -271,11 +295,20 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         if (P.post) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                sums[2][e] = fmaf(d[e], x[e], sums[2][e]);
-                if (LAYER) sums[3][e] += d[e];
+                sums[2][e] = fmaf(d[e], y[e], sums[2][e]);
+                if (LAYER) sums[3][e] += there ? d[e] : 0.f;
             }
             if (P.post_weight) affine<Pt>(d, P.post_weight, nullptr, P.w_bf16, width, t);
-            norm_gradient<Pt, G, THREADS>(d, x, inv, LAYER, width, t, lds, slot);
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                m[0] = fmaf(d[e], y[e], m[0]);
+                if (LAYER) m[1] += Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? d[e] : 0.f;
+            }
+            group_sum<2, G, THREADS>(m, lds, slot);
+            const float along = m[0] * inv_width, mean = m[1] * inv_width;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = inv_y * (d[e] - mean - y[e] * along);
         }
         if (P.dy.p) Pt::store(P.dy, row, width, t, there, d);
     }
