@@ -1,6 +1,7 @@
 // The norms around a block, fused with its gate and residual: h' = r h + g u, n = norm(h'), u = y or norm(y), and their
 // gradients.  Every tensor is read once and written once; rows stay in registers between the sums that a norm needs.
 #include "block.hpp"
+#include <type_traits>
 
 namespace onecomp {
 namespace block {
@@ -12,6 +13,42 @@ struct Part {
     typedef T_ T;
     static constexpr int VEC = 16 / int(sizeof(T)), E = VEC * NV;
     static __device__ __forceinline__ int col(int t, int v) { return VEC * (t + G * v); }
+    // A row on its way: loads whose values nobody has asked for yet.
+    struct Raw {
+        uint4v v[NV];
+    };
+    static __device__ __forceinline__ void fetch(Raw& x, const Rows& r, int64_t row, int width, int t, bool there) {
+        const T* p = static_cast<const T*>(r.p) + row * r.stride;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = col(t, v);
+            uint4v y = {0u, 0u, 0u, 0u};
+            if (there && c + VEC <= width) {
+                y = *reinterpret_cast<const uint4u*>(p + c);
+            } else if (there && c < width) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    if (c + i >= width) continue;
+                    if (sizeof(T) == 2) y[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[c + i]) << (16 * (i & 1));
+                    else y[i & 3] = reinterpret_cast<const uint32_t*>(p)[c + i];
+                }
+            }
+            x.v[v] = y;
+        }
+    }
+    static __device__ __forceinline__ void values(float (&x)[E], const Raw& r) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (sizeof(T) == 2) {
+                    x[v * VEC + 2 * i] = bf16_value(r.v[v][i] & 0xffffu);
+                    x[v * VEC + (2 * i + 1) % VEC] = __uint_as_float(r.v[v][i] & 0xffff0000u);
+                } else {
+                    x[v * VEC + i] = __uint_as_float(r.v[v][i]);
+                }
+            }
+    }
     // zeros behind the width
     static __device__ __forceinline__ void load(float (&x)[E], const Rows& r, int64_t row, int width, int t, bool there) {
         const T* p = static_cast<const T*>(r.p) + row * r.stride;
@@ -81,37 +118,51 @@ struct Part {
     }
 };
 
-// Sums of K numbers over the G threads of each group of a workgroup.  `slot` alternates between two places in LDS, so that one
-// barrier a sum is enough.  Every thread of the workgroup takes part.
+// Sum over the lanes up to each: the last lane has the whole wave's.  In the vector pipe; shuffles would take a trip through
+// LDS for each of the six steps.
+__device__ __forceinline__ float lane_sum(float x) {
+    auto moved = [](float v, auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    using std::integral_constant;
+    x += moved(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+    x += moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return x;
+}
+
+// Sums of K numbers (up to 4) over the G threads of each group of a workgroup.  `slot` alternates between two places in LDS, so
+// that one barrier a sum is enough.  Every thread of the workgroup takes part.
 template <int K, int G, int THREADS>
-__device__ __forceinline__ void group_sum(float (&x)[K], float* lds, int& slot) {
+__device__ __forceinline__ void group_sum(float (&x)[K], float4v* lds, int& slot) {
+    float4v all = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) all[k] = lane_sum(x[k]);
+    if (G == 64) {
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) x[k] += __shfl_xor(x[k], o, 64);
-    if (G > 64) {
-        constexpr int WAVES = THREADS / 64, EACH = G / 64;
-        float* to = lds + slot * 4 * WAVES;
-        slot ^= 1;
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) to[k * WAVES + wave] = x[k];
-        }
-        __syncthreads();
-        const int first = wave / EACH * EACH;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            x[k] = 0.f;
-#pragma unroll
-            for (int w = 0; w < EACH; ++w) x[k] += to[k * WAVES + first + w];
-        }
+        for (int k = 0; k < K; ++k) x[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(all[k]), 63));
+        return;
     }
+    constexpr int WAVES = THREADS / 64, EACH = G / 64;
+    float4v* to = lds + slot * WAVES;
+    slot ^= 1;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) to[wave] = all;
+    __syncthreads();
+    const float4v* from = to + wave / EACH * EACH;
+    all = from[0];
+#pragma unroll
+    for (int w = 1; w < EACH; ++w) all += from[w];
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = all[k];
 }
 
 // x to (x - mean) / size in place: size^2 = mean of squares + eps; the mean for layer norms only
 template <class Pt, int G, int THREADS>
-__device__ __forceinline__ float normalise(float (&x)[Pt::E], bool layer, int width, float eps, int t, float* lds, int& slot) {
+__device__ __forceinline__ float normalise(float (&x)[Pt::E], bool layer, int width, float eps, int t, float4v* lds, int& slot) {
     const float inv_width = 1.f / float(width);
     if (layer) {
         float s[1] = {0.f};
@@ -152,10 +203,10 @@ template <class T, int NV, int G>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params P) {
     constexpr int THREADS = G < 256 ? 256 : G;
     typedef Part<T, NV, G> Pt;
-    __shared__ float lds[2 * 4 * (THREADS / 64)];
+    __shared__ float4v lds[2 * (THREADS / 64)];
     int slot = 0;
     const int t = threadIdx.x % G;
-    const int64_t row = int64_t(blockIdx.x) * (THREADS / G) + threadIdx.x / G;
+    const int64_t row = int64_t(blockIdx.x) * (THREADS / G) + __builtin_amdgcn_readfirstlane(threadIdx.x / G);   // the same in a whole wave
     const bool there = row < P.rows;
     const int width = P.width;
     float x[Pt::E];
@@ -188,7 +239,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params
 
 // Subtracts the mean of x, and of y too if it goes through a norm, from their entries.
 template <class Pt, int G, int THREADS>
-__device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], bool both, int width, int t, float* lds, int& slot) {
+__device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], bool both, int width, int t, float4v* lds, int& slot) {
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < Pt::E; ++e) {
@@ -215,10 +266,10 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
     typedef Part<T, NV, G> Pt;
     constexpr int E = Pt::E;
-    __shared__ float lds[2 * 4 * (THREADS / 64)];
+    __shared__ float4v lds[2 * (THREADS / 64)];
     __shared__ float meet[GROUPS > 1 ? THREADS * E : 1];
     int slot = 0;
-    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    const int t = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G);   // the same in a whole wave
     const int width = P.width;
     const float inv_width = 1.f / float(width);
     float sums[5][E];     // weight, bias, post_weight, post_bias, gate
@@ -226,14 +277,24 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     for (int i = 0; i < 5; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) sums[i][e] = 0.f;
+    // the next rows are on their way while these are worked on
+    typename Pt::Raw raw[4];
+    auto fetch = [&](int64_t row) {
+        Pt::fetch(raw[0], P.h, row, width, t, row < P.rows && P.dn.p);
+        Pt::fetch(raw[1], P.dn, row, width, t, row < P.rows && P.dn.p);
+        Pt::fetch(raw[2], P.dh_out, row, width, t, row < P.rows && P.dh_out.p);
+        Pt::fetch(raw[3], P.y, row, width, t, row < P.rows && P.y.p);
+    };
+    fetch(int64_t(blockIdx.x) * GROUPS + group);
     for (int64_t first = int64_t(blockIdx.x) * GROUPS; first < P.rows; first += int64_t(gridDim.x) * GROUPS) {
         const int64_t row = first + group;
         const bool there = row < P.rows;
         float x[E], y[E], dn[E], d[E];                            // h', the block's output, gradients of n and of h'
-        Pt::load(x, P.h, row, width, t, there && P.dn.p);
-        Pt::load(dn, P.dn, row, width, t, there && P.dn.p);
-        Pt::load(d, P.dh_out, row, width, t, there && P.dh_out.p);
-        Pt::load(y, P.y, row, width, t, there && P.y.p);
+        Pt::values(x, raw[0]);
+        Pt::values(dn, raw[1]);
+        Pt::values(d, raw[2]);
+        Pt::values(y, raw[3]);
+        fetch(row + int64_t(gridDim.x) * GROUPS);
         if (LAYER) {
             centre<Pt, G, THREADS>(x, y, P.post, width, t, lds, slot);
         }
