@@ -7,33 +7,46 @@ namespace onecomp {
 namespace block {
 namespace {
 
-// G threads have a row: thread t of them the values VEC (t + G v) .. + VEC - 1, v < NV; 16 bytes of T each.
-template <class T_, int NV, int G>
+// G threads have a row: thread t of them the values VEC (t + G v) .. + VEC - 1, v < NV; 16 bytes of T each.  WHOLE: addresses,
+// strides and widths of whole vectors; then rows are read and written through buffer descriptors as long as the row, whose
+// bounds check does what comparisons and branches around every access would.
+template <class T_, int NV, int G, bool WHOLE>
 struct Part {
     typedef T_ T;
     static constexpr int VEC = 16 / int(sizeof(T)), E = VEC * NV;
     static __device__ __forceinline__ int col(int t, int v) { return VEC * (t + G * v); }
-    // A row on its way: loads whose values nobody has asked for yet.
+    static __device__ __forceinline__ bool inside(int t, int e, int width) { return col(t, e / VEC) + (WHOLE ? 0 : e % VEC) < width; }
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void* p, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+    }
+
+    // A row on its way: loads whose values nobody has asked for yet.  Zeros behind the width.
     struct Raw {
         uint4v v[NV];
     };
     static __device__ __forceinline__ void fetch(Raw& x, const Rows& r, int64_t row, int width, int t, bool there) {
         const T* p = static_cast<const T*>(r.p) + row * r.stride;
+        if constexpr (WHOLE) {
+            const __amdgpu_buffer_rsrc_t d = descriptor(p, there ? width * int(sizeof(T)) : 0);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = col(t, v);
-            uint4v y = {0u, 0u, 0u, 0u};
-            if (there && c + VEC <= width) {
-                y = *reinterpret_cast<const uint4u*>(p + c);
-            } else if (there && c < width) {
+            for (int v = 0; v < NV; ++v) x.v[v] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(d, col(t, v) * int(sizeof(T)), 0, 0));
+        } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    if (c + i >= width) continue;
-                    if (sizeof(T) == 2) y[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[c + i]) << (16 * (i & 1));
-                    else y[i & 3] = reinterpret_cast<const uint32_t*>(p)[c + i];
+            for (int v = 0; v < NV; ++v) {
+                const int c = col(t, v);
+                uint4v y = {0u, 0u, 0u, 0u};
+                if (there && c + VEC <= width) {
+                    y = *reinterpret_cast<const uint4u*>(p + c);
+                } else if (there && c < width) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        if (c + i >= width) continue;
+                        if (sizeof(T) == 2) y[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[c + i]) << (16 * (i & 1));
+                        else y[i & 3] = reinterpret_cast<const uint32_t*>(p)[c + i];
+                    }
                 }
+                x.v[v] = y;
             }
-            x.v[v] = y;
         }
     }
     static __device__ __forceinline__ void values(float (&x)[E], const Raw& r) {
@@ -49,25 +62,10 @@ struct Part {
                 }
             }
     }
-    // zeros behind the width
     static __device__ __forceinline__ void load(float (&x)[E], const Rows& r, int64_t row, int width, int t, bool there) {
-        const T* p = static_cast<const T*>(r.p) + row * r.stride;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = col(t, v);
-            float y[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = 0.f;
-            if (there && c + VEC <= width) {
-                load_vector(y, p + c);
-            } else if (there && c < width) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    if (c + i < width) y[i] = load_one(p + c + i);
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[v * VEC + i] = y[i];
-        }
+        Raw raw;
+        fetch(raw, r, row, width, t, there);
+        values(x, raw);
     }
     static __device__ __forceinline__ void store(const Rows& r, int64_t row, int width, int t, bool there, const float (&x)[E]) {
         T* p = static_cast<T*>(r.p) + row * r.stride;
@@ -77,7 +75,9 @@ struct Part {
             float y[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) y[i] = x[v * VEC + i];
-            if (there && c + VEC <= width) {
+            if constexpr (WHOLE) {
+                __builtin_amdgcn_raw_buffer_store_b128(packed(y), descriptor(p, there ? width * int(sizeof(T)) : 0), c * int(sizeof(T)), 0, 0);
+            } else if (there && c + VEC <= width) {
                 store_vector(p + c, y);
             } else if (there && c < width) {
 #pragma unroll
@@ -87,34 +87,72 @@ struct Part {
         }
     }
     // this thread's entries of a parameter, in either type
+    static __device__ __forceinline__ void parameter(float (&x)[E], const void* p, bool bf16, int width, int t) {
+        if constexpr (WHOLE) {
+            const __amdgpu_buffer_rsrc_t d = descriptor(p, width * (bf16 ? 2 : 4));
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = col(t, v);
+                if (bf16) {
+                    uint4v y = {0u, 0u, 0u, 0u};
+                    if (VEC == 8) {
+                        y = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(d, c * 2, 0, 0));
+                    } else {
+                        const auto z = __builtin_amdgcn_raw_buffer_load_b64(d, c * 2, 0, 0);
+                        y[0] = z[0];
+                        y[1] = z[1];
+                    }
+#pragma unroll
+                    for (int i = 0; i < VEC / 2; ++i) {
+                        x[v * VEC + 2 * i] = bf16_value(y[i] & 0xffffu);
+                        x[v * VEC + 2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VEC / 4; ++j) {
+                        const uint4v y = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(d, c * 4 + 16 * j, 0, 0));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[v * VEC + 4 * j + i] = __uint_as_float(y[i]);
+                    }
+                }
+            }
+        } else if (bf16) {
+            parameter(x, static_cast<const uint16_t*>(p), width, t);
+        } else {
+            parameter(x, static_cast<const float*>(p), width, t);
+        }
+    }
     template <class W>
     static __device__ __forceinline__ void parameter(float (&x)[E], const W* p, int width, int t) {
-        constexpr int N = 16 / int(sizeof(W));
+        constexpr int N = 16 / int(sizeof(W)) < VEC ? 16 / int(sizeof(W)) : VEC;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = col(t, v);
-            if (c + VEC <= width) {
-                if (VEC >= N) {
 #pragma unroll
-                    for (int i = 0; i < VEC / N; ++i) {
-                        float y[N];
-                        load_vector(y, p + c + N * i);
+            for (int j = 0; j < VEC; j += N) {
+                if (N == 16 / int(sizeof(W)) && c + j + N <= width) {
+                    float y[16 / sizeof(W)];
+                    load_vector(y, p + c + j);
 #pragma unroll
-                        for (int e = 0; e < N; ++e) x[v * VEC + (N * i + e) % VEC] = y[e];
-                    }
-                } else {                                          // fp32 rows with bf16 parameters: half a vector of these
+                    for (int i = 0; i < N; ++i) x[v * VEC + j + i] = y[i];
+                } else {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) x[v * VEC + i] = load_one(p + c + i);
+                    for (int i = 0; i < N; ++i) x[v * VEC + j + i] = c + j + i < width ? load_one(p + c + j + i) : 0.f;
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) x[v * VEC + i] = c + i < width ? load_one(p + c + i) : 0.f;
             }
         }
     }
-    static __device__ __forceinline__ void parameter(float (&x)[E], const void* p, bool bf16, int width, int t) {
-        if (bf16) parameter(x, static_cast<const uint16_t*>(p), width, t);
-        else parameter(x, static_cast<const float*>(p), width, t);
+    static __device__ __forceinline__ auto packed(const float (&y)[VEC]) {
+        uint4v r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (sizeof(T) == 2)
+                r[i] = uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[2 * i]))) |
+                       uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[(2 * i + 1) % VEC]))) << 16;
+            else
+                r[i] = __float_as_uint(y[i % VEC]);
+        }
+        return r;
     }
 };
 
@@ -171,7 +209,7 @@ __device__ __forceinline__ float normalise(float (&x)[Pt::E], bool layer, int wi
         group_sum<1, G, THREADS>(s, lds, slot);
         const float mean = s[0] * inv_width;
 #pragma unroll
-        for (int e = 0; e < Pt::E; ++e) x[e] = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? x[e] - mean : 0.f;
+        for (int e = 0; e < Pt::E; ++e) x[e] = Pt::inside(t, e, width) ? x[e] - mean : 0.f;
     }
     float s[1] = {0.f};
 #pragma unroll
@@ -199,10 +237,10 @@ __device__ __forceinline__ void affine(float (&x)[Pt::E], const void* w, const v
     }
 }
 
-template <class T, int NV, int G>
+template <class T, int NV, int G, bool WHOLE>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params P) {
     constexpr int THREADS = G < 256 ? 256 : G;
-    typedef Part<T, NV, G> Pt;
+    typedef Part<T, NV, G, WHOLE> Pt;
     __shared__ float4v lds[2 * (THREADS / 64)];
     int slot = 0;
     const int t = threadIdx.x % G;
@@ -250,7 +288,7 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
     const float mx = s[0] / float(width), my = both ? s[1] / float(width) : 0.f;
 #pragma unroll
     for (int e = 0; e < Pt::E; ++e) {
-        const bool in = Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width;
+        const bool in = Pt::inside(t, e, width);
         x[e] = in ? x[e] - mx : 0.f;
         y[e] = in ? y[e] - my : 0.f;
     }
@@ -261,10 +299,10 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
 // With x^ = x inv the normalised row, the gradient of the rows in front of a norm is inv (d - x^ mean(d x^) - mean(d)), the
 // last for layer norms only.  Both norms' squares and the first norm's means are added up in one go (mean(d x^) =
 // inv mean(d x)), the second norm's means in another; layer norms take one more for the means of the rows.
-template <class T, int NV, int G, bool LAYER>
+template <class T, int NV, int G, bool WHOLE, bool LAYER>
 __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
-    typedef Part<T, NV, G> Pt;
+    typedef Part<T, NV, G, WHOLE> Pt;
     constexpr int E = Pt::E;
     __shared__ float4v lds[2 * (THREADS / 64)];
     __shared__ float meet[GROUPS > 1 ? THREADS * E : 1];
@@ -295,6 +333,8 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         Pt::values(d, raw[2]);
         Pt::values(y, raw[3]);
         fetch(row + int64_t(gridDim.x) * GROUPS);
+        // parameters are read where they are used: read early they would push the sums out of the registers
+        __builtin_amdgcn_sched_barrier(0);
         if (LAYER) {
             centre<Pt, G, THREADS>(x, y, P.post, width, t, lds, slot);
         }
@@ -324,12 +364,14 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
                 d[e] += inv * (dn[e] * w[e] - mean - hat * along);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (P.dh.p) {
             float dh[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) dh[e] = P.scale * d[e];
             Pt::store(P.dh, row, width, t, there, dh);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (!P.y.p) continue;
         if (P.post) {
 #pragma unroll
@@ -353,6 +395,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] *= g[e];
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (P.post) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -364,7 +407,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 m[0] = fmaf(d[e], y[e], m[0]);
-                if (LAYER) m[1] += Pt::col(t, e / Pt::VEC) + e % Pt::VEC < width ? d[e] : 0.f;
+                if (LAYER) m[1] += Pt::inside(t, e, width) ? d[e] : 0.f;
             }
             group_sum<2, G, THREADS>(m, lds, slot);
             const float along = m[0] * inv_width, mean = m[1] * inv_width;
@@ -426,25 +469,42 @@ int gradient_workgroups(int64_t rows, int groups) {
     return int(all < 1 ? 1 : all < most ? all : most);            // one even without rows: the sums are 0
 }
 
-template <class T, int NV, int G>
-onecomp_status launch(const Params& P, bool gradient, hipStream_t stream) {
+template <class T, int NV, int G, bool WHOLE>
+onecomp_status launch_whole(const Params& P, bool gradient, hipStream_t stream) {
     if (!gradient) {
         constexpr int THREADS = G < 256 ? 256 : G;
         const int64_t grid = ceil_div(P.rows, THREADS / G);
         if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
-        forward_kernel<T, NV, G><<<dim3(unsigned(grid)), dim3(THREADS), 0, stream>>>(P);
+        forward_kernel<T, NV, G, WHOLE><<<dim3(unsigned(grid)), dim3(THREADS), 0, stream>>>(P);
         ONECOMP_CHECK_LAUNCH();
         return ONECOMP_OK;
     }
     const int grid = gradient_workgroups(P.rows, 1024 / G);
-    if (P.layer) gradient_kernel<T, NV, G, true><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
-    else gradient_kernel<T, NV, G, false><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
+    if (P.layer) gradient_kernel<T, NV, G, WHOLE, true><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
+    else gradient_kernel<T, NV, G, WHOLE, false><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
     ONECOMP_CHECK_LAUNCH();
     if (const int n = __builtin_popcount(P.wanted)) {
         columns_kernel<<<dim3(unsigned((P.width + 63) / 64), unsigned(n)), dim3(1024), 0, stream>>>(P, grid);
         ONECOMP_CHECK_LAUNCH();
     }
     return ONECOMP_OK;
+}
+
+// widths, addresses and strides of whole vectors
+template <class T>
+bool whole_vectors(const Params& P) {
+    constexpr int V = 16 / int(sizeof(T));
+    uintptr_t rest = uintptr_t(P.width % V);
+    for (const Rows* r : {&P.h, &P.y, &P.h_out, &P.n, &P.dn, &P.dh_out, &P.dh, &P.dy, &P.dgate})
+        if (r->p) rest |= reinterpret_cast<uintptr_t>(r->p) % 16 | uintptr_t(r->stride % V);
+    if (P.gate.p) rest |= reinterpret_cast<uintptr_t>(P.gate.p) % 16 | (P.gate_rows ? uintptr_t(P.gate.stride % V) : 0);
+    for (const void* p : {P.weight, P.bias, P.post_weight, P.post_bias}) rest |= reinterpret_cast<uintptr_t>(p) % 16;
+    return rest == 0;
+}
+
+template <class T, int NV, int G>
+onecomp_status launch(const Params& P, bool gradient, hipStream_t stream) {
+    return whole_vectors<T>(P) ? launch_whole<T, NV, G, true>(P, gradient, stream) : launch_whole<T, NV, G, false>(P, gradient, stream);
 }
 
 // As few threads as hold a row with 16 bytes each: sums cross the fewest waves, and registers stay free for the parameters'
