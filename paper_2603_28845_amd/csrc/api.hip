@@ -400,7 +400,7 @@ ONECOMP_API onecomp_status onecomp_mfma_rate_probe(int kind, int waves_per_simd,
 
 ONECOMP_API size_t onecomp_attention_workspace_bytes(const onecomp_attention_shape* shape) {
     if (check_attention(shape) != ONECOMP_OK) return 0;
-    return attn::forward_workspace_bytes(attention_params(shape));
+    return attn::forward_workspace_bytes(shape->dtype, attention_params(shape));
 }
 
 ONECOMP_API onecomp_status onecomp_attention_forward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
@@ -412,7 +412,7 @@ ONECOMP_API onecomp_status onecomp_attention_forward(const onecomp_attention_sha
         !check_heads(shape, v, shape->total_k) || !aligned(lse, 4))
         return ONECOMP_ERR_INVALID_ARG;
     attn::Params P = attention_params(shape);
-    const size_t need = attn::forward_workspace_bytes(P);
+    const size_t need = attn::forward_workspace_bytes(shape->dtype, P);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
     if (P.total_q == 0) return ONECOMP_OK;
     P.q = view(q);

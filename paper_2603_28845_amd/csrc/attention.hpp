@@ -23,7 +23,8 @@ struct Params {
     View d_o, dq, dk, dv;
     float* lse;            // [heads, total_q], may be null in the forward call
     float* aux;            // scratch of the gradients: [2, heads, total_q], -lse / scale and -d_out . out
-    float* part;           // scratch of the split forward call
+    float* part;           // scratch of calls whose keys or queries are split
+    int splits_q, splits_k;   // gradients: shares of the keys for dq, of the queries for dk and dv
     const int32_t *cu_q, *cu_k, *len_k;
     int64_t total_q, total_k;
     int n_seqs, heads, kv_heads, group, dim, causal;
@@ -387,7 +388,7 @@ __device__ __forceinline__ void careful_values(float (&sum)[2], const Params& P,
     }
 }
 
-size_t forward_workspace_bytes(const Params& P);
+size_t forward_workspace_bytes(onecomp_dtype dtype, const Params& P);
 size_t backward_workspace_bytes(const Params& P);
 onecomp_status forward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);
 onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);

@@ -117,6 +117,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int end_mine = mine >= S.nq ? 0 : P.causal ? max(0, min(S.nk, last_mine + 1 + S.shift)) : S.nk;
     const int end_all = P.causal ? min(S.nk, mine + 1 + S.shift) : S.nk;
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
+    // this workgroup's share of them, where the keys are split
+    const int share = (end + KEYS * P.splits_q - 1) / (KEYS * P.splits_q) * KEYS, from = int(blockIdx.y) * share, to = min(end, from + share);
 
     Loader<E, DT, KEYS, WAVES> lk, lv;
     lk.init(wave, lane, P.k.token, P.dim);
@@ -127,7 +129,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         lk.load(base + uint32_t(buf) * 2 * SIZE, at<E>(P.k, S.k0 + j, kv), end - j, wave);
         lv.load(base + uint32_t(buf) * 2 * SIZE + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
     };
-    if (end > 0) bring(0, 0);
+    const bool own_delta = sizeof(typename E::T) == 2 && end <= 256;
+    if (own_delta ? end > 0 : from < to) bring(own_delta ? 0 : from, 0);
 
     Operand<E, DT> q, d;
     q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     // gradient together (short sequences: dq and dk 2.0 times as far off as a single rounding, 1.4 times otherwise).  Where a
     // workgroup's rows see up to 256 keys, delta_i = sum_j p_ij (d_out_i . v_j) is added up in a pass of its own: one tile in
     // 36 of a causal prompt of 2048.
-    if (sizeof(typename E::T) == 2 && end <= 256) {
+    if (own_delta) {
         for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
             __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
             __syncthreads();
@@ -164,10 +167,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
                 }
             }
         }
-        if (end > 0) {
-            __syncthreads();
-            bring(0, 0);
-        }
+        __syncthreads();
+        if (from < to) bring(from, 0);
     } else {
         Operand<E, DT> o;
         o.load(at<E>(P.o, S.q0 + query, head), there, P.dim, half);
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
             for (int e = 0; e < E::PER_CHUNK; ++e) delta = fmaf(float(o.x[s][e]), float(d.x[s][e]), delta);
     }
     delta += other_half(delta);
-    if (there && half == 0) {
+    if (there && half == 0 && blockIdx.y == 0) {
         P.aux[at_q] = -lse / P.c;
         P.aux[int64_t(P.heads) * P.total_q + at_q] = -delta;
     }
@@ -185,10 +186,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
 #pragma unroll
     for (int n = 0; n < DT; ++n) dq[n] = zero16();
 
-    for (int j = 0, buf = 0; j < end; j += KEYS, buf ^= 1) {
+    for (int j = from, buf = 0; j < to; j += KEYS, buf ^= 1) {
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
         __syncthreads();
-        if (j + KEYS < end) bring(j + KEYS, buf ^ 1);
+        if (j + KEYS < to) bring(j + KEYS, buf ^ 1);
         if (j >= end_mine) continue;
         const char *kt = lds + buf * 2 * SIZE, *vt = kt + SIZE;
         const bool all_seen = j + KEYS <= end_all;
@@ -215,17 +216,24 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         }
     }
     const bool broken = there && lse == lse && delta == delta && not_finite(dq);
+    const int64_t rows_q = int64_t(P.heads) * P.total_q;
+    float* part = P.part + int64_t(blockIdx.y) * rows_q * (32 * DT);
     if (there && !broken) {
-        char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
+        if (P.splits_q == 1) {
+            char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
 #pragma unroll
-        for (int n = 0; n < DT; ++n) store_column<E>(row, dq[n], P.scale, n, P.dim, half);
+            for (int n = 0; n < DT; ++n) store_column<E>(row, dq[n], P.scale, n, P.dim, half);
+        } else {
+#pragma unroll
+            for (int n = 0; n < DT; ++n) store_column<F32>(reinterpret_cast<char*>(part + at_q * (32 * DT)), dq[n], P.scale, n, 32 * DT, half);
+        }
     }
     for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
-        const int r = __ffs(rows) - 1, keys = __shfl(last, r, 64) + 1;
+        const int r = __ffs(rows) - 1, keys = min(to, __shfl(last, r, 64) + 1);
         const float lse_r = __shfl(-lse / P.c, r, 64), delta_r = __shfl(-delta, r, 64);
         const int64_t token = S.q0 + mine + r;
         float sum[2] = {0.f, 0.f};
-        for (int j0 = 0; j0 < keys; j0 += 64) {
+        for (int j0 = from; j0 < keys; j0 += 64) {
             float ds = 0.f;
             if (j0 + lane < keys)
                 ds = score_grad<E>(P, token, head, S.k0 + j0 + lane, lse_r, delta_r).ds;
@@ -233,7 +241,10 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < P.dim) put<E>(const_cast<char*>(at<E>(P.dq, token, head)), lane + 64 * e, sum[e] * P.scale);
+            if (lane + 64 * e < P.dim) {
+                if (P.splits_q == 1) put<E>(const_cast<char*>(at<E>(P.dq, token, head)), lane + 64 * e, sum[e] * P.scale);
+                else part[(int64_t(head) * P.total_q + token) * (32 * DT) + lane + 64 * e] = sum[e] * P.scale;
+            }
     }
 }
 
@@ -350,7 +361,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int begin = first >= S.nk ? S.nq : P.causal ? min(S.nq, max(0, first - S.shift)) / ROWS * ROWS : 0;
     const int begin_mine = mine >= S.nk ? S.nq : P.causal ? max(0, mine - S.shift) : 0;
     const int all = P.causal ? mine + 31 - S.shift : 0;
-    const int steps = begin < S.nq ? (S.nq - begin + ROWS - 1) / ROWS : 0, total = steps * P.group;
+    // steps through the queries of one head after the other; this workgroup's share of them
+    const int steps = begin < S.nq ? (S.nq - begin + ROWS - 1) / ROWS : 0, all_steps = steps * P.group;
+    const int step0 = int(int64_t(all_steps) * int(blockIdx.y) / P.splits_k), total = int(int64_t(all_steps) * (int(blockIdx.y) + 1) / P.splits_k);
 
     Loader<E, DT, ROWS, WAVES> lq, ld;
     lq.init(wave, lane, P.q.token, P.dim);
@@ -367,7 +380,12 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         }
     };
     const int head0 = kv * P.group;
-    if (total > 0) bring(head0, begin, 0);
+    int head = head0, r0 = begin;
+    if (step0 < total) {
+        head += step0 / steps;
+        r0 += step0 % steps * ROWS;
+        bring(head, r0, 0);
+    }
 
     Operand<E, DT> k, v;
     k.load(at<E>(P.k, S.k0 + key, kv), key < S.nk, P.dim, half);
@@ -378,8 +396,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
 #pragma unroll
     for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
 
-    int head = head0, r0 = begin;
-    for (int step = 0, buf = 0; step < total; ++step, buf ^= 1) {
+    for (int step = step0, buf = 0; step < total; ++step, buf ^= 1) {
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
         __syncthreads();
         int next_head = head, next = r0 + ROWS;
@@ -401,37 +418,84 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
     }
     const bool broken = not_finite(dk) || not_finite(dv);
+    // sums of a share: those for dk, then those for dv
+    const int64_t rows_k = int64_t(P.kv_heads) * P.total_k;
+    float* part = P.part + P.splits_q * (P.splits_q > 1) * int64_t(P.heads) * P.total_q * (32 * DT) + 2 * int64_t(blockIdx.y) * rows_k * (32 * DT);
     if (key < S.room && !broken) {
-        char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
-        char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
+        if (P.splits_k == 1) {
+            char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
+            char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
 #pragma unroll
-        for (int n = 0; n < DT; ++n) {
-            store_column<E>(row_k, dk[n], P.scale, n, P.dim, half);
-            store_column<E>(row_v, dv[n], 1.f, n, P.dim, half);
+            for (int n = 0; n < DT; ++n) {
+                store_column<E>(row_k, dk[n], P.scale, n, P.dim, half);
+                store_column<E>(row_v, dv[n], 1.f, n, P.dim, half);
+            }
+        } else {
+            float* to = part + (int64_t(kv) * P.total_k + S.k0 + key) * (32 * DT);
+#pragma unroll
+            for (int n = 0; n < DT; ++n) {
+                store_column<F32>(reinterpret_cast<char*>(to), dk[n], P.scale, n, 32 * DT, half);
+                store_column<F32>(reinterpret_cast<char*>(to + rows_k * (32 * DT)), dv[n], 1.f, n, 32 * DT, half);
+            }
         }
     }
     for (unsigned cols = unsigned(__ballot(broken)); cols; cols &= cols - 1) {
-        const int j = mine + __ffs(cols) - 1, from = P.causal ? max(0, j - S.shift) : 0;
+        const int j = mine + __ffs(cols) - 1, seen_from = P.causal ? max(0, j - S.shift) : 0;
         float sum_k[2] = {0.f, 0.f}, sum_v[2] = {0.f, 0.f};
-        for (int h = head0; h < head0 + P.group; ++h)
-            for (int i0 = from; i0 < S.nq; i0 += 64) {
-                Pair x = {0.f, 0.f};
-                if (i0 + lane < S.nq) {
-                    const int64_t at_q = int64_t(h) * P.total_q + S.q0 + i0 + lane;
-                    x = score_grad<E>(P, S.q0 + i0 + lane, h, S.k0 + j, P.aux[at_q], P.aux[int64_t(P.heads) * P.total_q + at_q]);
-                }
-                for (int t = 0; t < 64 && i0 + t < S.nq; ++t) {
-                    add_row<E>(sum_v, __shfl(x.p, t, 64), at<E>(P.d_o, S.q0 + i0 + t, h), P.dim, lane);
-                    add_row<E>(sum_k, __shfl(x.ds, t, 64), at<E>(P.q, S.q0 + i0 + t, h), P.dim, lane);
-                }
+        for (int step = step0; step < total; ++step) {
+            const int h = head0 + step / steps, first_q = begin + step % steps * ROWS;
+            Pair x = {0.f, 0.f};
+            const int q = first_q + lane;
+            if (lane < ROWS && q >= seen_from && q < S.nq) {
+                const int64_t at_q = int64_t(h) * P.total_q + S.q0 + q;
+                x = score_grad<E>(P, S.q0 + q, h, S.k0 + j, P.aux[at_q], P.aux[int64_t(P.heads) * P.total_q + at_q]);
             }
+            for (int t = 0; t < ROWS; ++t) {
+                if (first_q + t < seen_from || first_q + t >= S.nq) continue;
+                add_row<E>(sum_v, __shfl(x.p, t, 64), at<E>(P.d_o, S.q0 + first_q + t, h), P.dim, lane);
+                add_row<E>(sum_k, __shfl(x.ds, t, 64), at<E>(P.q, S.q0 + first_q + t, h), P.dim, lane);
+            }
+        }
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < P.dim) {
-                put<E>(const_cast<char*>(at<E>(P.dk, S.k0 + j, kv)), lane + 64 * e, sum_k[e] * P.scale);
-                put<E>(const_cast<char*>(at<E>(P.dv, S.k0 + j, kv)), lane + 64 * e, sum_v[e]);
+        for (int e = 0; e < 2; ++e) {
+            const int d = lane + 64 * e;
+            if (d >= P.dim) continue;
+            if (P.splits_k == 1) {
+                put<E>(const_cast<char*>(at<E>(P.dk, S.k0 + j, kv)), d, sum_k[e] * P.scale);
+                put<E>(const_cast<char*>(at<E>(P.dv, S.k0 + j, kv)), d, sum_v[e]);
+            } else {
+                float* to = part + (int64_t(kv) * P.total_k + S.k0 + j) * (32 * DT) + d;
+                to[0] = sum_k[e] * P.scale;
+                to[rows_k * (32 * DT)] = sum_v[e];
             }
+        }
     }
+}
+
+// The shares' sums of one gradient meet, in their order: out[token, head] = sum over s of part[s][head, token].
+template <class E, int DT>
+__global__ __launch_bounds__(256) void join_kernel(const View out, const float* part, const int splits, const int64_t stride, const int64_t tokens, const int heads,
+                                                   const int dim) {
+    constexpr int COLS = 32 * DT, LANES = COLS / 4;               // four columns a lane
+    const int64_t at_row = (int64_t(blockIdx.x) * 256 + threadIdx.x) / LANES;
+    const int d = int((int64_t(blockIdx.x) * 256 + threadIdx.x) % LANES) * 4;
+    if (at_row >= tokens * heads || d >= dim) return;
+    float4v sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const float4v*>(part + s * stride + at_row * COLS + d);
+    const int head = int(at_row / tokens);
+    char* to = const_cast<char*>(at<E>(out, at_row - int64_t(head) * tokens, head));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) put<E>(to, d + e, sum[e]);
+}
+
+template <class E, int DT>
+onecomp_status join(const View& out, const float* part, int splits, int64_t stride, int64_t tokens, int heads, int dim, hipStream_t stream) {
+    const int64_t grid = ceil_div(tokens * heads * (8 * DT), 256);
+    if (grid > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
+    join_kernel<E, DT><<<dim3(unsigned(grid)), dim3(256), 0, stream>>>(out, part, splits, stride, tokens, heads, dim);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
 }
 
 template <class E, int DT, int WQ, int WK>
@@ -446,21 +510,54 @@ onecomp_status launch_backward(const Params& P, hipStream_t stream) {
     const int64_t grid_q = (P.total_q / (WQ * 32) + P.n_seqs + 1) * P.heads, grid_k = (P.total_k / (WK * 32) + P.n_seqs + 1) * P.kv_heads;
     if (grid_q > 0x7fffffff || grid_k > 0x7fffffff) return ONECOMP_ERR_UNSUPPORTED;
     if (P.total_q > 0) {
-        grad_q_kernel<E, DT, WQ><<<dim3(unsigned(grid_q)), dim3(WQ * 64), LDS_Q, stream>>>(P);
+        grad_q_kernel<E, DT, WQ><<<dim3(unsigned(grid_q), unsigned(P.splits_q)), dim3(WQ * 64), LDS_Q, stream>>>(P);
         ONECOMP_CHECK_LAUNCH();
     }
     if (P.total_k > 0) {
-        grad_kv_kernel<E, DT, WK><<<dim3(unsigned(grid_k)), dim3(WK * 64), LDS_K, stream>>>(P);
+        grad_kv_kernel<E, DT, WK><<<dim3(unsigned(grid_k), unsigned(P.splits_k)), dim3(WK * 64), LDS_K, stream>>>(P);
         ONECOMP_CHECK_LAUNCH();
+    }
+    const int64_t cols = 32 * DT, part_q = P.total_q * P.heads * cols, part_k = P.total_k * P.kv_heads * cols;
+    const float* parts = P.part;
+    if (P.splits_q > 1) {
+        if (const onecomp_status e = join<E, DT>(P.dq, parts, P.splits_q, part_q, P.total_q, P.heads, P.dim, stream)) return e;
+        parts += P.splits_q * part_q;
+    }
+    if (P.splits_k > 1) {
+        if (const onecomp_status e = join<E, DT>(P.dk, parts, P.splits_k, 2 * part_k, P.total_k, P.kv_heads, P.dim, stream)) return e;
+        if (const onecomp_status e = join<E, DT>(P.dv, parts + part_k, P.splits_k, 2 * part_k, P.total_k, P.kv_heads, P.dim, stream)) return e;
     }
     return ONECOMP_OK;
 }
 
+// Where whole sequences make too few workgroups to fill the chip, their inner loops are split: the keys of dq's rows, the
+// queries of dk's and dv's.
+void plan(Params& P) {
+    const int64_t groups_q = (P.total_q / 128 + P.n_seqs) * P.heads, groups_k = (P.total_k / 128 + P.n_seqs) * P.kv_heads;
+    auto splits = [](int64_t groups, int64_t steps) {
+        const int64_t n = groups < 1 ? 1 : 512 / groups, most = steps / 2;   // two tiles at least for each
+        return int(n < 2 || most < 2 ? 1 : n < most ? n : most);
+    };
+    P.splits_q = P.total_q ? splits(groups_q, ceil_div(P.max_k, 64)) : 1;
+    P.splits_k = P.total_k ? splits(groups_k, ceil_div(P.max_q, 64) * P.group) : 1;
+}
+
 }  // namespace
 
-size_t backward_workspace_bytes(const Params& P) { return align_up(size_t(P.total_q) * P.heads * 8, 256); }
+size_t backward_workspace_bytes(const Params& in) {
+    Params P = in;
+    plan(P);
+    const size_t cols = size_t(P.dim + 31) / 32 * 32, rows_q = size_t(P.total_q) * P.heads, rows_k = size_t(P.total_k) * P.kv_heads;
+    size_t floats = align_up(2 * rows_q, 64);
+    if (P.splits_q > 1) floats += P.splits_q * rows_q * cols;
+    if (P.splits_k > 1) floats += 2 * P.splits_k * rows_k * cols;
+    return align_up(floats * 4, 256);
+}
 
-onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream) {
+onecomp_status backward_run(onecomp_dtype dtype, const Params& in, hipStream_t stream) {
+    Params P = in;
+    plan(P);
+    P.part = P.aux + align_up(size_t(P.total_q) * P.heads * 2, 64);
     const int dt = (P.dim + 31) / 32;
     if (dtype == ONECOMP_BF16)
         return dt == 1   ? launch_backward<Bf16, 1, 4, 4>(P, stream)

@@ -508,12 +508,13 @@ onecomp_status launch_few(const Params& P, hipStream_t stream) {
 
 // How the keys are shared out where there are few rows; splits = 0: whole prompts.  Estimates in microseconds from
 // measurements at 128 wide bf16 heads: 0.8 for 64 keys of a prompt's tile of 128 rows, two of them at a time on each CU, and
-// 0.6 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join.
-void plan(Params& P) {
+// 0.6 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join; fp32 products take 6 times as long.
+void plan(onecomp_dtype dtype, Params& P) {
     P.splits = P.run = 0;
     const double tiles = double(P.heads) * (double(P.total_q) / 128 + P.n_seqs), blocks = double(row_blocks(P)) * P.kv_heads;
-    const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * 0.8 + 5;
-    const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * 0.6 + 12;
+    const double slow = dtype == ONECOMP_F32 ? 6 : 1;
+    const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * 0.8 * slow + 5;
+    const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * 0.6 * slow + 12;
     if (P.max_q * P.group > 32 && few > prompt) return;
     // four pieces of work for each CU, none shorter than 256 keys: 32 requests of 100 to 16384 keys 100 us, with half as many again
     // 106, with 768 in all 105
@@ -532,9 +533,9 @@ onecomp_status forward(const Params& P, hipStream_t stream) {
 
 }  // namespace
 
-size_t forward_workspace_bytes(const Params& in) {
+size_t forward_workspace_bytes(onecomp_dtype dtype, const Params& in) {
     Params P = in;
-    plan(P);
+    plan(dtype, P);
     if (P.splits < 2) return 0;
     const size_t cols = size_t(P.dim + 31) / 32 * 32;
     const size_t rows = size_t(P.total_q) * P.heads;
@@ -543,7 +544,7 @@ size_t forward_workspace_bytes(const Params& in) {
 
 onecomp_status forward_run(onecomp_dtype dtype, const Params& in, hipStream_t stream) {
     Params P = in;
-    plan(P);
+    plan(dtype, P);
     const int dt = (P.dim + 31) / 32;
     if (dtype == ONECOMP_BF16)
         return dt == 1 ? forward<Bf16, 1>(P, stream) : dt == 2 ? forward<Bf16, 2>(P, stream) : dt == 3 ? forward<Bf16, 3>(P, stream) : forward<Bf16, 4>(P, stream);
