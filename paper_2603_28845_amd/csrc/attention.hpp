@@ -338,6 +338,53 @@ struct Operand {
     }
 };
 
+// ---- rows of one wave through LDS -------------------------------------------------------------------------------------------
+// The operands and results of a wave are 32 rows of which every lane holds 8 or 16 bytes here and there, rows that lie a
+// token's stride apart in memory.  Through LDS they are read and written 16 lanes to a row, in whole cache lines.  (Straight
+// from and to memory, 128 queries without any keys took 11 us; 32768 x 32 x 128 bf16 read and written: 175 us.)
+// `tile`: LDS of 32 rows that this wave alone uses.
+template <class E, int DT>
+struct Rows {
+    typedef attn::Tile<E, DT> T;
+    static constexpr int BYTES = T::bytes(32);
+    // begins to bring rows first .. first + valid - 1; they are there after a wait for the wave's loads
+    static __device__ __forceinline__ void bring(uint32_t tile, const char* first, int valid, int64_t token_stride, int dim, int lane) {
+        Loader<E, DT, 32, 1> l;
+        l.init(0, lane, token_stride, dim);
+        l.load(tile, first, valid, 0);
+    }
+    static __device__ __forceinline__ void take(Operand<E, DT>& x, const Reader<E, DT>& rd, const char* tile) {
+#pragma unroll
+        for (int s = 0; s < T::STEPS; ++s) x.x[s] = rd.rows(tile, 0, s);
+    }
+    // acc f (the lane's token in column, its entries in rows) to the rows whose bit is set in `which`
+    static __device__ __forceinline__ void store(char* tile, const float16v (&acc)[DT], float f, char* first, int64_t token_stride, unsigned which, int dim,
+                                                 int lane) {
+        static_assert(sizeof(typename E::T) == 2, "bf16");
+        const int half = lane >> 5, col = lane & 31;
+        char* row = tile + col * T::PITCH + half * 8;
+#pragma unroll
+        for (int n = 0; n < DT; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                short4v x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(short, static_cast<__bf16>(acc[n][4 * g + i] * f));
+                *reinterpret_cast<short4v*>(row + (((4 * n + g) ^ T::swizzle(col)) << 4)) = x;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // other lanes' entries are read next
+        constexpr int ROWS = 64 / T::CHUNKS;                      // at a time
+        const int chunk = lane % T::CHUNKS;
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const int r = i * ROWS + lane / T::CHUNKS;
+            const uint4v x = *reinterpret_cast<const uint4v*>(tile + r * T::PITCH + ((chunk ^ T::swizzle(r)) << 4));
+            if ((which >> r & 1) && chunk * 8 < dim) *reinterpret_cast<uint4v*>(first + int64_t(r) * token_stride * 2 + chunk * 16) = x;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+};
+
 // ---- results that are not finite ------------------------------------------------------------------------------------------
 // A score that a query must not see has probability 0, but 0 times a value that is infinite or no number is no number.  Tiles
 // behind a sequence's end hold zeros, so this can only come from later tokens of the query's own prompt.  The kernels look at

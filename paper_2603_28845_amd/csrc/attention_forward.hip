@@ -184,8 +184,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int end_all = P.causal ? min(S.nk, mine + 1 + S.shift) : S.nk;      // keys that every query of the wave sees
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
 
+    constexpr bool STAGED = sizeof(typename E::T) == 2;           // rows of queries and of the output through LDS
     Operand<E, DT> q;
-    q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
+    if constexpr (!STAGED) q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
 
     Loader<E, DT, KEYS, WAVES> lk, lv;
     lk.init(wave, lane, P.k.token, P.dim);
@@ -226,10 +227,18 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         }
         acc.settle(top, P.c);
     };
+    // queries go where the second tile of values will be, and behind it
+    constexpr int AT_Q = 3 * SIZE;
+    if constexpr (STAGED)
+        Rows<E, DT>::bring(base + AT_Q + uint32_t(wave) * Rows<E, DT>::BYTES, at<E>(P.q, S.q0 + mine, head), S.nq - mine, P.q.token, P.dim, lane);
     bring_k(0);
     bring_v(0);
     bring_k(1);
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+    if constexpr (STAGED) {
+        asm volatile("" ::: "memory");
+        Rows<E, DT>::take(q, rd, lds + AT_Q + wave * Rows<E, DT>::BYTES);
+    }
     __syncthreads();
     int t = 0;
     if (n_mine > 0) {
@@ -254,7 +263,11 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     for (; t < n; ++t) next(t);
     const float l = acc.l + other_half(acc.l), f = l == 0.f ? 0.f : 1.f / l;
     const bool broken = there && l == l && not_finite(acc.o);
-    if (there && !broken) {
+    if constexpr (STAGED) {
+        __syncthreads();                                          // every wave is done with the tiles
+        Rows<E, DT>::store(lds + wave * Rows<E, DT>::BYTES, acc.o, f, const_cast<char*>(at<E>(P.o, S.q0 + mine, head)), P.o.token,
+                           unsigned(__ballot(there && !broken)), P.dim, lane);
+    } else if (there && !broken) {
         char* row = const_cast<char*>(at<E>(P.o, S.q0 + query, head));
 #pragma unroll
         for (int n = 0; n < DT; ++n) store_column<E>(row, acc.o[n], f, n, P.dim, half);
@@ -470,7 +483,8 @@ __global__ __launch_bounds__(256) void join_kernel(const Params P) {
 template <class E, int DT, int WAVES>
 onecomp_status launch_forward(const Params& P, hipStream_t stream) {
     constexpr int KEYS = sizeof(typename E::T) == 2 ? 64 : 32;
-    constexpr int LDS = 4 * Tile<E, DT>::bytes(KEYS);
+    // bf16: behind the tiles of keys and values what the queries need besides the last of them
+    constexpr int SIZE = Tile<E, DT>::bytes(KEYS), LDS = sizeof(typename E::T) == 2 ? 3 * SIZE + WAVES * Rows<E, DT>::BYTES : 4 * SIZE;
     static std::atomic<uint64_t> done{0};
     const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(forward_kernel<E, DT, WAVES>), LDS, done);
     if (st != ONECOMP_OK) return st;
