@@ -129,14 +129,29 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         lk.load(base + uint32_t(buf) * 2 * SIZE, at<E>(P.k, S.k0 + j, kv), end - j, wave);
         lv.load(base + uint32_t(buf) * 2 * SIZE + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
     };
-    const bool own_delta = sizeof(typename E::T) == 2 && end <= 256;
-    if (own_delta ? end > 0 : from < to) bring(own_delta ? 0 : from, 0);
-
-    Operand<E, DT> q, d;
-    q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
-    d.load(at<E>(P.d_o, S.q0 + query, head), there, P.dim, half);
+    constexpr bool STAGED = sizeof(typename E::T) == 2;           // rows through LDS
+    const bool own_delta = STAGED && end <= 256;
     Reader<E, DT> rd;
     rd.init(lane);
+    Operand<E, DT> q, d;
+    typedef Rows<E, DT> R;
+    static_assert(!STAGED || WAVES * R::BYTES == 2 * SIZE, "the waves' rows fill one pair of tiles");
+    const int mine_at = wave * (STAGED ? R::BYTES : 0);
+    if constexpr (STAGED) {
+        R::bring(base + mine_at, at<E>(P.q, S.q0 + mine, head), S.nq - mine, P.q.token, P.dim, lane);
+        R::bring(base + 2 * SIZE + mine_at, at<E>(P.d_o, S.q0 + mine, head), S.nq - mine, P.d_o.token, P.dim, lane);
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        asm volatile("" ::: "memory");
+        R::take(q, rd, lds + mine_at);
+        R::take(d, rd, lds + 2 * SIZE + mine_at);
+        __syncthreads();
+        // outputs, for delta, where the second tiles of keys and values will be
+        if (!own_delta) R::bring(base + 2 * SIZE + mine_at, at<E>(P.o, S.q0 + mine, head), S.nq - mine, P.o.token, P.dim, lane);
+    } else {
+        q.load(at<E>(P.q, S.q0 + query, head), there, P.dim, half);
+        d.load(at<E>(P.d_o, S.q0 + query, head), there, P.dim, half);
+    }
+    if (own_delta ? end > 0 : from < to) bring(own_delta ? 0 : from, 0);
     const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
     float delta = 0.f, lse = there ? P.lse[at_q] * LOG2E : 0.f;
     if (lse == NEG_INF) lse = -NEG_INF;                           // a query that sees nothing: all its probabilities are 0
@@ -171,7 +186,13 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         if (from < to) bring(from, 0);
     } else {
         Operand<E, DT> o;
-        o.load(at<E>(P.o, S.q0 + query, head), there, P.dim, half);
+        if constexpr (STAGED) {
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            asm volatile("" ::: "memory");
+            R::take(o, rd, lds + 2 * SIZE + mine_at);
+        } else {
+            o.load(at<E>(P.o, S.q0 + query, head), there, P.dim, half);
+        }
 #pragma unroll
         for (int s = 0; s < T::STEPS; ++s)
 #pragma unroll
@@ -218,7 +239,12 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const bool broken = there && lse == lse && delta == delta && not_finite(dq);
     const int64_t rows_q = int64_t(P.heads) * P.total_q;
     float* part = P.part + int64_t(blockIdx.y) * rows_q * (32 * DT);
-    if (there && !broken) {
+    if (STAGED && P.splits_q == 1) {
+        if constexpr (STAGED) {
+            __syncthreads();
+            R::store(lds + mine_at, dq, P.scale, const_cast<char*>(at<E>(P.dq, S.q0 + mine, head)), P.dq.token, unsigned(__ballot(there && !broken)), P.dim, lane);
+        }
+    } else if (there && !broken) {
         if (P.splits_q == 1) {
             char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
 #pragma unroll
@@ -379,6 +405,25 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
             lds_load4(to + 2 * SIZE + uint32_t(wave) * 256u, uint32_t(lane) * 4u, rsrc);
         }
     };
+    constexpr bool STAGED = sizeof(typename E::T) == 2;           // rows through LDS
+    Reader<E, DT> rd;
+    rd.init(lane);
+    Operand<E, DT> k, v;
+    typedef Rows<E, DT> R;
+    static_assert(!STAGED || WAVES * R::BYTES == 2 * SIZE, "the waves' rows fill one pair of tiles");
+    const int mine_at = wave * (STAGED ? R::BYTES : 0);
+    if constexpr (STAGED) {
+        R::bring(base + mine_at, at<E>(P.k, S.k0 + mine, kv), S.nk - mine, P.k.token, P.dim, lane);
+        R::bring(base + 2 * SIZE + mine_at, at<E>(P.v, S.k0 + mine, kv), S.nk - mine, P.v.token, P.dim, lane);
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        asm volatile("" ::: "memory");
+        R::take(k, rd, lds + mine_at);
+        R::take(v, rd, lds + 2 * SIZE + mine_at);
+        __syncthreads();
+    } else {
+        k.load(at<E>(P.k, S.k0 + key, kv), key < S.nk, P.dim, half);
+        v.load(at<E>(P.v, S.k0 + key, kv), key < S.nk, P.dim, half);
+    }
     const int head0 = kv * P.group;
     int head = head0, r0 = begin;
     if (step0 < total) {
@@ -386,12 +431,6 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         r0 += step0 % steps * ROWS;
         bring(head, r0, 0);
     }
-
-    Operand<E, DT> k, v;
-    k.load(at<E>(P.k, S.k0 + key, kv), key < S.nk, P.dim, half);
-    v.load(at<E>(P.v, S.k0 + key, kv), key < S.nk, P.dim, half);
-    Reader<E, DT> rd;
-    rd.init(lane);
     float16v dk[DT], dv[DT];
 #pragma unroll
     for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
@@ -421,7 +460,14 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     // sums of a share: those for dk, then those for dv
     const int64_t rows_k = int64_t(P.kv_heads) * P.total_k;
     float* part = P.part + P.splits_q * (P.splits_q > 1) * int64_t(P.heads) * P.total_q * (32 * DT) + 2 * int64_t(blockIdx.y) * rows_k * (32 * DT);
-    if (key < S.room && !broken) {
+    if (STAGED && P.splits_k == 1) {
+        if constexpr (STAGED) {
+            __syncthreads();
+            const unsigned which = unsigned(__ballot(key < S.room && !broken));
+            R::store(lds + mine_at, dk, P.scale, const_cast<char*>(at<E>(P.dk, S.k0 + mine, kv)), P.dk.token, which, P.dim, lane);
+            R::store(lds + 2 * SIZE + mine_at, dv, 1.f, const_cast<char*>(at<E>(P.dv, S.k0 + mine, kv)), P.dv.token, which, P.dim, lane);
+        }
+    } else if (key < S.room && !broken) {
         if (P.splits_k == 1) {
             char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
             char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
