@@ -71,8 +71,9 @@ struct F32 {
     static __device__ __forceinline__ float to_float(T x) { return x; }
 };
 
-// A tile of ROWS rows in LDS.  Rows are PITCH bytes, a power of two; the 16-byte chunk c of row r lies at c ^ swizzle(r), so
-// that the 32 rows of one chunk, and the four rows of a transposed read, spread over the banks.
+// A tile of ROWS rows in LDS.  Rows are PITCH bytes, a power of two; the 16-byte chunk c of row r lies at c ^ swizzle(r).
+// Sixteen rows of one chunk (row reads) lie in different banks, and so do four chunks in a row of four rows (transposed
+// reads, which go by 32 lanes).
 template <class E, int DT>
 struct Tile {
     static constexpr int ESZ = int(sizeof(typename E::T));
@@ -80,9 +81,8 @@ struct Tile {
     static constexpr int CHUNKS = PITCH / 16;                     // of a row
     static constexpr int STEPS = 32 * DT * ESZ / 32;              // pairs of chunks that hold data: inner steps of a row product
     static __device__ __forceinline__ int swizzle(int r) {
-        if (CHUNKS >= 16) return ((r & 7) << 1) | ((r >> 3) & 1);
-        if (CHUNKS == 8) return ((r & 3) << 1) | ((r >> 2) & 1);
-        return ((r & 1) << 1) | ((r >> 1) & 1);
+        const int fours = (r >> 2) & 3;
+        return CHUNKS >= 16 ? (r & 3) << 2 | fours : CHUNKS == 8 ? (r >> 1 & 1) << 2 | fours : fours;
     }
     static constexpr int bytes(int rows) { return rows * PITCH; }
 };
@@ -150,8 +150,7 @@ template <int DT>
 __device__ __forceinline__ bf16x8 columns(const Reader<Bf16, DT>& rd, const char* tile, int step, int n) {
     typedef Tile<Bf16, DT> T;
     const char* a = tile + step * 16 * T::PITCH;
-    // rows 8 further on: the swizzle's lowest bit for rows of 256 bytes, none otherwise
-    const int far = T::CHUNKS >= 16 ? 16 : 0;
+    constexpr int far = 2 << 4;                                   // swizzle(r + 8) = swizzle(r) ^ 2 for r < 8
     const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + (rd.tr ^ (n << 6))));
     const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 8 * T::PITCH + (rd.tr ^ (n << 6) ^ far)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
