@@ -277,7 +277,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params
 
 // Subtracts the mean of x, and of y too if it goes through a norm, from their entries.
 template <class Pt, int G, int THREADS>
-__device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], bool both, int width, int t, float4v* lds, int& slot) {
+__device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], bool both, float& mx, float& my, int width, int t, float4v* lds, int& slot) {
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < Pt::E; ++e) {
@@ -285,7 +285,8 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
         s[1] += y[e];
     }
     group_sum<2, G, THREADS>(s, lds, slot);
-    const float mx = s[0] / float(width), my = both ? s[1] / float(width) : 0.f;
+    mx = s[0] / float(width);
+    my = both ? s[1] / float(width) : 0.f;
 #pragma unroll
     for (int e = 0; e < Pt::E; ++e) {
         const bool in = Pt::inside(t, e, width);
@@ -299,13 +300,21 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
 // With x^ = x inv the normalised row, the gradient of the rows in front of a norm is inv (d - x^ mean(d x^) - mean(d)), the
 // last for layer norms only.  Both norms' squares and the first norm's means are added up in one go (mean(d x^) =
 // inv mean(d x)), the second norm's means in another; layer norms take one more for the means of the rows.
-template <class T, int NV, int G, bool WHOLE, bool LAYER>
+//
+// SUMS: as said.  Wider rows leave no registers for the parameters' sums (over 8192, layer norms over 4096; spilled to memory
+// they cost 4 to 8 times the rest): then only what a row's entries need is left in scratch, and strips_kernel adds up.
+struct RowNumbers {
+    float mean_h, inv_h, mean_d, along, mean_y, inv_y, unused[2];
+};
+constexpr bool own_sums(int capacity, bool layer) { return capacity <= (layer ? 4096 : 8192); }
+
+template <class T, int NV, int G, bool WHOLE, bool LAYER, bool SUMS>
 __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
     typedef Part<T, NV, G, WHOLE> Pt;
     constexpr int E = Pt::E;
     __shared__ float4v lds[2 * (THREADS / 64)];
-    __shared__ float meet[GROUPS > 1 ? THREADS * E : 1];
+    __shared__ float meet[GROUPS > 1 && SUMS ? THREADS * E : 1];
     int slot = 0;
     const int t = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G);   // the same in a whole wave
     const int width = P.width;
@@ -315,7 +324,8 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     for (int i = 0; i < 5; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) sums[i][e] = 0.f;
-    // the next rows are on their way while these are worked on
+    // the next rows are on their way while these are worked on, where registers allow
+    constexpr bool AHEAD = NV == 1;
     typename Pt::Raw raw[4];
     auto fetch = [&](int64_t row) {
         Pt::fetch(raw[0], P.h, row, width, t, row < P.rows && P.dn.p);
@@ -323,22 +333,24 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         Pt::fetch(raw[2], P.dh_out, row, width, t, row < P.rows && P.dh_out.p);
         Pt::fetch(raw[3], P.y, row, width, t, row < P.rows && P.y.p);
     };
-    fetch(int64_t(blockIdx.x) * GROUPS + group);
+    if (AHEAD) fetch(int64_t(blockIdx.x) * GROUPS + group);
     for (int64_t first = int64_t(blockIdx.x) * GROUPS; first < P.rows; first += int64_t(gridDim.x) * GROUPS) {
         const int64_t row = first + group;
         const bool there = row < P.rows;
         float x[E], y[E], dn[E], d[E];                            // h', the block's output, gradients of n and of h'
+        if (!AHEAD) fetch(row);
         Pt::values(x, raw[0]);
         Pt::values(dn, raw[1]);
         Pt::values(d, raw[2]);
         Pt::values(y, raw[3]);
         typename Pt::Raw raw_gate;
         if (P.gate_rows) Pt::fetch(raw_gate, P.gate, row, width, t, there);
-        fetch(row + int64_t(gridDim.x) * GROUPS);
+        if (AHEAD) fetch(row + int64_t(gridDim.x) * GROUPS);
         // parameters are read where they are used: read early they would push the sums out of the registers
         __builtin_amdgcn_sched_barrier(0);
+        float mean_h = 0.f, mean_y = 0.f;
         if (LAYER) {
-            centre<Pt, G, THREADS>(x, y, P.post, width, t, lds, slot);
+            centre<Pt, G, THREADS>(x, y, P.post, mean_h, mean_y, width, t, lds, slot);
         }
         float s[4] = {0.f, 0.f, 0.f, 0.f}, w[E];                  // x^2, dn w x, dn w, y^2
         if (P.weight) {
@@ -356,13 +368,14 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         }
         group_sum<4, G, THREADS>(s, lds, slot);
         const float inv_y = 1.f / sqrtf(fmaf(s[3], inv_width, P.eps));
+        const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)), along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
+        if (!SUMS && there && t == 0) reinterpret_cast<RowNumbers*>(P.row_numbers)[row] = RowNumbers{mean_h, inv, mean, along, mean_y, inv_y, {0.f, 0.f}};
         if (P.dn.p) {
-            const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)), along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float hat = x[e] * inv;
-                sums[0][e] = fmaf(dn[e], hat, sums[0][e]);
-                if (LAYER) sums[1][e] += dn[e];
+                if (SUMS) sums[0][e] = fmaf(dn[e], hat, sums[0][e]);
+                if (SUMS && LAYER) sums[1][e] += dn[e];
                 d[e] += inv * (dn[e] * w[e] - mean - hat * along);
             }
         }
@@ -391,7 +404,8 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
                 if (P.dgate.p) Pt::store(P.dgate, row, width, t, there, u);
             } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) sums[4][e] += there ? u[e] : 0.f;
+                for (int e = 0; e < E; ++e)
+                    if (SUMS) sums[4][e] += there ? u[e] : 0.f;
                 Pt::parameter(g, P.gate.p, P.w_bf16, width, t);
             }
 #pragma unroll
@@ -401,8 +415,8 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         if (P.post) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                sums[2][e] = fmaf(d[e], y[e], sums[2][e]);
-                if (LAYER) sums[3][e] += there ? d[e] : 0.f;
+                if (SUMS) sums[2][e] = fmaf(d[e], y[e], sums[2][e]);
+                if (SUMS && LAYER) sums[3][e] += there ? d[e] : 0.f;
             }
             if (P.post_weight) affine<Pt>(d, P.post_weight, nullptr, P.w_bf16, width, t);
             float m[2] = {0.f, 0.f};
@@ -418,6 +432,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         }
         if (P.dy.p) Pt::store(P.dy, row, width, t, there, d);
     }
+    if (!SUMS) return;
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
         if (!(P.wanted >> i & 1)) continue;
@@ -443,7 +458,82 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     }
 }
 
-// Sums over the workgroups of the kernel above: 64 columns of one parameter per workgroup, 16 waves with every sixteenth row.
+// The parameters' gradients of wide rows: a wave has a strip of 64 vectors and goes down every fourth row of its workgroup's
+// run of rows; what the rows' sums were is in scratch.  Everything is read once more (10 passes over the tensors' bytes instead
+// of 6), in return for sums that stay in registers at any width.
+template <class T, bool WHOLE, bool LAYER>
+__global__ __launch_bounds__(256) void strips_kernel(const Params P, const int runs) {
+    typedef Part<T, 1, 64, WHOLE> Pt;
+    constexpr int E = Pt::E, STRIP = 64 * E;
+    __shared__ float meet[4][STRIP];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // this strip of every tensor and parameter, as if it were the whole
+    const int first_col = blockIdx.x * STRIP, width = min(P.width - first_col, STRIP);
+    auto strip = [&](const Rows& r) { return Rows{r.p ? static_cast<T*>(r.p) + first_col : nullptr, r.stride}; };
+    auto strip_of = [&](const void* p) { return p ? static_cast<const char*>(p) + first_col * (P.w_bf16 ? 2 : 4) : nullptr; };
+    const Rows h = strip(P.h), y = strip(P.y), dn = strip(P.dn), dh_out = strip(P.dh_out), gate = P.gate_rows ? strip(P.gate) : P.gate;
+    float w[E], pw[E], pb[E], g[E];
+    auto parameter = [&](float (&x)[E], const void* p, float otherwise) {
+        if (p) {
+            Pt::parameter(x, strip_of(p), P.w_bf16, width, lane);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = otherwise;
+        }
+    };
+    parameter(w, P.weight, 1.f);
+    parameter(pw, P.post_weight, 1.f);
+    parameter(pb, P.post_bias, 0.f);
+    parameter(g, P.gate_rows ? nullptr : P.gate.p, 1.f);
+    float sums[5][E];
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[i][e] = 0.f;
+    const int64_t begin = P.rows * blockIdx.y / runs, end = P.rows * (blockIdx.y + 1) / runs;
+    typename Pt::Raw raw[4];
+    auto fetch = [&](int64_t row) {
+        Pt::fetch(raw[0], h, row, width, lane, row < end && P.dn.p);
+        Pt::fetch(raw[1], dn, row, width, lane, row < end && P.dn.p);
+        Pt::fetch(raw[2], dh_out, row, width, lane, row < end && P.dh_out.p);
+        Pt::fetch(raw[3], y, row, width, lane, row < end && P.y.p);
+    };
+    fetch(begin + wave);
+    for (int64_t row = begin + wave; row < end; row += 4) {
+        float x[E], d[E], dx[E], u[E];
+        Pt::values(x, raw[0]);
+        Pt::values(dx, raw[1]);
+        Pt::values(d, raw[2]);
+        Pt::values(u, raw[3]);
+        const RowNumbers n = reinterpret_cast<const RowNumbers*>(P.row_numbers)[row];
+        if (P.gate_rows) Pt::load(g, gate, row, width, lane, true);
+        fetch(row + 4);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float hat = (x[e] - n.mean_h) * n.inv_h;
+            sums[0][e] = fmaf(dx[e], hat, sums[0][e]);
+            if (LAYER) sums[1][e] += dx[e];
+            const float total = P.dn.p ? d[e] + n.inv_h * (dx[e] * w[e] - n.mean_d - hat * n.along) : d[e];
+            const float yhat = P.post ? (u[e] - n.mean_y) * n.inv_y : u[e];
+            if (P.wanted & 16) sums[4][e] = fmaf(total, fmaf(yhat, pw[e], pb[e]), sums[4][e]);
+            const float du = total * g[e];
+            sums[2][e] = fmaf(du, yhat, sums[2][e]);
+            if (LAYER) sums[3][e] += du;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        if (!(P.wanted >> i & 1)) continue;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) meet[wave][lane * E + e] = sums[i][e];
+        __syncthreads();
+        float* to = P.part + (int64_t(__popc(P.wanted & ((1 << i) - 1))) * runs + blockIdx.y) * P.width + first_col;
+        for (int c = threadIdx.x; c < width; c += 256) to[c] = (meet[0][c] + meet[1][c]) + (meet[2][c] + meet[3][c]);
+    }
+}
+
+// Sums over the workgroups of the kernels above: 64 columns of one parameter per workgroup, 16 waves with every sixteenth row.
 __global__ __launch_bounds__(1024) void columns_kernel(const Params P, const int n_parts) {
     __shared__ float meet[16][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane;
@@ -471,6 +561,12 @@ int gradient_workgroups(int64_t rows, int groups) {
     return int(all < 1 ? 1 : all < most ? all : most);            // one even without rows: the sums are 0
 }
 
+// runs of rows of the strips: four workgroups for each CU at 256 entries a strip
+int strip_runs(int64_t rows, int width) {
+    const int64_t runs = 1024 / ((width + 511) / 512), most = ceil_div(rows, 8);
+    return int(most < 1 ? 1 : runs < most ? runs : most);
+}
+
 template <class T, int NV, int G, bool WHOLE>
 onecomp_status launch_whole(const Params& P, bool gradient, hipStream_t stream) {
     if (!gradient) {
@@ -481,12 +577,34 @@ onecomp_status launch_whole(const Params& P, bool gradient, hipStream_t stream) 
         ONECOMP_CHECK_LAUNCH();
         return ONECOMP_OK;
     }
-    const int grid = gradient_workgroups(P.rows, 1024 / G);
-    if (P.layer) gradient_kernel<T, NV, G, WHOLE, true><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
-    else gradient_kernel<T, NV, G, WHOLE, false><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
-    ONECOMP_CHECK_LAUNCH();
+    int parts = gradient_workgroups(P.rows, 1024 / G);
+    constexpr int V = 16 / int(sizeof(T));
+    auto go = [&](auto layer) -> onecomp_status {
+        constexpr bool LAYER = decltype(layer)::value, SUMS = own_sums(V * NV * G, LAYER);
+        const int grid = parts;
+        // strips read the gradients anew: where the results go over them, the rows' numbers are formed in a pass of their own
+        const bool over = !SUMS && P.wanted && (P.dh.p == P.dh_out.p || P.dy.p == P.dn.p || P.dh.p == P.dn.p || P.dy.p == P.dh_out.p);
+        Params Q = P;
+        if (over) Q.dh.p = Q.dy.p = Q.dgate.p = nullptr;
+        gradient_kernel<T, NV, G, WHOLE, LAYER, SUMS><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(Q);
+        ONECOMP_CHECK_LAUNCH();
+        if constexpr (!SUMS) {
+            if (P.wanted) {
+                const int strips = (P.width + 64 * V - 1) / (64 * V);
+                parts = strip_runs(P.rows, P.width);
+                strips_kernel<T, WHOLE, LAYER><<<dim3(unsigned(strips), unsigned(parts)), dim3(256), 0, stream>>>(P, parts);
+                ONECOMP_CHECK_LAUNCH();
+            }
+            if (over) {
+                gradient_kernel<T, NV, G, WHOLE, LAYER, SUMS><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(P);
+                ONECOMP_CHECK_LAUNCH();
+            }
+        }
+        return ONECOMP_OK;
+    };
+    if (const onecomp_status st = P.layer ? go(std::true_type{}) : go(std::false_type{})) return st;
     if (const int n = __builtin_popcount(P.wanted)) {
-        columns_kernel<<<dim3(unsigned((P.width + 63) / 64), unsigned(n)), dim3(1024), 0, stream>>>(P, grid);
+        columns_kernel<<<dim3(unsigned((P.width + 63) / 64), unsigned(n)), dim3(1024), 0, stream>>>(P, parts);
         ONECOMP_CHECK_LAUNCH();
     }
     return ONECOMP_OK;
@@ -529,12 +647,19 @@ onecomp_status run(const Params& P, bool gradient, hipStream_t s) {
 
 }  // namespace
 
-size_t gradient_workspace_bytes(int64_t rows, int64_t width, int wanted) {
-    const int64_t most = rows < 1 ? 1 : rows < 1024 ? rows : 1024;               // no device has more workgroups of these at a time
-    return align_up(size_t(most) * size_t(width) * size_t(__builtin_popcount(unsigned(wanted))) * 4, 256);
+size_t numbers_bytes(int64_t rows, int64_t width) {
+    return width > 4096 ? align_up(size_t(rows < 1 ? 1 : rows) * sizeof(RowNumbers), 256) : 0;
 }
 
-onecomp_status norm_run(onecomp_dtype dtype, const Params& P, bool gradient, hipStream_t stream) {
+size_t gradient_workspace_bytes(int64_t rows, int64_t width, int wanted) {
+    const int64_t most = rows < 1 ? 1 : rows < 1024 ? rows : 1024;               // no device has more workgroups of these at a time
+    return numbers_bytes(rows, width) + align_up(size_t(most) * size_t(width) * size_t(__builtin_popcount(unsigned(wanted))) * 4, 256);
+}
+
+onecomp_status norm_run(onecomp_dtype dtype, const Params& in, bool gradient, hipStream_t stream) {
+    Params P = in;
+    P.row_numbers = reinterpret_cast<float*>(P.part);
+    P.part = reinterpret_cast<float*>(reinterpret_cast<char*>(P.part) + numbers_bytes(P.rows, P.width));
     return dtype == ONECOMP_BF16 ? run<uint16_t>(P, gradient, stream) : run<float>(P, gradient, stream);
 }
 

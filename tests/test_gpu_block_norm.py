@@ -239,8 +239,9 @@ def test_gradients_against_differences():
         assert abs(slope - want) <= 5e-3 + 5e-3 * float(g.double().norm()), name
 
 
-def test_in_place_and_given_buffers():
-    x, grads = _inputs(50, 1024, BF16, BF16, 10, post=True, gate="channel")
+@pytest.mark.parametrize("width", [1024, 9000])
+def test_in_place_and_given_buffers(width):
+    x, grads = _inputs(50, width, BF16, BF16, 10, post=True, gate="channel")
     h, n = og.onecomp_block_norm_forward(**x)
     mine = x["h"].clone()
     h2, n2 = og.onecomp_block_norm_forward(**dict(x, h=mine), h_out=mine)
