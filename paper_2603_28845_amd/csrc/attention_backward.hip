@@ -285,7 +285,9 @@ __device__ __forceinline__ void grad_kv_block(float16v (&dk)[DT], float16v (&dv)
     typedef Tile<E, DT> T;
     constexpr int N = 2 * T::STEPS, AHEAD = 2;
     asm volatile("" : "+v"(rd.row), "+v"(rd.tr));                 // offsets anew, instead of 16 registers for them
-    float16v s, dp;
+    // (fp32 adds them at the end: in front, every step of a sum of a score's size would be rounded to a log-sum-exp's)
+    constexpr bool FIRST = sizeof(typename E::T) == 2;
+    float16v s, dp, s0, dp0;
     typename E::Row a[AHEAD];
     auto read = [&](int i) {
         if (i < N) a[i % AHEAD] = rd.rows(i & 1 ? dt : qt, 0, i >> 1);
@@ -295,10 +297,12 @@ __device__ __forceinline__ void grad_kv_block(float16v (&dk)[DT], float16v (&dv)
         const float4v x = *reinterpret_cast<const float4v*>(numbers + 8 * g + 4 * half), y = *reinterpret_cast<const float4v*>(numbers + 64 + 8 * g + 4 * half);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            s[4 * g + e] = x[e];
-            dp[4 * g + e] = y[e];
+            s0[4 * g + e] = x[e];
+            dp0[4 * g + e] = y[e];
         }
     }
+    s = FIRST ? s0 : zero16();
+    dp = FIRST ? dp0 : zero16();
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read(i);
     __builtin_amdgcn_sched_barrier(0);
@@ -309,6 +313,13 @@ __device__ __forceinline__ void grad_kv_block(float16v (&dk)[DT], float16v (&dv)
         else s = E::mma(a[i % AHEAD], k.x[x], s);
         read(i + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!FIRST) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] += s0[r];
+            dp[r] += dp0[r];
+        }
     }
     if (!all_seen) {
         asm volatile("");
