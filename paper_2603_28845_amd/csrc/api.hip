@@ -426,7 +426,7 @@ ONECOMP_API onecomp_status onecomp_attention_forward(const onecomp_attention_sha
 
 ONECOMP_API size_t onecomp_attention_backward_workspace_bytes(const onecomp_attention_shape* shape) {
     if (check_attention(shape) != ONECOMP_OK) return 0;
-    return attn::backward_workspace_bytes(attention_params(shape));
+    return attn::backward_workspace_bytes(shape->dtype, attention_params(shape));
 }
 
 ONECOMP_API onecomp_status onecomp_attention_backward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,
@@ -440,7 +440,7 @@ ONECOMP_API onecomp_status onecomp_attention_backward(const onecomp_attention_sh
         !check_heads(shape, dk, shape->total_k) || !check_heads(shape, dv, shape->total_k) || (!lse && shape->total_q) || !aligned(lse, 4))
         return ONECOMP_ERR_INVALID_ARG;
     attn::Params P = attention_params(shape);
-    const size_t need = attn::backward_workspace_bytes(P);
+    const size_t need = attn::backward_workspace_bytes(shape->dtype, P);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
     P.q = view(q);
     P.k = view(k);

@@ -435,7 +435,7 @@ __device__ __forceinline__ void careful_values(float (&sum)[2], const Params& P,
 }
 
 size_t forward_workspace_bytes(onecomp_dtype dtype, const Params& P);
-size_t backward_workspace_bytes(const Params& P);
+size_t backward_workspace_bytes(onecomp_dtype dtype, const Params& P);
 onecomp_status forward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);
 onecomp_status backward_run(onecomp_dtype dtype, const Params& P, hipStream_t stream);
 

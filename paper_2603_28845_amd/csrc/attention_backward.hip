@@ -588,11 +588,14 @@ onecomp_status launch_backward(const Params& P, hipStream_t stream) {
 }
 
 // Where whole sequences make too few workgroups to fill the chip, their inner loops are split: the keys of dq's rows, the
-// queries of dk's and dv's.
-void plan(Params& P) {
+// queries of dk's and dv's.  512 workgroups are two on each CU; more cost more in partial sums than they bring (2048 tokens,
+// 8 / 2 heads of 128: 284 us whole, 90 with 512, 120 with 1024).  A share is worth the launches that join it from 8 tiles of 64
+// on (4 x 512 tokens, 8 heads: 43 us whole, 62 in shares of 4 tiles), in fp32, whose products take longer, from the first on
+// (300 tokens, 4 / 1 heads of 32: 128 us whole, 31 split).
+void plan(onecomp_dtype dtype, Params& P) {
     const int64_t groups_q = (P.total_q / 128 + P.n_seqs) * P.heads, groups_k = (P.total_k / 128 + P.n_seqs) * P.kv_heads;
-    auto splits = [](int64_t groups, int64_t steps) {
-        const int64_t n = groups < 1 ? 1 : 512 / groups, most = steps / 2;   // two tiles at least for each
+    auto splits = [&](int64_t groups, int64_t steps) {
+        const int64_t n = groups < 1 ? 1 : 512 / groups, most = dtype == ONECOMP_F32 ? steps : steps / 8;
         return int(n < 2 || most < 2 ? 1 : n < most ? n : most);
     };
     P.splits_q = P.total_q ? splits(groups_q, ceil_div(P.max_k, 64)) : 1;
@@ -601,9 +604,9 @@ void plan(Params& P) {
 
 }  // namespace
 
-size_t backward_workspace_bytes(const Params& in) {
+size_t backward_workspace_bytes(onecomp_dtype dtype, const Params& in) {
     Params P = in;
-    plan(P);
+    plan(dtype, P);
     const size_t cols = size_t(P.dim + 31) / 32 * 32, rows_q = size_t(P.total_q) * P.heads, rows_k = size_t(P.total_k) * P.kv_heads;
     size_t floats = align_up(2 * rows_q, 64);
     if (P.splits_q > 1) floats += P.splits_q * rows_q * cols;
@@ -613,7 +616,7 @@ size_t backward_workspace_bytes(const Params& in) {
 
 onecomp_status backward_run(onecomp_dtype dtype, const Params& in, hipStream_t stream) {
     Params P = in;
-    plan(P);
+    plan(dtype, P);
     P.part = P.aux + align_up(size_t(P.total_q) * P.heads * 2, 64);
     const int dt = (P.dim + 31) / 32;
     if (dtype == ONECOMP_BF16)
