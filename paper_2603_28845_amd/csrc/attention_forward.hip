@@ -522,13 +522,14 @@ onecomp_status launch_few(const Params& P, hipStream_t stream) {
 
 // How the keys are shared out where there are few rows; splits = 0: whole prompts.  Estimates in microseconds from
 // measurements at 128 wide bf16 heads: 0.8 for 64 keys of a prompt's tile of 128 rows, two of them at a time on each CU, and
-// 0.6 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join; fp32 products take 6 times as long.
+// 0.8 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join.  fp32 products take 5 and 10 times as
+// long, and blocks of rows wider than 64 get two waves on a CU.
 void plan(onecomp_dtype dtype, Params& P) {
     P.splits = P.run = 0;
     const double tiles = double(P.heads) * (double(P.total_q) / 128 + P.n_seqs), blocks = double(row_blocks(P)) * P.kv_heads;
-    const double slow = dtype == ONECOMP_F32 ? 6 : 1;
-    const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * 0.8 * slow + 5;
-    const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * 0.6 * slow + 12;
+    const bool f32 = dtype == ONECOMP_F32, wide = P.dim > 64;
+    const double prompt = ceil(tiles / 512) * (double(P.max_k) / 64) * (!f32 ? 0.8 : wide ? 8 : 4) + 5;
+    const double few = ceil(blocks * (double(P.max_k) / 32) / 1024) * (!f32 ? 0.8 : wide ? 8 : 2.5) + 12;
     if (P.max_q * P.group > 32 && few > prompt) return;
     // four pieces of work for each CU, none shorter than 256 keys: 32 requests of 100 to 16384 keys 100 us, with half as many again
     // 106, with 768 in all 105
