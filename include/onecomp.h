@@ -18,6 +18,9 @@
  * onecomp_crossgram_accumulate and onecomp_qep_target (error propagation, Sec. 4.3.1);
  * onecomp_rtn_sensitivity (error metric of the bit allocation, Sec. 4.1).
  *
+ * Around the linear layers (calibration passes that produce X, tuning of what stays in floating point):
+ * onecomp_attention_forward / _backward, onecomp_block_norm_forward / _backward, onecomp_clip_gradients.
+ *
  * Storage convention: W is d_out x d_in row-major (rows = output channels); this
  * is the transpose of the paper's N x M weight matrix.  "Column j" is input
  * channel j; a group is `group_size` consecutive input channels of one row.

@@ -539,6 +539,6 @@ ONECOMP_API const char* onecomp_status_string(onecomp_status status) {
     return "unknown status";
 }
 
-ONECOMP_API int onecomp_version(void) { return 100; }
+ONECOMP_API int onecomp_version(void) { return 200; }
 
 }  // extern "C"
