@@ -524,7 +524,7 @@ def _head_fields(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, sh
     n, h, d = shape
     if one != 1 and d > 1 and n > 0:
         raise ValueError(f"rows of {name} must be dense")
-    return t.data_ptr(), token if n > 1 else max(token, h * d), head if h > 1 else d
+    return t.data_ptr(), token if n > 1 else h * d, head if h > 1 else d
 
 
 def _index_address(t: Optional[torch.Tensor], name: str, device: int, n: int) -> int:
