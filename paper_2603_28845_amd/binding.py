@@ -508,6 +508,11 @@ class _Buffer(threading.local):
 _buffer = _Buffer()
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A dense tensor of t's shape, dtype and device (1.3 us; torch.empty takes 2.2)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _raw_stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
@@ -586,7 +591,7 @@ def onecomp_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     device = _attention_shape(q, k, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
     dtype, shape, k_shape = q.dtype, q.shape, k.shape
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
+        out = _like(q)
     if lse is None and want_lse:
         lse = torch.empty((shape[1], shape[0]), dtype=torch.float32, device=q.device)
     at, base = _SHAPE.size, _buffer.at
@@ -611,9 +616,9 @@ def onecomp_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Te
     lib = _lib or load_library()
     device = _attention_shape(q, k, cu_q, cu_k, max_q, max_k, causal, scale, len_k)
     dtype, shape, k_shape, dev = q.dtype, q.shape, k.shape, q.device
-    dq = torch.empty(shape, dtype=dtype, device=dev) if dq is None else dq
-    dk = torch.empty(k_shape, dtype=dtype, device=dev) if dk is None else dk
-    dv = torch.empty(k_shape, dtype=dtype, device=dev) if dv is None else dv
+    dq = _like(q) if dq is None else dq
+    dk = _like(k) if dk is None else dk
+    dv = _like(v) if dv is None else dv
     at, base = _SHAPE.size, _buffer.at
     struct.pack_into("Pqq" * 8, _buffer.data, at, *_head_fields(q, "q", dtype, device, shape), *_head_fields(k, "k", dtype, device, k_shape),
                      *_head_fields(v, "v", dtype, device, k_shape), *_head_fields(out, "out", dtype, device, shape),
@@ -700,9 +705,9 @@ def onecomp_block_norm_forward(h: torch.Tensor, y: Optional[torch.Tensor] = None
         if h_out is not None:
             raise ValueError("h_out goes with y: without it h' is h")
     elif h_out is None:
-        h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        h_out = _like(h)
     if n is None and want_n:
-        n = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        n = _like(h)
     at, base = _NORM_SHAPE.size, _buffer.at
     struct.pack_into("Pq" * 5, _buffer.data, at, *_row_fields(h, "h", h), *_row_fields(y, "y", h), *gate_fields, *_row_fields(h_out, "h_out", h),
                      *_row_fields(n, "n", h))
@@ -731,7 +736,7 @@ def onecomp_block_norm_backward(dn: Optional[torch.Tensor], dh_out: Optional[tor
     if out is None:
         for name, t in res.items():
             if t is not None:
-                res[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+                res[name] = _like(t)
     else:
         for name, t in res.items():
             if t is not None:
