@@ -8,12 +8,17 @@ namespace block {
 namespace {
 
 // G threads have a row: thread t of them the values VEC (t + G v) .. + VEC - 1, v < NV; 16 bytes of T each.  WHOLE: addresses,
-// strides and widths of whole vectors; then rows are read and written through buffer descriptors as long as the row, whose
-// bounds check does what comparisons and branches around every access would.
+// strides and widths of whole vectors.  Those rows, and all rows of fp32, are read and written through buffer descriptors as
+// long as the row, whose bounds check, dword by dword, does what comparisons and branches around every access would.  An odd
+// row of bf16 can end inside a dword: its last vector is read from where a whole one ends with the row and shifted into place
+// (SHIFT), unless a thread has more than one (widths over 8192), which leaves no registers for it: entry by entry then, which
+// waits for these and all loads before them.  Gradients of 32 M entries, rms, entry by entry and so: bf16 1001 wide 267 and
+// 193 us, 4095 wide 257 and 170; fp32 1359 wide 379 and 249.
 template <class T_, int NV, int G, bool WHOLE>
 struct Part {
     typedef T_ T;
     static constexpr int VEC = 16 / int(sizeof(T)), E = VEC * NV;
+    static constexpr bool RANGES = WHOLE || sizeof(T) == 4, SHIFT = !RANGES && NV == 1;
     static __device__ __forceinline__ int col(int t, int v) { return VEC * (t + G * v); }
     static __device__ __forceinline__ bool inside(int t, int e, int width) { return col(t, e / VEC) + (WHOLE ? 0 : e % VEC) < width; }
     static __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void* p, int bytes) {
@@ -26,7 +31,7 @@ struct Part {
     };
     static __device__ __forceinline__ void fetch(Raw& x, const Rows& r, int64_t row, int width, int t, bool there) {
         const T* p = static_cast<const T*>(r.p) + row * r.stride;
-        if constexpr (WHOLE) {
+        if constexpr (RANGES) {
             const __amdgpu_buffer_rsrc_t d = descriptor(p, there ? width * int(sizeof(T)) : 0);
 #pragma unroll
             for (int v = 0; v < NV; ++v) x.v[v] = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(d, col(t, v) * int(sizeof(T)), 0, 0));
@@ -35,21 +40,29 @@ struct Part {
             for (int v = 0; v < NV; ++v) {
                 const int c = col(t, v);
                 uint4v y = {0u, 0u, 0u, 0u};
-                if (there && c + VEC <= width) {
-                    y = *reinterpret_cast<const uint4u*>(p + c);
+                if (SHIFT ? width >= VEC : there && c + VEC <= width) {
+                    if (there && c < width) y = *reinterpret_cast<const uint4u*>(p + (SHIFT ? min(c, width - VEC) : c));
                 } else if (there && c < width) {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        if (c + i >= width) continue;
-                        if (sizeof(T) == 2) y[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[c + i]) << (16 * (i & 1));
-                        else y[i & 3] = reinterpret_cast<const uint32_t*>(p)[c + i];
-                    }
+                    for (int i = 0; i < VEC; ++i)
+                        if (c + i < width) y[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[c + i]) << (16 * (i & 1));
                 }
                 x.v[v] = y;
             }
         }
     }
-    static __device__ __forceinline__ void values(float (&x)[E], const Raw& r) {
+    // bf16 entries `by` .. 7 to the front, zeros behind them
+    static __device__ __forceinline__ void shift(uint4v& x, int by) {
+        const uint64_t lo = uint64_t(x[1]) << 32 | x[0], hi = uint64_t(x[3]) << 32 | x[2];
+        const int bits = 16 * by;
+        const uint64_t a = bits >= 64 ? hi >> (bits - 64) : bits ? lo >> bits | hi << (64 - bits) : lo, b = bits >= 64 ? 0 : hi >> bits;
+        x = uint4v{uint32_t(a), uint32_t(a >> 32), uint32_t(b), uint32_t(b >> 32)};
+    }
+    static __device__ __forceinline__ void values(float (&x)[E], Raw r, int width, int t) {
+        if constexpr (SHIFT) {
+            const int c = col(t, 0), by = c < width && width >= VEC ? max(0, c + VEC - width) : 0;
+            if (__any(by)) shift(r.v[0], by);
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -65,7 +78,7 @@ struct Part {
     static __device__ __forceinline__ void load(float (&x)[E], const Rows& r, int64_t row, int width, int t, bool there) {
         Raw raw;
         fetch(raw, r, row, width, t, there);
-        values(x, raw);
+        values(x, raw, width, t);
     }
     static __device__ __forceinline__ void store(const Rows& r, int64_t row, int width, int t, bool there, const float (&x)[E]) {
         T* p = static_cast<T*>(r.p) + row * r.stride;
@@ -75,7 +88,7 @@ struct Part {
             float y[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) y[i] = x[v * VEC + i];
-            if constexpr (WHOLE) {
+            if constexpr (RANGES) {
                 __builtin_amdgcn_raw_buffer_store_b128(packed(y), descriptor(p, there ? width * int(sizeof(T)) : 0), c * int(sizeof(T)), 0, 0);
             } else if (there && c + VEC <= width) {
                 store_vector(p + c, y);
@@ -343,10 +356,10 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         const bool there = row < P.rows;
         float x[E], y[E], dn[E], d[E];                            // h', the block's output, gradients of n and of h'
         if (!AHEAD) fetch(row);
-        Pt::values(x, raw[0]);
-        Pt::values(dn, raw[1]);
-        Pt::values(d, raw[2]);
-        Pt::values(y, raw[3]);
+        Pt::values(x, raw[0], width, t);
+        Pt::values(dn, raw[1], width, t);
+        Pt::values(d, raw[2], width, t);
+        Pt::values(y, raw[3], width, t);
         typename Pt::Raw raw_gate;
         if (P.gate_rows) Pt::fetch(raw_gate, P.gate, row, width, t, there);
         if (AHEAD) fetch(row + int64_t(gridDim.x) * GROUPS);
@@ -404,7 +417,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
 #pragma unroll
             for (int e = 0; e < E; ++e) u[e] *= d[e];
             if (P.gate_rows) {
-                Pt::values(g, raw_gate);
+                Pt::values(g, raw_gate, width, t);
                 if (P.dgate.p) Pt::store(P.dgate, row, width, t, there, u);
             } else {
 #pragma unroll
@@ -505,10 +518,10 @@ __global__ __launch_bounds__(256) void strips_kernel(const Params P, const int r
     fetch(begin + wave);
     for (int64_t row = begin + wave; row < end; row += 4) {
         float x[E], d[E], dx[E], u[E];
-        Pt::values(x, raw[0]);
-        Pt::values(dx, raw[1]);
-        Pt::values(d, raw[2]);
-        Pt::values(u, raw[3]);
+        Pt::values(x, raw[0], width, lane);
+        Pt::values(dx, raw[1], width, lane);
+        Pt::values(d, raw[2], width, lane);
+        Pt::values(u, raw[3], width, lane);
         const RowNumbers n = reinterpret_cast<const RowNumbers*>(P.row_numbers)[row];
         if (P.gate_rows) Pt::load(g, gate, row, width, lane, true);
         fetch(row + 4);
@@ -632,7 +645,7 @@ onecomp_status launch(const Params& P, bool gradient, hipStream_t stream) {
 }
 
 // As few threads as hold a row with 16 bytes each: sums cross the fewest waves, and registers stay free for the parameters'
-// sums.  (fp32 with two vectors a thread: gradients of 3001 rows of 1359 68 us instead of 50.)  Rows over 8192 (bf16) or 4096
+// sums.  (fp32 with two vectors a thread: gradients of 3001 rows of 1359 52 us instead of 47.)  Rows over 8192 (bf16) or 4096
 // (fp32) take more per thread.
 template <class T>
 onecomp_status run(const Params& P, bool gradient, hipStream_t s) {

@@ -270,3 +270,26 @@ def test_a_row_that_is_not_finite_stays_alone():
     got = og.onecomp_block_norm_forward(**x)
     for c, g in zip(clean, got):
         assert torch.equal(c[:4], g[:4]) and torch.equal(c[5:], g[5:]) and bool(torch.isnan(g[4].float()).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("width", [1, 3, 7, 9, 1001, 1359, 4099, 9001])
+def test_odd_rows_in_place_and_their_neighbours(width, dtype):
+    """Rows that end inside a vector: results over the inputs are those beside them, and the entries between rows keep theirs."""
+    print(f"[case] width {width} {dtype}", flush=True)
+    x, grads = _inputs(21, width, dtype, dtype, 13, post=True, gate="rows")
+
+    def over(values):
+        whole = torch.full((values.shape[0], width + 3), 77.0, dtype=dtype, device=DEV)
+        whole[:, :width] = values
+        return whole, whole[:, :width]
+
+    h, n = og.onecomp_block_norm_forward(**x)
+    want = og.onecomp_block_norm_backward(grads["dn"], grads["dh_out"], **dict(x, h=h))
+    (all_h, mine), (all_dn, dn), (all_dh, dh) = over(x["h"]), over(grads["dn"]), over(grads["dh_out"])
+    h2, n2 = og.onecomp_block_norm_forward(**dict(x, h=mine), h_out=mine)
+    assert torch.equal(h, h2) and torch.equal(n, n2)
+    og.onecomp_block_norm_backward(dn, dh, **dict(x, h=mine), out={"h": dh, "y": dn})
+    assert torch.equal(dh, want["h"]) and torch.equal(dn, want["y"])
+    for whole in (all_h, all_dn, all_dh):
+        assert bool((whole[:, width:] == 77.0).all())
