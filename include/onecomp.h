@@ -526,7 +526,8 @@ typedef struct {
  * if there is none.  h is h' as the forward call left it (h itself without y).  With G the gradient of h':
  *   dh = residual_scale G, dgate = G u, du = gate G, dy = du or that of the norm behind the block.
  * dh may be dh_out, dy may be dn (same strides).
- *   workspace  >= onecomp_block_norm_workspace_bytes(shape), 256-byte aligned.
+ *   workspace  >= onecomp_block_norm_workspace_bytes(shape), 256-byte aligned; not used, and NULL will do, where no parameter's
+ *              gradient (dweight .. dgate_channel) is wanted.
  */
 onecomp_status onecomp_block_norm_backward(const onecomp_norm_shape* shape, const onecomp_rows* dn, const onecomp_rows* dh_out,
                                            const onecomp_rows* h, const onecomp_rows* y, const void* weight, const void* post_weight,

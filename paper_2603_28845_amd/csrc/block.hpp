@@ -56,7 +56,7 @@ struct Params {
     Rows dn, dh_out, dh, dy, dgate;
     const void *weight, *bias, *post_weight, *post_bias;
     void* d_param[5];      // gradients of weight, bias, post_weight, post_bias, gate per channel
-    float *part, *row_numbers;   // scratch
+    float *part, *row_numbers;   // scratch; null where no parameter's gradient is wanted
     int64_t rows;
     int width, layer, post, gate_rows, w_bf16, wanted;   // wanted: bits of the d_param that are given
     float scale, eps;

@@ -1,6 +1,7 @@
 // The norms around a block, fused with its gate and residual: h' = r h + g u, n = norm(h'), u = y or norm(y), and their
 // gradients.  Every tensor is read once and written once; rows stay in registers between the sums that a norm needs.
 #include "block.hpp"
+#include "block_plan.hpp"
 #include <type_traits>
 
 namespace onecomp {
@@ -319,12 +320,8 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
 // 55 % of the vector pipes are the bound (512 threads a workgroup, two on a CU: 183 to 200 us, but twice the sums to join).
 //
 // SUMS: as said.  Wider rows leave no registers for the parameters' sums (over 8192, layer norms over 4096; spilled to memory
-// they cost 4 to 8 times the rest): then only what a row's entries need is left in scratch, and strips_kernel adds up.
-struct RowNumbers {
-    float mean_h, inv_h, mean_d, along, mean_y, inv_y, unused[2];
-};
-constexpr bool own_sums(int capacity, bool layer) { return capacity <= (layer ? 4096 : 8192); }
-
+// they cost 4 to 8 times the rest): then only what a row's entries need is left in scratch, for strips_kernel, which adds up; not
+// even that where no parameter's gradient is wanted.
 template <class T, int NV, int G, bool WHOLE, bool LAYER, bool SUMS>
 __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
@@ -386,7 +383,7 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
         group_sum<4, G, THREADS>(s, lds, slot);
         const float inv_y = 1.f / sqrtf(fmaf(s[3], inv_width, P.eps));
         const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)), along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
-        if (!SUMS && there && t == 0) reinterpret_cast<RowNumbers*>(P.row_numbers)[row] = RowNumbers{mean_h, inv, mean, along, mean_y, inv_y, {0.f, 0.f}};
+        if (!SUMS && P.row_numbers && there && t == 0) reinterpret_cast<RowNumbers*>(P.row_numbers)[row] = RowNumbers{mean_h, inv, mean, along, mean_y, inv_y, {0.f, 0.f}};
         if (P.dn.p) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -664,10 +661,6 @@ onecomp_status run(const Params& P, bool gradient, hipStream_t s) {
 
 }  // namespace
 
-size_t numbers_bytes(int64_t rows, int64_t width) {
-    return width > 4096 ? align_up(size_t(rows < 1 ? 1 : rows) * sizeof(RowNumbers), 256) : 0;
-}
-
 size_t gradient_workspace_bytes(int64_t rows, int64_t width, int wanted) {
     const int64_t most = rows < 1 ? 1 : rows < 1024 ? rows : 1024;               // no device has more workgroups of these at a time
     return numbers_bytes(rows, width) + align_up(size_t(most) * size_t(width) * size_t(__builtin_popcount(unsigned(wanted))) * 4, 256);
@@ -675,8 +668,9 @@ size_t gradient_workspace_bytes(int64_t rows, int64_t width, int wanted) {
 
 onecomp_status norm_run(onecomp_dtype dtype, const Params& in, bool gradient, hipStream_t stream) {
     Params P = in;
-    P.row_numbers = reinterpret_cast<float*>(P.part);
-    P.part = reinterpret_cast<float*>(reinterpret_cast<char*>(P.part) + numbers_bytes(P.rows, P.width));
+    const Scratch scratch = scratch_of(P.part, P.rows, P.width, P.wanted);
+    P.row_numbers = reinterpret_cast<float*>(scratch.numbers);
+    P.part = reinterpret_cast<float*>(scratch.sums);
     return dtype == ONECOMP_BF16 ? run<uint16_t>(P, gradient, stream) : run<float>(P, gradient, stream);
 }
 
