@@ -381,8 +381,9 @@ __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
             s[3] = fmaf(y[e], y[e], s[3]);
         }
         group_sum<4, G, THREADS>(s, lds, slot);
-        const float inv_y = 1.f / sqrtf(fmaf(s[3], inv_width, P.eps));
-        const float inv = 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)), along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
+        // a group behind the last row holds zeros, whose size is 0 without an eps: 0 times infinity would reach the parameters' sums
+        const float inv_y = there ? 1.f / sqrtf(fmaf(s[3], inv_width, P.eps)) : 0.f;
+        const float inv = there ? 1.f / sqrtf(fmaf(s[0], inv_width, P.eps)) : 0.f, along = s[1] * inv * inv_width, mean = LAYER ? s[2] * inv_width : 0.f;
         if (!SUMS && P.row_numbers && there && t == 0) reinterpret_cast<RowNumbers*>(P.row_numbers)[row] = RowNumbers{mean_h, inv, mean, along, mean_y, inv_y, {0.f, 0.f}};
         if (P.dn.p) {
 #pragma unroll
