@@ -31,5 +31,14 @@ inline Scratch scratch_of(void* workspace, int64_t rows, int64_t width, int want
     return Scratch{at, at + numbers_bytes(rows, width)};
 }
 
+// Whether any of the outputs lies over one of the inputs; NULL: not there.
+template <int N, int M>
+inline bool over_inputs(const void* const (&outputs)[N], const void* const (&inputs)[M]) {
+    for (const void* o : outputs)
+        for (const void* i : inputs)
+            if (o && o == i) return true;
+    return false;
+}
+
 }  // namespace block
 }  // namespace onecomp

@@ -33,8 +33,31 @@ static void check_scratch() {
     for (int capacity : {512, 2048, 4096}) REQUIRE(own_sums(capacity, true) && own_sums(capacity, false), "%d", capacity);
 }
 
+// The strips read every input anew: a result over any of them has to wait, one that is not wanted over an input that is not
+// there does not.
+static void check_over() {
+    char b[8];
+    const char* in[5] = {b, b + 1, b + 2, b + 3, b + 4};         // h, y, dn, dh_out, gate
+    for (int missing = 0; missing < 32; ++missing) {
+        const void* inputs[5];
+        for (int i = 0; i < 5; ++i) inputs[i] = missing >> i & 1 ? nullptr : in[i];
+        for (int which = 0; which < 27; ++which) {                // each output not wanted, apart, or over the chosen input
+            for (int input = 0; input < 5; ++input) {
+                const void* outputs[3];
+                bool any = false;
+                for (int o = 0, w = which; o < 3; ++o, w /= 3) {
+                    outputs[o] = w % 3 == 0 ? nullptr : w % 3 == 1 ? b + 5 + o : static_cast<const void*>(in[input]);
+                    any = any || (w % 3 == 2 && inputs[input]);
+                }
+                REQUIRE(over_inputs(outputs, inputs) == any, "outputs %d, input %d, missing %d", which, input, missing);
+            }
+        }
+    }
+}
+
 int main() {
     check_scratch();
+    check_over();
     std::printf("ok %ld\n", checked);
     return 0;
 }
