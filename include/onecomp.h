@@ -525,7 +525,7 @@ typedef struct {
  * Gradients of the forward call from those of n (dn) and of h' (dh_out; what comes back along the residual), either of them NULL
  * if there is none.  h is h' as the forward call left it (h itself without y).  With G the gradient of h':
  *   dh = residual_scale G, dgate = G u, du = gate G, dy = du or that of the norm behind the block.
- * dh may be dh_out, dy may be dn (same strides).
+ * dh, dy and dgate may each be one of the inputs h, y, dn, dh_out and gate (same strides).
  *   workspace  >= onecomp_block_norm_workspace_bytes(shape), 256-byte aligned; not used, and NULL will do, where no parameter's
  *              gradient (dweight .. dgate_channel) is wanted.
  */

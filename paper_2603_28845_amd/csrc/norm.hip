@@ -598,7 +598,7 @@ onecomp_status launch_whole(const Params& P, bool gradient, hipStream_t stream) 
         constexpr bool LAYER = decltype(layer)::value, SUMS = own_sums(V * NV * G, LAYER);
         const int grid = parts;
         // strips read the gradients anew: where the results go over them, the rows' numbers are formed in a pass of their own
-        const bool over = !SUMS && P.wanted && over_inputs({P.dh.p, P.dy.p}, {P.dn.p, P.dh_out.p});
+        const bool over = !SUMS && P.wanted && over_inputs({P.dh.p, P.dy.p, P.dgate.p}, {P.h.p, P.y.p, P.dn.p, P.dh_out.p, P.gate_rows ? P.gate.p : nullptr});
         Params Q = P;
         if (over) Q.dh.p = Q.dy.p = Q.dgate.p = nullptr;
         gradient_kernel<T, NV, G, WHOLE, LAYER, SUMS><<<dim3(unsigned(grid)), dim3(1024), 0, stream>>>(Q);

@@ -37,3 +37,21 @@ def test_rows_gradients_alone_leave_the_workspace(width, dtype, kind):
         for name in out:
             assert torch.equal(out[name], want[name]), name
         assert bool((room == 77).all())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("width", [640, 9000])
+@pytest.mark.parametrize("over", [{"h": "h"}, {"h": "y"}, {"y": "y", "h": "dh_out"}, {"y": "h"}, {"gate": "gate"}, {"gate": "dn", "y": "gate"}])
+def test_results_over_any_input(over, width, kind):
+    """dh, dy and a gate's gradient written over what the call reads: the rows in place, and the parameters' sums over all of them."""
+    print(f"[case] {over} {width} {kind}", flush=True)
+    x, dn, dh_out = _inputs(40, width, BF16, kind, 2)
+    want = og.onecomp_block_norm_backward(dn, dh_out, **x)
+    x, given = dict(x), {"dn": dn.clone(), "dh_out": dh_out.clone()}
+    for name in ("h", "y", "gate"):
+        given[name] = x[name] = x[name].clone()
+    out = {name: torch.empty_like(t) for name, t in x.items() if torch.is_tensor(t)}
+    out.update({result: given[name] for result, name in over.items()})
+    og.onecomp_block_norm_backward(given["dn"], given["dh_out"], **x, out=out)
+    for name in out:
+        assert torch.equal(out[name], want[name]), name
