@@ -461,6 +461,7 @@ size_t onecomp_attention_workspace_bytes(const onecomp_attention_shape* shape);
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
  * dk and dv summed over the heads of a group.  dq, dk and dv are overwritten (rows of k and v that no query sees get 0).
  * Sums in fp32, bf16 factors of the products as in the forward call, no atomics: the same inputs give the same bits.
+ * An infinity or NaN among the inputs reaches the gradients of the pairs that see it, which are then not finite, and no others.
  *   workspace  >= onecomp_attention_backward_workspace_bytes(shape), 256-byte aligned.
  */
 onecomp_status onecomp_attention_backward(const onecomp_attention_shape* shape, const onecomp_heads* q, const onecomp_heads* k,

@@ -121,6 +121,34 @@ struct Loader {
             if (LOADS % WAVES == 0 || wave + i * WAVES < LOADS)
                 lds_load16(lds + uint32_t(wave + i * WAVES) * 1024u, SAME ? off[0] + uint32_t(i * STEP) * row_bytes : off[i], rsrc);
     }
+    // Puts zeros for what is not finite in what this wave brought, and tells f of each: (row of the tile, column, whether it raises
+    // a sum, whether it lowers it); what is no number does both.
+    template <class F>
+    static __device__ __forceinline__ void clean(char* tile, int wave, int lane, F f) {
+        typedef typename E::T X;
+#pragma unroll 1
+        for (int i = 0; i < MINE; ++i) {
+            if (LOADS % WAVES != 0 && wave + i * WAVES >= LOADS) break;
+            const int at = (wave + i * WAVES) * 64 + lane, r = at / T::CHUNKS, col = ((at % T::CHUNKS) ^ T::swizzle(r)) * E::PER_CHUNK;
+            uint4v* to = reinterpret_cast<uint4v*>(tile + at * 16);
+            uint4v x = *to;
+            bool odd = false;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) odd = odd || (x[w] & 0x7f800000u) == 0x7f800000u || (sizeof(X) == 2 && (x[w] & 0x7f80u) == 0x7f80u);
+            if (!odd) continue;
+#pragma unroll
+            for (int e = 0; e < E::PER_CHUNK; ++e) {
+                const int w = e * int(sizeof(X)) / 4;
+                const bool low = sizeof(X) == 2 && (e & 1) == 0;
+                const uint32_t bits = sizeof(X) == 4 ? x[w] : low ? x[w] << 16 : x[w] & 0xffff0000u, size = bits & 0x7fffffffu;
+                if (size >= 0x7f800000u) {
+                    f(r, col + e, size > 0x7f800000u || bits == size, size > 0x7f800000u || bits != size);
+                    x[w] = sizeof(X) == 4 ? 0u : low ? x[w] & 0xffff0000u : x[w] & 0xffffu;
+                }
+            }
+            *to = x;
+        }
+    }
 };
 
 // Reads of a tile by one lane, as left operands.
@@ -400,53 +428,81 @@ struct Rows {
     }
 };
 
-// ---- results that are not finite ------------------------------------------------------------------------------------------
-// A score that a query must not see has probability 0, but 0 times a value that is infinite or no number is no number.  Tiles
-// behind a sequence's end hold zeros, so this can only come from later tokens of the query's own prompt.  The kernels look at
-// their sums once, at the end, and where one is not finite they form it again here, term by term, over the seen pairs alone:
-// nothing in the ordinary case, and slow where numbers have broken down already.
-template <class E>
-__device__ __forceinline__ float dot_rows(const char* a, const char* b, int dim) {
-    float x = 0.f;
-    for (int d = 0; d < dim; ++d)
-        x = fmaf(E::to_float(reinterpret_cast<const typename E::T*>(a)[d]), E::to_float(reinterpret_cast<const typename E::T*>(b)[d]), x);
-    return x;
-}
-
-// sum[e] += f v[lane + 64 e] for the lanes' columns of one row
-template <class E>
-__device__ __forceinline__ void add_row(float (&sum)[2], float f, const char* row, int dim, int lane) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-        if (lane + 64 * e < dim) sum[e] = fmaf(f, E::to_float(reinterpret_cast<const typename E::T*>(row)[lane + 64 * e]), sum[e]);
-}
-
 template <class E>
 __device__ __forceinline__ void put(char* row, int d, float x) {
     if (sizeof(typename E::T) == 2) reinterpret_cast<__bf16*>(row)[d] = static_cast<__bf16>(x);
     else reinterpret_cast<float*>(row)[d] = x;
 }
 
+// ---- results that are not finite ------------------------------------------------------------------------------------------
+// A score that a query must not see has probability 0, but 0 times a value that is infinite or no number is no number.  Tiles
+// behind a sequence's end hold zeros, so this can only come from later tokens of the query's own prompt.  The kernels look at
+// their sums once, when they have been stored, and where one is not finite its wave or workgroup takes its tiles once more, with zeros for
+// what is not finite in them.  A query sees a prefix of the keys (a key is seen by a suffix of the queries), so the first (last) row of each
+// column that is not finite says which results it reaches: their sums get it back at the end.  Nothing in the ordinary case, and
+// one more pass where numbers have broken down, in simpler loops (2 to 7 times the clean call).
+
 // true in the lanes whose column of the accumulators holds an entry that is not finite
 template <int DT>
 __device__ __forceinline__ bool not_finite(const float16v (&acc)[DT]) {
-    float x = 0.f;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < DT; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x = fmaf(acc[n][r], 0.f, x);
-    return !(x + other_half(x) == 0.f);
+        for (int r = 0; r < 16; ++r) x[r & 3] = fmaf(acc[n][r], 0.f, x[r & 3]);
+    x[0] = (x[0] + x[1]) + (x[2] + x[3]);
+    return !(x[0] + other_half(x[0]) == 0.f);
 }
 
-// sum_j 2^(c s_j - base) v_j over keys begin .. end - 1 of a row
-template <class E>
-__device__ __forceinline__ void careful_values(float (&sum)[2], const Params& P, const Seq& S, int64_t q_row, int head, int begin, int end, float base, int lane) {
-    const int kv = head / P.group;
-    sum[0] = sum[1] = 0.f;
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        float p = 0.f;
-        if (j0 + lane < end) p = __builtin_amdgcn_exp2f(fmaf(dot_rows<E>(at<E>(P.q, q_row, head), at<E>(P.k, S.k0 + j0 + lane, kv), P.dim), P.c, -base));
-        for (int t = 0; t < 64 && j0 + t < end; ++t) add_row<E>(sum, __shfl(p, t, 64), at<E>(P.v, S.k0 + j0 + t, kv), P.dim, lane);
+// The lane again: what the second pass derives from it is formed there, not kept in registers through the first (kept, it spilled
+// operands of the 128 wide bf16 gradients: 8 x 2048 tokens, forward and gradients 1340 us instead of 1285).
+__device__ __forceinline__ int lane_anew() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// LDS of a workgroup for this: what its waves say, and rows: of two kinds in any column, and per column, of what raises and of what
+// lowers a sum.
+struct Marks {
+    int said[8], any[2], column[256];
+    __device__ __forceinline__ int& up(int c) { return column[c]; }
+    __device__ __forceinline__ int& down(int c) { return column[128 + c]; }
+};
+
+// Whether any wave of the workgroup says so.  A barrier.
+template <int WAVES>
+__device__ __forceinline__ bool any_wave(Marks& marks, int wave, bool x) {
+    const int mine = __any(x);
+    if ((threadIdx.x & 63) == 0) marks.said[wave] = mine;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all |= marks.said[w];
+    return __builtin_amdgcn_readfirstlane(all) != 0;
+}
+
+// All rows to `none`, by `threads` threads; what waits for them makes it known to others.
+__device__ __forceinline__ void clear(Marks& marks, int none, int thread, int threads) {
+    for (int i = thread; i < 256; i += threads) marks.column[i] = none;
+    if (thread < 2) marks.any[thread] = none;
+}
+
+// One more row that is not finite: the first, or the last, stays.
+__device__ __forceinline__ void mark_first(int& mark, int row) {
+    if (row < mark) atomicMin(&mark, row);
+}
+__device__ __forceinline__ void mark_last(int& mark, int row) {
+    if (row > mark) atomicMax(&mark, row);
+}
+
+// Column 32 n + .. of a result gets back what is not finite: reached(row) says whether the marked row reaches this lane's.
+template <class F>
+__device__ __forceinline__ void give_back(float16v& acc, Marks& marks, int n, int half, F reached) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int col = 32 * n + acc_row(r, half);
+        acc[r] += (reached(marks.up(col)) ? -NEG_INF : 0.f) + (reached(marks.down(col)) ? NEG_INF : 0.f);
     }
 }
 

@@ -11,19 +11,6 @@ namespace {
 template <class E>
 constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1;            // blocks of 32 rows in a tile
 
-// One pair's probability and its gradient, from memory.
-struct Pair {
-    float p, ds;
-};
-template <class E>
-__device__ __forceinline__ Pair score_grad(const Params& P, int64_t q_row, int head, int64_t k_row, float minus_lse, float minus_delta) {
-    const int kv = head / P.group;
-    const float s = dot_rows<E>(at<E>(P.q, q_row, head), at<E>(P.k, k_row, kv), P.dim);
-    const float dp = dot_rows<E>(at<E>(P.d_o, q_row, head), at<E>(P.v, k_row, kv), P.dim);
-    const float p = __builtin_amdgcn_exp2f((s + minus_lse) * P.c);
-    return {p, p * (dp + minus_delta)};
-}
-
 // Scores of unseen keys to -inf: their probabilities are 0.
 __device__ __forceinline__ void mask(float16v& s, int last, int half) {
     asm volatile("");                                             // a branch around this stays one
@@ -94,6 +81,30 @@ __device__ __forceinline__ void grad_q_tile(float16v (&dq)[DT], const Reader<Bf1
         read_k(i + AHEAD_C);
         if (i < N / 2) arithmetic(1, i, N / 2);
         __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The same of 32 keys, one part after the other.
+template <class E, int DT>
+__device__ __forceinline__ void grad_q_block(float16v (&dq)[DT], const Reader<E, DT>& rd, const char* kt, const char* vt, const Operand<E, DT>& q,
+                                             const Operand<E, DT>& d, float c, float lse, float delta, bool all_seen, int last, int half) {
+    typedef Tile<E, DT> T;
+    float16v s = zero16(), dp = zero16();
+#pragma unroll
+    for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(kt, 0, x), q.x[x], s);
+#pragma unroll
+    for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(vt, 0, x), d.x[x], dp);
+    if (!all_seen) mask(s, last, half);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse)) * (dp[r] - delta);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        float x[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) x[r] = s[8 * t + r];
+        const typename E::Score ds = E::pack(x);
+#pragma unroll
+        for (int n = 0; n < DT; ++n) dq[n] = mma_t<DT>(rd, kt, t, n, ds, dq[n]);
     }
 }
 
@@ -218,60 +229,69 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         if constexpr (KB<E> == 2) {
             grad_q_tile<DT>(dq, rd, kt, vt, q, d, P.c, lse, delta, all_seen, last - j, half);
         } else {
-            float16v s = zero16(), dp = zero16();
-#pragma unroll
-            for (int x = 0; x < T::STEPS; ++x) s = E::mma(rd.rows(kt, 0, x), q.x[x], s);
-#pragma unroll
-            for (int x = 0; x < T::STEPS; ++x) dp = E::mma(rd.rows(vt, 0, x), d.x[x], dp);
-            if (!all_seen) mask(s, last - j, half);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.c, -lse)) * (dp[r] - delta);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float x[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) x[r] = s[8 * t + r];
-                const typename E::Score ds = E::pack(x);
-#pragma unroll
-                for (int n = 0; n < DT; ++n) dq[n] = mma_t<DT>(rd, kt, t, n, ds, dq[n]);
-            }
+            grad_q_block<E, DT>(dq, rd, kt, vt, q, d, P.c, lse, delta, all_seen, last - j, half);
         }
     }
-    const bool broken = there && lse == lse && delta == delta && not_finite(dq);
     const int64_t rows_q = int64_t(P.heads) * P.total_q;
     float* part = P.part + int64_t(blockIdx.y) * rows_q * (32 * DT);
-    if (STAGED && P.splits_q == 1) {
-        if constexpr (STAGED) {
-            __syncthreads();
-            R::store(lds + mine_at, dq, P.scale, const_cast<char*>(at<E>(P.dq, S.q0 + mine, head)), P.dq.token, unsigned(__ballot(there && !broken)), P.dim, lane);
-        }
-    } else if (there && !broken) {
-        if (P.splits_q == 1) {
-            char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
+    // lane, query: as the kernel's own
+    auto finish = [&](int lane, int query) {
+        const int half = lane >> 5;
+        const int64_t at_q = int64_t(head) * P.total_q + S.q0 + query;
+        const bool there = query < S.nq;
+        if (STAGED && P.splits_q == 1) {
+            if constexpr (STAGED)
+                R::store(lds + mine_at, dq, P.scale, const_cast<char*>(at<E>(P.dq, S.q0 + mine, head)), P.dq.token, unsigned(__ballot(there)), P.dim, lane);
+        } else if (there) {
+            if (P.splits_q == 1) {
+                char* row = const_cast<char*>(at<E>(P.dq, S.q0 + query, head));
 #pragma unroll
-            for (int n = 0; n < DT; ++n) store_column<E>(row, dq[n], P.scale, n, P.dim, half);
-        } else {
+                for (int n = 0; n < DT; ++n) store_column<E>(row, dq[n], P.scale, n, P.dim, half);
+            } else {
 #pragma unroll
-            for (int n = 0; n < DT; ++n) store_column<F32>(reinterpret_cast<char*>(part + at_q * (32 * DT)), dq[n], P.scale, n, 32 * DT, half);
-        }
-    }
-    for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
-        const int r = __ffs(rows) - 1, keys = min(to, __shfl(last, r, 64) + 1);
-        const float lse_r = __shfl(-lse / P.c, r, 64), delta_r = __shfl(-delta, r, 64);
-        const int64_t token = S.q0 + mine + r;
-        float sum[2] = {0.f, 0.f};
-        for (int j0 = from; j0 < keys; j0 += 64) {
-            float ds = 0.f;
-            if (j0 + lane < keys)
-                ds = score_grad<E>(P, token, head, S.k0 + j0 + lane, lse_r, delta_r).ds;
-            for (int t = 0; t < 64 && j0 + t < keys; ++t) add_row<E>(sum, __shfl(ds, t, 64), at<E>(P.k, S.k0 + j0 + t, kv), P.dim, lane);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < P.dim) {
-                if (P.splits_q == 1) put<E>(const_cast<char*>(at<E>(P.dq, token, head)), lane + 64 * e, sum[e] * P.scale);
-                else part[(int64_t(head) * P.total_q + token) * (32 * DT) + lane + 64 * e] = sum[e] * P.scale;
+                for (int n = 0; n < DT; ++n) store_column<F32>(reinterpret_cast<char*>(part + at_q * (32 * DT)), dq[n], P.scale, n, 32 * DT, half);
             }
+        }
+    };
+    __syncthreads();                                              // every wave is done with the tiles
+    finish(lane, query);
+    Marks& marks = *reinterpret_cast<Marks*>(lds + 4 * SIZE);
+    if (__builtin_expect(any_wave<WAVES>(marks, wave, there && lse == lse && delta == delta && not_finite(dq)), 0)) {
+        // Once more.  A key or value that is not finite makes no number of every entry of the dq that it reaches.
+        clear(marks, S.nk, threadIdx.x, WAVES * 64);
+#pragma unroll
+        for (int n = 0; n < DT; ++n) dq[n] = zero16();
+        const int lane = lane_anew(), half = lane >> 5, query = mine + (lane & 31), last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
+        Loader<E, DT, KEYS, WAVES> lk, lv;
+        lk.init(wave, lane, P.k.token, P.dim);
+        lv.init(wave, lane, P.v.token, P.dim);
+        Reader<E, DT> rd;
+        rd.init(lane);
+        Operand<E, DT> q, d;
+        q.load(at<E>(P.q, S.q0 + query, head), query < S.nq, P.dim, half);
+        d.load(at<E>(P.d_o, S.q0 + query, head), query < S.nq, P.dim, half);
+        for (int j = from; j < to; j += KEYS) {
+            lk.load(base, at<E>(P.k, S.k0 + j, kv), end - j, wave);
+            lv.load(base + SIZE, at<E>(P.v, S.k0 + j, kv), end - j, wave);
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            __syncthreads();
+            const auto mark = [&](int r, int, bool, bool) { mark_first(marks.any[0], j + r); };
+            lk.clean(lds, wave, lane, mark);
+            lv.clean(lds + SIZE, wave, lane, mark);
+            __syncthreads();
+            if (j < end_mine) {
+#pragma unroll 1
+                for (int b = 0; b < KB<E>; ++b) grad_q_block<E, DT>(dq, rd, lds + b * 32 * T::PITCH, lds + SIZE + b * 32 * T::PITCH, q, d, P.c, lse, delta, false, last - j - 32 * b, half);
+            }
+            __syncthreads();
+        }
+        if (marks.any[0] <= last) {
+#pragma unroll
+            for (int n = 0; n < DT; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dq[n][r] = __builtin_nanf("");
+        }
+        finish(lane, query);
     }
 }
 
@@ -409,7 +429,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     lq.init(wave, lane, P.q.token, P.dim);
     ld.init(wave, lane, P.d_o.token, P.dim);
     const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((ONECOMP_LDS char*)lds));
-    auto bring = [&](int head, int r, int buf) {
+    auto bring_with = [&](const Loader<E, DT, ROWS, WAVES>& lq, const Loader<E, DT, ROWS, WAVES>& ld, int lane, int head, int r, int buf) {
         const uint32_t to = base + uint32_t(buf) * BUF;
         lq.load(to, at<E>(P.q, S.q0 + r, head), S.nq - r, wave);
         ld.load(to + SIZE, at<E>(P.d_o, S.q0 + r, head), S.nq - r, wave);
@@ -419,6 +439,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
             lds_load4(to + 2 * SIZE + uint32_t(wave) * 256u, uint32_t(lane) * 4u, rsrc);
         }
     };
+    auto bring = [&](int head, int r, int buf) { bring_with(lq, ld, lane, head, r, buf); };
     constexpr bool STAGED = sizeof(typename E::T) == 2;           // rows through LDS
     Reader<E, DT> rd;
     rd.init(lane);
@@ -466,69 +487,99 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         head = next_head;
         r0 = next;
     }
-    if (key >= S.nk) {
-#pragma unroll
-        for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
-    }
-    const bool broken = not_finite(dk) || not_finite(dv);
     // sums of a share: those for dk, then those for dv
     const int64_t rows_k = int64_t(P.kv_heads) * P.total_k;
     float* part = P.part + P.splits_q * (P.splits_q > 1) * int64_t(P.heads) * P.total_q * (32 * DT) + 2 * int64_t(blockIdx.y) * rows_k * (32 * DT);
-    if (STAGED && P.splits_k == 1) {
-        if constexpr (STAGED) {
-            __syncthreads();
-            const unsigned which = unsigned(__ballot(key < S.room && !broken));
-            R::store(lds + mine_at, dk, P.scale, const_cast<char*>(at<E>(P.dk, S.k0 + mine, kv)), P.dk.token, which, P.dim, lane);
-            R::store(lds + 2 * SIZE + mine_at, dv, 1.f, const_cast<char*>(at<E>(P.dv, S.k0 + mine, kv)), P.dv.token, which, P.dim, lane);
-        }
-    } else if (key < S.room && !broken) {
-        if (P.splits_k == 1) {
-            char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
-            char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
+    // lane, key: as the kernel's own
+    auto finish = [&](int lane, int key) {
+        const int half = lane >> 5;
+        if (key >= S.nk) {
 #pragma unroll
-            for (int n = 0; n < DT; ++n) {
-                store_column<E>(row_k, dk[n], P.scale, n, P.dim, half);
-                store_column<E>(row_v, dv[n], 1.f, n, P.dim, half);
-            }
-        } else {
-            float* to = part + (int64_t(kv) * P.total_k + S.k0 + key) * (32 * DT);
-#pragma unroll
-            for (int n = 0; n < DT; ++n) {
-                store_column<F32>(reinterpret_cast<char*>(to), dk[n], P.scale, n, 32 * DT, half);
-                store_column<F32>(reinterpret_cast<char*>(to + rows_k * (32 * DT)), dv[n], 1.f, n, 32 * DT, half);
-            }
+            for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
         }
-    }
-    for (unsigned cols = unsigned(__ballot(broken)); cols; cols &= cols - 1) {
-        const int j = mine + __ffs(cols) - 1, seen_from = P.causal ? max(0, j - S.shift) : 0;
-        float sum_k[2] = {0.f, 0.f}, sum_v[2] = {0.f, 0.f};
-        for (int step = step0; step < total; ++step) {
-            const int h = head0 + step / steps, first_q = begin + step % steps * ROWS;
-            Pair x = {0.f, 0.f};
-            const int q = first_q + lane;
-            if (lane < ROWS && q >= seen_from && q < S.nq) {
-                const int64_t at_q = int64_t(h) * P.total_q + S.q0 + q;
-                x = score_grad<E>(P, S.q0 + q, h, S.k0 + j, P.aux[at_q], P.aux[int64_t(P.heads) * P.total_q + at_q]);
+        if (STAGED && P.splits_k == 1) {
+            if constexpr (STAGED) {
+                const unsigned which = unsigned(__ballot(key < S.room));
+                R::store(lds + mine_at, dk, P.scale, const_cast<char*>(at<E>(P.dk, S.k0 + mine, kv)), P.dk.token, which, P.dim, lane);
+                R::store(lds + 2 * SIZE + mine_at, dv, 1.f, const_cast<char*>(at<E>(P.dv, S.k0 + mine, kv)), P.dv.token, which, P.dim, lane);
             }
-            for (int t = 0; t < ROWS; ++t) {
-                if (first_q + t < seen_from || first_q + t >= S.nq) continue;
-                add_row<E>(sum_v, __shfl(x.p, t, 64), at<E>(P.d_o, S.q0 + first_q + t, h), P.dim, lane);
-                add_row<E>(sum_k, __shfl(x.ds, t, 64), at<E>(P.q, S.q0 + first_q + t, h), P.dim, lane);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int d = lane + 64 * e;
-            if (d >= P.dim) continue;
+        } else if (key < S.room) {
             if (P.splits_k == 1) {
-                put<E>(const_cast<char*>(at<E>(P.dk, S.k0 + j, kv)), d, sum_k[e] * P.scale);
-                put<E>(const_cast<char*>(at<E>(P.dv, S.k0 + j, kv)), d, sum_v[e]);
+                char* row_k = const_cast<char*>(at<E>(P.dk, S.k0 + key, kv));
+                char* row_v = const_cast<char*>(at<E>(P.dv, S.k0 + key, kv));
+#pragma unroll
+                for (int n = 0; n < DT; ++n) {
+                    store_column<E>(row_k, dk[n], P.scale, n, P.dim, half);
+                    store_column<E>(row_v, dv[n], 1.f, n, P.dim, half);
+                }
             } else {
-                float* to = part + (int64_t(kv) * P.total_k + S.k0 + j) * (32 * DT) + d;
-                to[0] = sum_k[e] * P.scale;
-                to[rows_k * (32 * DT)] = sum_v[e];
+                float* to = part + (int64_t(kv) * P.total_k + S.k0 + key) * (32 * DT);
+#pragma unroll
+                for (int n = 0; n < DT; ++n) {
+                    store_column<F32>(reinterpret_cast<char*>(to), dk[n], P.scale, n, 32 * DT, half);
+                    store_column<F32>(reinterpret_cast<char*>(to + rows_k * (32 * DT)), dv[n], 1.f, n, 32 * DT, half);
+                }
             }
         }
+    };
+    __syncthreads();                                              // every wave is done with the tiles
+    finish(lane, key);
+    Marks& marks = *reinterpret_cast<Marks*>(lds + 2 * BUF);
+    if (__builtin_expect(any_wave<WAVES>(marks, wave, not_finite(dk) || not_finite(dv)), 0)) {
+        // Once more.  A query or log-sum-exp that is not finite makes no numbers of the dk and dv that it reaches (any[0]), a row of
+        // d_out or a delta of those dk (any[1]).
+        clear(marks, -1, threadIdx.x, WAVES * 64);
+#pragma unroll
+        for (int n = 0; n < DT; ++n) dk[n] = dv[n] = zero16();
+        const int lane = lane_anew(), half = lane >> 5, key = mine + (lane & 31);
+        Loader<E, DT, ROWS, WAVES> lq, ld;
+        lq.init(wave, lane, P.q.token, P.dim);
+        ld.init(wave, lane, P.d_o.token, P.dim);
+        Reader<E, DT> rd;
+        rd.init(lane);
+        Operand<E, DT> k, v;
+        k.load(at<E>(P.k, S.k0 + key, kv), key < S.nk, P.dim, half);
+        v.load(at<E>(P.v, S.k0 + key, kv), key < S.nk, P.dim, half);
+        for (int step = step0; step < total; ++step) {
+            const int r = begin + step % steps * ROWS;
+            bring_with(lq, ld, lane, head0 + step / steps, r, 0);
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            __syncthreads();
+            lq.clean(lds, wave, lane, [&](int row, int, bool, bool) { mark_last(marks.any[0], r + row); });
+            ld.clean(lds + SIZE, wave, lane, [&](int row, int c, bool up, bool down) {
+                if (up) mark_last(marks.up(c), r + row);
+                if (down) mark_last(marks.down(c), r + row);
+                mark_last(marks.any[1], r + row);
+            });
+            if (wave < 2) {
+                float& x = reinterpret_cast<float*>(lds + 2 * SIZE)[64 * wave + lane];
+                // -inf in front of the scores is a query that sees nothing
+                if (!(wave == 0 ? x < -NEG_INF : x * 0.f == 0.f)) {
+                    mark_last(marks.any[wave], r + lane);
+                    x = wave == 0 ? NEG_INF : 0.f;
+                }
+            }
+            __syncthreads();
+            if (r + ROWS > begin_mine) {
+#pragma unroll 1
+                for (int b = 0; b < KB<E>; ++b)
+                    grad_kv_block<E, DT>(dk, dv, rd, lds + b * 32 * T::PITCH, lds + SIZE + b * 32 * T::PITCH, reinterpret_cast<const float*>(lds + 2 * SIZE) + 32 * b, k, v,
+                                         P.c, r >= all, key - S.shift - r - 32 * b, half);
+            }
+            __syncthreads();
+        }
+        const int seen_from = P.causal ? max(0, key - S.shift) : 0;
+        const float no_k = max(marks.any[0], marks.any[1]) >= seen_from ? __builtin_nanf("") : 0.f, no_v = marks.any[0] >= seen_from ? __builtin_nanf("") : 0.f;
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+            give_back(dv[n], marks, n, half, [&](int row) { return row >= seen_from; });
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                dk[n][r] += no_k;
+                dv[n][r] += no_v;
+            }
+        }
+        finish(lane, key);
     }
 }
 
@@ -561,7 +612,7 @@ onecomp_status join(const View& out, const float* part, int splits, int64_t stri
 template <class E, int DT, int WQ, int WK>
 onecomp_status launch_backward(const Params& P, hipStream_t stream) {
     typedef Tile<E, DT> T;
-    constexpr int LDS_Q = 4 * T::bytes(32 * KB<E>), LDS_K = LDS_Q + 1024;
+    constexpr int TILES = 4 * T::bytes(32 * KB<E>), LDS_Q = TILES + int(sizeof(Marks)), LDS_K = TILES + 1024 + int(sizeof(Marks));
     static std::atomic<uint64_t> done_q{0}, done_k{0};
     onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(grad_q_kernel<E, DT, WQ>), LDS_Q, done_q);
     if (st != ONECOMP_OK) return st;

@@ -167,6 +167,14 @@ struct Rows32 {
 // values and half for the scores of two tiles.  16384 tokens, 32 / 8 heads of 128: 1.99 ms, 1.1 PFLOP/s at 1.66 GHz (power), the
 // matrix pipes busy 62 %; 32 x 2048: 1.31 ms.
 template <class E, int DT, int WAVES>
+struct Whole {
+    static constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1, SIZE = Tile<E, DT>::bytes(32 * KB);
+    // two tiles of keys, two of values; bf16: behind them what the queries need besides the last; or a wave's own tiles of a second pass
+    static constexpr int OWN = (2 * Tile<E, DT>::bytes(32) + int(sizeof(Marks)) + 1023) / 1024 * 1024, TILES = 3 * SIZE + (KB == 2 ? WAVES * Rows<E, DT>::BYTES : SIZE);
+    static constexpr int LDS = TILES > WAVES * OWN ? TILES : WAVES * OWN;
+};
+
+template <class E, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void forward_kernel(const Params P) {
     constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1, KEYS = 32 * KB;
     typedef Tile<E, DT> T;
@@ -265,29 +273,66 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
         }
     }
     for (; t < n; ++t) next(t);
-    const float l = acc.l + other_half(acc.l), f = l == 0.f ? 0.f : 1.f / l;
-    const bool broken = there && l == l && not_finite(acc.o);
-    if constexpr (STAGED) {
-        __syncthreads();                                          // every wave is done with the tiles
-        Rows<E, DT>::store(lds + wave * Rows<E, DT>::BYTES, acc.o, f, const_cast<char*>(at<E>(P.o, S.q0 + mine, head)), P.o.token,
-                           unsigned(__ballot(there && !broken)), P.dim, lane);
-    } else if (there && !broken) {
-        char* row = const_cast<char*>(at<E>(P.o, S.q0 + query, head));
+    constexpr int OWN = Whole<E, DT, WAVES>::OWN;
+    // lane, query: as the kernel's own; true where the sums are to be looked at
+    auto finish = [&](int lane, int query) {
+        const int half = lane >> 5;
+        const bool there = query < S.nq;
+        const float l = acc.l + other_half(acc.l), f = l == 0.f ? 0.f : 1.f / l;
+        if constexpr (STAGED) {
+            Rows<E, DT>::store(lds + wave * OWN, acc.o, f, const_cast<char*>(at<E>(P.o, S.q0 + mine, head)), P.o.token, unsigned(__ballot(there)), P.dim, lane);
+        } else if (there) {
+            char* row = const_cast<char*>(at<E>(P.o, S.q0 + query, head));
 #pragma unroll
-        for (int n = 0; n < DT; ++n) store_column<E>(row, acc.o[n], f, n, P.dim, half);
+            for (int n = 0; n < DT; ++n) store_column<E>(row, acc.o[n], f, n, P.dim, half);
+        }
+        if (there && P.lse && half == 0)
+            P.lse[int64_t(head) * P.total_q + S.q0 + query] = l == 0.f ? NEG_INF : (acc.m + __builtin_amdgcn_logf(l)) * LN2;
+        return there && l == l;
+    };
+    const bool look = P.causal && not_finite(acc.o);
+    __syncthreads();                                              // every wave is done with the tiles
+    if (__builtin_expect(!__any(finish(lane, query) && look), 1)) return;
+
+    // Once more, each wave by itself.
+    const int lane_2 = lane_anew(), half_2 = lane_2 >> 5, query_2 = mine + (lane_2 & 31), last_2 = min(S.nk - 1, query_2 + S.shift);
+    char* own = lds + wave * OWN;
+    const uint32_t own_base = base + uint32_t(wave) * OWN;
+    constexpr int TILE = T::bytes(32);
+    Marks& marks = *reinterpret_cast<Marks*>(own + 2 * TILE);
+    clear(marks, S.nk, lane_2, 64);
+    Loader<E, DT, 32, 1> keys, values;
+    keys.init(0, lane_2, P.k.token, P.dim);
+    values.init(0, lane_2, P.v.token, P.dim);
+    Reader<E, DT> rd_2;
+    rd_2.init(lane_2);
+    q.load(at<E>(P.q, S.q0 + query_2, head), query_2 < S.nq, P.dim, half_2);
+    acc.init();
+    auto bring_2 = [&](const Loader<E, DT, 32, 1>& rows, uint32_t to, const View& from, int j) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the last tile is read
+        if (j < end_mine) rows.load(to, at<E>(from, S.k0 + j, kv), end_mine - j, 0);
+    };
+    bring_2(keys, own_base, P.k, 0);
+    bring_2(values, own_base + TILE, P.v, 0);
+    for (int j = 0; j < end_mine; j += 32) {
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        asm volatile("" ::: "memory");
+        float16v s[1];
+        acc.template scores<1>(s, rd_2, own, q);
+        bring_2(keys, own_base, P.k, j + 32);
+        acc.settle(acc.mask(s, last_2 - j, half_2), P.c);
+        values.clean(own + TILE, 0, lane_2, [&](int r, int c, bool up, bool down) {
+            if (up) mark_first(marks.up(c), j + r);
+            if (down) mark_first(marks.down(c), j + r);
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        acc.template values<1>(s, rd_2, own + TILE, P.c);
+        bring_2(values, own_base + TILE, P.v, j + 32);
     }
-    if (there && P.lse && half == 0)
-        P.lse[int64_t(head) * P.total_q + S.q0 + query] = l == 0.f ? NEG_INF : (acc.m + __builtin_amdgcn_logf(l)) * LN2;
-    for (unsigned rows = unsigned(__ballot(broken)); rows; rows &= rows - 1) {
-        const int r = __ffs(rows) - 1;
-        const float m = __shfl(acc.m, r, 64), g = __shfl(f, r, 64);
-        const int64_t token = S.q0 + mine + r;
-        float sum[2];
-        careful_values<E>(sum, P, S, token, head, 0, __shfl(last, r, 64) + 1, m == NEG_INF ? 0.f : m, lane);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < P.dim) put<E>(const_cast<char*>(at<E>(P.o, token, head)), lane + 64 * e, sum[e] * g);
-    }
+    for (int n = 0; n < DT; ++n) give_back(acc.o[n], marks, n, half_2, [&](int row) { return row <= last_2; });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    finish(lane_2, query_2);
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
@@ -301,9 +346,9 @@ struct Few {
     static constexpr int SIZE = T::bytes(32);
     // two tiles of keys and of values per wave; 64 KB, so that one workgroup begins or ends beside another's work
     static constexpr int WAVES = SIZE >= 16 * 1024 ? 1 : SIZE >= 8 * 1024 ? 2 : 4;
-    static constexpr int LDS = 4 * SIZE * WAVES;
+    static constexpr int TILES = 4 * SIZE * WAVES, LDS = TILES + int(sizeof(Marks));
     static constexpr int COLS = 32 * DT;                               // of a partial sum's row
-    static_assert(LDS >= WAVES * DT * 4096 + WAVES * 256, "the waves' sums meet in the same memory");
+    static_assert(TILES >= WAVES * DT * 4096 + WAVES * 256, "the waves' sums meet in the same memory");
 };
 
 // Scratch: runs of each row [rows], maximum and sum of each run [splits, rows, 2], its sums of values [splits, rows, COLS].
@@ -325,6 +370,7 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Parts parts(P);
+    Marks& marks = *reinterpret_cast<Marks*>(lds + F::TILES);
     // pieces of work in turn, whatever number of workgroups the host thought enough
     for (int piece = blockIdx.x;; piece += gridDim.x) {
     const int kv = piece % P.kv_heads;
@@ -340,6 +386,8 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     const int end_all = P.causal ? min(S.nk, first_q + 1 + S.shift) : S.nk;
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
 
+    // again: once more, with zeros for values that are not finite
+    for (bool again = false;; again = true) {
     Rows32<E, DT> acc;
     acc.init();
     if (begin < end) {
@@ -369,6 +417,13 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
                 __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
             }
             asm volatile("" ::: "memory");
+            if (again) {
+                lv.clean(own + buf * 2 * F::SIZE + F::SIZE, 0, lane, [&](int r, int c, bool up, bool down) {
+                    if (up) mark_first(marks.up(c), j + r);
+                    if (down) mark_first(marks.down(c), j + r);
+                });
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
             float16v s[1];
             acc.template scores<1>(s, rd, own + buf * 2 * F::SIZE, q);
             acc.settle(acc.mask(s, last - j, half), P.c);
@@ -404,35 +459,22 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     const int64_t at_row = int64_t(head) * P.total_q + S.q0 + query, rows = int64_t(P.heads) * P.total_q;
     const bool whole = P.splits == 1;
     const float out = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    bool broken = false;
     for (int n = wave; n < DT; n += F::WAVES) {
         float16v o = zero16();
 #pragma unroll
         for (int w = 0; w < F::WAVES; ++w)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[r] = fmaf(f[w], sums[((w * DT + n) * 16 + r) * 64 + lane], o[r]);
+        if (again) give_back(o, marks, n, half, [&](int key) { return key <= last; });
         float16v one[1] = {o};
-        const bool broken = there && l == l && not_finite(one);
-        if (there && !broken) {
+        broken = broken || (there && l == l && not_finite(one));
+        if (there) {
             if (whole) {
                 store_column<E>(const_cast<char*>(at<E>(P.o, S.q0 + query, head)), o, out, n, P.dim, half);
             } else {
                 char* to = reinterpret_cast<char*>(parts.sums + (split * rows + at_row) * F::COLS);
                 store_column<F32>(to, o, 1.f, n, F::COLS, half);
-            }
-        }
-        for (unsigned bad = unsigned(__ballot(broken)); bad; bad &= bad - 1) {
-            const int r = __ffs(bad) - 1;
-            const int64_t token = S.q0 + __shfl(query, r, 64);
-            const int h = __shfl(head, r, 64);
-            const float m = __shfl(zero, r, 64), g = __shfl(out, r, 64);
-            float sum[2];
-            careful_values<E>(sum, P, S, token, h, begin, min(end, __shfl(last, r, 64) + 1), m, lane);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int d = lane + 64 * e;
-                if (d / 32 != n) continue;
-                if (whole && d < P.dim) put<E>(const_cast<char*>(at<E>(P.o, token, h)), d, sum[e] * g);
-                if (!whole) parts.sums[(split * rows + int64_t(h) * P.total_q + token) * F::COLS + d] = sum[e];
             }
         }
     }
@@ -444,6 +486,11 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
         } else if (P.lse) {
             P.lse[at_row] = l == 0.f ? NEG_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
         }
+    }
+    if (again) break;
+    if (__builtin_expect(!any_wave<F::WAVES>(marks, wave, P.causal && broken), 1)) break;
+    clear(marks, S.nk, threadIdx.x, F::WAVES * 64);
+    __syncthreads();
     }
     __syncthreads();                                              // the next piece's tiles go where the sums met
     }
@@ -486,9 +533,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Params P) {
 
 template <class E, int DT, int WAVES>
 onecomp_status launch_forward(const Params& P, hipStream_t stream) {
-    constexpr int KEYS = sizeof(typename E::T) == 2 ? 64 : 32;
-    // bf16: behind the tiles of keys and values what the queries need besides the last of them
-    constexpr int SIZE = Tile<E, DT>::bytes(KEYS), LDS = sizeof(typename E::T) == 2 ? 3 * SIZE + WAVES * Rows<E, DT>::BYTES : 4 * SIZE;
+    constexpr int LDS = Whole<E, DT, WAVES>::LDS;
     static std::atomic<uint64_t> done{0};
     const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(forward_kernel<E, DT, WAVES>), LDS, done);
     if (st != ONECOMP_OK) return st;
