@@ -8,6 +8,7 @@
 // score ever moves between lanes.
 #pragma once
 #include "common.hpp"
+#include "attention_plan.hpp"
 
 namespace onecomp {
 namespace attn {
@@ -243,14 +244,6 @@ __device__ __forceinline__ int wave_max(int x) {
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// Few rows: keys of one piece of work.  Runs of P.run or, where the host knew of fewer keys than there are, as many as it
-// takes for P.splits runs to cover them all.
-__device__ __forceinline__ int run_of(const Params& P, int nk) { return max(P.run, (nk + P.splits * 128 - 1) / (P.splits * 128) * 128); }
-__device__ __forceinline__ int runs_of(const Params& P, int nk) {
-    const int run = run_of(P, nk);
-    return max(1, (nk + run - 1) / run);
-}
-
 // What is counted: tiles of `size` queries, tiles of `size` keys with the room behind them, or pieces of work of few rows
 // (blocks of 32 rows, of which every query has one per head of a group, times runs of keys).
 enum What { QUERIES, KEYS, PIECES };
@@ -275,7 +268,7 @@ __device__ __forceinline__ bool find_tile(const Params& P, int size, int t, Seq&
             nq = rows_of(P.cu_q, P.total_q, P.n_seqs, i, q0);
             room = rows_of(P.cu_k, P.total_k, P.n_seqs, i, k0);
             nk = i == P.n_seqs ? 0 : P.len_k ? int(clamp64(P.len_k[i], 0, room)) : room;
-            if (WHAT == PIECES) count = int((int64_t(nq) * P.group + 31) / 32) * runs_of(P, nk);
+            if (WHAT == PIECES) count = int((int64_t(nq) * P.group + 31) / 32) * runs_of(P.run, P.splits, nk);
             else count = int((int64_t(WHAT == KEYS ? room : nq) + size - 1) / size);
         }
         int mine = count;                                         // tiles of this lane's sequence among those looked at

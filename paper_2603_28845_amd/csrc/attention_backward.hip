@@ -130,7 +130,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int end_all = P.causal ? min(S.nk, mine + 1 + S.shift) : S.nk;
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
     // this workgroup's share of them, where the keys are split
-    const int share = (end + KEYS * P.splits_q - 1) / (KEYS * P.splits_q) * KEYS, from = int(blockIdx.y) * share, to = min(end, from + share);
+    const Range share = share_of(end, KEYS, P.splits_q, int(blockIdx.y));
+    const int from = share.begin, to = share.end;
 
     Loader<E, DT, KEYS, WAVES> lk, lv;
     lk.init(wave, lane, P.k.token, P.dim);

@@ -377,12 +377,13 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     int x, pieces;
     Seq S;
     if (!find_tile<PIECES>(P, 0, piece / P.kv_heads, S, x, pieces)) return;
-    const int run = run_of(P, S.nk), runs = runs_of(P, S.nk), tile = x / runs, split = x % runs;
+    const int run = run_of(P.run, P.splits, S.nk), runs = runs_of(P.run, P.splits, S.nk), tile = x / runs, split = x % runs;
     const int row = tile * 32 + col, query = row / P.group, head = kv * P.group + row % P.group;
     const bool there = query < S.nq;
     const int last_q = min((tile * 32 + 31) / P.group, S.nq - 1), first_q = tile * 32 / P.group;
     const int seen = P.causal ? max(0, min(S.nk, last_q + 1 + S.shift)) : S.nk;
-    const int begin = split * run, end = min(seen, begin + run);
+    const Range keys = run_range(run, split, seen);
+    const int begin = keys.begin, end = keys.end;
     const int end_all = P.causal ? min(S.nk, first_q + 1 + S.shift) : S.nk;
     const int last = P.causal ? min(S.nk - 1, query + S.shift) : S.nk - 1;
 
