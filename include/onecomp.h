@@ -422,8 +422,8 @@ typedef struct {
  * cu_k[i + 1] - 1, or len_k[i] of them (a cache with room behind the sequence).  cu_q[0] = cu_k[0] = 0, non-decreasing.
  *   causal   query i of a sequence of a queries and b keys sees the keys 0 .. i + b - a (its own token is the last); without
  *            it, all b.  A query that sees no key has output 0, log-sum-exp -inf and gradient 0.
- *   max_q, max_k   the longest sequence's lengths.  They choose between launch shapes and say nothing about the results:
- *            lengths are read from the arrays, cut to the tensors' rows.
+ *   max_q, max_k   the longest sequence's lengths, or more if they are not known (total_q, total_k).  They choose between launch
+ *            shapes and say nothing about the results: lengths are read from the arrays, cut to the tensors' rows.
  * Rows behind the last sequence are padding: outputs and gradients there are set to 0 (log-sum-exps to -inf). */
 typedef struct {
     onecomp_dtype dtype;       /* of q, k, v, out and their gradients */

@@ -140,8 +140,9 @@ attn::Params attention_params(const onecomp_attention_shape* s) {
     P.causal = s->causal != 0;
     P.scale = s->scale;
     P.c = s->scale * attn::LOG2E;
-    P.max_q = s->max_q;
-    P.max_k = s->max_k;
+    // no sequence has more keys than all of them; more queries than there are still ask for the launch shape of so many
+    P.max_q = s->max_q < (int64_t(1) << 31) ? s->max_q : int64_t(1) << 31;
+    P.max_k = s->max_k < s->total_k ? s->max_k : s->total_k;
     return P;
 }
 }  // namespace

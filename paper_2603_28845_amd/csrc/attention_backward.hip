@@ -654,7 +654,7 @@ void plan(onecomp_dtype dtype, Params& P) {
         return int(n < 2 || most < 2 ? 1 : n < most ? n : most);
     };
     P.splits_q = P.total_q ? splits(groups_q, ceil_div(P.max_k, 64)) : 1;
-    P.splits_k = P.total_k ? splits(groups_k, ceil_div(P.max_q, 64) * P.group) : 1;
+    P.splits_k = P.total_k ? splits(groups_k, ceil_div(P.max_q < P.total_q ? P.max_q : P.total_q, 64) * P.group) : 1;
 }
 
 }  // namespace
