@@ -445,7 +445,7 @@ typedef struct {
  * the keys with running maximum and sum in fp32; bf16 products are exact and added in fp32, the probabilities are rounded to
  * bf16 for their product with v, fp32 inputs are multiplied in fp32.  What lies behind a query's last key never reaches its
  * result, NaN and infinities included.
- *   out        [total_q, n_heads, head_dim]
+ *   out        [total_q, n_heads, head_dim], over none of the inputs
  *   lse        device fp32 [n_heads, total_q], or NULL (it is wanted for onecomp_attention_backward)
  *   workspace  >= onecomp_attention_workspace_bytes(shape) bytes, 256-byte aligned (0 bytes: may be NULL).  Where there are few
  *              rows the keys are split between workgroups, whose sums meet there, in an order that depends on the sizes alone.
@@ -459,7 +459,8 @@ size_t onecomp_attention_workspace_bytes(const onecomp_attention_shape* shape);
  * Gradients of onecomp_attention_forward from that of its output, d_out, with out and lse as it left them:
  *   dv_j = sum_i p_ij d_out_i,  ds_ij = p_ij (d_out_i . v_j - d_out_i . out_i),
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
- * dk and dv summed over the heads of a group.  dq, dk and dv are overwritten (rows of k and v that no query sees get 0).
+ * dk and dv summed over the heads of a group.  dq, dk and dv are overwritten (rows of k and v that no query sees get 0); they
+ * lie over none of each other and of the inputs.
  * Sums in fp32, bf16 factors of the products as in the forward call, no atomics: the same inputs give the same bits.
  * An infinity or NaN among the inputs reaches the gradients of the pairs that see it, which are then not finite, and no others.
  *   workspace  >= onecomp_attention_backward_workspace_bytes(shape), 256-byte aligned.

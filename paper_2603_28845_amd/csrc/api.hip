@@ -67,6 +67,9 @@ bool check_heads(const onecomp_attention_shape* s, const onecomp_heads* h, int64
            h->head_stride <= (int64_t(1) << 40) && (h->token_stride * esz) % 16 == 0 && (h->head_stride * esz) % 16 == 0;
 }
 
+// whether two tensors begin at the same place; rows: 0 if either has none
+bool same(const onecomp_heads* a, const onecomp_heads* b, int64_t rows) { return rows > 0 && a->data == b->data; }
+
 onecomp_status check_norm(const onecomp_norm_shape* s) {
     if (!s) return ONECOMP_ERR_INVALID_ARG;
     if ((s->dtype != ONECOMP_F32 && s->dtype != ONECOMP_BF16) || (s->w_dtype != ONECOMP_F32 && s->w_dtype != ONECOMP_BF16)) return ONECOMP_ERR_UNSUPPORTED;
@@ -416,6 +419,7 @@ ONECOMP_API onecomp_status onecomp_attention_forward(const onecomp_attention_sha
     const size_t need = attn::forward_workspace_bytes(shape->dtype, P);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
     if (P.total_q == 0) return ONECOMP_OK;
+    if (same(out, k, shape->total_k) || same(out, v, shape->total_k)) return ONECOMP_ERR_INVALID_ARG;
     P.q = view(q);
     P.k = view(k);
     P.v = view(v);
@@ -443,6 +447,13 @@ ONECOMP_API onecomp_status onecomp_attention_backward(const onecomp_attention_sh
     attn::Params P = attention_params(shape);
     const size_t need = attn::backward_workspace_bytes(shape->dtype, P);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
+    // dk and dv are formed from all queries and d_out when dq has been written, dq from all keys and values
+    const bool q_k = P.total_q && P.total_k;
+    for (const onecomp_heads* in : {q, d_out})
+        if (same(dq, in, P.total_q) || same(dk, in, q_k) || same(dv, in, q_k)) return ONECOMP_ERR_INVALID_ARG;
+    for (const onecomp_heads* other : {k, v, dk, dv})
+        if (same(dq, other, q_k)) return ONECOMP_ERR_INVALID_ARG;
+    if (same(dk, dv, P.total_k)) return ONECOMP_ERR_INVALID_ARG;
     P.q = view(q);
     P.k = view(k);
     P.v = view(v);

@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from test_block_host import _shape, lib  # noqa: F401
+from test_block_host import INVALID, P, _backward, _forward, _heads, _shape, lib  # noqa: F401
 
 
 @pytest.mark.parametrize("total_q,total_k", [(3000, 100000), (40, 5000), (4, 200000)])
@@ -18,3 +18,17 @@ def test_longest_lengths_beyond_the_tensors(lib, name, total_q, total_k):  # noq
         assert need(total_q, most) == want
         # launch shapes of many queries need no more than those of few
         assert need(most, total_k) <= want and need(most, most) <= want
+
+
+def test_results_over_what_is_still_read(lib):  # noqa: F811
+    """Gradients of queries over q or d_out, which those of keys are formed from next, and the like: refused before anything runs."""
+    def apart():
+        return [_heads(data=P * (i + 1)) for i in range(8)]           # q, k, v, out, d_out, dq, dk, dv
+
+    for result, over in ((5, 0), (5, 1), (5, 2), (5, 4), (6, 0), (6, 4), (7, 0), (7, 4), (6, 5), (7, 5), (7, 6)):
+        views = apart()
+        views[result] = views[over]
+        assert _backward(lib, views=views) == INVALID, (result, over)
+    q, k, v, out = apart()[:4]
+    assert _forward(lib, q=q, k=k, v=v, out=k) == INVALID
+    assert _forward(lib, q=q, k=k, v=v, out=v) == INVALID
