@@ -248,18 +248,56 @@ __device__ __forceinline__ int wave_max(int x) {
 // (blocks of 32 rows, of which every query has one per head of a group, times runs of keys).
 enum What { QUERIES, KEYS, PIECES };
 
-// The t-th of all sequences: its sequence, its number x there and how many the sequence has; false if there are fewer.  What
-// the arrays say is cut to the tensors' rows.  Of up to 63 sequences they come by their number x, the largest first and at the
+enum Found { NOTHING, IDLE, TILE };
+
+// The t-th of all sequences: its sequence, its number x there and how many the sequence has; IDLE if there is no such tile but may be
+// some behind it, NOTHING if there are none.  What the arrays say is cut to the tensors' rows.
+//
+// Sequences are counted, a lane each.  Of up to 63 the tiles come by their number x, the largest first and at the
 // same x by sequence: x + 1 tiles of keys lie before a causal prompt's tile x, so that long work starts early and the last
 // workgroups are short (gradients of 8 x 2048 keys: 540 us instead of 680 sequence by sequence).  Tiles of queries come
 // sequence by sequence, each from its largest x down, where the last sequence cannot keep the others waiting: all are equally
 // long, or the longest tile is an eighth of the work of each of 512 workgroups at most.  Then the tiles at work at a time share
 // keys and values in the L2 (32 x 2048 tokens: 0.9 GB over the fabric instead of 2.8, 1.32 ms instead of 1.40).  More
 // sequences come one after the other in any case: counting by number would read the arrays many times.
+//
+// Many sequences are not counted, which would make every workgroup read all of them before its own: slots are searched, 64 places
+// at a time.  16384 prompts of 1 to 16 tokens, 8 / 2 heads of 64: 16.9 ms counted, 0.72 searched, their gradients 28 and 2.6, 500
+// of 20 to 200 tokens 113 and 86 us, 128 of 100 to 500 65 and 67.  A few rows' slots stand for runs of keys that are not there too, so that
+// counting pays for longer: 500 tokens 154 us counted and 247 searched, 1000 308 and 311, 4000 1500 and 175.
 // Every lane of a wave takes part and gets the same answer.
 template <What WHAT>
-__device__ __forceinline__ bool find_tile(const Params& P, int size, int t, Seq& S, int& x, int& tiles) {
+__device__ __forceinline__ Found find_tile(const Params& P, int size, int t, Seq& S, int& x, int& tiles) {
     const int lane = threadIdx.x & 63;
+    if (P.n_seqs >= (WHAT == PIECES ? MANY_TOKENS : MANY)) {
+        const int32_t* cu = WHAT == KEYS ? P.cu_k : P.cu_q;
+        const int64_t total = WHAT == KEYS ? P.total_k : P.total_q, rows = WHAT == PIECES ? P.group : 1;
+        const int unit = WHAT == PIECES ? 32 : size, slot = WHAT == PIECES ? t / P.splits : t;
+        if (slot >= all_slots(total * rows, unit, P.n_seqs)) return NOTHING;
+        int lo = 0, hi = P.n_seqs + 1;                            // the last sequence whose slots begin at `slot` or before
+        do {
+            const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const unsigned long long before = __ballot(at < hi && first_slot(clamp64(cu[min(at, P.n_seqs)], 0, total) * rows, unit, at) <= slot);
+            if (!before) return IDLE;                             // rows in front of the first sequence
+            lo += (63 - __clzll((long long)before)) * step;
+            hi = min(hi, lo + step);
+        } while (hi - lo > 1);
+        int q0, k0;
+        const int nq = rows_of(P.cu_q, P.total_q, P.n_seqs, lo, q0), room = rows_of(P.cu_k, P.total_k, P.n_seqs, lo, k0);
+        S.q0 = __builtin_amdgcn_readfirstlane(q0);
+        S.k0 = __builtin_amdgcn_readfirstlane(k0);
+        S.nq = __builtin_amdgcn_readfirstlane(nq);
+        S.room = __builtin_amdgcn_readfirstlane(room);
+        S.nk = lo == P.n_seqs ? 0 : P.len_k ? __builtin_amdgcn_readfirstlane(int(clamp64(P.len_k[lo], 0, room))) : S.room;
+        S.shift = S.nk - S.nq;
+        const int runs = WHAT == PIECES ? runs_of(P.run, P.splits, S.nk) : 1, split = WHAT == PIECES ? t % P.splits : 0;
+        const int count = int((int64_t(WHAT == KEYS ? S.room : S.nq) * rows + unit - 1) / unit);
+        const int64_t nth = slot - first_slot((WHAT == KEYS ? S.k0 : S.q0) * rows, unit, lo);
+        if (nth < 0 || nth >= count || split >= runs) return IDLE;
+        tiles = count * runs;
+        x = (count - 1 - int(nth)) * runs + split;
+        return TILE;
+    }
     int done = 0;
     for (int base = 0; base <= P.n_seqs; base += 64) {
         int q0 = 0, k0 = 0, nq = 0, nk = 0, room = 0, count = 0;
@@ -305,11 +343,11 @@ __device__ __forceinline__ bool find_tile(const Params& P, int size, int t, Seq&
             S.nk = __builtin_amdgcn_readlane(nk, who);
             S.room = __builtin_amdgcn_readlane(room, who);
             S.shift = S.nk - S.nq;
-            return x >= 0 && x < tiles;                           // sums of starts that make no sense may have wrapped
+            return x >= 0 && x < tiles ? TILE : NOTHING;          // sums of starts that make no sense may have wrapped
         }
         done += __builtin_amdgcn_readlane(upto, 63);
     }
-    return false;
+    return NOTHING;
 }
 
 // Head of the i-th of `heads` workgroups that have the same rows.  Workgroups go round the eight XCDs one by one; the heads

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int head = head_at(P, int(blockIdx.x) % P.heads), kv = head / P.group;
     int tile, tiles;
     Seq S;
-    if (!find_tile<QUERIES>(P, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
+    if (find_tile<QUERIES>(P, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles) != TILE) return;
     const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
     const bool there = query < S.nq;
     const int last_q = min(first + WAVES * 32, S.nq) - 1, last_mine = min(mine + 31, S.nq - 1);
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int kv = int(blockIdx.x) % P.kv_heads;
     int tile, tiles;
     Seq S;
-    if (!find_tile<attn::KEYS>(P, WAVES * 32, int(blockIdx.x) / P.kv_heads, S, tile, tiles)) return;
+    if (find_tile<attn::KEYS>(P, WAVES * 32, int(blockIdx.x) / P.kv_heads, S, tile, tiles) != TILE) return;
     tile = tiles - 1 - tile;                                      // a causal prompt's first keys are seen by all that follow
     const int first = tile * WAVES * 32, mine = first + wave * 32, key = mine + col;
     // queries that see any key of the workgroup, of this wave: from `begin` on; from `all` on they see all of the wave's

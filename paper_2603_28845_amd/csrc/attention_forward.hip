@@ -184,7 +184,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) voi
     const int head = head_at(P, int(blockIdx.x) % P.heads);
     int tile, tiles;
     Seq S;
-    if (!find_tile<QUERIES>(P, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles)) return;
+    if (find_tile<QUERIES>(P, WAVES * 32, int(blockIdx.x) / P.heads, S, tile, tiles) != TILE) return;
     const int first = tile * WAVES * 32, mine = first + wave * 32, query = mine + col;
     const bool there = query < S.nq;
     const int kv = head / P.group;
@@ -376,7 +376,9 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
     const int kv = piece % P.kv_heads;
     int x, pieces;
     Seq S;
-    if (!find_tile<PIECES>(P, 0, piece / P.kv_heads, S, x, pieces)) return;
+    const Found found = find_tile<PIECES>(P, 0, piece / P.kv_heads, S, x, pieces);
+    if (found == NOTHING) return;
+    if (found == IDLE) continue;
     const int run = run_of(P.run, P.splits, S.nk), runs = runs_of(P.run, P.splits, S.nk), tile = x / runs, split = x % runs;
     const int row = tile * 32 + col, query = row / P.group, head = kv * P.group + row % P.group;
     const bool there = query < S.nq;
@@ -560,6 +562,8 @@ onecomp_status launch_few(const Params& P, hipStream_t stream) {
     if (st != ONECOMP_OK) return st;
     const int64_t rows = P.total_q * P.heads;
     int64_t grid = row_blocks(P) * (P.splits > 1 ? ceil_div(P.total_k, int64_t(P.run) * (P.n_seqs < 1 ? 1 : P.n_seqs)) + 1 : 1) * P.kv_heads;
+    if (P.n_seqs >= MANY_TOKENS) grid = all_slots(P.total_q * P.group, 32, P.n_seqs) * P.splits * P.kv_heads;
+    if (grid > 0x7fffffff - 16384) return ONECOMP_ERR_UNSUPPORTED;    // pieces are counted in 32 bits
     grid = grid > 16384 ? 16384 : grid;                           // workgroups go on to further pieces
     few_rows_kernel<E, DT><<<dim3(unsigned(grid)), dim3(F::WAVES * 64), F::LDS, stream>>>(P);
     ONECOMP_CHECK_LAUNCH();
@@ -587,7 +591,8 @@ void plan(onecomp_dtype dtype, Params& P) {
     double run = ceil(blocks * each / 1024 / 128) * 128;
     run = run < 256 ? 256 : run > (1 << 30) ? (1 << 30) : run;
     const int64_t splits = ceil_div(P.max_k, int64_t(run));
-    P.splits = int(splits < 1 ? 1 : splits > 256 ? 256 : splits);
+    const int most = most_splits(P.n_seqs);
+    P.splits = int(splits < 1 ? 1 : splits > most ? most : splits);
     P.run = int(run);
 }
 

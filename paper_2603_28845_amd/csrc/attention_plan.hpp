@@ -23,6 +23,19 @@ ONECOMP_HD int runs_of(int run, int splits, int nk) {
     return runs > 1 ? int(runs) : 1;
 }
 
+// Many sequences: each has its slots, as many units of `unit` rows (tiles of tokens from MANY sequences on, blocks of a few rows from
+// MANY_TOKENS on) as its place can need and one more at most, so that a slot's sequence is found by search and not by counting
+// all before it: ceil((b - a) / unit) <= floor(b / unit) - floor(a / unit) + 1 for a sequence of rows a .. b - 1.
+constexpr int MANY = 256, MANY_TOKENS = 1024;
+ONECOMP_HD int64_t first_slot(int64_t rows_before, int unit, int sequence) { return rows_before / unit + sequence; }
+// slots of all sequences and of the padding behind them
+ONECOMP_HD int64_t all_slots(int64_t rows, int unit, int sequences) { return rows / unit + sequences + 1; }
+// Runs of keys for each slot of a few rows: a slot that has fewer is looked at for nothing, so that many sequences get few.
+ONECOMP_HD int most_splits(int sequences) {
+    const int n = sequences < MANY_TOKENS ? 256 : 65536 / sequences;
+    return n < 1 ? 1 : n > 256 ? 256 : n;
+}
+
 struct Range {
     int begin, end;
 };
