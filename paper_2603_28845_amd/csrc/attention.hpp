@@ -269,7 +269,7 @@ enum Found { NOTHING, IDLE, TILE };
 template <What WHAT>
 __device__ __forceinline__ Found find_tile(const Params& P, int size, int t, Seq& S, int& x, int& tiles) {
     const int lane = threadIdx.x & 63;
-    if (P.n_seqs >= (WHAT == PIECES ? MANY_TOKENS : MANY)) {
+    if (__builtin_expect(P.n_seqs >= (WHAT == PIECES ? MANY_TOKENS : MANY), 0)) {
         const int32_t* cu = WHAT == KEYS ? P.cu_k : P.cu_q;
         const int64_t total = WHAT == KEYS ? P.total_k : P.total_q, rows = WHAT == PIECES ? P.group : 1;
         const int unit = WHAT == PIECES ? 32 : size, slot = WHAT == PIECES ? t / P.splits : t;

@@ -420,7 +420,7 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
                 __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
             }
             asm volatile("" ::: "memory");
-            if (again) {
+            if (__builtin_expect(again, 0)) {
                 lv.clean(own + buf * 2 * F::SIZE + F::SIZE, 0, lane, [&](int r, int c, bool up, bool down) {
                     if (up) mark_first(marks.up(c), j + r);
                     if (down) mark_first(marks.down(c), j + r);
@@ -469,7 +469,7 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
         for (int w = 0; w < F::WAVES; ++w)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[r] = fmaf(f[w], sums[((w * DT + n) * 16 + r) * 64 + lane], o[r]);
-        if (again) give_back(o, marks, n, half, [&](int key) { return key <= last; });
+        if (__builtin_expect(again, 0)) give_back(o, marks, n, half, [&](int key) { return key <= last; });
         float16v one[1] = {o};
         broken = broken || (there && l == l && not_finite(one));
         if (there) {
@@ -490,12 +490,15 @@ __global__ __launch_bounds__((Few<E, DT>::WAVES * 64), 1) void few_rows_kernel(c
             P.lse[at_row] = l == 0.f ? NEG_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
         }
     }
-    if (again) break;
-    if (__builtin_expect(!any_wave<F::WAVES>(marks, wave, P.causal && broken), 1)) break;
+    // a barrier in either case: the next tiles go where the sums met.  Only keys that some rows do not see can do harm.
+    if (again || end <= end_all) {
+        __syncthreads();
+        break;
+    }
+    if (__builtin_expect(!any_wave<F::WAVES>(marks, wave, broken), 1)) break;
     clear(marks, S.nk, threadIdx.x, F::WAVES * 64);
     __syncthreads();
     }
-    __syncthreads();                                              // the next piece's tiles go where the sums met
     }
 }
 

@@ -13,14 +13,15 @@ namespace onecomp {
 namespace attn {
 
 // Few rows: keys of one piece of work.  Runs of `run` or, where the host knew of fewer keys than there are, as many as it takes for
-// `splits` runs to cover them all.  Lengths reach 2^31 - 4096: sums of theirs take 64 bits.
+// `splits` runs to cover them all.  Lengths reach 2^31 - 4096, runs 2^30 and the keys of all shares in a tile's steps 2^15: sums
+// of two of these take 32 bits without a sign.  (In 64 bits the divisions cost a call of single tokens 2 us of 100.)
 ONECOMP_HD int run_of(int run, int splits, int nk) {
-    const int64_t least = (int64_t(nk) + int64_t(splits) * 128 - 1) / (int64_t(splits) * 128) * 128;
-    return least > run ? int(least) : run;
+    const uint32_t unit = uint32_t(splits) * 128u, least = (uint32_t(nk) + unit - 1u) / unit * 128u;
+    return least > uint32_t(run) ? int(least) : run;
 }
 ONECOMP_HD int runs_of(int run, int splits, int nk) {
-    const int64_t each = run_of(run, splits, nk), runs = (nk + each - 1) / each;
-    return runs > 1 ? int(runs) : 1;
+    const uint32_t each = uint32_t(run_of(run, splits, nk)), runs = (uint32_t(nk) + each - 1u) / each;
+    return runs > 1u ? int(runs) : 1;
 }
 
 // Many sequences: each has its slots, as many units of `unit` rows (tiles of tokens from MANY sequences on, blocks of a few rows from
@@ -41,14 +42,14 @@ struct Range {
 };
 // Run `split` of the keys 0 .. seen - 1.
 ONECOMP_HD Range run_range(int run, int split, int seen) {
-    const int64_t begin = int64_t(run) * split, end = begin + run;
-    return Range{int(begin), int(end < seen ? end : seen)};
+    const uint32_t begin = uint32_t(run) * uint32_t(split), end = begin + uint32_t(run);
+    return Range{int(begin), int(end < uint32_t(seen) ? end : uint32_t(seen))};
 }
 // Share `which` of `shares` of the keys 0 .. end - 1, in tiles of `keys`; empty where begin >= end.
 ONECOMP_HD Range share_of(int end, int keys, int shares, int which) {
-    const int64_t unit = int64_t(keys) * shares, share = (end + unit - 1) / unit * keys, begin = share * which, to = begin + share;
-    if (begin >= end) return Range{0, 0};
-    return Range{int(begin), int(to < end ? to : end)};
+    const uint32_t unit = uint32_t(keys) * uint32_t(shares), share = (uint32_t(end) + unit - 1u) / unit * uint32_t(keys), begin = share * uint32_t(which), to = begin + share;
+    if (begin >= uint32_t(end)) return Range{0, 0};
+    return Range{int(begin), int(to < uint32_t(end) ? to : uint32_t(end))};
 }
 
 }  // namespace attn
