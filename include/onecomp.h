@@ -431,7 +431,7 @@ typedef struct {
     int head_dim;              /* up to 128, a multiple of 8 (bf16) or 4 (fp32) */
     int n_seqs;
     int causal;
-    float scale;               /* > 0, finite */
+    float scale;               /* 2^-100 to 2^100 */
     int64_t total_q, total_k;  /* rows of q and of k */
     int64_t max_q, max_k;
     const int32_t* cu_q;       /* device, n_seqs + 1 */

@@ -52,6 +52,8 @@ onecomp_status check_attention(const onecomp_attention_shape* s) {
         return ONECOMP_ERR_INVALID_ARG;
     if (s->head_dim > 128 || s->head_dim % (s->dtype == ONECOMP_BF16 ? 8 : 4) != 0 || s->n_heads > (1 << 16)) return ONECOMP_ERR_UNSUPPORTED;
     if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return ONECOMP_ERR_INVALID_ARG;
+    // scale log2(e) is a normal number, and so is a log-sum-exp over it, with which the gradients begin their scores
+    if (s->scale < 0x1p-100f || s->scale > 0x1p100f) return ONECOMP_ERR_UNSUPPORTED;
     const int64_t most = (int64_t(1) << 31) - 4096;
     if (s->total_q < 0 || s->total_k < 0 || s->max_q < 0 || s->max_k < 0 || s->total_q > most || s->total_k > most || s->n_seqs > (1 << 24))
         return ONECOMP_ERR_INVALID_ARG;

@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from test_block_host import INVALID, P, _backward, _forward, _heads, _shape, lib  # noqa: F401
+from test_block_host import INVALID, P, UNSUPPORTED, WORKSPACE, _backward, _forward, _heads, _shape, lib  # noqa: F401
 
 
 @pytest.mark.parametrize("total_q,total_k", [(3000, 100000), (40, 5000), (4, 200000)])
@@ -32,3 +32,12 @@ def test_results_over_what_is_still_read(lib):  # noqa: F811
     q, k, v, out = apart()[:4]
     assert _forward(lib, q=q, k=k, v=v, out=k) == INVALID
     assert _forward(lib, q=q, k=k, v=v, out=v) == INVALID
+
+
+def test_scales_beyond_what_the_arithmetic_holds(lib):  # noqa: F811
+    """With 1e-38 the gradients' log-sum-exps over the scale were infinite, and dv 0; with 3e38 scale log2(e) was."""
+    for call in (_forward, _backward):
+        for scale in (1e-38, 1e-45, 2.0 ** -101, 2.0 ** 101, 3e38):
+            assert call(lib, scale=scale, ws=None) == UNSUPPORTED, scale
+    for scale in (2.0 ** -100, 1e-3, 1.0, 2.0 ** 100):
+        assert _backward(lib, scale=scale, ws=None) == WORKSPACE, scale

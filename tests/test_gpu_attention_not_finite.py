@@ -154,3 +154,19 @@ def test_cost(nq, nk, dtype):
     dirty = _time(lambda: _gradients(x, nq, nk, out, lse, v=everything, k=everything), passes)
     print(f"[time] all keys and values {dirty:.3f} ms", flush=True)
     assert dirty <= 10 * clean
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_smallest_scale(dtype):
+    """Probabilities are all alike, whatever the log-sum-exps over the scale are."""
+    nq = nk = [70, 33]
+    x = _inputs(nq, nk, 2, 1, 64, dtype, 33)
+    scale = 2.0 ** -100
+    out, lse = _forward(x, nq, nk, True, scale=scale)
+    want = attention(x["q"], x["k"], x["v"], x["cu_q"], x["cu_k"], True, scale, None, x["d_out"])
+    check(out, want["out"], "out")
+    check(lse, want["lse"], "lse")
+    dq, dk, dv = og.onecomp_attention_backward(x["d_out"], x["q"], x["k"], x["v"], out, lse, x["cu_q"], x["cu_k"], 70, 70, scale=scale)
+    check(dv, want["dv"], "dv")
+    check(dq, want["dq"], "dq")
+    check(dk, want["dk"], "dk")
