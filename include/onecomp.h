@@ -508,8 +508,8 @@ typedef struct {
  * Forward.  Arithmetic in fp32 on each entry, rounded once where it is stored (n follows from h' before it is rounded).
  *   weight, bias, post_weight, post_bias   [width] of w_dtype, NULL: 1 and 0.  post_*: only with post_norm; biases: layer norms only.
  *   gate    onecomp_rows (row_stride unused for one factor per channel), NULL with ONECOMP_GATE_NONE
- *   h_out   NULL if not wanted; may be h itself (same stride).  Only with y.
- *   n       NULL if not wanted; not h_out, not h.
+ *   h_out   NULL if not wanted; may be h, y or the gate itself (same stride).  Only with y.
+ *   n       NULL if not wanted; not h_out, not h; may be y or the gate itself (same stride).
  * Any address and stride of whole elements will do; whole 16 bytes are best.
  */
 onecomp_status onecomp_block_norm_forward(const onecomp_norm_shape* shape, const onecomp_rows* h, const onecomp_rows* y, const void* weight,
@@ -527,7 +527,7 @@ typedef struct {
  * Gradients of the forward call from those of n (dn) and of h' (dh_out; what comes back along the residual), either of them NULL
  * if there is none.  h is h' as the forward call left it (h itself without y).  With G the gradient of h':
  *   dh = residual_scale G, dgate = G u, du = gate G, dy = du or that of the norm behind the block.
- * dh, dy and dgate may each be one of the inputs h, y, dn, dh_out and gate (same strides).
+ * dh, dy and dgate may each be one of the inputs h, y, dn, dh_out and gate (same strides), but not each other.
  *   workspace  >= onecomp_block_norm_workspace_bytes(shape), 256-byte aligned; not used, and NULL will do, where no parameter's
  *              gradient (dweight .. dgate_channel) is wanted.
  */

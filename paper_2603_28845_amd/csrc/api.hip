@@ -3,6 +3,7 @@
 #include "attention.hpp"
 #include "block.hpp"
 #include <cmath>
+#include <initializer_list>
 #include <dlfcn.h>
 #include <cstdlib>
 
@@ -90,6 +91,18 @@ bool check_rows(const onecomp_norm_shape* s, const onecomp_rows* r) {
     return r->data && aligned(r->data, s->dtype == ONECOMP_BF16 ? 2 : 4) && r->row_stride >= s->width && r->row_stride <= (int64_t(1) << 31);
 }
 bool check_param(const onecomp_norm_shape* s, const void* p) { return aligned(p, s->w_dtype == ONECOMP_BF16 ? 2 : 4); }
+
+// Results over inputs are written row by row as the rows are read: no other row may begin where the result's does.
+bool apart_or_same(const onecomp_norm_shape* s, std::initializer_list<const onecomp_rows*> results, std::initializer_list<const onecomp_rows*> inputs) {
+    if (s->rows == 0) return true;
+    for (const onecomp_rows* r : results)
+        for (const onecomp_rows* i : inputs)
+            if (r && i && r->data == i->data && r->row_stride != i->row_stride && s->rows > 1) return false;
+    for (const onecomp_rows* const* r = results.begin(); r != results.end(); ++r)
+        for (const onecomp_rows* const* other = results.begin(); other != r; ++other)
+            if (*r && *other && (*r)->data == (*other)->data) return false;
+    return true;
+}
 
 block::Rows rows_of(const onecomp_rows* r) { return r ? block::Rows{r->data, r->row_stride} : block::Rows{nullptr, 0}; }
 
@@ -480,6 +493,7 @@ ONECOMP_API onecomp_status onecomp_block_norm_forward(const onecomp_norm_shape* 
     if (!check_rows(shape, h_out) || !check_rows(shape, n) || (!h_out && !n) || (h_out && !y)) return ONECOMP_ERR_INVALID_ARG;
     if (shape->rows == 0) return ONECOMP_OK;
     if (n && (n->data == h->data || (h_out && n->data == h_out->data))) return ONECOMP_ERR_INVALID_ARG;
+    if (!apart_or_same(shape, {h_out, n}, {h, y, P.gate_rows ? gate : nullptr})) return ONECOMP_ERR_INVALID_ARG;
     P.h_out = rows_of(h_out);
     P.n = rows_of(n);
     return block::norm_run(shape->dtype, P, false, static_cast<hipStream_t>(hip_stream));
@@ -515,6 +529,7 @@ ONECOMP_API onecomp_status onecomp_block_norm_backward(const onecomp_norm_shape*
     }
     if (P.wanted && (!workspace || !aligned(workspace, 256) || workspace_bytes < onecomp_block_norm_workspace_bytes(shape))) return ONECOMP_ERR_WORKSPACE;
     if (shape->rows == 0 && !P.wanted) return ONECOMP_OK;
+    if (!apart_or_same(shape, {out->dh, out->dy, out->dgate}, {dn, dh_out, h, y, P.gate_rows ? gate : nullptr})) return ONECOMP_ERR_INVALID_ARG;
     P.part = static_cast<float*>(workspace);
     P.dn = rows_of(dn);
     P.dh_out = rows_of(dh_out);
