@@ -44,6 +44,10 @@ struct Bf16 {
     static constexpr int PER_CHUNK = 8;          // elements of a 16-byte chunk
     typedef bf16x8 Row;                          // a chunk as an operand whose inner index is the head dimension
     typedef bf16x8 Score;                        // eight score registers as a right operand
+    // Probabilities and their gradients are rounded to bf16 here, for the matrix pipes to take them beside the inputs: each term of a
+    // sum moves by 2^-9 of itself at most, at random, which leaves results 1.2 to 1.4 times as far from exact ones as their own rounding
+    // does (outputs 0.0019 to 0.0022 instead of 0.0015 to 0.0017, gradients 0.0024 instead of 0.0017, root mean square).  Two bf16 halves of
+    // each would take that away and double the products they enter.
     static __device__ __forceinline__ Score pack(const float* s) {
         bf16x8 r;
 #pragma unroll

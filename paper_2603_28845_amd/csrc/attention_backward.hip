@@ -1,7 +1,8 @@
 // Gradients of the attention of packed sequences, in two kernels: one with the queries in lanes (dq, and the per-query numbers
 // that both need), one with the keys in lanes (dk and dv).  Each forms the scores and the probabilities' gradients anew, seven
-// products where the definition has five, and in return no sum of one workgroup depends on another's: no atomics, no partial
-// gradients in memory.
+// products where the definition has five, and in return no sum of one workgroup depends on another's and none needs atomics.  Calls
+// of too few workgroups share out their inner loops (plan()): the shares' sums of dq, dk and dv, 32 bits each, go to the
+// workspace and are joined there in their order.
 #include "attention.hpp"
 
 namespace onecomp {
@@ -110,7 +111,8 @@ __device__ __forceinline__ void grad_q_block(float16v (&dq)[DT], const Reader<E,
 
 // dq_i = scale sum_j ds_ij k_j for WAVES x 32 queries of one head.  Also leaves in scratch what the other kernel's sums of
 // products begin with: -lse / scale for the scores and -delta_i = -d_out_i . out_i for the probabilities' gradients.  Three products
-// a tile: 8 x 2048 tokens, 32 / 8 heads of 128, 430 to 450 us, 0.92 to 0.96 PFLOP/s executed, matrix pipes busy 50 %.
+// a tile: 8 x 2048 tokens, 32 / 8 heads of 128, 435 to 475 us, 0.87 to 0.95 PFLOP/s executed, matrix pipes busy 49 %; 12 registers spilled, none
+// in the loop.
 template <class E, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void grad_q_kernel(const Params P) {
     constexpr int KEYS = 32 * KB<E>;
@@ -402,8 +404,9 @@ __device__ __forceinline__ void grad_kv_block(float16v (&dk)[DT], float16v (&dv)
 }
 
 // dv_j = sum_i p_ij d_out_i and dk_j = scale sum_i ds_ij q_i over the queries of all heads of a group, for WAVES x 32 keys.  Four
-// products a tile: 8 x 2048 tokens 506 to 530 us, 1.04 to 1.09 PFLOP/s executed, matrix pipes busy 55 %.  The registers are full:
-// what spilled of the keys' operands was read back every tile behind the loads under way, and doubled the time.
+// products a tile: 8 x 2048 tokens 500 to 550 us, 1.0 to 1.1 PFLOP/s executed, matrix pipes busy 57 %.  The registers are full:
+// what spilled of the keys' operands was once read back every tile behind the loads under way, and doubled the time; the 17 that
+// spill now are read back behind the loop.
 template <class E, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void grad_kv_kernel(const Params P) {
     constexpr int ROWS = 32 * KB<E>;

@@ -161,11 +161,7 @@ struct Rows32 {
 };
 
 // ---- whole prompts ------------------------------------------------------------------------------------------------------
-// A workgroup has WAVES x 32 queries of one head and walks through the keys in tiles that all waves share.  Four waves, so that
-// two workgroups share a CU and one's beginning or end lies beside the other's work (eight waves: 8 x 2048 tokens 384 us, four
-// 361 when this was decided).  A wave's 32 queries use a quarter of its registers for the queries, a quarter for the sums of
-// values and half for the scores of two tiles.  16384 tokens, 32 / 8 heads of 128: 1.99 ms, 1.1 PFLOP/s at 1.66 GHz (power), the
-// matrix pipes busy 62 %; 32 x 2048: 1.31 ms.
+// LDS of the kernel below.
 template <class E, int DT, int WAVES>
 struct Whole {
     static constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1, SIZE = Tile<E, DT>::bytes(32 * KB);
@@ -174,6 +170,12 @@ struct Whole {
     static constexpr int LDS = TILES > WAVES * OWN ? TILES : WAVES * OWN;
 };
 
+// A workgroup has WAVES x 32 queries of one head and walks through the keys in tiles that all waves share.  Four waves, so that
+// two workgroups share a CU and one's beginning or end lies beside the other's work (eight waves: 8 x 2048 tokens 384 us, four
+// 361 when this was decided).  A wave's 32 queries use a quarter of its registers for the queries, a quarter for the sums of
+// values and half for the scores of two tiles.  16384 tokens, 32 / 8 heads of 128: 1.89 to 1.96 ms, 1.1 PFLOP/s at 1.61 to 1.66 GHz
+// (power), the matrix pipes busy 63 %; 32 x 2048: 1.19 to 1.25 ms, 47 %.  18 registers are spilled at 128 wide bf16, none of them in
+// the loop.
 template <class E, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(typename E::T) == 2 ? 2 : 1) void forward_kernel(const Params P) {
     constexpr int KB = sizeof(typename E::T) == 2 ? 2 : 1, KEYS = 32 * KB;
@@ -579,8 +581,11 @@ onecomp_status launch_few(const Params& P, hipStream_t stream) {
 
 // How the keys are shared out where there are few rows; splits = 0: whole prompts.  Estimates in microseconds from
 // measurements at 128 wide bf16 heads: 0.8 for 64 keys of a prompt's tile of 128 rows, two of them at a time on each CU, and
-// 0.8 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join.  fp32 products take 5 and 10 times as
-// long, and blocks of rows wider than 64 get two waves on a CU.
+// 0.8 for 32 keys of a block of 32 rows, four on each CU, with 12 to begin, end and join.  fp32, up to 64 wide and wider: 4 and 8
+// for a prompt's 64 keys, 2.5 and 8 for a block's 32 (blocks wider than 64 get two waves on a CU).  With 1 to 512 new tokens behind
+// 1 x 16384, 8 x 4096 and 32 x 1024 keys, both types, 64 and 128 wide, the shape chosen is the better one, by 5 to 30 % at 16 tokens
+// and 1.7 to 9 times from 64 on (512 tokens behind 16384 keys, bf16, 128 wide: 251 us whole and 1510 in blocks of 32 rows), but for
+// 16 tokens of bf16 behind 16384 keys, where other runs of the same kernel take 30 and 47 us instead of 36 and 51.
 void plan(onecomp_dtype dtype, Params& P) {
     P.splits = P.run = 0;
     const double tiles = double(P.heads) * (double(P.total_q) / 128 + P.n_seqs), blocks = double(row_blocks(P)) * P.kv_heads;

@@ -252,7 +252,7 @@ __device__ __forceinline__ void affine(float (&x)[Pt::E], const void* w, const v
 }
 
 // One row for each group of G threads, held in registers from its loads to its stores: the bytes are the bound.  65536 x 4096
-// bf16 with y: 342 to 356 us, 6.0 TB/s (a copy of 2 GiB: 4.9); 8 rows: 3.3 us.
+// bf16 with y: 342 to 364 us, 5.9 TB/s (a copy of 2 GiB: 4.9); 8 rows: 3.3 us.
 template <class T, int NV, int G, bool WHOLE>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void forward_kernel(const Params P) {
     constexpr int THREADS = G < 256 ? 256 : G;
@@ -316,12 +316,17 @@ __device__ __forceinline__ void centre(float (&x)[Pt::E], float (&y)[Pt::E], boo
 // With x^ = x inv the normalised row, the gradient of the rows in front of a norm is inv (d - x^ mean(d x^) - mean(d)), the
 // last for layer norms only.  Both norms' squares and the first norm's means are added up in one go (mean(d x^) =
 // inv mean(d x)), the second norm's means in another; layer norms take one more for the means of the rows.  16384 x 4096 bf16,
-// rms on both sides, gate per channel: 187 to 200 us, 4.1 TB/s; registers allow 16 waves on a CU, and their loads in flight and
+// rms on both sides, gate per channel: 187 to 203 us, 3.9 to 4.2 TB/s; registers allow 16 waves on a CU, and their loads in flight and
 // 55 % of the vector pipes are the bound (512 threads a workgroup, two on a CU: 183 to 200 us, but twice the sums to join).
 //
 // SUMS: as said.  Wider rows leave no registers for the parameters' sums (over 8192, layer norms over 4096; spilled to memory
 // they cost 4 to 8 times the rest): then only what a row's entries need is left in scratch, for strips_kernel, which adds up; not
 // even that where no parameter's gradient is wanted.
+//
+// Registers: 128 a thread at 1024 threads a workgroup.  Spilled, rms / layer norms, whole vectors: bf16 up to 4096 wide 0 / 20, 8192
+// 0 / 0, 16384 0 / 14, 32768 81 / 117; fp32 up to 4096 wide 0 / 3, 8192 0 / 0, 16384 0 / 49, 32768 112 / 170; odd rows up to 34 at
+// 4096 and 480 at 32768.  The kernel's share of a wide call: 5461 x 12288 fp32 layer norms 550 us of 775, 4681 x 14336 bf16 rms
+// 189 of 295.
 template <class T, int NV, int G, bool WHOLE, bool LAYER, bool SUMS>
 __global__ __launch_bounds__(1024) void gradient_kernel(const Params P) {
     constexpr int THREADS = 1024, GROUPS = THREADS / G;
