@@ -173,7 +173,8 @@ def prepare(case, seed):
 # ---- plain forms --------------------------------------------------------------------------------------------------------
 def _plain_linear(s):
     x = s["x"].float()
-    scale = x.abs().amax(1, keepdim=True) / 127
+    top = x.abs().amax(1, keepdim=True)
+    scale = top / torch.full_like(top, 127.0)         # divided: by a number, it would be multiplied with the rounded 1 / 127
     codes = torch.where(scale > 0, torch.round(x / scale), 0.0).clamp_(-127, 127)
     y = (codes @ (s["q"].float() - s["zeros"]).t()) * scale * s["scales"].t()
     if s["bias"] is not None:
@@ -286,7 +287,7 @@ def work(case):
 def _linear64(case, s):
     """The codes are the rounded quotients of 32-bit numbers; everything behind them in 64 bits."""
     x = s["x"].double()
-    scale = (x.abs().amax(dim=1).float() / 127.0)
+    scale = (x.abs().amax(dim=1) / 127.0).float()
     codes = torch.zeros_like(x)
     for i in range(0, case["tokens"], 4096):
         part = (x[i:i + 4096] / scale[i:i + 4096, None].double()).float()          # rounded to 32 bits once, as a division is
