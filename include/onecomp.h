@@ -21,6 +21,9 @@
  * Around the linear layers (calibration passes that produce X, tuning of what stays in floating point):
  * onecomp_attention_forward / _backward, onecomp_block_norm_forward / _backward, onecomp_clip_gradients.
  *
+ * From a quantized model's tokens to its loss: onecomp_embedding_forward / _backward, onecomp_quantize_tokens and
+ * onecomp_linear_int8 (a layer run on its 8-bit codes), onecomp_token_loss_forward / _backward.
+ *
  * Storage convention: W is d_out x d_in row-major (rows = output channels); this
  * is the transpose of the paper's N x M weight matrix.  "Column j" is input
  * channel j; a group is `group_size` consecutive input channels of one row.
@@ -556,6 +559,97 @@ typedef struct {
 onecomp_status onecomp_clip_gradients(const onecomp_gradient* grads, int n, float max_norm, float* norm, void* workspace,
                                       size_t workspace_bytes, void* hip_stream);
 size_t onecomp_clip_workspace_bytes(void);
+
+/* ---- From tokens to the loss --------------------------------------------------------------------------------------
+ * What a quantized model needs besides its blocks to be scored (perplexity), run and tuned: the embedding in front of them,
+ * linear layers on the codes of onecomp_quantize_layer, and the loss over the vocabulary behind them, with gradients.
+ * Tokens and targets are int32; one outside 0 .. vocab - 1 (a negative one, say) marks a token that takes no part.
+ */
+
+/*
+ * out_t = scale table[tokens_t]; zeros where the token is outside the vocabulary.  Multiplied in fp32 and rounded once.
+ *   tokens   device int32 [n]
+ *   table    [vocab, width] of dtype; out [n, width], not over the table.  Any address and stride of whole elements; whole 16
+ *            bytes are best.
+ */
+onecomp_status onecomp_embedding_forward(const int32_t* tokens, int64_t n, onecomp_dtype dtype, const onecomp_rows* table, int64_t vocab,
+                                         int64_t width, float scale, const onecomp_rows* out, void* hip_stream);
+
+/*
+ * Gradient of the table: d_table_v = base_v + scale sum of d_out_t over the tokens t = v, for every row of the vocabulary.  Sums in
+ * fp32 in the order of the tokens (sorted by a stable sort), in pieces that the sizes and the tokens decide, no atomics on
+ * them: the same inputs give the same bits.  Rows of d_out whose token is outside the vocabulary are not read.
+ *   base       [vocab, width] or NULL (0): what the gradient is added to (of a tied output layer, of earlier batches).  It may be
+ *              d_table itself with the same stride: then rows without a token are left as they are.  Anywhere else it lies apart.
+ *   workspace  >= onecomp_embedding_workspace_bytes(n, vocab, width), 256-byte aligned
+ */
+onecomp_status onecomp_embedding_backward(const int32_t* tokens, int64_t n, onecomp_dtype dtype, const onecomp_rows* d_out, int64_t vocab,
+                                          int64_t width, float scale, const onecomp_rows* base, const onecomp_rows* d_table, void* workspace,
+                                          size_t workspace_bytes, void* hip_stream);
+size_t onecomp_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width);
+
+/*
+ * Activations to 8-bit codes with a scale per token: s_t = max_k |x_tk| / 127, codes_tk = x_tk / s_t rounded to the nearest (ties to
+ * even; quotients of 32 bits) in -127 .. 127, sums_t = sum_k codes_tk.  Several layers that share x share the codes.  A token
+ * of zeros has scale 0; one that holds an infinity or NaN has codes 0 and scale NaN, so that what follows from it is NaN.
+ *   x       [tokens, width] of dtype, any address and stride of whole elements; width a multiple of 16, at most 65520
+ *   codes   device int8 [tokens, width], dense, 16-byte aligned
+ *   scales  device fp32 [tokens];  sums  device int32 [tokens]
+ */
+onecomp_status onecomp_quantize_tokens(const onecomp_rows* x, onecomp_dtype dtype, int64_t tokens, int64_t width, int8_t* codes, float* scales,
+                                       int32_t* sums, void* hip_stream);
+
+/*
+ * A linear layer on its codes: y_tn = token_scales_t scales_n sum_k codes_tk (Q_codes_nk - zeros_n) + bias_n, with Q_codes, scales and
+ * zeros as onecomp_quantize_layer left them for any bits and grid with one group per row (group_size = d_in).  The sums are exact
+ * (32-bit integers); the result is formed in fp32 and rounded once.
+ *   codes, token_scales, token_sums   of onecomp_quantize_tokens; codes [tokens, d_in] dense, 16-byte aligned
+ *   Q_codes   device uint8 [d_out, d_in], dense, 16-byte aligned; d_in a multiple of 16, at most 65520
+ *   scales, zeros  device fp32 [d_out]; zeros are whole numbers of 0 .. 255
+ *   bias      [d_out] of dtype, or NULL
+ *   y         [tokens, d_out] of dtype, any address and stride of whole elements
+ *   workspace >= onecomp_linear_int8_workspace_bytes(tokens, d_out, d_in), 256-byte aligned (0 bytes: may be NULL)
+ */
+onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scales, const int32_t* token_sums, const uint8_t* Q_codes,
+                                   const float* scales, const float* zeros, const void* bias, onecomp_dtype dtype, int64_t tokens, int64_t d_out,
+                                   int64_t d_in, const onecomp_rows* y, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
+
+/* The loss of a model's last layer.  h and weight: base addresses and strides of whole 16 bytes, width a multiple of 8 (bf16) or
+ * 4 (fp32), row strides below 2^23 bytes; tokens, width and vocab at most 2^24. */
+typedef struct {
+    onecomp_dtype dtype;       /* of h, weight and their gradients */
+    int64_t tokens, width, vocab;
+    float scale;               /* of the logits, 2^-100 to 2^100 */
+} onecomp_loss_shape;
+
+/*
+ * With the logits z_tv = scale h_t . weight_v: lse_t = log sum_v exp(z_tv), loss_t = lse_t - z_t,targets_t (the token's negative log
+ * likelihood); both 0 where the target is outside the vocabulary.  Logits are formed in tiles and not kept: the workspace
+ * grows with tokens (width + vocab / 16), not tokens x vocab.  bf16 products are exact and added in fp32, fp32 inputs are multiplied
+ * in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.
+ *   h          [tokens, width], weight [vocab, width], targets device int32 [tokens]
+ *   loss, lse  device fp32 [tokens]; either may be NULL (lse is wanted for onecomp_token_loss_backward)
+ *   workspace  >= onecomp_token_loss_workspace_bytes(shape), 256-byte aligned
+ */
+onecomp_status onecomp_token_loss_forward(const onecomp_loss_shape* shape, const onecomp_rows* h, const onecomp_rows* weight, const int32_t* targets,
+                                          float* loss, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t onecomp_token_loss_workspace_bytes(const onecomp_loss_shape* shape);
+
+/*
+ * Gradients from those of the losses (d_loss) and of the log-sum-exps (d_lse, NULL if there are none), with lse as the forward call
+ * left it:  g_tv = (d_loss_t + d_lse_t) exp(z_tv - lse_t) - d_loss_t [v = targets_t],
+ *   dh_t = scale sum_v g_tv weight_v,  dweight_v = scale sum_t g_tv h_t.
+ * Left-out tokens have dh 0 and no part in dweight.  The vocabulary is taken in pieces whose g (in dtype, 512 MB at most, or 2048
+ * columns) lies in the workspace.  Sums in fp32, no atomics: the same inputs give the same bits.
+ *   d_loss, d_lse  device fp32 [tokens]
+ *   dh, dweight    like h and weight, overwritten, over none of the inputs; either may be NULL
+ *   workspace      >= onecomp_token_loss_backward_workspace_bytes(shape), 256-byte aligned
+ */
+onecomp_status onecomp_token_loss_backward(const onecomp_loss_shape* shape, const float* d_loss, const float* d_lse, const onecomp_rows* h,
+                                           const onecomp_rows* weight, const int32_t* targets, const float* lse, const onecomp_rows* dh,
+                                           const onecomp_rows* dweight, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t onecomp_token_loss_backward_workspace_bytes(const onecomp_loss_shape* shape);
 
 /* Static, NUL-terminated description of a status code. */
 /*

@@ -16,18 +16,24 @@ from .binding import (  # noqa: F401
     onecomp_block_norm_forward,
     onecomp_clip_gradients,
     onecomp_crossgram_accumulate,
+    onecomp_embedding_backward,
+    onecomp_embedding_forward,
     onecomp_factor_workspace_bytes,
     onecomp_hessian_accumulate,
     onecomp_hessian_factor,
     onecomp_jointq_refine,
     onecomp_jointq_workspace_bytes,
+    onecomp_linear_int8,
     onecomp_mfma_rate_probe,
     onecomp_qep_target,
     onecomp_qep_workspace_bytes,
     onecomp_quantize_layer,
+    onecomp_quantize_tokens,
     onecomp_quantize_workspace_bytes,
     onecomp_rtn_sensitivity,
     onecomp_rtn_sensitivity_static,
+    onecomp_token_loss_backward,
+    onecomp_token_loss_forward,
     onecomp_version,
     status_string,
 )

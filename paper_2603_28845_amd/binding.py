@@ -60,6 +60,16 @@ EXPORTED_SYMBOLS = (
     "onecomp_block_norm_workspace_bytes",
     "onecomp_clip_gradients",
     "onecomp_clip_workspace_bytes",
+    "onecomp_embedding_forward",
+    "onecomp_embedding_backward",
+    "onecomp_embedding_workspace_bytes",
+    "onecomp_quantize_tokens",
+    "onecomp_linear_int8",
+    "onecomp_linear_int8_workspace_bytes",
+    "onecomp_token_loss_forward",
+    "onecomp_token_loss_workspace_bytes",
+    "onecomp_token_loss_backward",
+    "onecomp_token_loss_backward_workspace_bytes",
     "onecomp_status_string",
     "onecomp_version",
 )
@@ -102,6 +112,11 @@ class NormGradients(ctypes.Structure):
 class Gradient(ctypes.Structure):
     """onecomp_gradient"""
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class LossShape(ctypes.Structure):
+    """onecomp_loss_shape"""
+    _fields_ = [("dtype", ctypes.c_int), ("tokens", ctypes.c_int64), ("width", ctypes.c_int64), ("vocab", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
 class OnecompError(RuntimeError):
@@ -183,6 +198,26 @@ def load_library() -> ctypes.CDLL:
     lib.onecomp_clip_gradients.restype = i32
     lib.onecomp_clip_workspace_bytes.argtypes = []
     lib.onecomp_clip_workspace_bytes.restype = sz
+    lib.onecomp_embedding_forward.argtypes = [vp, i64, i32, vp, i64, i64, f32, vp, vp]
+    lib.onecomp_embedding_forward.restype = i32
+    lib.onecomp_embedding_backward.argtypes = [vp, i64, i32, vp, i64, i64, f32, vp, vp, vp, sz, vp]
+    lib.onecomp_embedding_backward.restype = i32
+    lib.onecomp_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.onecomp_embedding_workspace_bytes.restype = sz
+    lib.onecomp_quantize_tokens.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp]
+    lib.onecomp_quantize_tokens.restype = i32
+    lib.onecomp_linear_int8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, vp, sz, vp]
+    lib.onecomp_linear_int8.restype = i32
+    lib.onecomp_linear_int8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.onecomp_linear_int8_workspace_bytes.restype = sz
+    lib.onecomp_token_loss_forward.argtypes = [vp] * 7 + [sz, vp]
+    lib.onecomp_token_loss_forward.restype = i32
+    lib.onecomp_token_loss_workspace_bytes.argtypes = [vp]
+    lib.onecomp_token_loss_workspace_bytes.restype = sz
+    lib.onecomp_token_loss_backward.argtypes = [vp] * 10 + [sz, vp]
+    lib.onecomp_token_loss_backward.restype = i32
+    lib.onecomp_token_loss_backward_workspace_bytes.argtypes = [vp]
+    lib.onecomp_token_loss_backward_workspace_bytes.restype = sz
     lib.onecomp_status_string.argtypes = [i32]
     lib.onecomp_status_string.restype = ctypes.c_char_p
     lib.onecomp_version.argtypes = []
@@ -795,3 +830,197 @@ def onecomp_clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, out: 
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_clip_gradients")
     return to, norm
+
+
+# ---- from tokens to the loss ---------------------------------------------------------------------------------------
+_LOSS_SHAPE = struct.Struct("iqqqf4x")            # onecomp_loss_shape
+_LOSS_AT = _LOSS_SHAPE.size                       # where the tensors behind it begin
+
+
+def _code_of(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype} of {name}: float32 or bfloat16 expected")
+    return code
+
+
+def _plain_rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, rows: int, width: int) -> Tuple[int, int]:
+    """(address, row stride) of a [rows, width] tensor."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+        raise ValueError(f"{name} must be [{rows}, {width}]")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}")
+    row, one = t.stride()
+    if one != 1 and width > 1 and rows > 0:
+        raise ValueError(f"rows of {name} must be dense")
+    return t.data_ptr(), row if rows > 1 else max(width, 1)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: int, n: int) -> int:
+    """Address of n dense entries (any shape that holds as many)."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must have {n} dense entries")
+    return t.data_ptr()
+
+
+def onecomp_embedding_forward(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[tokens], zeros for tokens outside the table.  tokens: int32 [n]; table: [vocab, width] bf16/fp32 (rows may be
+    strided).  Returns [n, width]."""
+    lib = _lib or load_library()
+    code, device = _code_of(table, "table"), table.get_device()
+    if table.dim() != 2 or tokens.dim() != 1:
+        raise ValueError("shapes: tokens [n], table [vocab, width]")
+    n, (vocab, width) = tokens.shape[0], table.shape
+    if out is None:
+        out = table.new_empty((n, width))
+    struct.pack_into("Pq" * 2, _buffer.data, 0, *_plain_rows(table, "table", table.dtype, device, vocab, width),
+                     *_plain_rows(out, "out", table.dtype, device, n, width))
+    rc = lib.onecomp_embedding_forward(_vector(tokens, "tokens", torch.int32, device, n), n, code, _buffer.at, vocab, width, scale, _buffer.at + 16,
+                                       _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_embedding_forward")
+    return out
+
+
+def onecomp_embedding_backward(tokens: torch.Tensor, d_out: torch.Tensor, vocab: int, scale: float = 1.0, base: Optional[torch.Tensor] = None,
+                               d_table: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The table's gradient [vocab, width]: base (or 0) + scale * the sums of d_out's rows [n, width] over each token's places.
+    base may be d_table itself, whose rows without a token are then left as they are."""
+    lib = _lib or load_library()
+    code, device = _code_of(d_out, "d_out"), d_out.get_device()
+    if d_out.dim() != 2 or tokens.dim() != 1:
+        raise ValueError("shapes: tokens [n], d_out [n, width]")
+    n, width = tokens.shape[0], d_out.shape[1]
+    if d_table is None:
+        d_table = d_out.new_empty((vocab, width))
+    base_fields = (0, 0) if base is None else _plain_rows(base, "base", d_out.dtype, device, vocab, width)
+    struct.pack_into("Pq" * 3, _buffer.data, 0, *_plain_rows(d_out, "d_out", d_out.dtype, device, n, width),
+                     *_plain_rows(d_table, "d_table", d_out.dtype, device, vocab, width), *base_fields)
+    at = _buffer.at
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_embedding_workspace_bytes(n, vocab, width), d_out.device)
+    rc = lib.onecomp_embedding_backward(_vector(tokens, "tokens", torch.int32, device, n), n, code, at, vocab, width, scale,
+                                        at + 32 if base is not None else 0, at + 16, ws, ws_bytes, _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_embedding_backward")
+    return d_table
+
+
+def onecomp_quantize_tokens(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                            sums: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """8-bit codes of x [tokens, width] (bf16/fp32, rows may be strided) with a scale per token.  Returns (codes int8 [tokens, width],
+    scales fp32 [tokens], sums of the codes int32 [tokens]), what onecomp_linear_int8 takes."""
+    lib = _lib or load_library()
+    code, device = _code_of(x, "x"), x.get_device()
+    if x.dim() != 2:
+        raise ValueError("x must be [tokens, width]")
+    tokens, width = x.shape
+    if codes is None:
+        codes = x.new_empty((tokens, width), dtype=torch.int8)
+    if scales is None:
+        scales = x.new_empty(tokens, dtype=torch.float32)
+    if sums is None:
+        sums = x.new_empty(tokens, dtype=torch.int32)
+    struct.pack_into("Pq", _buffer.data, 0, *_plain_rows(x, "x", x.dtype, device, tokens, width))
+    rc = lib.onecomp_quantize_tokens(_buffer.at, code, tokens, width, _vector(codes, "codes", torch.int8, device, tokens * width),
+                                     _vector(scales, "scales", torch.float32, device, tokens), _vector(sums, "sums", torch.int32, device, tokens),
+                                     _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_quantize_tokens")
+    return codes, scales, sums
+
+
+def onecomp_linear_int8(codes: torch.Tensor, token_scales: torch.Tensor, token_sums: torch.Tensor, Q_codes: torch.Tensor, scales: torch.Tensor,
+                        zeros: torch.Tensor, bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A quantized layer on quantized tokens: [tokens, d_out] of dtype.  codes, token_scales, token_sums: onecomp_quantize_tokens;
+    Q_codes [d_out, d_in], scales, zeros: onecomp_quantize_layer with group_size = d_in; bias: [d_out] of dtype."""
+    lib = _lib or load_library()
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}: float32 or bfloat16 expected")
+    if not codes.is_cuda:
+        raise ValueError("codes must live on the GPU")
+    if codes.dim() != 2 or Q_codes.dim() != 2 or codes.shape[1] != Q_codes.shape[1]:
+        raise ValueError("shapes: codes [tokens, d_in], Q_codes [d_out, d_in]")
+    device, tokens, (d_out, d_in) = codes.get_device(), codes.shape[0], Q_codes.shape
+    if out is None:
+        out = codes.new_empty((tokens, d_out), dtype=dtype)
+    struct.pack_into("Pq", _buffer.data, 0, *_plain_rows(out, "out", dtype, device, tokens, d_out))
+    need = lib.onecomp_linear_int8_workspace_bytes(tokens, d_out, d_in)
+    ws, ws_bytes, _keep = _scratch(workspace, need, codes.device)
+    rc = lib.onecomp_linear_int8(_vector(codes, "codes", torch.int8, device, tokens * d_in), _vector(token_scales, "token_scales", torch.float32, device, tokens),
+                                 _vector(token_sums, "token_sums", torch.int32, device, tokens),
+                                 _vector(Q_codes, "Q_codes", torch.uint8, device, d_out * d_in), _vector(scales, "scales", torch.float32, device, d_out),
+                                 _vector(zeros, "zeros", torch.float32, device, d_out), _vector(bias, "bias", dtype, device, d_out), code, tokens, d_out, d_in,
+                                 _buffer.at, ws, ws_bytes, _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_linear_int8")
+    return out
+
+
+def _loss_shape(h, weight, targets, scale) -> Tuple[int, int, int, int]:
+    """Packs onecomp_loss_shape, h and weight to the start of the buffer; returns (device, tokens, vocab, address of targets)."""
+    code, device = _code_of(h, "h"), h.get_device()
+    if h.dim() != 2 or weight.dim() != 2 or weight.shape[1] != h.shape[1]:
+        raise ValueError("shapes: h [tokens, width], weight [vocab, width], targets [tokens]")
+    (tokens, width), vocab = h.shape, weight.shape[0]
+    _LOSS_SHAPE.pack_into(_buffer.data, 0, code, tokens, width, vocab, scale)
+    struct.pack_into("Pq" * 2, _buffer.data, _LOSS_AT, *_plain_rows(h, "h", h.dtype, device, tokens, width),
+                     *_plain_rows(weight, "weight", h.dtype, device, vocab, width))
+    return device, tokens, vocab, _vector(targets, "targets", torch.int32, device, tokens)
+
+
+def onecomp_token_loss_forward(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, want_lse: bool = True,
+                               loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Cross entropy of each token over the vocabulary, without keeping logits.  h: [tokens, width], weight: [vocab, width] bf16/fp32
+    (rows may be strided), targets: int32 [tokens], outside the vocabulary where a token is left out (loss 0).  Returns (loss,
+    log-sum-exps of the logits scale * h weight^T or None), fp32 [tokens]."""
+    lib = _lib or load_library()
+    device, tokens, _, targets_at = _loss_shape(h, weight, targets, scale)
+    if loss is None:
+        loss = h.new_empty(tokens, dtype=torch.float32)
+    if lse is None and want_lse:
+        lse = h.new_empty(tokens, dtype=torch.float32)
+    at = _buffer.at
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_token_loss_workspace_bytes(at), h.device)
+    rc = lib.onecomp_token_loss_forward(at, at + _LOSS_AT, at + _LOSS_AT + 16, targets_at, _vector(loss, "loss", torch.float32, device, tokens),
+                                        _vector(lse, "lse", torch.float32, device, tokens), ws, ws_bytes, _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_token_loss_forward")
+    return loss, lse
+
+
+def onecomp_token_loss_backward(d_loss: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                                scale: float = 1.0, d_lse: Optional[torch.Tensor] = None, want_dh: bool = True, want_dweight: bool = True,
+                                dh: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                                workspace: Optional[torch.Tensor] = None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Returns (dh, dweight) from the gradients of the forward call's losses (fp32 [tokens]) and, if given, of its log-sum-exps; None for
+    what is not wanted."""
+    lib = _lib or load_library()
+    device, tokens, vocab, targets_at = _loss_shape(h, weight, targets, scale)
+    if dh is None and want_dh:
+        dh = _like(h)
+    if dweight is None and want_dweight:
+        dweight = _like(weight)
+    at, width = _buffer.at, h.shape[1]
+    out = _LOSS_AT + 32
+    struct.pack_into("Pq" * 2, _buffer.data, out, *((0, 0) if dh is None else _plain_rows(dh, "dh", h.dtype, device, tokens, width)),
+                     *((0, 0) if dweight is None else _plain_rows(dweight, "dweight", h.dtype, device, vocab, width)))
+    ws, ws_bytes, _keep = _scratch(workspace, lib.onecomp_token_loss_backward_workspace_bytes(at), h.device)
+    rc = lib.onecomp_token_loss_backward(at, _vector(d_loss, "d_loss", torch.float32, device, tokens), _vector(d_lse, "d_lse", torch.float32, device, tokens),
+                                         at + _LOSS_AT, at + _LOSS_AT + 16, targets_at, _vector(lse, "lse", torch.float32, device, tokens),
+                                         at + out if dh is not None else 0, at + out + 16 if dweight is not None else 0, ws, ws_bytes, _raw_stream())
+    if rc != ONECOMP_OK:
+        raise OnecompError(rc, "onecomp_token_loss_backward")
+    return dh, dweight

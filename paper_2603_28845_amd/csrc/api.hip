@@ -2,6 +2,7 @@
 #include "common.hpp"
 #include "attention.hpp"
 #include "block.hpp"
+#include "token.hpp"
 #include <cmath>
 #include <initializer_list>
 #include <dlfcn.h>
@@ -161,6 +162,46 @@ attn::Params attention_params(const onecomp_attention_shape* s) {
     // no sequence has more keys than all of them; more queries than there are still ask for the launch shape of so many
     P.max_q = s->max_q < (int64_t(1) << 31) ? s->max_q : int64_t(1) << 31;
     P.max_k = s->max_k < s->total_k ? s->max_k : s->total_k;
+    return P;
+}
+
+bool known(onecomp_dtype t) { return t == ONECOMP_F32 || t == ONECOMP_BF16; }
+size_t size_of(onecomp_dtype t) { return t == ONECOMP_BF16 ? 2 : 4; }
+
+// rows of `width` whole elements (none: nothing to look at)
+bool check_plain(const onecomp_rows* r, onecomp_dtype dtype, int64_t rows, int64_t width) {
+    if (!r) return false;
+    return rows == 0 || (r->data && aligned(r->data, size_of(dtype)) && r->row_stride >= width && r->row_stride <= (int64_t(1) << 31));
+}
+
+onecomp_status check_loss(const onecomp_loss_shape* s) {
+    if (!s) return ONECOMP_ERR_INVALID_ARG;
+    if (!known(s->dtype)) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->tokens < 0 || s->width <= 0 || s->vocab <= 0 || !(s->scale > 0.f) || !std::isfinite(s->scale)) return ONECOMP_ERR_INVALID_ARG;
+    const int64_t most = int64_t(1) << 24;
+    if (s->tokens > most || s->width > most || s->vocab > most || s->scale < 0x1p-100f || s->scale > 0x1p100f) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->width * int64_t(size_of(s->dtype)) % 16 != 0 || s->width * int64_t(size_of(s->dtype)) >= (int64_t(1) << 23)) return ONECOMP_ERR_UNSUPPORTED;
+    // workgroups of a launch: tiles of 128 x 128
+    if (ceil_div(s->tokens, 128) * ceil_div(s->vocab, 128) > (int64_t(1) << 30)) return ONECOMP_ERR_UNSUPPORTED;
+    return ONECOMP_OK;
+}
+bool check_operand(const onecomp_loss_shape* s, const onecomp_rows* r, int64_t rows) {
+    if (!r) return false;
+    if (rows == 0) return true;
+    const int64_t stride = r->row_stride;
+    if (!r->data || !aligned(r->data, 16) || stride < s->width || stride >= (int64_t(1) << 23)) return false;
+    return stride * int64_t(size_of(s->dtype)) % 16 == 0 && stride * int64_t(size_of(s->dtype)) < (int64_t(1) << 23);
+}
+token::Loss loss_params(const onecomp_loss_shape* s, const onecomp_rows* h, const onecomp_rows* weight, const int32_t* targets, void* workspace) {
+    token::Loss P{};
+    P.h = rows_of(h);
+    P.weight = rows_of(weight);
+    P.targets = targets;
+    P.tokens = s->tokens;
+    P.width = s->width;
+    P.vocab = s->vocab;
+    P.scale = s->scale;
+    P.workspace = workspace;
     return P;
 }
 }  // namespace
@@ -556,6 +597,128 @@ ONECOMP_API onecomp_status onecomp_clip_gradients(const onecomp_gradient* grads,
     return block::clip_run(grads, n, max_norm, norm, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
+ONECOMP_API onecomp_status onecomp_embedding_forward(const int32_t* tokens, int64_t n, onecomp_dtype dtype, const onecomp_rows* table, int64_t vocab,
+                                                     int64_t width, float scale, const onecomp_rows* out, void* hip_stream) {
+    const ApiRange range("onecomp_embedding_forward");
+    if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
+    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
+        return ONECOMP_ERR_INVALID_ARG;
+    if ((n > 0 && !tokens) || !aligned(tokens, 4) || !check_plain(table, dtype, vocab, width) || !check_plain(out, dtype, n, width)) return ONECOMP_ERR_INVALID_ARG;
+    if (n == 0) return ONECOMP_OK;
+    if (out->data == table->data) return ONECOMP_ERR_INVALID_ARG;
+    return token::embedding_forward_run(dtype, tokens, n, rows_of(table), vocab, width, scale, rows_of(out), static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width) {
+    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24)) return 0;
+    return token::embedding_space(n, vocab, width).all;
+}
+
+ONECOMP_API onecomp_status onecomp_embedding_backward(const int32_t* tokens, int64_t n, onecomp_dtype dtype, const onecomp_rows* d_out, int64_t vocab,
+                                                      int64_t width, float scale, const onecomp_rows* base, const onecomp_rows* d_table,
+                                                      void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const ApiRange range("onecomp_embedding_backward");
+    if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
+    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
+        return ONECOMP_ERR_INVALID_ARG;
+    if ((n > 0 && !tokens) || !aligned(tokens, 4) || !check_plain(d_out, dtype, n, width) || !check_plain(d_table, dtype, vocab, width) ||
+        (base && !check_plain(base, dtype, vocab, width)))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < token::embedding_space(n, vocab, width).all) return ONECOMP_ERR_WORKSPACE;
+    if (n > 0 && d_table->data == d_out->data) return ONECOMP_ERR_INVALID_ARG;
+    if (base && base->data == d_table->data && base->row_stride != d_table->row_stride && vocab > 1) return ONECOMP_ERR_INVALID_ARG;
+    return token::embedding_backward_run(dtype, tokens, n, rows_of(d_out), vocab, width, scale, rows_of(base), rows_of(d_table), workspace,
+                                         static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API onecomp_status onecomp_quantize_tokens(const onecomp_rows* x, onecomp_dtype dtype, int64_t tokens, int64_t width, int8_t* codes, float* scales,
+                                                   int32_t* sums, void* hip_stream) {
+    const ApiRange range("onecomp_quantize_tokens");
+    if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
+    if (tokens < 0 || tokens > (int64_t(1) << 30) || width <= 0 || !check_plain(x, dtype, tokens, width)) return ONECOMP_ERR_INVALID_ARG;
+    if (width % 16 != 0 || width > 65520) return ONECOMP_ERR_UNSUPPORTED;
+    if (tokens == 0) return ONECOMP_OK;
+    if (!codes || !scales || !sums || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(sums, 4) || static_cast<const void*>(codes) == x->data)
+        return ONECOMP_ERR_INVALID_ARG;
+    return token::quantize_tokens_run(dtype, rows_of(x), tokens, width, codes, scales, sums, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in) {
+    if (tokens <= 0 || tokens > (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || d_in % 16 != 0 || d_in > 65520) return 0;
+    return token::linear_workspace_bytes(tokens, d_out, d_in);
+}
+
+ONECOMP_API onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scales, const int32_t* token_sums, const uint8_t* Q_codes,
+                                               const float* scales, const float* zeros, const void* bias, onecomp_dtype dtype, int64_t tokens,
+                                               int64_t d_out, int64_t d_in, const onecomp_rows* y, void* workspace, size_t workspace_bytes,
+                                               void* hip_stream) {
+    const ApiRange range("onecomp_linear_int8");
+    if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
+    if (tokens < 0 || tokens > (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || !check_plain(y, dtype, tokens, d_out))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (d_in % 16 != 0 || d_in > 65520 || ceil_div(tokens, 128) * ceil_div(d_out, 128) > (int64_t(1) << 30)) return ONECOMP_ERR_UNSUPPORTED;
+    if (!Q_codes || !scales || !zeros || !aligned(Q_codes, 16) || !aligned(scales, 4) || !aligned(zeros, 4) || !aligned(bias, size_of(dtype)))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (tokens == 0) return ONECOMP_OK;
+    if (!codes || !token_scales || !token_sums || !aligned(codes, 16) || !aligned(token_scales, 4) || !aligned(token_sums, 4)) return ONECOMP_ERR_INVALID_ARG;
+    if (y->data == static_cast<const void*>(codes) || y->data == static_cast<const void*>(Q_codes)) return ONECOMP_ERR_INVALID_ARG;
+    const size_t need = token::linear_workspace_bytes(tokens, d_out, d_in);
+    if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
+    const token::Linear P{codes, token_scales, token_sums, Q_codes, scales, zeros, bias, rows_of(y), tokens, d_out, d_in, workspace};
+    return token::linear_run(dtype, P, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_token_loss_workspace_bytes(const onecomp_loss_shape* shape) {
+    if (check_loss(shape) != ONECOMP_OK) return 0;
+    return token::loss_workspace_bytes(shape->dtype, shape->tokens, shape->width, shape->vocab, false);
+}
+
+ONECOMP_API onecomp_status onecomp_token_loss_forward(const onecomp_loss_shape* shape, const onecomp_rows* h, const onecomp_rows* weight,
+                                                      const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                                                      void* hip_stream) {
+    const ApiRange range("onecomp_token_loss_forward");
+    if (const onecomp_status st = check_loss(shape)) return st;
+    if (!check_operand(shape, h, shape->tokens) || !check_operand(shape, weight, shape->vocab) || (shape->tokens && !targets) || !aligned(targets, 4) ||
+        !aligned(loss, 4) || !aligned(lse, 4) || (shape->tokens && loss == lse))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < onecomp_token_loss_workspace_bytes(shape)) return ONECOMP_ERR_WORKSPACE;
+    if (shape->tokens == 0) return ONECOMP_OK;
+    token::Loss P = loss_params(shape, h, weight, targets, workspace);
+    P.loss = loss;
+    P.lse = lse;
+    return token::loss_forward_run(shape->dtype, P, static_cast<hipStream_t>(hip_stream));
+}
+
+ONECOMP_API size_t onecomp_token_loss_backward_workspace_bytes(const onecomp_loss_shape* shape) {
+    if (check_loss(shape) != ONECOMP_OK) return 0;
+    return token::loss_workspace_bytes(shape->dtype, shape->tokens, shape->width, shape->vocab, true);
+}
+
+ONECOMP_API onecomp_status onecomp_token_loss_backward(const onecomp_loss_shape* shape, const float* d_loss, const float* d_lse, const onecomp_rows* h,
+                                                       const onecomp_rows* weight, const int32_t* targets, const float* lse, const onecomp_rows* dh,
+                                                       const onecomp_rows* dweight, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const ApiRange range("onecomp_token_loss_backward");
+    if (const onecomp_status st = check_loss(shape)) return st;
+    if (!check_operand(shape, h, shape->tokens) || !check_operand(shape, weight, shape->vocab) || (!dh && !dweight) ||
+        (dh && !check_operand(shape, dh, shape->tokens)) || (dweight && !check_operand(shape, dweight, shape->vocab)))
+        return ONECOMP_ERR_INVALID_ARG;
+    if ((shape->tokens && (!targets || !lse || !d_loss)) || !aligned(targets, 4) || !aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(d_lse, 4))
+        return ONECOMP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < onecomp_token_loss_backward_workspace_bytes(shape)) return ONECOMP_ERR_WORKSPACE;
+    for (const onecomp_rows* out : {dh, dweight}) {
+        if (!out) continue;
+        if (out->data == weight->data || (shape->tokens && out->data == h->data)) return ONECOMP_ERR_INVALID_ARG;
+    }
+    if (dh && dweight && shape->tokens && dh->data == dweight->data) return ONECOMP_ERR_INVALID_ARG;
+    token::Loss P = loss_params(shape, h, weight, targets, workspace);
+    P.lse = const_cast<float*>(lse);
+    P.d_loss = d_loss;
+    P.d_lse = d_lse;
+    P.dh = rows_of(dh);
+    P.dweight = rows_of(dweight);
+    return token::loss_backward_run(shape->dtype, P, static_cast<hipStream_t>(hip_stream));
+}
+
 ONECOMP_API const char* onecomp_status_string(onecomp_status status) {
     switch (status) {
         case ONECOMP_OK: return "ok";
@@ -568,6 +731,6 @@ ONECOMP_API const char* onecomp_status_string(onecomp_status status) {
     return "unknown status";
 }
 
-ONECOMP_API int onecomp_version(void) { return 200; }
+ONECOMP_API int onecomp_version(void) { return 300; }
 
 }  // extern "C"

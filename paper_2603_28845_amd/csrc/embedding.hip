@@ -1,0 +1,319 @@
+// Rows of an embedding table, scaled, and the table's gradient.
+//   out_t = scale table[token_t],   d table_v = base_v + scale sum over t with token_t = v of d_out_t
+// Tokens outside the vocabulary mark padding: zeros forward, no part in the gradient.
+//
+// Gradient: three kernels.  (1) Sorting: a workgroup owns a range of the vocabulary and goes through all tokens twice, counting its
+// own per wave and row, then placing them; no workgroup waits for another, and equal tokens stay in their order.  (2) Sums: waves
+// add up `segment` sorted tokens each in 32 bits; rows whose tokens all lie in one segment are finished there, the others leave a
+// partial sum per segment.  Rows without a token are filled by further workgroups of the same launch.  (3) Rows that cross segments
+// are joined in their order.  So frequent tokens are spread over the chip, and the same inputs give the same bits.
+#include "token.hpp"
+
+namespace onecomp {
+namespace token {
+namespace {
+
+using block::load_one;
+using block::load_vector;
+using block::store_one;
+using block::store_vector;
+
+// n of a vector's entries, at the end of a row
+template <class T, int N>
+__device__ __forceinline__ void load_some(float (&x)[N], const T* p, int n) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = e < n ? load_one(p + e) : 0.f;
+}
+template <class T, int N>
+__device__ __forceinline__ void store_some(T* p, const float (&x)[N], int n) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e < n) store_one(p + e, x[e]);
+}
+template <class T, int N>
+__device__ __forceinline__ void load_any(float (&x)[N], const T* p, int n) {
+    if (n >= N) load_vector(x, p);
+    else load_some(x, p, n);
+}
+template <class T, int N>
+__device__ __forceinline__ void store_any(T* p, const float (&x)[N], int n) {
+    if (n >= N) store_vector(p, x);
+    else store_some(p, x, n);
+}
+
+struct Lookup {
+    const int32_t* tokens;
+    Rows table, out;
+    int64_t n, vocab;
+    int width;
+    float scale;
+};
+// A wave per token.
+template <class T>
+__global__ __launch_bounds__(256) void lookup_kernel(Lookup P) {
+    constexpr int N = 16 / int(sizeof(T));
+    const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (t >= P.n) return;
+    const int token = P.tokens[t];
+    const bool inside = token >= 0 && token < P.vocab;
+    const T* from = static_cast<const T*>(P.table.p) + (inside ? token : 0) * P.table.stride;
+    T* to = static_cast<T*>(P.out.p) + t * P.out.stride;
+#pragma unroll 4
+    for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) {
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = 0.f;
+        if (inside) load_any(x, from + c, P.width - c);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] *= P.scale;
+        store_any(to + c, x, P.width - c);
+    }
+}
+
+struct Sort {
+    const int32_t* tokens;
+    int64_t n;
+    int vocab, rows;                         // rows of the vocabulary per workgroup
+    int32_t *order, *starts;
+};
+__global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
+    extern __shared__ int32_t at[];          // [wave][row]
+    __shared__ int32_t s_wave[SORT_WAVES], s_below;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lo = blockIdx.x * P.rows, rows = min(P.rows, P.vocab - lo);
+    const int64_t each = (P.n + SORT_WAVES * 64 - 1) / (SORT_WAVES * 64) * 64;
+    const int64_t begin = wave * each, end = begin + each < P.n ? begin + each : P.n;
+    for (int i = threadIdx.x; i < SORT_WAVES * P.rows; i += 64 * SORT_WAVES) at[i] = 0;
+    if (threadIdx.x == 0) s_below = 0;
+    __syncthreads();
+    int32_t* const mine = at + wave * P.rows;
+    int below = 0;
+#pragma unroll 4
+    for (int64_t t = begin + lane; t < end; t += 64) {
+        const int token = P.tokens[t], row = token - lo;
+        below += token >= 0 && row < 0;
+        if (row >= 0 && row < rows) atomicAdd(&mine[row], 1);      // whole numbers: any order
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
+    if (lane == 0 && below) atomicAdd(&s_below, below);
+    __syncthreads();
+    // counts -> places: row by row, in a row wave by wave
+    const int r = threadIdx.x;
+    int total = 0;
+    if (r < rows)
+        for (int w = 0; w < SORT_WAVES; ++w) total += at[w * P.rows + r];
+    int sum = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += x;
+    }
+    if (lane == 63) s_wave[wave] = sum;
+    __syncthreads();
+    int place = s_below + sum - total;
+    for (int w = 0; w < wave; ++w) place += s_wave[w];
+    if (r < rows) {
+        P.starts[lo + r] = place;
+        if (lo + r == P.vocab - 1) P.starts[P.vocab] = place + total;
+        for (int w = 0; w < SORT_WAVES; ++w) {
+            const int n = at[w * P.rows + r];
+            at[w * P.rows + r] = place;
+            place += n;
+        }
+    }
+    __syncthreads();
+    for (int64_t t0 = begin; t0 < end; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const int row = t < end ? P.tokens[t] - lo : -1;
+        unsigned long long left = __ballot(row >= 0 && row < rows);
+        while (left) {                                             // one token of the 64 after the other, all its places at a time
+            const int same_row = __builtin_amdgcn_readlane(row, __ffsll(left) - 1);
+            const unsigned long long same = __ballot(row == same_row);
+            const int from = mine[same_row];
+            if (row == same_row) P.order[from + __popcll(same & ((1ull << lane) - 1))] = int32_t(t);
+            if (lane == 0) mine[same_row] = from + __popcll(same);
+            __builtin_amdgcn_wave_barrier();
+            left &= ~same;
+        }
+    }
+}
+
+struct Sums {
+    const int32_t *tokens, *order, *starts;
+    Rows d_out, base, grad;
+    int64_t vocab;
+    int width, segment, strips, in_place;
+    int64_t sum_blocks, units;               // workgroups that add up, and their waves' pieces of work
+    float scale;
+    float* parts;                            // [segment][0: begun before, 1: begun here][width]
+};
+
+// a row's sum, finished
+template <class T, int N>
+__device__ __forceinline__ void finish_row(const Sums& P, int64_t row, int c, int n, const float (&sum)[N]) {
+    float y[N];
+    if (P.base.p) load_any(y, static_cast<const T*>(P.base.p) + row * P.base.stride + c, n);
+    else
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = fmaf(P.scale, sum[e], y[e]);
+    store_any(static_cast<T*>(P.grad.p) + row * P.grad.stride + c, y, n);
+}
+
+// A wave per segment and strip of 64 vectors.
+template <class T>
+__device__ void add_up(const Sums& P, int64_t unit) {
+    constexpr int N = 16 / int(sizeof(T)), AHEAD = 8;
+    const int lane = threadIdx.x & 63;
+    const int64_t segment = unit / P.strips;
+    const int c = (int(unit % P.strips) * 64 + lane) * N, n = P.width - c;
+    const int64_t first = segment * P.segment, all = P.starts[P.vocab];
+    if (first >= all) return;
+    const int many = int(all - first < P.segment ? all - first : P.segment);
+    // a lane's token: its row of d_out, whether the row's tokens begin or end with it
+    int t = 0, token = -1;
+    bool begins = false, ends = false;
+    if (lane < many) {
+        t = P.order[first + lane];
+        token = P.tokens[t];
+        begins = P.starts[token] == first + lane;
+        ends = P.starts[token + 1] == first + lane + 1;
+    }
+    const unsigned long long begin_mask = __ballot(begins), end_mask = __ballot(ends);
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+    bool here = false;                                             // whether the present row began in this segment
+    for (int i0 = 0; i0 < many; i0 += AHEAD) {
+        float x[AHEAD][N];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i0 + u < many && n > 0)
+                load_any(x[u], static_cast<const T*>(P.d_out.p) + int64_t(__builtin_amdgcn_readlane(t, i0 + u)) * P.d_out.stride + c, n);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = i0 + u;
+            if (i >= many) break;
+            if (begin_mask >> i & 1) {
+                here = true;
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] += x[u][e];
+            const bool end = end_mask >> i & 1;
+            if (!end && i + 1 < many) continue;
+            if (n > 0) {
+                if (end && here) {
+                    finish_row<T>(P, __builtin_amdgcn_readlane(token, i), c, n, sum);
+                } else {
+                    float* to = P.parts + (segment * 2 + (here ? 1 : 0)) * P.width + c;
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e < n) to[e] = sum[e];
+                }
+            }
+            here = false;
+        }
+    }
+}
+template <class T>
+__global__ __launch_bounds__(256) void sums_kernel(Sums P) {
+    if (int64_t(blockIdx.x) < P.sum_blocks) {
+        const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+        if (unit < P.units) add_up<T>(P, unit);
+        return;
+    }
+    // rows without a token
+    constexpr int N = 16 / int(sizeof(T));
+    const int64_t row = (int64_t(blockIdx.x) - P.sum_blocks) * 4 + (threadIdx.x >> 6);
+    if (row >= P.vocab || P.starts[row] != P.starts[row + 1]) return;
+    const float none[N] = {};
+    for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) finish_row<T>(P, row, c, P.width - c, none);
+}
+
+// The row that begins in a segment and goes on behind it: its segments' sums in their order.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(Sums P) {
+    constexpr int N = 16 / int(sizeof(T));
+    const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (unit >= P.units) return;
+    const int64_t segment = unit / P.strips, last = (segment + 1) * P.segment - 1;
+    if (last + 1 >= P.starts[P.vocab]) return;
+    const int token = P.tokens[P.order[last]];
+    const int64_t begin = P.starts[token], end = P.starts[token + 1];
+    if (begin < segment * P.segment || end <= last + 1) return;
+    const int c = (int(unit % P.strips) * 64 + (threadIdx.x & 63)) * N, n = P.width - c;
+    if (n <= 0) return;
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+    for (int64_t s = segment; s * P.segment < end; ++s) {
+        const float* from = P.parts + (s * 2 + (s == segment ? 1 : 0)) * P.width + c;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n) sum[e] += from[e];
+    }
+    finish_row<T>(P, token, c, n, sum);
+}
+
+template <class T>
+onecomp_status backward(const Sums& P, const Sort& S, hipStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    const int lds = SORT_WAVES * S.rows * 4;
+    if (const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(sort_kernel), SORT_WAVES * SORT_MOST * 4, done)) return st;
+    sort_kernel<<<dim3(unsigned(ceil_div(S.vocab, S.rows))), dim3(64 * SORT_WAVES), lds, stream>>>(S);
+    ONECOMP_CHECK_LAUNCH();
+    const int64_t fill = P.in_place ? 0 : ceil_div(P.vocab, 4);
+    if (P.sum_blocks + fill > 0) {
+        sums_kernel<T><<<dim3(unsigned(P.sum_blocks + fill)), dim3(256), 0, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    if (S.n > P.segment) {
+        join_kernel<T><<<dim3(unsigned(P.sum_blocks)), dim3(256), 0, stream>>>(P);
+        ONECOMP_CHECK_LAUNCH();
+    }
+    return ONECOMP_OK;
+}
+
+}  // namespace
+
+onecomp_status embedding_forward_run(onecomp_dtype dtype, const int32_t* tokens, int64_t n, const Rows& table, int64_t vocab, int64_t width, float scale,
+                                     const Rows& out, hipStream_t stream) {
+    const Lookup P{tokens, table, out, n, vocab, int(width), scale};
+    const dim3 grid(unsigned(ceil_div(n, 4)));
+    if (dtype == ONECOMP_BF16) lookup_kernel<uint16_t><<<grid, dim3(256), 0, stream>>>(P);
+    else lookup_kernel<float><<<grid, dim3(256), 0, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
+}
+
+onecomp_status embedding_backward_run(onecomp_dtype dtype, const int32_t* tokens, int64_t n, const Rows& d_out, int64_t vocab, int64_t width, float scale,
+                                      const Rows& base, const Rows& d_table, void* workspace, hipStream_t stream) {
+    const EmbeddingSpace s = embedding_space(n, vocab, width);
+    char* ws = static_cast<char*>(workspace);
+    Sort S{tokens, n, int(vocab), sort_rows(vocab), reinterpret_cast<int32_t*>(ws + s.order), reinterpret_cast<int32_t*>(ws + s.starts)};
+    Sums P{};
+    P.tokens = tokens;
+    P.order = S.order;
+    P.starts = S.starts;
+    P.d_out = d_out;
+    P.base = base;
+    P.grad = d_table;
+    P.vocab = vocab;
+    P.width = int(width);
+    P.segment = segment_of(n);
+    P.strips = int(ceil_div(width, 64 * (dtype == ONECOMP_BF16 ? 8 : 4)));
+    P.in_place = base.p == d_table.p;
+    P.units = s.segments * P.strips;
+    P.sum_blocks = ceil_div(P.units, 4);
+    P.scale = scale;
+    P.parts = reinterpret_cast<float*>(ws + s.parts);
+    return dtype == ONECOMP_BF16 ? backward<uint16_t>(P, S, stream) : backward<float>(P, S, stream);
+}
+
+}  // namespace token
+}  // namespace onecomp

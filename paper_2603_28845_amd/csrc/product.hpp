@@ -1,0 +1,290 @@
+// Tiles of matrix products for the 32 x 32 matrix instructions, from operands of 8, 16 or 32 bits in either order.
+//
+//   C[m][n] = sum_k A[n][k] B[m][k]
+//
+// n is the axis along which results are dense in memory: in the accumulators a lane holds four neighbours of n (rows of the
+// instruction's result) for one m (its column), so that sums over n stay in a lane and results go out in vectors.  An operand is
+// given ALONG k (k dense in memory) or ACROSS it (n, or m, dense: rows of k).
+//
+// Whatever the type, a step is 64 bytes of k per row and an instruction's fragment 16 bytes per lane: lanes 0 .. 31 hold the
+// first, lanes 32 .. 63 the second 16 bytes of 32 (8 bf16, 16 int8, 4 fp32 values).  Tiles reach LDS by direct loads through a ring
+// of SLOTS steps; fragments of a half step are read while the other half is multiplied, reads and loads one by one behind
+// the matrix instructions.
+//   ALONG   a row's 64 bytes are four chunks of 16; chunk c of row r lies at c ^ ((r >> 1) & 3), so that eight rows' same chunk fall
+//           into different banks.
+//   ACROSS  rows of k as they are; in bf16 chunk c of row r lies at c ^ ((r & 3) << 2) and fragments are transposed reads (four
+//           rows of a read in four groups of banks); in fp32 a fragment is four plain reads.
+// What lies behind the operands' ends becomes zeros by the loads' bounds check.
+#pragma once
+#include "common.hpp"
+#include "token_plan.hpp"
+#include <type_traits>
+
+namespace onecomp {
+namespace product {
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int16v __attribute__((ext_vector_type(16)));
+
+struct Bf16 {
+    typedef uint16_t T;
+    typedef float16v Acc;
+    static constexpr int ESZ = 2;
+    static __device__ __forceinline__ uint4v left(uint4v a) { return a; }
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct F32 {
+    typedef float T;
+    typedef float16v Acc;
+    static constexpr int ESZ = 4;
+    static __device__ __forceinline__ uint4v left(uint4v a) { return a; }
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        const float4v x = __builtin_bit_cast(float4v, a), y = __builtin_bit_cast(float4v, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+};
+// left operand unsigned, less 128 (which turns its zeros behind the end into -128, times zeros of the right one); right signed
+struct Int8 {
+    typedef uint8_t T;
+    typedef int16v Acc;
+    static constexpr int ESZ = 1;
+    static __device__ __forceinline__ uint4v left(uint4v a) { return a ^ 0x80808080u; }
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(int4v, a), __builtin_bit_cast(int4v, b), c, 0, 0, 0);
+    }
+};
+
+enum Layout { ALONG, ACROSS };
+
+// rows: how many n (m) there are; stride: bytes between rows of n (ALONG) or of k (ACROSS), below 2^23 and, like the address, a
+// multiple of 16
+struct Operand {
+    const char* data;
+    int64_t stride, rows;
+};
+
+// WR x WC waves of FR x FC fragments each: a tile of 32 WR FR (n) by 32 WC FC (m)
+template <int WR_, int WC_, int FR_, int FC_, int PER_CU_>
+struct Shape {
+    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, PER_CU = PER_CU_, SLOTS = 4;
+    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
+    static constexpr int TN = 32 * WR * FR, TM = 32 * WC * FC;
+    static constexpr int STAGE = (TN + TM) * 64, LDS = SLOTS * STAGE;
+};
+typedef Shape<2, 2, 4, 4, 1> Big;      // 256 x 256
+typedef Shape<2, 2, 2, 2, 2> Mid;      // 128 x 128
+
+constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
+
+// One operand's tile: how a wave brings its part of a step to LDS, and how a lane reads fragments from there.
+template <class E, Layout L, int T, int WAVES>
+struct Side {
+    static constexpr int LOADS = T / 16 / WAVES;                  // of 1 KB, per wave and step
+    static_assert(T % (16 * WAVES) == 0, "whole loads per wave");
+    static constexpr int ROWB = T * E::ESZ, CHUNKS = ROWB / 16;   // ACROSS: a row of k
+    uint32_t off[LOADS], chunk;
+    const char* p;
+    int64_t left, step;                                           // bytes: what is left of the operand (ALONG: of a row), one step
+    int read0;
+    __device__ __forceinline__ void init(const Operand& o, int64_t first, int64_t inner, int wave, int lane) {
+        if constexpr (L == ALONG) {
+            p = o.data + first * o.stride;
+            left = inner * E::ESZ;
+            step = 64;
+            chunk = uint32_t((lane & 3) ^ ((lane >> 3) & 3)) * 16u;
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) {
+                const int r = (wave * LOADS + q) * 16 + (lane >> 2);
+                off[q] = first + r < o.rows ? uint32_t(r) * uint32_t(o.stride) + chunk : NOWHERE;
+            }
+            const int r = lane & 31;
+            read0 = r * 64 + (((lane >> 5) ^ ((r >> 1) & 3)) << 4);
+        } else {
+            p = o.data + first * E::ESZ;
+            left = inner * o.stride - first * E::ESZ;
+            step = int64_t(64 / E::ESZ) * o.stride;
+            chunk = 0;
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) {
+                const int at = (wave * LOADS + q) * 64 + lane, r = at / CHUNKS;
+                const int c = (at % CHUNKS) ^ (E::ESZ == 2 ? (r & 3) << 2 : 0);
+                off[q] = first + c * (16 / E::ESZ) < o.rows ? uint32_t(r) * uint32_t(o.stride) + uint32_t(c) * 16u : NOWHERE;
+            }
+            if constexpr (E::ESZ == 2) {
+                // inside 16 lanes, lane 4 k + c points at four columns of row k and lane i receives column i of rows 0 .. 3
+                const int i16 = lane & 15, kq = i16 >> 2;
+                read0 = ((lane >> 5) * 8 + kq) * ROWB + (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+            } else {
+                read0 = (lane >> 5) * 4 * ROWB + (lane & 31) * 4;
+            }
+        }
+    }
+    struct Step {
+        __amdgpu_buffer_rsrc_t rsrc;
+        uint32_t mask;
+    };
+    // the next step: an empty range (or mask) behind the last one
+    __device__ __forceinline__ Step next() {
+        Step s;
+        const int64_t range = L == ALONG ? 0x7FFFFFFF : left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
+        s.rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, int(range), 0x00020000);
+        const int here = left > 64 ? 64 : int(left);
+        s.mask = L == ALONG ? (int(chunk) < here ? 0u : NOWHERE) : 0u;
+        p += step;
+        left -= step;
+        return s;
+    }
+    __device__ __forceinline__ void load(const Step& s, uint32_t lds, int wave, int q) const {
+        lds_load16(lds + uint32_t(wave * LOADS + q) * 1024u, L == ALONG ? off[q] | s.mask : off[q], s.rsrc);
+    }
+    // fragment f of the tile (32 of n or m), half step s
+    __device__ __forceinline__ uint4v read(const char* tile, int f, int s, int lane) const {
+        if constexpr (L == ALONG) {
+            return *reinterpret_cast<const uint4v*>(tile + f * 2048 + (read0 ^ (s << 5)));
+        } else if constexpr (E::ESZ == 2) {
+            const char* a = tile + s * 16 * ROWB + read0 + ((f ^ ((lane & 15) >> 2)) << 6);
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a));
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 4 * ROWB));
+            return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const char* a = tile + s * 8 * ROWB + read0 + f * 128;
+            uint4v v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(a + i * ROWB);
+            return v;
+        }
+    }
+};
+
+// acc = the products of tile (n0, m0) over `inner` values of k.  lds: S::LDS bytes, free again for the caller behind a barrier.
+template <class E, Layout LA, Layout LB, class S>
+__device__ __forceinline__ void multiply(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t m0, int64_t inner,
+                                         typename E::Acc (&acc)[S::FR][S::FC]) {
+    constexpr int FR = S::FR, FC = S::FC, SLOTS = S::SLOTS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / S::WC, wc = wave % S::WC;
+    typedef Side<E, LA, S::TN, S::WAVES> SideA;
+    typedef Side<E, LB, S::TM, S::WAVES> SideB;
+    constexpr int LOADS = SideA::LOADS + SideB::LOADS, FRAGS = FR + FC, PRODUCTS = FR * FC;
+    constexpr int B_AT = S::TN * 64;
+    SideA a;
+    SideB b;
+    a.init(A, n0, inner, wave, lane);
+    b.init(B, m0, inner, wave, lane);
+    const uint32_t lds0 = uint32_t(uintptr_t((ONECOMP_LDS char*)lds));
+    struct Step {
+        typename SideA::Step a;
+        typename SideB::Step b;
+    };
+    auto next = [&]() __attribute__((always_inline)) { return Step{a.next(), b.next()}; };
+    auto load = [&](const Step& s, int slot, int i) __attribute__((always_inline)) {   // number i of a step's
+        if (i < SideA::LOADS) a.load(s.a, lds0 + slot * S::STAGE, wave, i);
+        else b.load(s.b, lds0 + slot * S::STAGE + B_AT, wave, i - SideA::LOADS);
+    };
+    for (int st = 0; st < SLOTS - 1; ++st) {
+        const Step s = next();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(s, st, i);
+    }
+#pragma unroll
+    for (int i = 0; i < FR; ++i)
+#pragma unroll
+        for (int j = 0; j < FC; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    struct Frags {
+        uint4v a[FR], b[FC];
+    };
+    Frags F0, F1;
+    // fragment r of FRAGS, those of both operands in turn
+    auto read = [&](Frags& f, int r, int slot, int s) __attribute__((always_inline)) {
+        constexpr int BOTH = 2 * (FR < FC ? FR : FC);
+        const bool of_a = r < BOTH ? !(r & 1) : FR > FC;
+        const int i = r < BOTH ? r >> 1 : r - BOTH / 2;
+        if (of_a) f.a[i] = a.read(lds + slot * S::STAGE, wr * FR + i, s, lane);
+        else f.b[i] = b.read(lds + slot * S::STAGE + B_AT, wc * FC + i, s, lane);
+    };
+    // `behind(n)` goes behind product n
+    auto products = [&](Frags& f, auto&& behind) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < PRODUCTS; ++n) {
+            const int i = n / FC, j = i & 1 ? FC - 1 - n % FC : n % FC;   // one operand stays from one product to the next
+            if (n % FC == 0) f.a[i] = E::left(f.a[i]);
+            acc[i][j] = E::mma(f.a[i], f.b[j], acc[i][j]);
+            behind(n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const int64_t bytes = inner * E::ESZ;
+    const int n_st = int((bytes + 63) >> 6);
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS * (SLOTS - 2)));
+    __syncthreads();
+    {
+        const Step s = next();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(s, SLOTS - 1, i);
+    }
+#pragma unroll
+    for (int r = 0; r < FRAGS; ++r) read(F0, r, 0, 0);
+    // what of `all` things goes behind product n
+    auto share = [](int n, int all, auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = n * all / PRODUCTS; x < (n + 1) * all / PRODUCTS; ++x) f(x);
+    };
+    auto stage = [&](auto slot_c) __attribute__((always_inline)) {
+        constexpr int slot = decltype(slot_c)::value, follow = (slot + 1) % SLOTS;
+        products(F0, [&](int n) __attribute__((always_inline)) {
+            constexpr int EARLY = PRODUCTS > FRAGS ? PRODUCTS / FRAGS : 1;        // a half step's reads in the first half of its products
+            if constexpr (EARLY > 1) {
+                if (n < FRAGS) read(F1, n, slot, 1);
+            } else {
+                share(n, FRAGS, [&](int r) __attribute__((always_inline)) { read(F1, r, slot, 1); });
+            }
+        });
+        // the next step has landed; every wave has read this one
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS * (SLOTS - 2)));
+        __syncthreads();
+        const Step s = next();
+        products(F1, [&](int n) __attribute__((always_inline)) {
+            share(n, LOADS + FRAGS, [&](int x) __attribute__((always_inline)) {
+                constexpr int BOTH = 2 * (LOADS < FRAGS ? LOADS : FRAGS);
+                const bool is_read = x < BOTH ? !(x & 1) : FRAGS > LOADS;
+                const int i = x < BOTH ? x >> 1 : x - BOTH / 2;
+                if (is_read) read(F0, i, follow, 0);
+                else load(s, slot, i);
+            });
+        });
+    };
+    int st = 0;
+#pragma unroll 1
+    for (; st + SLOTS <= n_st; st += SLOTS) {
+        stage(std::integral_constant<int, 0>{});
+        stage(std::integral_constant<int, 1>{});
+        stage(std::integral_constant<int, 2>{});
+        stage(std::integral_constant<int, 3>{});
+    }
+    if (st < n_st) stage(std::integral_constant<int, 0>{});
+    if (st + 1 < n_st) stage(std::integral_constant<int, 1>{});
+    if (st + 2 < n_st) stage(std::integral_constant<int, 2>{});
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));                    // no LDS write may be in flight when the tile ends
+}
+
+// f(i, j, q, n of the first of four neighbours, m) for each of a lane's groups of four results; n and m inside the tile
+template <class S, class F>
+__device__ __forceinline__ void each_four(F&& f) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / S::WC, wc = wave % S::WC;
+#pragma unroll
+    for (int j = 0; j < S::FC; ++j)
+#pragma unroll
+        for (int i = 0; i < S::FR; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                f(i, j, q, (wr * S::FR + i) * 32 + 8 * q + 4 * (lane >> 5), (wc * S::FC + j) * 32 + (lane & 31));
+}
+
+}  // namespace product
+}  // namespace onecomp

@@ -1,0 +1,111 @@
+// Sizes, pieces and workspaces of the calls from tokens to loss: plain host logic, apart from the launches so that a host program
+// can check it (tests/token_plan_check.cpp).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#if defined(__HIPCC__)
+#define ONECOMP_TOKEN_FN __host__ __device__ inline
+#else
+#define ONECOMP_TOKEN_FN inline
+#endif
+
+namespace onecomp {
+namespace product {
+
+// Workgroup -> tile.  Workgroup b runs on XCD b % 8; an XCD takes a run of ranks, which go through bands of BAND tiles of m
+// column by column of n, so that the tiles at work at a time share operands in its L2.
+constexpr int BAND = 8;
+ONECOMP_TOKEN_FN bool tile_of(unsigned block, int64_t m_tiles, int64_t n_tiles, int64_t& tm, int64_t& tn) {
+    const int64_t all = m_tiles * n_tiles, run = (all + 7) / 8, rank = int64_t(block & 7) * run + (block >> 3);
+    if (int64_t(block >> 3) >= run || rank >= all) return false;
+    const int64_t band = rank / (BAND * n_tiles), rest = rank - band * BAND * n_tiles;
+    const int64_t high = m_tiles - band * BAND < BAND ? m_tiles - band * BAND : BAND;
+    tn = rest / high;
+    tm = band * BAND + rest % high;
+    return true;
+}
+// workgroups that reach every tile
+ONECOMP_TOKEN_FN int64_t tile_blocks(int64_t m_tiles, int64_t n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
+
+}  // namespace product
+namespace token {
+
+inline int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t round_256(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// ---- embedding gradient ----
+// Vocabulary rows of a sorting workgroup: about one workgroup per compute unit, sixteen counters a row in LDS.
+constexpr int SORT_WAVES = 16, SORT_MOST = 1024;
+inline int sort_rows(int64_t vocab) {
+    const int64_t r = ceil_of(ceil_of(vocab, 256), 64) * 64;
+    return int(r > SORT_MOST ? SORT_MOST : r);
+}
+// Sorted tokens that a wave adds up.
+inline int segment_of(int64_t tokens) { return tokens < 16384 ? 16 : 64; }
+
+struct EmbeddingSpace {
+    size_t order, starts, parts, all;   // offsets, and the whole size
+    int64_t segments;
+};
+inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t width) {
+    EmbeddingSpace s;
+    s.segments = ceil_of(tokens, segment_of(tokens));
+    s.order = 0;
+    s.starts = s.order + round_256(size_t(tokens) * 4);
+    s.parts = s.starts + round_256((size_t(vocab) + 1) * 4);
+    s.all = s.parts + round_256(size_t(s.segments) * 2 * size_t(width) * 4);
+    return s;
+}
+
+// ---- loss ----
+// Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns.
+constexpr int64_t PIECE_BYTES = int64_t(512) << 20;
+inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
+    const int64_t rows = ceil_of(tokens < 1 ? 1 : tokens, 256) * 256, all = ceil_of(vocab, 256) * 256;
+    int64_t c = PIECE_BYTES / (rows * esz) / 256 * 256;
+    if (c < 2048) c = 2048;
+    if (c >= all) return all;
+    return ceil_of(ceil_of(all, ceil_of(all, c)), 256) * 256;   // pieces of about one size
+}
+// Shares of the inner sum of dh (over a piece's columns), where there are few tiles of it.
+inline int64_t dh_shares(int64_t tokens, int64_t width, int64_t columns) {
+    const int64_t tiles = ceil_of(tokens < 1 ? 1 : tokens, 128) * ceil_of(width, 128);
+    int64_t s = 512 / tiles;
+    if (s > columns / 512) s = columns / 512;
+    return s < 1 ? 1 : s > 16 ? 16 : s;
+}
+
+struct LossSpace {
+    size_t index, place, count, coef, rows, parts, hit, piece, dh, all;
+    int64_t columns, shares;
+};
+// n_parts: tiles of the vocabulary that leave a maximum and a sum per token
+inline LossSpace loss_space(int64_t tokens, int64_t width, int64_t vocab, int esz, int64_t n_parts, bool gradient) {
+    LossSpace s{};
+    const size_t t = size_t(tokens);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round_256(bytes);
+        return here;
+    };
+    s.count = take(4);
+    s.index = take(t * 4);
+    s.place = take(gradient ? t * 4 : 0);
+    s.coef = take(t * (gradient ? 16 : 4));
+    s.rows = take(t * size_t(width) * esz);
+    s.parts = take(gradient ? 0 : t * size_t(n_parts) * 8);
+    s.hit = take(gradient ? 0 : t * 4);
+    if (gradient) {
+        s.columns = piece_columns(tokens, vocab, esz);
+        s.shares = dh_shares(tokens, width, s.columns);
+        s.piece = take(t * size_t(s.columns) * esz);
+        s.dh = take(t * size_t(width) * 4 * size_t(s.shares));
+    }
+    s.all = at;
+    return s;
+}
+
+}  // namespace token
+}  // namespace onecomp

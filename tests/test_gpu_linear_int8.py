@@ -1,0 +1,139 @@
+"""Tokens quantized to 8 bits and their product with a quantized layer's codes, against the definition."""
+import pytest
+import torch
+
+import paper_2603_28845_amd as og
+from token_oracle import linear, quantize
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _gen(seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    return gen
+
+
+def _layer(gen, d_out, d_in):
+    return (torch.randint(0, 256, (d_out, d_in), generator=gen, device=DEV, dtype=torch.uint8),
+            torch.rand(d_out, 1, generator=gen, device=DEV) * 0.01 + 1e-3, torch.randint(0, 256, (d_out, 1), generator=gen, device=DEV).float())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,width", [(1, 16), (3, 4096), (70, 1360), (257, 2000), (2, 65520)])
+def test_codes(dtype, tokens, width):
+    gen = _gen(width)
+    x = (torch.randn(tokens, width, generator=gen, device=DEV) * torch.exp(torch.randn(tokens, 1, generator=gen, device=DEV) * 4)).to(dtype)
+    x[0, width // 2] = 0.0
+    if tokens > 2:
+        x[1] = 0
+    codes, scales, sums = og.onecomp_quantize_tokens(x)
+    want = quantize(x)
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1]) and torch.equal(sums, want[2])
+
+
+def test_ties_and_extremes():
+    """Halves go to even; the smallest and largest magnitudes, denormal ones among them."""
+    x = torch.zeros(6, 16, device=DEV)
+    x[0] = torch.arange(16, device=DEV) + 0.5
+    x[0, 15] = 127.0                                               # scale 1
+    x[1, :3] = torch.tensor([3e38, -1e38, 1e30], device=DEV)
+    x[2, :3] = torch.tensor([1e-45, -1e-45, 0.0], device=DEV)
+    x[3, :3] = torch.tensor([3e-43, -1e-43, 2e-43], device=DEV)
+    x[4] = -2.0
+    codes, scales, sums = og.onecomp_quantize_tokens(x)
+    want = quantize(x)
+    assert codes[0, :15].tolist() == [0, 2, 2, 4, 4, 6, 6, 8, 8, 10, 10, 12, 12, 14, 14]
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1]) and torch.equal(sums, want[2])
+    assert codes[4].tolist() == [-127] * 16 and float(scales[5]) == 0.0
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_tokens_that_are_not_finite_reach_their_own_results_alone(bad):
+    gen = _gen(2)
+    x = torch.randn(5, 64, generator=gen, device=DEV, dtype=F32)
+    x[3, 17] = bad
+    q, s, z = _layer(gen, 40, 64)
+    got = og.onecomp_quantize_tokens(x)
+    y = og.onecomp_linear_int8(*got, q, s, z, dtype=F32)
+    assert bool(got[1][3].isnan()) and not bool(got[0][3].any()) and int(got[2][3]) == 0
+    assert bool(y[3].isnan().all()) and not bool(y[[0, 1, 2, 4]].isnan().any())
+
+
+def test_codes_of_strided_rows():
+    gen = _gen(3)
+    room = torch.randn(40, 200, generator=gen, device=DEV).to(BF16)
+    x = room[:, 3:163]
+    got, want = og.onecomp_quantize_tokens(x), quantize(x.contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,d_out,d_in", [
+    (1, 1, 16), (1, 4096, 4096), (2, 33, 48), (8, 17, 1360), (16, 1000, 512), (17, 300, 4096), (31, 64, 65520), (32, 129, 144), (33, 500, 640), (64, 77, 208),
+    (65, 1024, 1024), (127, 128, 64), (128, 384, 96), (129, 257, 80), (300, 1000, 1360), (1999, 777, 2000), (2500, 4500, 336), (16500, 800, 64)])
+def test_product(dtype, tokens, d_out, d_in):
+    gen = _gen(tokens + d_out)
+    x = torch.randn(tokens, d_in, generator=gen, device=DEV)
+    q, s, z = _layer(gen, d_out, d_in)
+    codes = og.onecomp_quantize_tokens(x)
+    for bias in (None, torch.randn(d_out, generator=gen, device=DEV).to(dtype)):
+        y = og.onecomp_linear_int8(*codes, q, s, z, bias=bias, dtype=dtype)
+        want, off = linear(codes[0], codes[1], q, s, z, bias, dtype)
+        assert y.dtype == dtype and not bool(((y.double() - want).abs() > off).any())
+
+
+def test_largest_sums():
+    """All codes at their ends: sums reach 127 255 65520 = 2.12e9, below 2^31."""
+    tokens, d_out, d_in = 5, 40, 65520
+    codes = torch.full((tokens, d_in), 127, dtype=torch.int8, device=DEV)
+    codes[1] = -127
+    codes[2, ::2] = -127
+    sums = codes.sum(1, dtype=torch.int32)
+    ones = torch.ones(tokens, device=DEV)
+    q = torch.full((d_out, d_in), 255, dtype=torch.uint8, device=DEV)
+    q[1::2] = 0
+    z = torch.tensor([0.0, 255.0, 255.0, 0.0, 128.0], device=DEV).repeat(8)
+    s = torch.ones(d_out, device=DEV)
+    y = og.onecomp_linear_int8(codes, ones, sums, q, s, z, dtype=F32)
+    want = torch.mm(codes.double(), (q.double() - z.double()[:, None]).t().contiguous())
+    assert torch.equal(y, want.float())
+
+
+def test_results_only_where_they_belong():
+    gen = _gen(4)
+    q, s, z = _layer(gen, 45, 96)
+    codes = og.onecomp_quantize_tokens(torch.randn(37, 96, generator=gen, device=DEV))
+    room = torch.full((37, 60), 9.0, dtype=BF16, device=DEV)
+    og.onecomp_linear_int8(*codes, q, s, z, out=room[:, 7:52])
+    assert torch.equal(room[:, 7:52], og.onecomp_linear_int8(*codes, q, s, z)) and bool((room[:, :7] == 9).all()) and bool((room[:, 52:] == 9).all())
+
+
+@pytest.mark.parametrize("grid", ["minmax", "symmetric"])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_layer_as_the_sweep_leaves_it(grid, bits):
+    """Codes, scales and zero-points of onecomp_quantize_layer: the product is that of its W_hat with the tokens' codes."""
+    gen = _gen(6)
+    d_out, d_in = 96, 256
+    W = torch.randn(d_out, d_in, generator=gen, device=DEV) * 0.02
+    X = torch.randn(700, d_in, generator=gen, device=DEV)
+    H = torch.zeros(d_in, d_in, device=DEV)
+    og.onecomp_hessian_accumulate(X, H)
+    U, _, info = og.onecomp_hessian_factor(H, 0.01)
+    layer = og.onecomp_quantize_layer(W, U, bits, d_in, grid=grid)
+    assert int(info) == 0
+    codes, scales, sums = og.onecomp_quantize_tokens(X)
+    y = og.onecomp_linear_int8(codes, scales, sums, layer["Q_codes"], layer["scales"], layer["zeros"], dtype=F32)
+    want = torch.mm(codes.double() * scales.double()[:, None], layer["W_hat"].double().t().contiguous())
+    # W_hat's entries are rounded to 32 bits once more
+    size = torch.mm((codes.double() * scales.double()[:, None]).abs(), layer["W_hat"].double().abs().t().contiguous())
+    assert not bool(((y.double() - want).abs() > 6 * 2.0 ** -24 * size + 1e-40).any())
+
+
+def test_no_tokens():
+    empty = torch.empty(0, 64, device=DEV)
+    codes = og.onecomp_quantize_tokens(empty)
+    q, s, z = _layer(_gen(1), 8, 64)
+    assert codes[0].shape == (0, 64) and og.onecomp_linear_int8(*codes, q, s, z).shape == (0, 8)
