@@ -15,6 +15,7 @@ using product::ALONG;
 using product::Big;
 using product::Int8;
 using product::Mid;
+using product::Small;
 using product::Operand;
 
 // A workgroup per token.  The quotient is the rounded one of 32 bits (IEEE division), ties to even.  A token that holds an infinity
@@ -86,35 +87,72 @@ struct Args {
     int64_t y_stride, tokens, d_out;
 };
 
+// A column's scale, 128 less its zero-point, and bias, in LDS
+struct Columns {
+    float scale[256];
+    int zero[256];
+    float bias[256];
+};
 template <class T>
-__device__ __forceinline__ float bias_of(const void* bias, int64_t n) {
-    return bias ? block::load_one(static_cast<const T*>(bias) + n) : 0.f;
+__device__ __forceinline__ void load_columns(Columns& c, const Args& P, int64_t n0, int count) {
+    for (int n = threadIdx.x; n < count; n += blockDim.x) {
+        const int64_t at = n0 + n < P.d_out ? n0 + n : P.d_out - 1;
+        c.scale[n] = P.scales[at];
+        c.zero[n] = 128 - int(rintf(P.zeros[at]));
+        c.bias[n] = P.bias ? block::load_one(static_cast<const T*>(P.bias) + at) : 0.f;
+    }
 }
 // y from the sum of c (q - 128)
-__device__ __forceinline__ float value(int sum, int token_sum, float token_scale, float scale, float zero, float bias) {
-    const int all = sum + (128 - int(rintf(zero))) * token_sum;
-    return fmaf(float(all) * token_scale, scale, bias);
+__device__ __forceinline__ float value(int sum, int token_sum, float token_scale, float scale, int zero, float bias) {
+    return fmaf(float(sum + zero * token_sum) * token_scale, scale, bias);
 }
 
 template <class T, class S>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU) void linear_kernel(Args P) {
     extern __shared__ __align__(1024) char lds[];
-    int64_t tm, tn;
-    if (!product::tile_of(blockIdx.x, (P.tokens + S::TM - 1) / S::TM, (P.d_out + S::TN - 1) / S::TN, tm, tn)) return;
-    const int64_t n0 = tn * S::TN, m0 = tm * S::TM;
+    int tm, tn;
+    if (!product::my_tile(int((P.tokens + S::TM - 1) / S::TM), int((P.d_out + S::TN - 1) / S::TN), tm, tn)) return;
+    const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     product::int16v acc[S::FR][S::FC];
     product::multiply<Int8, ALONG, ALONG, S>(lds, P.q, P.codes, n0, m0, P.inner, acc);
-    product::each_four<S>([&](int i, int j, int q, int n, int m) __attribute__((always_inline)) {
-        if (m0 + m >= P.tokens) return;
-        const float ts = P.token_scales[m0 + m];
-        const int sum = P.token_sums[m0 + m];
-        T* to = static_cast<T*>(P.y) + (m0 + m) * P.y_stride + n0 + n;
+    __syncthreads();
+    static_assert(product::out_lds<T, S>() + sizeof(Columns) <= S::LDS, "room for the columns' numbers");
+    Columns& c = *reinterpret_cast<Columns*>(lds + product::out_lds<T, S>());
+    load_columns<T>(c, P, n0, S::TN);
+    const int lane = threadIdx.x & 63, wc = int(threadIdx.x >> 6) % S::WC;
+    float token_scale[S::FC];
+    int token_sum[S::FC];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t at = n0 + n + e;
-            if (at < P.d_out) block::store_one(to + e, value(acc[i][j][4 * q + e], sum, ts, P.scales[at], P.zeros[at], bias_of<T>(P.bias, at)));
-        }
-    });
+    for (int j = 0; j < S::FC; ++j) {
+        const int64_t m = m0 + (wc * S::FC + j) * 32 + (lane & 31), at = m < P.tokens ? m : P.tokens - 1;
+        token_scale[j] = P.token_scales[at];
+        token_sum[j] = P.token_sums[at];
+    }
+    __syncthreads();
+    product::store_tile<T, S, false>(
+        lds,
+        [&](float (&x)[4], int i, int j, int q, int n, int) __attribute__((always_inline)) {
+            const float4v s = *reinterpret_cast<const float4v*>(c.scale + n), b = *reinterpret_cast<const float4v*>(c.bias + n);
+            const product::int4v z = *reinterpret_cast<const product::int4v*>(c.zero + n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = value(acc[i][j][4 * q + e], token_sum[j], token_scale[j], s[e], z[e], b[e]);
+        },
+        [&](int m) __attribute__((always_inline)) { return m0 + m < P.tokens ? static_cast<T*>(P.y) + (m0 + m) * P.y_stride + n0 : nullptr; }, P.d_out - n0);
+}
+
+template <class T, int RF, int TF>
+__global__ __launch_bounds__(64 * product::FEW_WAVES) void few_tokens_kernel(Args P) {
+    __shared__ __align__(16) char lds[product::few_lds<RF, TF>()];
+    __shared__ Columns c;
+    const int64_t n0 = int64_t(blockIdx.x) * 16 * RF;
+    load_columns<T>(c, P, n0, 16 * RF);
+    product::multiply_few<Int8, RF, TF>(lds, P.q, P.codes, n0, P.inner);
+    for (int e = threadIdx.x; e < 256 * RF * TF; e += 64 * product::FEW_WAVES) {
+        const int n = e % (16 * RF), m = e / (16 * RF);
+        if (n0 + n < P.d_out && m < P.tokens)
+            block::store_one(static_cast<T*>(P.y) + m * P.y_stride + n0 + n,
+                             value(reinterpret_cast<const int*>(lds)[e], P.token_sums[m], P.token_scales[m], c.scale[n], c.zero[n], c.bias[n]));
+    }
 }
 
 template <class T, class S>
@@ -126,10 +164,22 @@ onecomp_status run(const Args& P, hipStream_t stream) {
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }
+template <class T, int RF, int TF>
+onecomp_status run_few(const Args& P, hipStream_t stream) {
+    few_tokens_kernel<T, RF, TF><<<dim3(unsigned(ceil_div(P.d_out, 16 * RF))), dim3(64 * product::FEW_WAVES), 0, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
+}
 template <class T>
 onecomp_status dispatch(const Args& P, hipStream_t stream) {
-    const bool big = P.tokens > 128 && ceil_div(P.tokens, 256) * ceil_div(P.d_out, 256) >= 192;
-    return big ? run<T, Big>(P, stream) : run<T, Mid>(P, stream);
+    if (P.tokens <= FEW) {
+        const bool wide = P.d_out > 8192;
+        if (P.tokens <= 16) return wide ? run_few<T, 2, 1>(P, stream) : run_few<T, 1, 1>(P, stream);
+        if (P.tokens <= 32) return wide ? run_few<T, 2, 2>(P, stream) : run_few<T, 1, 2>(P, stream);
+        return wide ? run_few<T, 2, 4>(P, stream) : run_few<T, 1, 4>(P, stream);
+    }
+    const int size = tile_size(P.tokens, P.d_out);
+    return size == 256 ? run<T, Big>(P, stream) : size == 128 ? run<T, Mid>(P, stream) : run<T, Small>(P, stream);
 }
 
 }  // namespace

@@ -18,6 +18,7 @@ using product::ACROSS;
 using product::ALONG;
 using product::Big;
 using product::Mid;
+using product::Small;
 using product::Operand;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -42,11 +43,12 @@ struct Gather {
 };
 
 // A workgroup takes 64 tokens: it counts the kept ones in front of its own (reading all targets before them: 256 KB from the
-// L2 for the last of 65536 tokens), numbers its own and copies their rows.
+// L2 for the last of 65536 tokens), numbers its own and copies a part of the columns of their rows.
 __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
     __shared__ int s_before[4], s_index[64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * 64;
     int n = 0;
+#pragma unroll 4
     for (int t = threadIdx.x; t < first; t += 256) n += uint32_t(g.targets[t]) < uint32_t(g.vocab);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
@@ -57,10 +59,10 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
     const bool kept = uint32_t(target) < uint32_t(g.vocab);
     const unsigned long long mask = __ballot(kept);
     const int many = __popcll(mask), rank = __popcll(mask & ((1ull << lane) - 1));
-    if (wave == 0) {
+    if (wave == 0 && kept) s_index[rank] = t;
+    if (wave == 0 && blockIdx.y == 0) {
         if (kept) {
             const int at = before + rank;
-            s_index[rank] = t;
             g.index[at] = t;
             if (g.coef) {
                 const float dl = g.d_loss[t], dz = g.d_lse ? g.d_lse[t] : 0.f;
@@ -76,15 +78,30 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
         if (lane == 0 && first + 64 >= g.tokens) *g.count = before + many;
     }
     __syncthreads();
-    const int chunks = int(g.width_bytes >> 4);
-    for (int r = wave; r < many; r += 4) {
-        const uint4v* from = reinterpret_cast<const uint4v*>(g.h + int64_t(s_index[r]) * g.h_stride);
-        uint4v* to = reinterpret_cast<uint4v*>(g.rows + int64_t(before + r) * g.width_bytes);
-        for (int c = lane; c < chunks; c += 64) to[c] = from[c];
+    // 1 KB of a row at a time, eight on their way
+    const int chunks = int(g.width_bytes >> 4), blocks = (chunks + 63) / 64, all = many * blocks;
+    const uint4v* const from = reinterpret_cast<const uint4v*>(g.h);
+    for (int i0 = (blockIdx.y * 4 + wave) * 8; i0 < all; i0 += gridDim.y * 32) {
+        uint4v v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int r = (i0 + u) / blocks, c = (i0 + u) % blocks * 64 + lane;
+            if (i0 + u < all && c < chunks) v[u] = from[int64_t(s_index[r]) * (g.h_stride >> 4) + c];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int r = (i0 + u) / blocks, c = (i0 + u) % blocks * 64 + lane;
+            if (i0 + u < all && c < chunks) reinterpret_cast<uint4v*>(g.rows + int64_t(before + r) * g.width_bytes)[c] = v[u];
+        }
     }
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void join_two(float2& x, float2 y) {
+    const float top = fmaxf(x.x, y.x), from = top == -__builtin_inff() ? 0.f : top;
+    x = make_float2(top, x.y * __builtin_amdgcn_exp2f(x.x - from) + y.y * __builtin_amdgcn_exp2f(y.x - from));
+}
+
 struct Logits {
     Operand weight, rows;                    // rows.rows: all tokens' room; what counts is *count
     const int32_t* count;
@@ -92,19 +109,18 @@ struct Logits {
     int64_t inner;
     int vocab;
     float c;                                 // scale log2(e)
-    float2* parts;                           // [tile of the vocabulary][token]: maximum (in powers of two) and sum
+    float2* parts;                           // [token][part of the vocabulary]: maximum (in powers of two) and sum
     float* hit;
-    int64_t tokens;                          // row length of parts
+    int64_t tokens, n_parts;
 };
 
 template <class E, class S>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logits_kernel(Logits P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
-    int64_t tm, tn;
-    const int64_t n_tiles = (P.vocab + S::TN - 1) / S::TN;
-    if (!product::tile_of(blockIdx.x, (count + S::TM - 1) / S::TM, n_tiles, tm, tn)) return;
-    const int64_t n0 = tn * S::TN, m0 = tm * S::TM;
+    int tm, tn;
+    if (!product::my_tile((count + S::TM - 1) / S::TM, (P.vocab + S::TN - 1) / S::TN, tm, tn)) return;
+    const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
     product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc);
@@ -157,12 +173,33 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logits_kernel(Logits P)
         if (m0 + col >= count) continue;
         float2 x = red[col];
 #pragma unroll
-        for (int w = 1; w < S::WR; ++w) {
-            const float2 y = red[w * S::TM + col];
-            const float top = fmaxf(x.x, y.x), from = top == -__builtin_inff() ? 0.f : top;
-            x = make_float2(top, x.y * __builtin_amdgcn_exp2f(x.x - from) + y.y * __builtin_amdgcn_exp2f(y.x - from));
-        }
-        P.parts[tn * P.tokens + m0 + col] = x;
+        for (int w = 1; w < S::WR; ++w) join_two(x, red[w * S::TM + col]);
+        P.parts[(m0 + col) * P.n_parts + tn] = x;
+    }
+}
+
+// Few tokens: 32 entries of the vocabulary per workgroup, a half wave per token.
+template <class E, int TF>
+__global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Logits P) {
+    __shared__ __align__(16) char lds[product::few_lds<2, TF>()];
+    const int count = *P.count;
+    const int64_t n0 = int64_t(blockIdx.x) * 32;
+    if (count == 0) return;
+    P.rows.rows = count;
+    product::multiply_few<E, 2, TF>(lds, P.weight, P.rows, n0, P.inner);
+    const int n = threadIdx.x & 31;
+    for (int m = threadIdx.x >> 5; m < count; m += 2 * product::FEW_WAVES) {
+        const float x = n0 + n < P.vocab ? reinterpret_cast<const float*>(lds)[m * 32 + n] : -__builtin_inff();
+        float top = x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+        top *= P.c;
+        const float from = top == -__builtin_inff() ? 0.f : top;
+        float sum = __builtin_amdgcn_exp2f(fmaf(x, P.c, -from));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (n == 0) P.parts[m * P.n_parts + blockIdx.x] = make_float2(top, sum);
+        if (P.target[m] == n0 + n) P.hit[m] = x * P.c;
     }
 }
 
@@ -170,31 +207,30 @@ struct Join {
     const int32_t *count, *index;
     const float2* parts;
     const float* hit;
-    int64_t tokens;
     int n_parts;
     float *loss, *lse;
 };
-__device__ __forceinline__ void join_two(float2& x, float2 y) {
-    const float top = fmaxf(x.x, y.x), from = top == -__builtin_inff() ? 0.f : top;
-    x = make_float2(top, x.y * __builtin_amdgcn_exp2f(x.x - from) + y.y * __builtin_amdgcn_exp2f(y.x - from));
-}
-// 64 tokens per workgroup, a lane each; sixteen waves take a sixteenth of the parts each, one after the other
-__global__ __launch_bounds__(1024) void join_kernel(Join P) {
-    __shared__ float2 red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = *P.count;
-    const int m = blockIdx.x * 64 + lane;
-    if (int(blockIdx.x) * 64 >= count) return;
-    const int each = (P.n_parts + 15) / 16, begin = wave * each, end = min(P.n_parts, begin + each);
+// LANES threads per token: each takes every LANES-th part, then they join in a tree.
+template <int LANES>
+__global__ __launch_bounds__(256) void join_kernel(Join P) {
+    __shared__ float2 red[4];
+    const int m = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, l = threadIdx.x % LANES;
     float2 x = make_float2(-__builtin_inff(), 0.f);
-    if (m < count) {
+    const bool there = m < *P.count;
+    if (there) {
+        const float2* const from = P.parts + int64_t(m) * P.n_parts;
 #pragma unroll 4
-        for (int i = begin; i < end; ++i) join_two(x, P.parts[int64_t(i) * P.tokens + m]);
+        for (int i = l; i < P.n_parts; i += LANES) join_two(x, from[i]);
     }
-    red[wave][lane] = x;
-    __syncthreads();
-    if (wave != 0 || m >= count) return;
 #pragma unroll
-    for (int w = 1; w < 16; ++w) join_two(x, red[w][lane]);
+    for (int o = 32; o > 0; o >>= 1) join_two(x, make_float2(__shfl_xor(x.x, o, 64), __shfl_xor(x.y, o, 64)));
+    if constexpr (LANES == 256) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = red[0];
+        for (int w = 1; w < 4; ++w) join_two(x, red[w]);
+    }
+    if (!there || l != 0) return;
     const float lse2 = x.x + __builtin_amdgcn_logf(x.y);           // of two
     const int t = P.index[m];
     if (P.loss) P.loss[t] = (lse2 - P.hit[m]) * LN2;
@@ -231,9 +267,9 @@ template <class E, class S>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logit_grads_kernel(LogitGrads P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
-    int64_t tm, tn;
-    if (!product::tile_of(blockIdx.x, (count + S::TM - 1) / S::TM, (P.columns + S::TN - 1) / S::TN, tm, tn)) return;
-    const int64_t n0 = tn * S::TN, m0 = tm * S::TM;
+    int tm, tn;
+    if (!product::my_tile((count + S::TM - 1) / S::TM, (P.columns + S::TN - 1) / S::TN, tm, tn)) return;
+    const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
     product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc);
@@ -244,24 +280,29 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logit_grads_kernel(Logi
         const int64_t m = m0 + (wc * S::FC + j) * 32 + (lane & 31);
         coef[j] = m < count ? P.coef[m] : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    product::each_four<S>([&](int i, int j, int q, int n, int m) __attribute__((always_inline)) {
-        const float4 k = coef[j];
-        const int at = int(n0) + n, target = __float_as_int(k.w) - P.first - at;
-        float x[4];
+    __syncthreads();
+    product::store_tile<typename E::T, S, false>(
+        lds,
+        [&](float (&x)[4], int i, int j, int q, int n, int) __attribute__((always_inline)) {
+            const float4 k = coef[j];
+            const int at = int(n0) + n, target = __float_as_int(k.w) - P.first - at;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] = k.x * __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], P.c, -k.z)) - (target == e ? k.y : 0.f);
-            if (at + e >= P.columns) x[e] = 0.f;                   // behind the vocabulary: nothing, for the product with the weight
-        }
-        if (m0 + m < count) store_four(reinterpret_cast<typename E::T*>(P.piece + (m0 + m) * P.stride) + at, x);
-    });
+            for (int e = 0; e < 4; ++e) {
+                x[e] = k.x * __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * q + e], P.c, -k.z)) - (target == e ? k.y : 0.f);
+                if (at + e >= P.columns) x[e] = 0.f;               // behind the vocabulary: nothing, for the product with the weight
+            }
+        },
+        [&](int m) __attribute__((always_inline)) {
+            return m0 + m < count ? reinterpret_cast<typename E::T*>(P.piece + (m0 + m) * P.stride) + n0 : nullptr;
+        },
+        S::TN);
 }
 
 struct GradRows {
     Operand weight, piece;                   // ACROSS, ALONG
     const int32_t* count;
-    int64_t columns, share;                  // of the piece; of a share of them
-    int shares, add;
+    int columns, full;                       // of this piece; of the largest
+    int most, add;                           // shares that there is room for; whether there is something to add to
     float* out;                              // [share][token][width]
     int64_t tokens;
     int width;
@@ -270,26 +311,27 @@ template <class E, class S>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU) void grad_rows_kernel(GradRows P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
-    int64_t tm, tn;
-    const int share = blockIdx.y;
-    if (!product::tile_of(blockIdx.x, (count + S::TM - 1) / S::TM, (P.width + S::TN - 1) / S::TN, tm, tn)) return;
-    const int64_t n0 = tn * S::TN, m0 = tm * S::TM, begin = share * P.share;
-    const int64_t inner = P.columns - begin < P.share ? P.columns - begin : P.share;
-    P.weight.data += begin * P.weight.stride;
-    P.piece.data += begin * E::ESZ;
+    int tm, tn;
+    const int m_tiles = (count + S::TM - 1) / S::TM, n_tiles = (P.width + S::TN - 1) / S::TN;
+    const int shares = __builtin_amdgcn_readfirstlane(shares_of(m_tiles * n_tiles, P.full, 256 * S::PER_CU, P.most)), share = blockIdx.y;
+    if (share >= shares || !product::my_tile(m_tiles, n_tiles, tm, tn)) return;
+    const int each = __builtin_amdgcn_readfirstlane((int(unsigned(P.columns + shares - 1) / unsigned(shares)) + 63) & ~63), begin = share * each;
+    const int inner = P.columns - begin < each ? P.columns - begin : each;
+    const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
+    P.weight.data += int64_t(begin) * P.weight.stride;
+    P.piece.data += int64_t(begin) * E::ESZ;
     P.piece.rows = count;
     float16v acc[S::FR][S::FC];
     product::multiply<E, ACROSS, ALONG, S>(lds, P.weight, P.piece, n0, m0, inner < 0 ? 0 : inner, acc);
+    __syncthreads();
     float* const out = P.out + share * P.tokens * P.width;
-    product::each_four<S>([&](int i, int j, int q, int n, int m) __attribute__((always_inline)) {
-        if (m0 + m >= count || n0 + n >= P.width) return;
-        float4v* to = reinterpret_cast<float4v*>(out + (m0 + m) * P.width + n0 + n);
-        float4v x;
+    auto value = [&](float (&x)[4], int i, int j, int q, int, int) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e];
-        if (P.add) x += *to;
-        *to = x;
-    });
+    };
+    auto row = [&](int m) __attribute__((always_inline)) { return m0 + m < count ? out + (m0 + m) * P.width + n0 : nullptr; };
+    if (P.add) product::store_tile<float, S, true>(lds, value, row, P.width - n0);
+    else product::store_tile<float, S, false>(lds, value, row, P.width - n0);
 }
 
 struct GradWeight {
@@ -303,38 +345,48 @@ struct GradWeight {
 template <class E, class S>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU) void grad_weight_kernel(GradWeight P) {
     extern __shared__ __align__(1024) char lds[];
-    int64_t tm, tn;
-    if (!product::tile_of(blockIdx.x, (P.columns + S::TM - 1) / S::TM, (P.width + S::TN - 1) / S::TN, tm, tn)) return;
-    const int64_t n0 = tn * S::TN, m0 = tm * S::TM;
+    int tm, tn;
+    if (!product::my_tile((P.columns + S::TM - 1) / S::TM, (P.width + S::TN - 1) / S::TN, tm, tn)) return;
+    const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     float16v acc[S::FR][S::FC];
     product::multiply<E, ACROSS, ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc);
-    product::each_four<S>([&](int i, int j, int q, int n, int m) __attribute__((always_inline)) {
-        if (m0 + m >= P.columns || n0 + n >= P.width) return;
-        float x[4];
+    __syncthreads();
+    product::store_tile<typename E::T, S, false>(
+        lds,
+        [&](float (&x)[4], int i, int j, int q, int, int) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e] * P.scale;
-        store_four(reinterpret_cast<typename E::T*>(P.out + (m0 + m) * P.stride) + n0 + n, x);
-    });
+            for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e] * P.scale;
+        },
+        [&](int m) __attribute__((always_inline)) {
+            return m0 + m < P.columns ? reinterpret_cast<typename E::T*>(P.out + (m0 + m) * P.stride) + n0 : nullptr;
+        },
+        P.width - n0);
 }
 
+struct Finish {
+    const float* parts;
+    const int32_t *place, *count;
+    int64_t tokens;
+    int full, width, tile, slots, most;            // as grad_rows_kernel had them
+    float scale;
+    Rows dh;
+};
 // dh of every token from the shares' sums: a wave per token, zeros where it was left out
 template <class T>
-__global__ __launch_bounds__(256) void finish_rows_kernel(const float* parts, const int32_t* place, int64_t tokens, int width, int shares, float scale, Rows dh) {
+__global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
     const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (t >= tokens) return;
-    const int at = place[t];
-    T* to = static_cast<T*>(dh.p) + t * dh.stride;
-    for (int c = (threadIdx.x & 63) * 4; c < width; c += 256) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t >= P.tokens) return;
+    const int at = P.place[t];
+    const int tiles = (*P.count + P.tile - 1) / P.tile * ((P.width + P.tile - 1) / P.tile);
+    const int shares = shares_of(tiles, P.full, P.slots, P.most);
+    T* to = static_cast<T*>(P.dh.p) + t * P.dh.stride;
+#pragma unroll 2
+    for (int c = (threadIdx.x & 63) * 4; c < P.width; c += 256) {
+        float4v x = {0.f, 0.f, 0.f, 0.f};
         if (at >= 0)
-            for (int s = 0; s < shares; ++s) {
-                const float4v v = *reinterpret_cast<const float4v*>(parts + (s * tokens + at) * width + c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] += v[e];
-            }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] *= scale;
-        store_four(to + c, x);
+            for (int s = 0; s < shares; ++s) x += *reinterpret_cast<const float4v*>(P.parts + (s * P.tokens + at) * P.width + c);
+        const float y[4] = {x[0] * P.scale, x[1] * P.scale, x[2] * P.scale, x[3] * P.scale};
+        store_four(to + c, y);
     }
 }
 
@@ -348,8 +400,12 @@ onecomp_status launch(K kernel, int lds, int threads, int64_t blocks, int64_t sh
     return ONECOMP_OK;
 }
 
-// 256 x 256 tiles where they are many enough
-bool big_tiles(int64_t m, int64_t n) { return m > 128 && ceil_div(m, 256) * ceil_div(n, 256) >= 192; }
+// f(shape) for the tiles that a product of m x n results takes
+template <class F>
+onecomp_status with_tiles(int64_t m, int64_t n, F&& f) {
+    const int size = tile_size(m, n);
+    return size == 256 ? f(Big{}) : size == 128 ? f(Mid{}) : f(Small{});
+}
 
 template <class E, class S>
 onecomp_status run_logits(const Logits& P, hipStream_t stream) {
@@ -364,7 +420,7 @@ onecomp_status run_logit_grads(const LogitGrads& P, int64_t tokens, hipStream_t 
 template <class E, class S>
 onecomp_status run_grad_rows(const GradRows& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(grad_rows_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.width, S::TN)), P.shares, P, done, stream);
+    return launch(grad_rows_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.width, S::TN)), P.most, P, done, stream);
 }
 template <class E, class S>
 onecomp_status run_grad_weight(const GradWeight& P, hipStream_t stream) {
@@ -372,7 +428,17 @@ onecomp_status run_grad_weight(const GradWeight& P, hipStream_t stream) {
     return launch(grad_weight_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.columns, S::TM), ceil_div(P.width, S::TN)), 1, P, done, stream);
 }
 
-int64_t vocabulary_tiles(int64_t tokens, int64_t vocab) { return ceil_div(vocab, big_tiles(tokens, vocab) ? Big::TN : Mid::TN); }
+template <class E>
+onecomp_status run_few_logits(const Logits& P, hipStream_t stream) {
+    const dim3 grid(unsigned(P.n_parts)), threads(64 * product::FEW_WAVES);
+    if (P.tokens <= 16) few_logits_kernel<E, 1><<<grid, threads, 0, stream>>>(P);
+    else if (P.tokens <= 32) few_logits_kernel<E, 2><<<grid, threads, 0, stream>>>(P);
+    else few_logits_kernel<E, 4><<<grid, threads, 0, stream>>>(P);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
+}
+
+int64_t n_parts(int64_t tokens, int64_t vocab) { return ceil_div(vocab, part_columns(tokens, vocab)); }
 
 onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient, hipStream_t stream) {
     char* ws = static_cast<char*>(P.workspace);
@@ -397,14 +463,18 @@ onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient,
         g.loss = P.loss;
         g.lse_out = P.lse;
     }
-    gather_kernel<<<dim3(unsigned(P.tokens ? ceil_div(P.tokens, 64) : 1)), dim3(256), 0, stream>>>(g);
+    // about two workgroups per compute unit, as long as there are 8 KB of rows for each
+    const int64_t groups = P.tokens ? ceil_div(P.tokens, 64) : 1, bytes = (P.tokens < 64 ? P.tokens : 64) * g.width_bytes;
+    int64_t parts = ceil_div(512, groups);
+    if (parts > bytes >> 13) parts = bytes >> 13;
+    gather_kernel<<<dim3(unsigned(groups), unsigned(parts < 1 ? 1 : parts)), dim3(256), 0, stream>>>(g);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }
 
 template <class E>
 onecomp_status forward(const Loss& P, hipStream_t stream) {
-    const LossSpace s = loss_space(P.tokens, P.width, P.vocab, E::ESZ, vocabulary_tiles(P.tokens, P.vocab), false);
+    const LossSpace s = loss_space(P.tokens, P.width, P.vocab, E::ESZ, n_parts(P.tokens, P.vocab), false);
     char* ws = static_cast<char*>(P.workspace);
     if (const onecomp_status st = gather(P, s, E::ESZ, false, stream)) return st;
     Logits L{};
@@ -418,10 +488,13 @@ onecomp_status forward(const Loss& P, hipStream_t stream) {
     L.parts = reinterpret_cast<float2*>(ws + s.parts);
     L.hit = reinterpret_cast<float*>(ws + s.hit);
     L.tokens = P.tokens;
-    const bool big = big_tiles(P.tokens, P.vocab);
-    if (const onecomp_status st = big ? run_logits<E, Big>(L, stream) : run_logits<E, Mid>(L, stream)) return st;
-    const Join J{L.count, reinterpret_cast<const int32_t*>(ws + s.index), L.parts, L.hit, P.tokens, int(vocabulary_tiles(P.tokens, P.vocab)), P.loss, P.lse};
-    join_kernel<<<dim3(unsigned(ceil_div(P.tokens, 64))), dim3(1024), 0, stream>>>(J);
+    L.n_parts = n_parts(P.tokens, P.vocab);
+    const onecomp_status st = P.tokens <= FEW ? run_few_logits<E>(L, stream)
+                                              : with_tiles(P.tokens, P.vocab, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); });
+    if (st) return st;
+    const Join J{L.count, reinterpret_cast<const int32_t*>(ws + s.index), L.parts, L.hit, int(L.n_parts), P.loss, P.lse};
+    if (P.tokens <= 1024) join_kernel<256><<<dim3(unsigned(P.tokens)), dim3(256), 0, stream>>>(J);
+    else join_kernel<64><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(J);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }
@@ -448,21 +521,22 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
         G.c = P.scale * LOG2E;
         G.piece = ws + s.piece;
         G.stride = pitch;
-        if (const onecomp_status st = big_tiles(P.tokens, columns) ? run_logit_grads<E, Big>(G, P.tokens, stream) : run_logit_grads<E, Mid>(G, P.tokens, stream))
+        if (const onecomp_status st =
+                with_tiles(P.tokens, columns, [&](auto shape) { return run_logit_grads<E, decltype(shape)>(G, P.tokens, stream); }))
             return st;
         if (P.dh.p) {
             GradRows R{};
             R.weight = Operand{w, P.weight.stride * E::ESZ, P.width};
             R.piece = Operand{ws + s.piece, pitch, P.tokens};
             R.count = count;
-            R.columns = columns;
-            R.shares = int(s.shares);
-            R.share = ceil_div(ceil_div(columns, s.shares), 64) * 64;
+            R.columns = int(columns);
+            R.full = int(s.columns);
+            R.most = int(s.shares);
             R.add = first > 0;
             R.out = reinterpret_cast<float*>(ws + s.dh);
             R.tokens = P.tokens;
             R.width = int(P.width);
-            if (const onecomp_status st = big_tiles(P.tokens, P.width) ? run_grad_rows<E, Big>(R, stream) : run_grad_rows<E, Mid>(R, stream)) return st;
+            if (const onecomp_status st = with_tiles(P.tokens, P.width, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); })) return st;
         }
         if (P.dweight.p) {
             GradWeight W{};
@@ -474,12 +548,14 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             W.scale = P.scale;
             W.out = static_cast<char*>(P.dweight.p) + first * P.dweight.stride * E::ESZ;
             W.stride = P.dweight.stride * E::ESZ;
-            if (const onecomp_status st = big_tiles(columns, P.width) ? run_grad_weight<E, Big>(W, stream) : run_grad_weight<E, Mid>(W, stream)) return st;
+            if (const onecomp_status st = with_tiles(columns, P.width, [&](auto shape) { return run_grad_weight<E, decltype(shape)>(W, stream); })) return st;
         }
     }
     if (P.dh.p && P.tokens) {
-        finish_rows_kernel<typename E::T><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(
-            reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), P.tokens, int(P.width), int(s.shares), P.scale, P.dh);
+        const int tile = tile_size(P.tokens, P.width);
+        const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(s.columns), int(P.width), tile,
+                       256 * (tile == 256 ? Big::PER_CU : tile == 128 ? Mid::PER_CU : Small::PER_CU), int(s.shares), P.scale, P.dh};
+        finish_rows_kernel<typename E::T><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(F);
         ONECOMP_CHECK_LAUNCH();
     }
     return ONECOMP_OK;
@@ -488,7 +564,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
 }  // namespace
 
 size_t loss_workspace_bytes(onecomp_dtype dtype, int64_t tokens, int64_t width, int64_t vocab, bool gradient) {
-    return loss_space(tokens, width, vocab, dtype == ONECOMP_BF16 ? 2 : 4, gradient ? 0 : vocabulary_tiles(tokens, vocab), gradient).all;
+    return loss_space(tokens, width, vocab, dtype == ONECOMP_BF16 ? 2 : 4, gradient ? 0 : n_parts(tokens, vocab), gradient).all;
 }
 onecomp_status loss_forward_run(onecomp_dtype dtype, const Loss& P, hipStream_t stream) {
     return dtype == ONECOMP_BF16 ? forward<product::Bf16>(P, stream) : forward<product::F32>(P, stream);

@@ -12,8 +12,8 @@
 // the matrix instructions.
 //   ALONG   a row's 64 bytes are four chunks of 16; chunk c of row r lies at c ^ ((r >> 1) & 3), so that eight rows' same chunk fall
 //           into different banks.
-//   ACROSS  rows of k as they are; in bf16 chunk c of row r lies at c ^ ((r & 3) << 2) and fragments are transposed reads (four
-//           rows of a read in four groups of banks); in fp32 a fragment is four plain reads.
+//   ACROSS  rows of k as they are; in bf16 their chunks lie permuted by fours (Side::swizzle) and fragments are transposed
+//           reads; in fp32 a fragment is four plain reads.
 // What lies behind the operands' ends becomes zeros by the loads' bounds check.
 #pragma once
 #include "common.hpp"
@@ -25,6 +25,7 @@ namespace product {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int16v __attribute__((ext_vector_type(16)));
+typedef uint4v uint4u __attribute__((aligned(2)));               // at any address of 16-bit elements
 
 struct Bf16 {
     typedef uint16_t T;
@@ -77,6 +78,7 @@ struct Shape {
 };
 typedef Shape<2, 2, 4, 4, 1> Big;      // 256 x 256
 typedef Shape<2, 2, 2, 2, 2> Mid;      // 128 x 128
+typedef Shape<2, 2, 1, 1, 4> Small;    // 64 x 64
 
 constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
 
@@ -86,6 +88,10 @@ struct Side {
     static constexpr int LOADS = T / 16 / WAVES;                  // of 1 KB, per wave and step
     static_assert(T % (16 * WAVES) == 0, "whole loads per wave");
     static constexpr int ROWB = T * E::ESZ, CHUNKS = ROWB / 16;   // ACROSS: a row of k
+    // ACROSS, bf16: which group of four chunks goes where in row r of k; the same for r + 4.  Four rows of a read lie 64 bytes
+    // apart in the banks (rows of 128 bytes: two and two).
+    static __device__ __forceinline__ int swizzle(int r) { return CHUNKS >= 16 ? r & 3 : (r >> 1) & 1; }
+    static_assert(L == ALONG || E::ESZ != 2 || CHUNKS == 8 || CHUNKS % 16 == 0, "the swizzle stays inside a row");
     uint32_t off[LOADS], chunk;
     const char* p;
     int64_t left, step;                                           // bytes: what is left of the operand (ALONG: of a row), one step
@@ -111,7 +117,7 @@ struct Side {
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
                 const int at = (wave * LOADS + q) * 64 + lane, r = at / CHUNKS;
-                const int c = (at % CHUNKS) ^ (E::ESZ == 2 ? (r & 3) << 2 : 0);
+                const int c = (at % CHUNKS) ^ (E::ESZ == 2 ? swizzle(r) << 2 : 0);
                 off[q] = first + c * (16 / E::ESZ) < o.rows ? uint32_t(r) * uint32_t(o.stride) + uint32_t(c) * 16u : NOWHERE;
             }
             if constexpr (E::ESZ == 2) {
@@ -146,7 +152,7 @@ struct Side {
         if constexpr (L == ALONG) {
             return *reinterpret_cast<const uint4v*>(tile + f * 2048 + (read0 ^ (s << 5)));
         } else if constexpr (E::ESZ == 2) {
-            const char* a = tile + s * 16 * ROWB + read0 + ((f ^ ((lane & 15) >> 2)) << 6);
+            const char* a = tile + s * 16 * ROWB + read0 + ((f ^ swizzle((lane & 15) >> 2)) << 6);
             const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a));
             const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 4 * ROWB));
             return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -273,17 +279,171 @@ __device__ __forceinline__ void multiply(char* lds, const Operand& A, const Oper
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));                    // no LDS write may be in flight when the tile ends
 }
 
-// f(i, j, q, n of the first of four neighbours, m) for each of a lane's groups of four results; n and m inside the tile
-template <class S, class F>
-__device__ __forceinline__ void each_four(F&& f) {
+// tile_of for a workgroup of this launch, in scalar registers
+__device__ __forceinline__ bool my_tile(int m_tiles, int n_tiles, int& tm, int& tn) {
+    if (!tile_of(blockIdx.x, m_tiles, n_tiles, tm, tn)) return false;
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    return true;
+}
+
+// The tile's results to memory through LDS, in whole lines: a wave's 32 FR of n for 32 of m at a time.  Straight from the
+// accumulators a store would touch 32 rows with 8 or 16 bytes each.
+//   value(x, i, j, q, n, m)   four neighbours of n from acc[i][j][4 q ..]; n and m inside the tile
+//   row(m)                    address of n = 0 of the tile in row m of the tile, or nullptr: no such row
+//   left                      how many n there are from the tile's first on
+// ADD: added to what is there (fp32).  lds: the tile's, behind a barrier; OUT_LDS bytes of it are used.
+template <class T, class S>
+constexpr int out_lds() { return S::WAVES * 32 * (32 * S::FR * int(sizeof(T)) + 16); }
+
+template <class T, class S, bool ADD, class V, class R>
+__device__ __forceinline__ void store_tile(char* lds, V&& value, R&& row, int64_t left) {
+    constexpr int NW = 32 * S::FR, PITCH = NW * int(sizeof(T)) + 16, CHUNKS = NW * int(sizeof(T)) / 16, N = 16 / int(sizeof(T));
+    static_assert(out_lds<T, S>() <= S::LDS, "room in the tile's LDS");
+    static_assert(!ADD || sizeof(T) == 4, "added in 32 bits");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / S::WC, wc = wave % S::WC;
+    char* const mine = lds + wave * 32 * PITCH;
 #pragma unroll
-    for (int j = 0; j < S::FC; ++j)
+    for (int j = 0; j < S::FC; ++j) {
 #pragma unroll
         for (int i = 0; i < S::FR; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                f(i, j, q, (wr * S::FR + i) * 32 + 8 * q + 4 * (lane >> 5), (wc * S::FC + j) * 32 + (lane & 31));
+            for (int q = 0; q < 4; ++q) {
+                const int n = i * 32 + 8 * q + 4 * (lane >> 5);
+                float x[4];
+                value(x, i, j, q, wr * NW + n, (wc * S::FC + j) * 32 + (lane & 31));
+                T* const to = reinterpret_cast<T*>(mine + (lane & 31) * PITCH) + n;
+                if constexpr (sizeof(T) == 2) {
+                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                    bf16x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = static_cast<__bf16>(x[e]);
+                    *reinterpret_cast<bf16x4*>(to) = v;
+                } else {
+                    float4v v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = x[e];
+                    *reinterpret_cast<float4v*>(to) = v;
+                }
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int it = 0; it < CHUNKS / 2; ++it) {
+            const int id = it * 64 + lane, r = id / CHUNKS, c = id % CHUNKS, n = wr * NW + c * N;
+            uint4v v = *reinterpret_cast<const uint4v*>(mine + r * PITCH + c * 16);
+            T* const to = row((wc * S::FC + j) * 32 + r);
+            if (!to || n >= left) continue;
+            if (n + N <= left) {
+                if constexpr (ADD) v = __builtin_bit_cast(uint4v, __builtin_bit_cast(float4v, v) + *reinterpret_cast<const float4v*>(to + n));
+                *reinterpret_cast<uint4u*>(to + n) = v;
+            } else {
+                const T* const from = reinterpret_cast<const T*>(mine + r * PITCH + c * 16);
+                for (int e = 0; n + e < left; ++e) {
+                    if constexpr (ADD) to[n + e] += from[e];
+                    else to[n + e] = from[e];
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- few rows of m ------------------------------------------------------------------------------------------------------
+// 16 RF of n by 16 TF of m per workgroup, whose eight waves share k out: every byte of A is read once, straight into the
+// registers of the 16 x 16 matrix instructions (64 bytes of k per row and step), and the waves' sums meet in LDS in their order.
+template <class E> struct Few;
+template <> struct Few<Bf16> {
+    typedef float4v Acc;
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Few<F32> {
+    typedef float4v Acc;
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        const float4v x = __builtin_bit_cast(float4v, a), y = __builtin_bit_cast(float4v, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct Few<Int8> {
+    typedef int4v Acc;
+    static __device__ __forceinline__ Acc mma(uint4v a, uint4v b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(int4v, a), __builtin_bit_cast(int4v, b), c, 0, 0, 0);
+    }
+};
+
+constexpr int FEW_WAVES = 8;
+template <int RF, int TF>
+constexpr int few_lds() { return FEW_WAVES * 16 * RF * 16 * TF * 4; }
+
+// sums[n + 16 RF m] in the first 1024 RF TF bytes of lds, behind a barrier
+template <class E, int RF, int TF>
+__device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t inner) {
+    typedef typename Few<E>::Acc Acc;
+    constexpr int AHEAD = RF * TF >= 8 ? 2 : 4;                   // steps on their way at a time
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bytes = int(inner) * E::ESZ, steps = (bytes + 63) >> 6;
+    uint32_t at[RF], bt[TF];
+    const uint32_t chunk = uint32_t(lane >> 4) * 16u;
+#pragma unroll
+    for (int i = 0; i < RF; ++i) {
+        const int r = i * 16 + (lane & 15);
+        at[i] = n0 + r < A.rows ? uint32_t(r) * uint32_t(A.stride) + chunk : NOWHERE;
+    }
+#pragma unroll
+    for (int j = 0; j < TF; ++j) {
+        const int r = j * 16 + (lane & 15);
+        bt[j] = r < B.rows ? uint32_t(r) * uint32_t(B.stride) + chunk : NOWHERE;
+    }
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(A.data + n0 * A.stride), 0, 0x7FFFFFFF, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(B.data), 0, 0x7FFFFFFF, 0x00020000);
+    Acc acc[RF][TF];
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < TF; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = 0;
+    for (int s0 = wave * AHEAD; s0 < steps; s0 += FEW_WAVES * AHEAD) {
+        uint4v a[AHEAD][RF], b[AHEAD][TF];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int k = (s0 + u) * 64;
+            const uint32_t mask = k + int(chunk) < bytes ? 0u : NOWHERE;
+#pragma unroll
+            for (int i = 0; i < RF; ++i) a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, (at[i] + k) | (at[i] == NOWHERE ? NOWHERE : mask), 0, 0);
+#pragma unroll
+            for (int j = 0; j < TF; ++j) b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, (bt[j] + k) | (bt[j] == NOWHERE ? NOWHERE : mask), 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < RF; ++i) {
+                const uint4v left = E::left(a[u][i]);
+#pragma unroll
+                for (int j = 0; j < TF; ++j) acc[i][j] = Few<E>::mma(left, b[u][j], acc[i][j]);
+            }
+    }
+    constexpr int ALL = 16 * RF * 16 * TF;
+    typedef std::conditional_t<std::is_same<Acc, int4v>::value, int, float> X;
+    X* const sums = reinterpret_cast<X*>(lds);
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < TF; ++j)
+            *reinterpret_cast<Acc*>(sums + wave * ALL + (j * 16 + (lane & 15)) * 16 * RF + i * 16 + 4 * (lane >> 4)) = acc[i][j];
+    __syncthreads();
+    for (int e = threadIdx.x; e < ALL; e += 64 * FEW_WAVES) {
+        X x = sums[e];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; ++w) x += sums[w * ALL + e];
+        sums[e] = x;                                              // its own place: nobody else reads it before the barrier
+    }
+    __syncthreads();
 }
 
 }  // namespace product

@@ -16,17 +16,17 @@ namespace product {
 // Workgroup -> tile.  Workgroup b runs on XCD b % 8; an XCD takes a run of ranks, which go through bands of BAND tiles of m
 // column by column of n, so that the tiles at work at a time share operands in its L2.
 constexpr int BAND = 8;
-ONECOMP_TOKEN_FN bool tile_of(unsigned block, int64_t m_tiles, int64_t n_tiles, int64_t& tm, int64_t& tn) {
-    const int64_t all = m_tiles * n_tiles, run = (all + 7) / 8, rank = int64_t(block & 7) * run + (block >> 3);
-    if (int64_t(block >> 3) >= run || rank >= all) return false;
-    const int64_t band = rank / (BAND * n_tiles), rest = rank - band * BAND * n_tiles;
-    const int64_t high = m_tiles - band * BAND < BAND ? m_tiles - band * BAND : BAND;
-    tn = rest / high;
-    tm = band * BAND + rest % high;
+ONECOMP_TOKEN_FN bool tile_of(unsigned block, int m_tiles, int n_tiles, int& tm, int& tn) {
+    const unsigned all = unsigned(m_tiles) * unsigned(n_tiles), run = (all + 7) / 8, rank = (block & 7) * run + (block >> 3);
+    if ((block >> 3) >= run || rank >= all) return false;
+    const unsigned band = rank / (BAND * unsigned(n_tiles)), rest = rank - band * BAND * unsigned(n_tiles);
+    const unsigned left = unsigned(m_tiles) - band * BAND, high = left < BAND ? left : unsigned(BAND);
+    tn = int(rest / high);
+    tm = int(band * BAND + rest % high);
     return true;
 }
 // workgroups that reach every tile
-ONECOMP_TOKEN_FN int64_t tile_blocks(int64_t m_tiles, int64_t n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
+inline int64_t tile_blocks(int64_t m_tiles, int64_t n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
 
 }  // namespace product
 namespace token {
@@ -58,7 +58,18 @@ inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t wid
     return s;
 }
 
+// ---- tiles of products ----
+// The largest tiles that are many enough for the chip: 256 x 256 (one per compute unit), 128 x 128, 64 x 64.  Up to FEW rows of m
+// are multiplied without tiles.
+constexpr int64_t FEW = 64;
+inline int tile_size(int64_t m, int64_t n) {
+    if (ceil_of(m, 256) * ceil_of(n, 256) >= 192) return 256;
+    return ceil_of(m, 128) * ceil_of(n, 128) >= 256 ? 128 : 64;
+}
+
 // ---- loss ----
+// Columns of the vocabulary that leave one maximum and sum per token.
+inline int64_t part_columns(int64_t tokens, int64_t vocab) { return tokens <= FEW ? 32 : tile_size(tokens, vocab); }
 // Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns.
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;
 inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
@@ -68,12 +79,25 @@ inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
     if (c >= all) return all;
     return ceil_of(ceil_of(all, ceil_of(all, c)), 256) * 256;   // pieces of about one size
 }
-// Shares of the inner sum of dh (over a piece's columns), where there are few tiles of it.
-inline int64_t dh_shares(int64_t tokens, int64_t width, int64_t columns) {
-    const int64_t tiles = ceil_of(tokens < 1 ? 1 : tokens, 128) * ceil_of(width, 128);
-    int64_t s = 512 / tiles;
-    if (s > columns / 512) s = columns / 512;
+// Shares of the inner sum of dh (over a piece's columns): room for up to 16 of them, in 1 GB.
+inline int64_t most_shares(int64_t tokens, int64_t width) {
+    const int64_t s = (int64_t(1) << 30) / ((tokens < 1 ? 1 : tokens) * width * 4);
     return s < 1 ? 1 : s > 16 ? 16 : s;
+}
+// How many are taken, from the number of kept tokens: the fewest rounds of the chip's `slots` tiles, by the columns that a
+// workgroup goes through one after the other and 256 for the beginning and end of each tile.
+ONECOMP_TOKEN_FN int shares_of(int tiles, int columns, int slots, int most) {
+    int best = 1;
+    uint64_t least = 0;
+    for (int s = 1; s <= most; ++s) {
+        const unsigned rounds = (unsigned(tiles) * unsigned(s) + unsigned(slots) - 1) / unsigned(slots);
+        const uint64_t cost = uint64_t(rounds) * ((unsigned(columns) + unsigned(s) - 1) / unsigned(s) + 256u);
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
 }
 
 struct LossSpace {
@@ -99,7 +123,7 @@ inline LossSpace loss_space(int64_t tokens, int64_t width, int64_t vocab, int es
     s.hit = take(gradient ? 0 : t * 4);
     if (gradient) {
         s.columns = piece_columns(tokens, vocab, esz);
-        s.shares = dh_shares(tokens, width, s.columns);
+        s.shares = most_shares(tokens, width);
         s.piece = take(t * size_t(s.columns) * esz);
         s.dh = take(t * size_t(width) * 4 * size_t(s.shares));
     }

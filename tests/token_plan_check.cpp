@@ -24,8 +24,8 @@ static void check_tiles() {
                 std::vector<int> seen(size_t(m * n), 0);
                 const int64_t blocks = product::tile_blocks(launched, n);
                 for (int64_t b = 0; b < blocks; ++b) {
-                    int64_t tm, tn;
-                    if (!product::tile_of(unsigned(b), m, n, tm, tn)) continue;
+                    int tm, tn;
+                    if (!product::tile_of(unsigned(b), int(m), int(n), tm, tn)) continue;
                     REQUIRE(tm >= 0 && tm < m && tn >= 0 && tn < n, "%ld of %ld x %ld", long(b), long(m), long(n));
                     ++seen[size_t(tm * n + tn)];
                 }
@@ -56,8 +56,12 @@ static void check_loss() {
                 REQUIRE(c > 0 && c % 256 == 0 && c < vocab + 256 + 2048, "%ld %ld", long(tokens), long(vocab));
                 REQUIRE(c <= 2048 || tokens * c * esz <= PIECE_BYTES, "%ld %ld", long(tokens), long(vocab));
                 for (int64_t width : {4, 64, 4096}) {
-                    const int64_t shares = dh_shares(tokens, width, c);
+                    const int64_t shares = most_shares(tokens, width);
                     REQUIRE(shares >= 1 && shares <= 16, "%ld", long(shares));
+                    for (int tiles : {0, 1, 20, 255, 256, 257, 320, 5000}) {
+                        const int taken = shares_of(tiles, int(c), 256, int(shares));
+                        REQUIRE(taken >= 1 && taken <= shares, "%d of %ld", taken, long(shares));
+                    }
                     for (bool gradient : {false, true}) {
                         const LossSpace s = loss_space(tokens, width, vocab, esz, ceil_of(vocab, 128), gradient);
                         const size_t t = size_t(tokens);
