@@ -12,31 +12,43 @@ namespace {
 
 using block::load_vector;
 using product::ALONG;
-using product::Big;
 using product::Int8;
-using product::Mid;
-using product::Small;
 using product::Operand;
 
-// A workgroup per token.  The quotient is the rounded one of 32 bits (IEEE division), ties to even.  A token that holds an infinity
-// or NaN gets codes of 0 and a NaN for its scale, so that its results are NaN and no others.
-template <class T>
+// A workgroup per token, whose row stays in registers (HELD 16-byte vectors a thread; what is wider is read twice).  The quotient
+// is the rounded one of 32 bits (IEEE division), ties to even.  A token that holds an infinity or NaN gets codes of 0 and a
+// NaN for its scale, so that its results are NaN and no others.
+template <class T, int HELD>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t stride, int width, int8_t* codes, float* scales, int32_t* sums) {
-    constexpr int N = 16 / int(sizeof(T));
+    constexpr int N = 16 / int(sizeof(T)), TURN = 256 * N;
     __shared__ float s_top[4];
     __shared__ int s_sum[4], s_odd[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = threadIdx.x * N;
     const T* from = x + blockIdx.x * stride;
     float top = 0.f;
     bool odd = false;
-    for (int c = threadIdx.x * N; c < width; c += 256 * N) {
-        float v[N];
-        load_vector(v, from + c);
+    auto look = [&](const float (&v)[N]) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             top = fmaxf(top, fabsf(v[e]));
             odd = odd || !(fabsf(v[e]) < __builtin_inff());
         }
+    };
+    uint4v held[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if (first + h * TURN < width) held[h] = *reinterpret_cast<const block::uint4u*>(from + first + h * TURN);
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if (first + h * TURN < width) {
+            float v[N];
+            load_vector(v, reinterpret_cast<const T*>(&held[h]));
+            look(v);
+        }
+    for (int c = first + HELD * TURN; c < width; c += TURN) {
+        float v[N];
+        load_vector(v, from + c);
+        look(v);
     }
     top = wave_max(top);
     odd = __any(odd);
@@ -48,23 +60,34 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t strid
     top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
     const float scale = top / 127.f;
+    const bool none = odd || !(scale > 0.f);
     int sum = 0;
-    int8_t* to = codes + int64_t(blockIdx.x) * width;
-    for (int c = threadIdx.x * N; c < width; c += 256 * N) {
-        float v[N];
-        load_vector(v, from + c);
+    int8_t* const to = codes + int64_t(blockIdx.x) * width;
+    auto put = [&](const float (&v)[N], int c) __attribute__((always_inline)) {
         uint32_t word[N / 4];
 #pragma unroll
         for (int w = 0; w < N / 4; ++w) word[w] = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float r = rintf(v[e] / scale);
-            const int code = odd || !(scale > 0.f) ? 0 : int(fminf(fmaxf(r, -127.f), 127.f));
+            const int code = none ? 0 : int(fminf(fmaxf(r, -127.f), 127.f));
             sum += code;
             word[e / 4] |= uint32_t(code & 255) << (8 * (e % 4));
         }
 #pragma unroll
         for (int w = 0; w < N / 4; ++w) reinterpret_cast<uint32_t*>(to + c)[w] = word[w];
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if (first + h * TURN < width) {
+            float v[N];
+            load_vector(v, reinterpret_cast<const T*>(&held[h]));
+            put(v, first + h * TURN);
+        }
+    for (int c = first + HELD * TURN; c < width; c += TURN) {
+        float v[N];
+        load_vector(v, from + c);
+        put(v, c);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
@@ -74,6 +97,16 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t strid
         scales[blockIdx.x] = odd ? __builtin_nanf("") : scale;
         sums[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
     }
+}
+template <class T>
+onecomp_status quantize(const Rows& x, int64_t tokens, int64_t width, int8_t* codes, float* scales, int32_t* sums, hipStream_t stream) {
+    const T* from = static_cast<const T*>(x.p);
+    const dim3 grid{unsigned(tokens)};
+    const int64_t vectors = ceil_div(width, 256 * 16 / int64_t(sizeof(T)));
+    if (vectors <= 2) quantize_kernel<T, 2><<<grid, dim3(256), 0, stream>>>(from, x.stride, int(width), codes, scales, sums);
+    else quantize_kernel<T, 4><<<grid, dim3(256), 0, stream>>>(from, x.stride, int(width), codes, scales, sums);
+    ONECOMP_CHECK_LAUNCH();
+    return ONECOMP_OK;
 }
 
 struct Args {
@@ -94,8 +127,8 @@ struct Columns {
     float bias[256];
 };
 template <class T>
-__device__ __forceinline__ void load_columns(Columns& c, const Args& P, int64_t n0, int count) {
-    for (int n = threadIdx.x; n < count; n += blockDim.x) {
+__device__ __forceinline__ void load_columns(Columns& c, const Args& P, int64_t n0, int count, int threads) {
+    for (int n = threadIdx.x; n < count; n += threads) {
         const int64_t at = n0 + n < P.d_out ? n0 + n : P.d_out - 1;
         c.scale[n] = P.scales[at];
         c.zero[n] = 128 - int(rintf(P.zeros[at]));
@@ -108,17 +141,17 @@ __device__ __forceinline__ float value(int sum, int token_sum, float token_scale
 }
 
 template <class T, class S>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU) void linear_kernel(Args P) {
+__global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void linear_kernel(Args P) {
     extern __shared__ __align__(1024) char lds[];
     int tm, tn;
     if (!product::my_tile(int((P.tokens + S::TM - 1) / S::TM), int((P.d_out + S::TN - 1) / S::TN), tm, tn)) return;
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     product::int16v acc[S::FR][S::FC];
-    product::multiply<Int8, ALONG, ALONG, S>(lds, P.q, P.codes, n0, m0, P.inner, acc);
+    if (!product::multiply<Int8, ALONG, ALONG, S>(lds, P.q, P.codes, n0, m0, P.inner, acc)) return;
     __syncthreads();
     static_assert(product::out_lds<T, S>() + sizeof(Columns) <= S::LDS, "room for the columns' numbers");
     Columns& c = *reinterpret_cast<Columns*>(lds + product::out_lds<T, S>());
-    load_columns<T>(c, P, n0, S::TN);
+    load_columns<T>(c, P, n0, S::TN, S::THREADS);
     const int lane = threadIdx.x & 63, wc = int(threadIdx.x >> 6) % S::WC;
     float token_scale[S::FC];
     int token_sum[S::FC];
@@ -145,7 +178,7 @@ __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_tokens_kernel(Arg
     __shared__ __align__(16) char lds[product::few_lds<RF, TF>()];
     __shared__ Columns c;
     const int64_t n0 = int64_t(blockIdx.x) * 16 * RF;
-    load_columns<T>(c, P, n0, 16 * RF);
+    load_columns<T>(c, P, n0, 16 * RF, 64 * product::FEW_WAVES);
     product::multiply_few<Int8, RF, TF>(lds, P.q, P.codes, n0, P.inner);
     for (int e = threadIdx.x; e < 256 * RF * TF; e += 64 * product::FEW_WAVES) {
         const int n = e % (16 * RF), m = e / (16 * RF);
@@ -160,7 +193,7 @@ onecomp_status run(const Args& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
     if (const onecomp_status st = allow_dynamic_lds(reinterpret_cast<const void*>(linear_kernel<T, S>), S::LDS, done)) return st;
     const int64_t blocks = product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.d_out, S::TN));
-    linear_kernel<T, S><<<dim3(unsigned(blocks)), dim3(S::THREADS), S::LDS, stream>>>(P);
+    linear_kernel<T, S><<<dim3(unsigned(blocks)), dim3(S::ALL_THREADS), S::LDS, stream>>>(P);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }
@@ -178,21 +211,14 @@ onecomp_status dispatch(const Args& P, hipStream_t stream) {
         if (P.tokens <= 32) return wide ? run_few<T, 2, 2>(P, stream) : run_few<T, 1, 2>(P, stream);
         return wide ? run_few<T, 2, 4>(P, stream) : run_few<T, 1, 4>(P, stream);
     }
-    const int size = tile_size(P.tokens, P.d_out);
-    return size == 256 ? run<T, Big>(P, stream) : size == 128 ? run<T, Mid>(P, stream) : run<T, Small>(P, stream);
+    return product::with_shape(choose_tiles(P.tokens, P.d_out), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
 }
 
 }  // namespace
 
 onecomp_status quantize_tokens_run(onecomp_dtype dtype, const Rows& x, int64_t tokens, int64_t width, int8_t* codes, float* scales, int32_t* sums,
                                    hipStream_t stream) {
-    const dim3 grid{unsigned(tokens)};
-    if (dtype == ONECOMP_BF16)
-        quantize_kernel<uint16_t><<<grid, dim3(256), 0, stream>>>(static_cast<const uint16_t*>(x.p), x.stride, int(width), codes, scales, sums);
-    else
-        quantize_kernel<float><<<grid, dim3(256), 0, stream>>>(static_cast<const float*>(x.p), x.stride, int(width), codes, scales, sums);
-    ONECOMP_CHECK_LAUNCH();
-    return ONECOMP_OK;
+    return dtype == ONECOMP_BF16 ? quantize<uint16_t>(x, tokens, width, codes, scales, sums, stream) : quantize<float>(x, tokens, width, codes, scales, sums, stream);
 }
 
 size_t linear_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }

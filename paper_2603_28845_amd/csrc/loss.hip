@@ -16,9 +16,6 @@ namespace {
 
 using product::ACROSS;
 using product::ALONG;
-using product::Big;
-using product::Mid;
-using product::Small;
 using product::Operand;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -115,7 +112,7 @@ struct Logits {
 };
 
 template <class E, class S>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU) void logits_kernel(Logits P) {
+__global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Logits P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
     int tm, tn;
@@ -123,7 +120,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logits_kernel(Logits P)
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
-    product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc);
+    if (!product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
     __syncthreads();
     // A lane holds 16 FR logits of a token: maximum, sum of powers, joined with the other half's and, through LDS, with the other
     // waves' of these tokens.
@@ -264,7 +261,7 @@ __device__ __forceinline__ void store_four(float* p, const float (&x)[4]) {
 }
 
 template <class E, class S>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU) void logit_grads_kernel(LogitGrads P) {
+__global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kernel(LogitGrads P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
     int tm, tn;
@@ -272,7 +269,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU) void logit_grads_kernel(Logi
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
-    product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc);
+    if (!product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
     const int wc = int(threadIdx.x >> 6) % S::WC, lane = threadIdx.x & 63;
     float4 coef[S::FC];
 #pragma unroll
@@ -308,7 +305,7 @@ struct GradRows {
     int width;
 };
 template <class E, class S>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU) void grad_rows_kernel(GradRows P) {
+__global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(GradRows P) {
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
     int tm, tn;
@@ -322,7 +319,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU) void grad_rows_kernel(GradRo
     P.piece.data += int64_t(begin) * E::ESZ;
     P.piece.rows = count;
     float16v acc[S::FR][S::FC];
-    product::multiply<E, ACROSS, ALONG, S>(lds, P.weight, P.piece, n0, m0, inner < 0 ? 0 : inner, acc);
+    if (!product::multiply<E, ACROSS, ALONG, S>(lds, P.weight, P.piece, n0, m0, inner < 0 ? 0 : inner, acc)) return;
     __syncthreads();
     float* const out = P.out + share * P.tokens * P.width;
     auto value = [&](float (&x)[4], int i, int j, int q, int, int) __attribute__((always_inline)) {
@@ -343,13 +340,13 @@ struct GradWeight {
     int64_t stride;
 };
 template <class E, class S>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU) void grad_weight_kernel(GradWeight P) {
+__global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_weight_kernel(GradWeight P) {
     extern __shared__ __align__(1024) char lds[];
     int tm, tn;
     if (!product::my_tile((P.columns + S::TM - 1) / S::TM, (P.width + S::TN - 1) / S::TN, tm, tn)) return;
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     float16v acc[S::FR][S::FC];
-    product::multiply<E, ACROSS, ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc);
+    if (!product::multiply<E, ACROSS, ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc)) return;
     __syncthreads();
     product::store_tile<typename E::T, S, false>(
         lds,
@@ -367,7 +364,7 @@ struct Finish {
     const float* parts;
     const int32_t *place, *count;
     int64_t tokens;
-    int full, width, tile, slots, most;            // as grad_rows_kernel had them
+    int full, width, tile_m, tile_n, slots, most;            // as grad_rows_kernel had them
     float scale;
     Rows dh;
 };
@@ -377,7 +374,7 @@ __global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
     const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (t >= P.tokens) return;
     const int at = P.place[t];
-    const int tiles = (*P.count + P.tile - 1) / P.tile * ((P.width + P.tile - 1) / P.tile);
+    const int tiles = (*P.count + P.tile_m - 1) / P.tile_m * ((P.width + P.tile_n - 1) / P.tile_n);
     const int shares = shares_of(tiles, P.full, P.slots, P.most);
     T* to = static_cast<T*>(P.dh.p) + t * P.dh.stride;
 #pragma unroll 2
@@ -403,29 +400,28 @@ onecomp_status launch(K kernel, int lds, int threads, int64_t blocks, int64_t sh
 // f(shape) for the tiles that a product of m x n results takes
 template <class F>
 onecomp_status with_tiles(int64_t m, int64_t n, F&& f) {
-    const int size = tile_size(m, n);
-    return size == 256 ? f(Big{}) : size == 128 ? f(Mid{}) : f(Small{});
+    return product::with_shape(choose_tiles(m, n), f);
 }
 
 template <class E, class S>
 onecomp_status run_logits(const Logits& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(logits_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.vocab, S::TN)), 1, P, done, stream);
+    return launch(logits_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.vocab, S::TN)), 1, P, done, stream);
 }
 template <class E, class S>
 onecomp_status run_logit_grads(const LogitGrads& P, int64_t tokens, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(logit_grads_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(tokens, S::TM), ceil_div(P.columns, S::TN)), 1, P, done, stream);
+    return launch(logit_grads_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(tokens, S::TM), ceil_div(P.columns, S::TN)), 1, P, done, stream);
 }
 template <class E, class S>
 onecomp_status run_grad_rows(const GradRows& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(grad_rows_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.width, S::TN)), P.most, P, done, stream);
+    return launch(grad_rows_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.width, S::TN)), P.most, P, done, stream);
 }
 template <class E, class S>
 onecomp_status run_grad_weight(const GradWeight& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(grad_weight_kernel<E, S>, S::LDS, S::THREADS, product::tile_blocks(ceil_div(P.columns, S::TM), ceil_div(P.width, S::TN)), 1, P, done, stream);
+    return launch(grad_weight_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(P.columns, S::TM), ceil_div(P.width, S::TN)), 1, P, done, stream);
 }
 
 template <class E>
@@ -552,9 +548,9 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
         }
     }
     if (P.dh.p && P.tokens) {
-        const int tile = tile_size(P.tokens, P.width);
-        const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(s.columns), int(P.width), tile,
-                       256 * (tile == 256 ? Big::PER_CU : tile == 128 ? Mid::PER_CU : Small::PER_CU), int(s.shares), P.scale, P.dh};
+        const TileShape tile = shape_of(choose_tiles(P.tokens, P.width));
+        const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(s.columns), int(P.width),
+                       tile.m, tile.n, 256 * tile.per_cu, int(s.shares), P.scale, P.dh};
         finish_rows_kernel<typename E::T><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(F);
         ONECOMP_CHECK_LAUNCH();
     }

@@ -19,6 +19,7 @@
 #include "common.hpp"
 #include "token_plan.hpp"
 #include <type_traits>
+#include <utility>
 
 namespace onecomp {
 namespace product {
@@ -68,17 +69,25 @@ struct Operand {
     int64_t stride, rows;
 };
 
-// WR x WC waves of FR x FC fragments each: a tile of 32 WR FR (n) by 32 WC FC (m)
-template <int WR_, int WC_, int FR_, int FC_, int PER_CU_>
+// WR x WC waves of FR x FC fragments each: a tile of 32 WR FR (n) by 32 WC FC (m).  SPLIT groups of such waves share the steps of k
+// out, each with a ring of its own; their sums meet in LDS in the groups' order.  PER_CU workgroups are meant to share a
+// compute unit.
+template <int WR_, int WC_, int FR_, int FC_, int SPLIT_, int PER_CU_>
 struct Shape {
-    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, PER_CU = PER_CU_, SLOTS = 4;
-    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
+    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, SPLIT = SPLIT_, PER_CU = PER_CU_, SLOTS = 4;
+    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES, ALL_THREADS = THREADS * SPLIT;   // of a group, of a workgroup
+    static constexpr int PER_SIMD = PER_CU * WAVES * SPLIT / 4;                                  // waves
     static constexpr int TN = 32 * WR * FR, TM = 32 * WC * FC;
-    static constexpr int STAGE = (TN + TM) * 64, LDS = SLOTS * STAGE;
+    static constexpr int STAGE = (TN + TM) * 64, RING = SLOTS * STAGE, LDS = SPLIT * RING;
+    static_assert((SPLIT - 1) * THREADS * FR * FC * 64 <= LDS, "room for the groups' sums");
 };
-typedef Shape<2, 2, 4, 4, 1> Big;      // 256 x 256
-typedef Shape<2, 2, 2, 2, 2> Mid;      // 128 x 128
-typedef Shape<2, 2, 1, 1, 4> Small;    // 64 x 64
+typedef Shape<2, 2, 4, 4, 1, 1> Big;          // 256 x 256
+typedef Shape<2, 2, 2, 2, 1, 2> Mid;          // 128 x 128
+typedef Shape<2, 2, 2, 2, 2, 1> MidSplit;
+typedef Shape<2, 2, 2, 1, 1, 3> Half;         // 128 x 64
+typedef Shape<2, 2, 2, 1, 3, 1> HalfSplit;
+typedef Shape<2, 2, 1, 1, 1, 4> Small;        // 64 x 64
+typedef Shape<2, 2, 1, 1, 4, 1> SmallSplit;
 
 constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
 
@@ -96,11 +105,12 @@ struct Side {
     const char* p;
     int64_t left, step;                                           // bytes: what is left of the operand (ALONG: of a row), one step
     int read0;
-    __device__ __forceinline__ void init(const Operand& o, int64_t first, int64_t inner, int wave, int lane) {
+    // group: of `split` that take the steps in turn
+    __device__ __forceinline__ void init(const Operand& o, int64_t first, int64_t inner, int wave, int lane, int group, int split) {
         if constexpr (L == ALONG) {
-            p = o.data + first * o.stride;
-            left = inner * E::ESZ;
-            step = 64;
+            p = o.data + first * o.stride + group * 64;
+            left = inner * E::ESZ - group * 64;
+            step = 64 * split;
             chunk = uint32_t((lane & 3) ^ ((lane >> 3) & 3)) * 16u;
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
@@ -110,9 +120,10 @@ struct Side {
             const int r = lane & 31;
             read0 = r * 64 + (((lane >> 5) ^ ((r >> 1) & 3)) << 4);
         } else {
-            p = o.data + first * E::ESZ;
-            left = inner * o.stride - first * E::ESZ;
-            step = int64_t(64 / E::ESZ) * o.stride;
+            const int64_t one = int64_t(64 / E::ESZ) * o.stride;
+            p = o.data + first * E::ESZ + group * one;
+            left = inner * o.stride - first * E::ESZ - group * one;
+            step = one * split;
             chunk = 0;
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
@@ -166,21 +177,30 @@ struct Side {
     }
 };
 
-// acc = the products of tile (n0, m0) over `inner` values of k.  lds: S::LDS bytes, free again for the caller behind a barrier.
+template <int... I, class F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+
+// acc = the products of tile (n0, m0) over `inner` values of k, in the first group of waves; the others return false and have
+// nothing left to do.  lds: S::LDS bytes, free again for the caller behind a barrier.
 template <class E, Layout LA, Layout LB, class S>
-__device__ __forceinline__ void multiply(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t m0, int64_t inner,
+__device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t m0, int64_t inner,
                                          typename E::Acc (&acc)[S::FR][S::FC]) {
     constexpr int FR = S::FR, FC = S::FC, SLOTS = S::SLOTS;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = S::SPLIT == 1 ? 0 : all_wave / S::WAVES, wave = S::SPLIT == 1 ? all_wave : all_wave % S::WAVES;
     const int wr = wave / S::WC, wc = wave % S::WC;
+    char* const all_lds = lds;
+    lds += group * S::RING;
     typedef Side<E, LA, S::TN, S::WAVES> SideA;
     typedef Side<E, LB, S::TM, S::WAVES> SideB;
     constexpr int LOADS = SideA::LOADS + SideB::LOADS, FRAGS = FR + FC, PRODUCTS = FR * FC;
     constexpr int B_AT = S::TN * 64;
     SideA a;
     SideB b;
-    a.init(A, n0, inner, wave, lane);
-    b.init(B, m0, inner, wave, lane);
+    a.init(A, n0, inner, wave, lane, group, S::SPLIT);
+    b.init(B, m0, inner, wave, lane, group, S::SPLIT);
     const uint32_t lds0 = uint32_t(uintptr_t((ONECOMP_LDS char*)lds));
     struct Step {
         typename SideA::Step a;
@@ -226,7 +246,7 @@ __device__ __forceinline__ void multiply(char* lds, const Operand& A, const Oper
         }
     };
     const int64_t bytes = inner * E::ESZ;
-    const int n_st = int((bytes + 63) >> 6);
+    const int n_st = (int((bytes + 63) >> 6) + S::SPLIT - 1) / S::SPLIT;
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS * (SLOTS - 2)));
     __syncthreads();
     {
@@ -267,16 +287,51 @@ __device__ __forceinline__ void multiply(char* lds, const Operand& A, const Oper
     };
     int st = 0;
 #pragma unroll 1
-    for (; st + SLOTS <= n_st; st += SLOTS) {
-        stage(std::integral_constant<int, 0>{});
-        stage(std::integral_constant<int, 1>{});
-        stage(std::integral_constant<int, 2>{});
-        stage(std::integral_constant<int, 3>{});
-    }
-    if (st < n_st) stage(std::integral_constant<int, 0>{});
-    if (st + 1 < n_st) stage(std::integral_constant<int, 1>{});
-    if (st + 2 < n_st) stage(std::integral_constant<int, 2>{});
+    for (; st + SLOTS <= n_st; st += SLOTS) each_of(std::make_integer_sequence<int, SLOTS>{}, stage);
+    const int rest = n_st - st;
+    each_of(std::make_integer_sequence<int, SLOTS - 1>{}, [&](auto slot_c) __attribute__((always_inline)) {
+        if (decltype(slot_c)::value < rest) stage(slot_c);
+    });
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));                    // no LDS write may be in flight when the tile ends
+    if constexpr (S::SPLIT > 1) {
+        typedef std::conditional_t<std::is_same<typename E::Acc, int16v>::value, int, float> X;
+        X* const sums = reinterpret_cast<X*>(all_lds) + threadIdx.x % S::THREADS;
+        constexpr int EACH = FR * FC * 16 * S::THREADS;
+        __syncthreads();
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int j = 0; j < FC; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sums[(group - 1) * EACH + ((i * FC + j) * 16 + r) * S::THREADS] = acc[i][j][r];
+        }
+        __syncthreads();
+        if (group > 0) return false;
+#pragma unroll
+        for (int g = 0; g < S::SPLIT - 1; ++g)
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int j = 0; j < FC; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] += sums[g * EACH + ((i * FC + j) * 16 + r) * S::THREADS];
+    }
+    return true;
+}
+
+// f(shape) for a choice of tiles
+template <class F>
+auto with_shape(token::Tiles t, F&& f) {
+    switch (t) {
+        case token::BIG: return f(Big{});
+        case token::MID: return f(Mid{});
+        case token::MID_SPLIT: return f(MidSplit{});
+        case token::HALF: return f(Half{});
+        case token::HALF_SPLIT: return f(HalfSplit{});
+        case token::SMALL: return f(Small{});
+        default: return f(SmallSplit{});
+    }
 }
 
 // tile_of for a workgroup of this launch, in scalar registers
@@ -384,7 +439,7 @@ constexpr int few_lds() { return FEW_WAVES * 16 * RF * 16 * TF * 4; }
 template <class E, int RF, int TF>
 __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t inner) {
     typedef typename Few<E>::Acc Acc;
-    constexpr int AHEAD = RF * TF >= 8 ? 2 : 4;                   // steps on their way at a time
+    constexpr int AHEAD = RF + TF >= 5 ? 2 : 4;                   // steps on their way at a time
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bytes = int(inner) * E::ESZ, steps = (bytes + 63) >> 6;
     uint32_t at[RF], bt[TF];
@@ -408,25 +463,42 @@ __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const 
         for (int j = 0; j < TF; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[i][j][r] = 0;
-    for (int s0 = wave * AHEAD; s0 < steps; s0 += FEW_WAVES * AHEAD) {
+    // Two sets of AHEAD steps: one on its way while the other is multiplied.
+    struct Set {
         uint4v a[AHEAD][RF], b[AHEAD][TF];
+    };
+    auto load = [&](Set& x, int s0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int k = (s0 + u) * 64;
-            const uint32_t mask = k + int(chunk) < bytes ? 0u : NOWHERE;
+            const bool there = k + int(chunk) < bytes;
 #pragma unroll
-            for (int i = 0; i < RF; ++i) a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, (at[i] + k) | (at[i] == NOWHERE ? NOWHERE : mask), 0, 0);
+            for (int i = 0; i < RF; ++i) x.a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, there && at[i] != NOWHERE ? at[i] + k : NOWHERE, 0, 0);
 #pragma unroll
-            for (int j = 0; j < TF; ++j) b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, (bt[j] + k) | (bt[j] == NOWHERE ? NOWHERE : mask), 0, 0);
+            for (int j = 0; j < TF; ++j) x.b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, there && bt[j] != NOWHERE ? bt[j] + k : NOWHERE, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto products = [&](const Set& x) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int i = 0; i < RF; ++i) {
-                const uint4v left = E::left(a[u][i]);
+                const uint4v left = E::left(x.a[u][i]);
 #pragma unroll
-                for (int j = 0; j < TF; ++j) acc[i][j] = Few<E>::mma(left, b[u][j], acc[i][j]);
+                for (int j = 0; j < TF; ++j) acc[i][j] = Few<E>::mma(left, x.b[u][j], acc[i][j]);
             }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int TURN = FEW_WAVES * AHEAD;
+    Set x, y;
+    if (wave * AHEAD < steps) load(x, wave * AHEAD);
+    for (int s0 = wave * AHEAD; s0 < steps; s0 += 2 * TURN) {
+        if (s0 + TURN < steps) load(y, s0 + TURN);
+        products(x);
+        if (s0 + TURN >= steps) break;
+        if (s0 + 2 * TURN < steps) load(x, s0 + 2 * TURN);
+        products(y);
     }
     constexpr int ALL = 16 * RF * 16 * TF;
     typedef std::conditional_t<std::is_same<Acc, int4v>::value, int, float> X;

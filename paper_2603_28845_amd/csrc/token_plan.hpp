@@ -59,17 +59,37 @@ inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t wid
 }
 
 // ---- tiles of products ----
-// The largest tiles that are many enough for the chip: 256 x 256 (one per compute unit), 128 x 128, 64 x 64.  Up to FEW rows of m
-// are multiplied without tiles.
+// Up to FEW rows of m are multiplied without tiles.
 constexpr int64_t FEW = 64;
-inline int tile_size(int64_t m, int64_t n) {
-    if (ceil_of(m, 256) * ceil_of(n, 256) >= 192) return 256;
-    return ceil_of(m, 128) * ceil_of(n, 128) >= 256 ? 128 : 64;
+enum Tiles { BIG, MID, MID_SPLIT, HALF, HALF_SPLIT, SMALL, SMALL_SPLIT };
+struct TileShape {
+    int n, m, per_cu;
+};
+inline TileShape shape_of(Tiles t) {
+    switch (t) {
+        case BIG: return {256, 256, 1};
+        case MID: return {128, 128, 2};
+        case MID_SPLIT: return {128, 128, 1};
+        case HALF: return {128, 64, 3};
+        case HALF_SPLIT: return {128, 64, 1};
+        case SMALL: return {64, 64, 4};
+        default: return {64, 64, 1};
+    }
+}
+inline int64_t tiles_of(Tiles t, int64_t m, int64_t n) { return ceil_of(m, shape_of(t).m) * ceil_of(n, shape_of(t).n); }
+// The largest tiles that are many enough for the chip.
+inline Tiles choose_tiles(int64_t m, int64_t n) {
+    if (tiles_of(BIG, m, n) >= 192) return BIG;
+    if (tiles_of(MID, m, n) > 256) return MID;
+    if (tiles_of(MID, m, n) > 192) return MID_SPLIT;
+    if (tiles_of(HALF, m, n) > 256) return HALF;
+    if (tiles_of(HALF, m, n) > 192) return HALF_SPLIT;
+    return tiles_of(SMALL, m, n) > 256 ? SMALL : SMALL_SPLIT;
 }
 
 // ---- loss ----
 // Columns of the vocabulary that leave one maximum and sum per token.
-inline int64_t part_columns(int64_t tokens, int64_t vocab) { return tokens <= FEW ? 32 : tile_size(tokens, vocab); }
+inline int64_t part_columns(int64_t tokens, int64_t vocab) { return tokens <= FEW ? 32 : shape_of(choose_tiles(tokens, vocab)).n; }
 // Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns.
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;
 inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
