@@ -400,7 +400,7 @@ onecomp_status launch(K kernel, int lds, int threads, int64_t blocks, int64_t sh
 // f(shape) for the tiles that a product of m x n results takes
 template <class F>
 onecomp_status with_tiles(int64_t m, int64_t n, F&& f) {
-    return product::with_shape(choose_tiles(m, n), f);
+    return product::with_shape<64>(choose_tiles(m, n), f);
 }
 
 template <class E, class S>

@@ -6,12 +6,12 @@
 // instruction's result) for one m (its column), so that sums over n stay in a lane and results go out in vectors.  An operand is
 // given ALONG k (k dense in memory) or ACROSS it (n, or m, dense: rows of k).
 //
-// Whatever the type, a step is 64 bytes of k per row and an instruction's fragment 16 bytes per lane: lanes 0 .. 31 hold the
-// first, lanes 32 .. 63 the second 16 bytes of 32 (8 bf16, 16 int8, 4 fp32 values).  Tiles reach LDS by direct loads through a ring
-// of SLOTS steps; fragments of a half step are read while the other half is multiplied, reads and loads one by one behind
-// the matrix instructions.
-//   ALONG   a row's 64 bytes are four chunks of 16; chunk c of row r lies at c ^ ((r >> 1) & 3), so that eight rows' same chunk fall
-//           into different banks.
+// Whatever the type, a step is 64 or 128 bytes of k per row and an instruction's fragment 16 bytes per lane: lanes 0 .. 31 hold
+// the first, lanes 32 .. 63 the second 16 bytes of 32 (8 bf16, 16 int8, 4 fp32 values).  Tiles reach LDS by direct loads through a
+// ring of four or two steps; the fragments of 32 bytes are read while those before are multiplied, reads and loads one by one
+// behind the matrix instructions.
+//   ALONG   a row's bytes of a step are chunks of 16, permuted per row (Side::turn) so that eight rows' same chunk fall into
+//           different banks.
 //   ACROSS  rows of k as they are; in bf16 their chunks lie permuted by fours (Side::swizzle) and fragments are transposed
 //           reads; in fp32 a fragment is four plain reads.
 // What lies behind the operands' ends becomes zeros by the loads' bounds check.
@@ -69,33 +69,27 @@ struct Operand {
     int64_t stride, rows;
 };
 
-// WR x WC waves of FR x FC fragments each: a tile of 32 WR FR (n) by 32 WC FC (m).  SPLIT groups of such waves share the steps of k
+// WR x WC waves of FR x FC fragments each: a tile of 32 WR FR (n) by 32 WC FC (m), in steps of STEP bytes of k.  SPLIT groups of such waves share the steps of k
 // out, each with a ring of its own; their sums meet in LDS in the groups' order.  PER_CU workgroups are meant to share a
 // compute unit.
-template <int WR_, int WC_, int FR_, int FC_, int SPLIT_, int PER_CU_>
+template <int WR_, int WC_, int FR_, int FC_, int STEP_, int SPLIT_, int PER_CU_>
 struct Shape {
-    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, SPLIT = SPLIT_, PER_CU = PER_CU_, SLOTS = 4;
+    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, STEP = STEP_, SPLIT = SPLIT_, PER_CU = PER_CU_, SLOTS = 256 / STEP;
     static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES, ALL_THREADS = THREADS * SPLIT;   // of a group, of a workgroup
     static constexpr int PER_SIMD = PER_CU * WAVES * SPLIT / 4;                                  // waves
     static constexpr int TN = 32 * WR * FR, TM = 32 * WC * FC;
-    static constexpr int STAGE = (TN + TM) * 64, RING = SLOTS * STAGE, LDS = SPLIT * RING;
+    static constexpr int STAGE = (TN + TM) * STEP, RING = SLOTS * STAGE, LDS = SPLIT * RING;
     static_assert((SPLIT - 1) * THREADS * FR * FC * 64 <= LDS, "room for the groups' sums");
 };
-typedef Shape<2, 2, 4, 4, 1, 1> Big;          // 256 x 256
-typedef Shape<2, 2, 2, 2, 1, 2> Mid;          // 128 x 128
-typedef Shape<2, 2, 2, 2, 2, 1> MidSplit;
-typedef Shape<2, 2, 2, 1, 1, 3> Half;         // 128 x 64
-typedef Shape<2, 2, 2, 1, 3, 1> HalfSplit;
-typedef Shape<2, 2, 1, 1, 1, 4> Small;        // 64 x 64
-typedef Shape<2, 2, 1, 1, 4, 1> SmallSplit;
-
 constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
 
 // One operand's tile: how a wave brings its part of a step to LDS, and how a lane reads fragments from there.
-template <class E, Layout L, int T, int WAVES>
+template <class E, Layout L, int T, int WAVES, int STEP>
 struct Side {
-    static constexpr int LOADS = T / 16 / WAVES;                  // of 1 KB, per wave and step
-    static_assert(T % (16 * WAVES) == 0, "whole loads per wave");
+    static constexpr int LOADS = T * STEP / 1024 / WAVES, ROW_CHUNKS = STEP / 16;                   // of 1 KB, per wave and step
+    static_assert(T * STEP % (1024 * WAVES) == 0, "whole loads per wave");
+    // ALONG: where the chunks of row r of the tile go
+    static __device__ __forceinline__ int turn(int r) { return STEP == 64 ? (r >> 1) & 3 : r & 7; }
     static constexpr int ROWB = T * E::ESZ, CHUNKS = ROWB / 16;   // ACROSS: a row of k
     // ACROSS, bf16: which group of four chunks goes where in row r of k; the same for r + 4.  Four rows of a read lie 64 bytes
     // apart in the banks (rows of 128 bytes: two and two).
@@ -108,19 +102,19 @@ struct Side {
     // group: of `split` that take the steps in turn
     __device__ __forceinline__ void init(const Operand& o, int64_t first, int64_t inner, int wave, int lane, int group, int split) {
         if constexpr (L == ALONG) {
-            p = o.data + first * o.stride + group * 64;
-            left = inner * E::ESZ - group * 64;
-            step = 64 * split;
-            chunk = uint32_t((lane & 3) ^ ((lane >> 3) & 3)) * 16u;
+            p = o.data + first * o.stride + group * STEP;
+            left = inner * E::ESZ - group * STEP;
+            step = STEP * split;
+            chunk = uint32_t((lane % ROW_CHUNKS) ^ turn(lane / ROW_CHUNKS)) * 16u;
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
-                const int r = (wave * LOADS + q) * 16 + (lane >> 2);
+                const int r = ((wave * LOADS + q) * 64 + lane) / ROW_CHUNKS;
                 off[q] = first + r < o.rows ? uint32_t(r) * uint32_t(o.stride) + chunk : NOWHERE;
             }
             const int r = lane & 31;
-            read0 = r * 64 + (((lane >> 5) ^ ((r >> 1) & 3)) << 4);
+            read0 = r * STEP + (((lane >> 5) ^ turn(r)) << 4);
         } else {
-            const int64_t one = int64_t(64 / E::ESZ) * o.stride;
+            const int64_t one = int64_t(STEP / E::ESZ) * o.stride;
             p = o.data + first * E::ESZ + group * one;
             left = inner * o.stride - first * E::ESZ - group * one;
             step = one * split;
@@ -149,7 +143,7 @@ struct Side {
         Step s;
         const int64_t range = L == ALONG ? 0x7FFFFFFF : left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
         s.rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, int(range), 0x00020000);
-        const int here = left > 64 ? 64 : int(left);
+        const int here = left > STEP ? STEP : int(left);
         s.mask = L == ALONG ? (int(chunk) < here ? 0u : NOWHERE) : 0u;
         p += step;
         left -= step;
@@ -161,7 +155,7 @@ struct Side {
     // fragment f of the tile (32 of n or m), half step s
     __device__ __forceinline__ uint4v read(const char* tile, int f, int s, int lane) const {
         if constexpr (L == ALONG) {
-            return *reinterpret_cast<const uint4v*>(tile + f * 2048 + (read0 ^ (s << 5)));
+            return *reinterpret_cast<const uint4v*>(tile + f * 32 * STEP + (read0 ^ (s << 5)));
         } else if constexpr (E::ESZ == 2) {
             const char* a = tile + s * 16 * ROWB + read0 + ((f ^ swizzle((lane & 15) >> 2)) << 6);
             const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a));
@@ -193,10 +187,10 @@ __device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Oper
     const int wr = wave / S::WC, wc = wave % S::WC;
     char* const all_lds = lds;
     lds += group * S::RING;
-    typedef Side<E, LA, S::TN, S::WAVES> SideA;
-    typedef Side<E, LB, S::TM, S::WAVES> SideB;
+    typedef Side<E, LA, S::TN, S::WAVES, S::STEP> SideA;
+    typedef Side<E, LB, S::TM, S::WAVES, S::STEP> SideB;
     constexpr int LOADS = SideA::LOADS + SideB::LOADS, FRAGS = FR + FC, PRODUCTS = FR * FC;
-    constexpr int B_AT = S::TN * 64;
+    constexpr int B_AT = S::TN * S::STEP, PARTS = S::STEP / 32;   // parts of a step: a fragment each
     SideA a;
     SideB b;
     a.init(A, n0, inner, wave, lane, group, S::SPLIT);
@@ -246,7 +240,7 @@ __device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Oper
         }
     };
     const int64_t bytes = inner * E::ESZ;
-    const int n_st = (int((bytes + 63) >> 6) + S::SPLIT - 1) / S::SPLIT;
+    const int n_st = (int((bytes + S::STEP - 1) / S::STEP) + S::SPLIT - 1) / S::SPLIT;
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS * (SLOTS - 2)));
     __syncthreads();
     {
@@ -263,14 +257,17 @@ __device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Oper
     };
     auto stage = [&](auto slot_c) __attribute__((always_inline)) {
         constexpr int slot = decltype(slot_c)::value, follow = (slot + 1) % SLOTS;
-        products(F0, [&](int n) __attribute__((always_inline)) {
-            constexpr int EARLY = PRODUCTS > FRAGS ? PRODUCTS / FRAGS : 1;        // a half step's reads in the first half of its products
-            if constexpr (EARLY > 1) {
-                if (n < FRAGS) read(F1, n, slot, 1);
-            } else {
-                share(n, FRAGS, [&](int r) __attribute__((always_inline)) { read(F1, r, slot, 1); });
-            }
-        });
+        auto early = [&](Frags& now, Frags& then, int part) __attribute__((always_inline)) {
+            products(now, [&](int n) __attribute__((always_inline)) {
+                if constexpr (PRODUCTS > FRAGS) {
+                    if (n < FRAGS) read(then, n, slot, part);
+                } else {
+                    share(n, FRAGS, [&](int r) __attribute__((always_inline)) { read(then, r, slot, part); });
+                }
+            });
+        };
+#pragma unroll
+        for (int part = 1; part < PARTS; ++part) early(part & 1 ? F0 : F1, part & 1 ? F1 : F0, part);
         // the next step has landed; every wave has read this one
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(LOADS * (SLOTS - 2)));
         __syncthreads();
@@ -321,16 +318,16 @@ __device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Oper
 }
 
 // f(shape) for a choice of tiles
-template <class F>
+template <int STEP, class F>
 auto with_shape(token::Tiles t, F&& f) {
     switch (t) {
-        case token::BIG: return f(Big{});
-        case token::MID: return f(Mid{});
-        case token::MID_SPLIT: return f(MidSplit{});
-        case token::HALF: return f(Half{});
-        case token::HALF_SPLIT: return f(HalfSplit{});
-        case token::SMALL: return f(Small{});
-        default: return f(SmallSplit{});
+        case token::BIG: return f(Shape<2, 2, 4, 4, STEP, 1, 1>{});          // 256 x 256
+        case token::MID: return f(Shape<2, 2, 2, 2, STEP, 1, 2>{});          // 128 x 128
+        case token::MID_SPLIT: return f(Shape<2, 2, 2, 2, STEP, 2, 1>{});
+        case token::HALF: return f(Shape<2, 2, 2, 1, STEP, 1, 3>{});         // 128 x 64
+        case token::HALF_SPLIT: return f(Shape<2, 2, 2, 1, STEP, 3, 1>{});
+        case token::SMALL: return f(Shape<2, 2, 1, 1, STEP, 1, 4>{});        // 64 x 64
+        default: return f(Shape<2, 2, 1, 1, STEP, 4, 1>{});
     }
 }
 
