@@ -616,7 +616,7 @@ onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scale
 size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
 
 /* The loss of a model's last layer.  h and weight: base addresses and strides of whole 16 bytes, width a multiple of 8 (bf16) or
- * 4 (fp32), row strides below 2^23 bytes; tokens, width and vocab at most 2^24. */
+ * 4 (fp32), row strides below 2^23 bytes; at most 2^20 tokens and a vocabulary of 2^24. */
 typedef struct {
     onecomp_dtype dtype;       /* of h, weight and their gradients */
     int64_t tokens, width, vocab;
@@ -640,7 +640,7 @@ size_t onecomp_token_loss_workspace_bytes(const onecomp_loss_shape* shape);
  * Gradients from those of the losses (d_loss) and of the log-sum-exps (d_lse, NULL if there are none), with lse as the forward call
  * left it:  g_tv = (d_loss_t + d_lse_t) exp(z_tv - lse_t) - d_loss_t [v = targets_t],
  *   dh_t = scale sum_v g_tv weight_v,  dweight_v = scale sum_t g_tv h_t.
- * Left-out tokens have dh 0 and no part in dweight.  The vocabulary is taken in pieces whose g (in dtype, 512 MB at most, or 2048
+ * Left-out tokens have dh 0 and no part in dweight.  The vocabulary is taken in pieces whose g (in dtype, 1 GB at most, or 2048
  * columns) lies in the workspace.  Sums in fp32, no atomics: the same inputs give the same bits.
  *   d_loss, d_lse  device fp32 [tokens]
  *   dh, dweight    like h and weight, overwritten, over none of the inputs; either may be NULL

@@ -179,7 +179,7 @@ onecomp_status check_loss(const onecomp_loss_shape* s) {
     if (!known(s->dtype)) return ONECOMP_ERR_UNSUPPORTED;
     if (s->tokens < 0 || s->width <= 0 || s->vocab <= 0 || !(s->scale > 0.f) || !std::isfinite(s->scale)) return ONECOMP_ERR_INVALID_ARG;
     const int64_t most = int64_t(1) << 24;
-    if (s->tokens > most || s->width > most || s->vocab > most || s->scale < 0x1p-100f || s->scale > 0x1p100f) return ONECOMP_ERR_UNSUPPORTED;
+    if (s->tokens > (int64_t(1) << 20) || s->width > most || s->vocab > most || s->scale < 0x1p-100f || s->scale > 0x1p100f) return ONECOMP_ERR_UNSUPPORTED;
     if (s->width * int64_t(size_of(s->dtype)) % 16 != 0 || s->width * int64_t(size_of(s->dtype)) >= (int64_t(1) << 23)) return ONECOMP_ERR_UNSUPPORTED;
     // workgroups of a launch: tiles of 128 x 128
     if (ceil_div(s->tokens, 128) * ceil_div(s->vocab, 128) > (int64_t(1) << 30)) return ONECOMP_ERR_UNSUPPORTED;

@@ -17,6 +17,8 @@ namespace {
 using product::ACROSS;
 using product::ALONG;
 using product::Operand;
+using product::PANELS_ACROSS;
+using product::PANELS_ALONG;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -30,7 +32,8 @@ struct Gather {
     int64_t h_stride, width_bytes;           // bytes
     int tokens, vocab;
     int32_t *count, *index, *place;
-    char* rows;
+    char* rows;                              // in panels
+    int64_t panel;
     // forward: target per kept token; what left-out tokens get
     int32_t* target;
     float *loss, *lse_out;
@@ -40,7 +43,7 @@ struct Gather {
 };
 
 // A workgroup takes 64 tokens: it counts the kept ones in front of its own (reading all targets before them: 256 KB from the
-// L2 for the last of 65536 tokens), numbers its own and copies a part of the columns of their rows.
+// L2 for the last of 65536 tokens), numbers its own and copies a part of their rows.
 __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
     __shared__ int s_before[4], s_index[64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * 64;
@@ -75,22 +78,8 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
         if (lane == 0 && first + 64 >= g.tokens) *g.count = before + many;
     }
     __syncthreads();
-    // 1 KB of a row at a time, eight on their way
-    const int chunks = int(g.width_bytes >> 4), blocks = (chunks + 63) / 64, all = many * blocks;
-    const uint4v* const from = reinterpret_cast<const uint4v*>(g.h);
-    for (int i0 = (blockIdx.y * 4 + wave) * 8; i0 < all; i0 += gridDim.y * 32) {
-        uint4v v[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int r = (i0 + u) / blocks, c = (i0 + u) % blocks * 64 + lane;
-            if (i0 + u < all && c < chunks) v[u] = from[int64_t(s_index[r]) * (g.h_stride >> 4) + c];
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int r = (i0 + u) / blocks, c = (i0 + u) % blocks * 64 + lane;
-            if (i0 + u < all && c < chunks) reinterpret_cast<uint4v*>(g.rows + int64_t(before + r) * g.width_bytes)[c] = v[u];
-        }
-    }
+    product::rows_to_panels([&](int r) __attribute__((always_inline)) { return g.h + s_index[r] * g.h_stride; }, many, g.width_bytes,
+                            g.rows + int64_t(before) * 64, g.panel, blockIdx.y * 4 + wave, gridDim.y * 4);
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
@@ -104,7 +93,7 @@ struct Logits {
     const int32_t* count;
     const int32_t* target;
     int64_t inner;
-    int vocab;
+    int columns;                             // of the vocabulary
     float c;                                 // scale log2(e)
     float2* parts;                           // [token][part of the vocabulary]: maximum (in powers of two) and sum
     float* hit;
@@ -116,17 +105,17 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Log
     extern __shared__ __align__(1024) char lds[];
     const int count = *P.count;
     int tm, tn;
-    if (!product::my_tile((count + S::TM - 1) / S::TM, (P.vocab + S::TN - 1) / S::TN, tm, tn)) return;
+    if (!product::my_tile((count + S::TM - 1) / S::TM, (P.columns + S::TN - 1) / S::TN, tm, tn)) return;
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
-    if (!product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
+    if (!product::multiply<E, ALONG, PANELS_ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
     __syncthreads();
     // A lane holds 16 FR logits of a token: maximum, sum of powers, joined with the other half's and, through LDS, with the other
     // waves' of these tokens.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / S::WC, wc = wave % S::WC, half = lane >> 5;
     float2* red = reinterpret_cast<float2*>(lds);
-    const int left = P.vocab - int(n0) - wr * S::FR * 32;          // of this wave's part
+    const int left = P.columns - int(n0) - wr * S::FR * 32;          // of this wave's part
     if (left < S::FR * 32) {
 #pragma unroll
         for (int i = 0; i < S::FR; ++i)
@@ -183,10 +172,10 @@ __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Log
     const int64_t n0 = int64_t(blockIdx.x) * 32;
     if (count == 0) return;
     P.rows.rows = count;
-    product::multiply_few<E, 2, TF>(lds, P.weight, P.rows, n0, P.inner);
+    product::multiply_few<E, 2, TF, PANELS_ALONG>(lds, P.weight, P.rows, n0, P.inner);
     const int n = threadIdx.x & 31;
     for (int m = threadIdx.x >> 5; m < count; m += 2 * product::FEW_WAVES) {
-        const float x = n0 + n < P.vocab ? reinterpret_cast<const float*>(lds)[m * 32 + n] : -__builtin_inff();
+        const float x = n0 + n < P.columns ? reinterpret_cast<const float*>(lds)[m * 32 + n] : -__builtin_inff();
         float top = x;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
@@ -242,8 +231,8 @@ struct LogitGrads {
     int64_t inner;
     int first, columns;                      // of the piece
     float c;
-    char* piece;                             // [token][column]
-    int64_t stride;                          // bytes
+    char* piece;                             // the gradients, tokens as rows, in panels
+    int64_t panel;
 };
 
 __device__ __forceinline__ void store_four(uint16_t* p, const float (&x)[4]) {
@@ -269,7 +258,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kerne
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.rows.rows = count;
     float16v acc[S::FR][S::FC];
-    if (!product::multiply<E, ALONG, ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
+    if (!product::multiply<E, ALONG, PANELS_ALONG, S>(lds, P.weight, P.rows, n0, m0, P.inner, acc)) return;
     const int wc = int(threadIdx.x >> 6) % S::WC, lane = threadIdx.x & 63;
     float4 coef[S::FC];
 #pragma unroll
@@ -290,13 +279,13 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kerne
             }
         },
         [&](int m) __attribute__((always_inline)) {
-            return m0 + m < count ? reinterpret_cast<typename E::T*>(P.piece + (m0 + m) * P.stride) + n0 : nullptr;
+            return m0 + m < count ? reinterpret_cast<typename E::T*>(P.piece + n0 * E::ESZ / 64 * P.panel + (m0 + m) * 64) : nullptr;
         },
-        S::TN);
+        S::TN, P.panel);
 }
 
 struct GradRows {
-    Operand weight, piece;                   // ACROSS, ALONG
+    Operand weight, piece;                   // ACROSS, PANELS_ALONG
     const int32_t* count;
     int columns, full;                       // of this piece; of the largest
     int most, add;                           // shares that there is room for; whether there is something to add to
@@ -316,10 +305,10 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(
     const int inner = P.columns - begin < each ? P.columns - begin : each;
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     P.weight.data += int64_t(begin) * P.weight.stride;
-    P.piece.data += int64_t(begin) * E::ESZ;
+    P.piece.data += int64_t(begin) * E::ESZ / 64 * P.piece.stride;
     P.piece.rows = count;
     float16v acc[S::FR][S::FC];
-    if (!product::multiply<E, ACROSS, ALONG, S>(lds, P.weight, P.piece, n0, m0, inner < 0 ? 0 : inner, acc)) return;
+    if (!product::multiply<E, ACROSS, PANELS_ALONG, S>(lds, P.weight, P.piece, n0, m0, inner < 0 ? 0 : inner, acc)) return;
     __syncthreads();
     float* const out = P.out + share * P.tokens * P.width;
     auto value = [&](float (&x)[4], int i, int j, int q, int, int) __attribute__((always_inline)) {
@@ -332,7 +321,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(
 }
 
 struct GradWeight {
-    Operand rows, piece;                     // both ACROSS
+    Operand rows, piece;                     // both PANELS_ACROSS
     const int32_t* count;
     int columns, width;
     float scale;
@@ -346,7 +335,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_weight_kerne
     if (!product::my_tile((P.columns + S::TM - 1) / S::TM, (P.width + S::TN - 1) / S::TN, tm, tn)) return;
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     float16v acc[S::FR][S::FC];
-    if (!product::multiply<E, ACROSS, ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc)) return;
+    if (!product::multiply<E, PANELS_ACROSS, PANELS_ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc)) return;
     __syncthreads();
     product::store_tile<typename E::T, S, false>(
         lds,
@@ -406,7 +395,7 @@ onecomp_status with_tiles(int64_t m, int64_t n, F&& f) {
 template <class E, class S>
 onecomp_status run_logits(const Logits& P, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return launch(logits_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.vocab, S::TN)), 1, P, done, stream);
+    return launch(logits_kernel<E, S>, S::LDS, S::ALL_THREADS, product::tile_blocks(ceil_div(P.tokens, S::TM), ceil_div(P.columns, S::TN)), 1, P, done, stream);
 }
 template <class E, class S>
 onecomp_status run_logit_grads(const LogitGrads& P, int64_t tokens, hipStream_t stream) {
@@ -448,6 +437,7 @@ onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient,
     g.count = reinterpret_cast<int32_t*>(ws + s.count);
     g.index = reinterpret_cast<int32_t*>(ws + s.index);
     g.rows = ws + s.rows;
+    g.panel = P.tokens * 64;
     if (gradient) {
         g.place = reinterpret_cast<int32_t*>(ws + s.place);
         g.coef = reinterpret_cast<float4*>(ws + s.coef);
@@ -462,7 +452,7 @@ onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient,
     // about two workgroups per compute unit, as long as there are 8 KB of rows for each
     const int64_t groups = P.tokens ? ceil_div(P.tokens, 64) : 1, bytes = (P.tokens < 64 ? P.tokens : 64) * g.width_bytes;
     int64_t parts = ceil_div(512, groups);
-    if (parts > bytes >> 13) parts = bytes >> 13;
+    if (parts > bytes >> 13) parts = bytes >> 13;                  // (a wave's unit of work)
     gather_kernel<<<dim3(unsigned(groups), unsigned(parts < 1 ? 1 : parts)), dim3(256), 0, stream>>>(g);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
@@ -474,17 +464,17 @@ onecomp_status forward(const Loss& P, hipStream_t stream) {
     char* ws = static_cast<char*>(P.workspace);
     if (const onecomp_status st = gather(P, s, E::ESZ, false, stream)) return st;
     Logits L{};
-    L.weight = Operand{static_cast<const char*>(P.weight.p), P.weight.stride * E::ESZ, P.vocab};
-    L.rows = Operand{ws + s.rows, P.width * E::ESZ, P.tokens};
+    L.rows = Operand{ws + s.rows, P.tokens * 64, P.tokens};
     L.count = reinterpret_cast<const int32_t*>(ws + s.count);
     L.target = reinterpret_cast<const int32_t*>(ws + s.coef);
     L.inner = P.width;
-    L.vocab = int(P.vocab);
     L.c = P.scale * LOG2E;
     L.parts = reinterpret_cast<float2*>(ws + s.parts);
     L.hit = reinterpret_cast<float*>(ws + s.hit);
     L.tokens = P.tokens;
     L.n_parts = n_parts(P.tokens, P.vocab);
+    L.weight = Operand{static_cast<const char*>(P.weight.p), P.weight.stride * E::ESZ, P.vocab};
+    L.columns = int(P.vocab);
     const onecomp_status st = P.tokens <= FEW ? run_few_logits<E>(L, stream)
                                               : with_tiles(P.tokens, P.vocab, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); });
     if (st) return st;
@@ -501,14 +491,13 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
     char* ws = static_cast<char*>(P.workspace);
     if (const onecomp_status st = gather(P, s, E::ESZ, true, stream)) return st;
     const int32_t* count = reinterpret_cast<const int32_t*>(ws + s.count);
-    const Operand rows{ws + s.rows, P.width * E::ESZ, P.tokens};
-    const int64_t pitch = s.columns * E::ESZ;
+    const int64_t panel = P.tokens * 64;     // of what has tokens for rows
     for (int64_t first = 0; first < P.vocab; first += s.columns) {
         const int64_t columns = P.vocab - first < s.columns ? P.vocab - first : s.columns;
-        const char* w = static_cast<const char*>(P.weight.p) + first * P.weight.stride * E::ESZ;
+        const char* const w = static_cast<const char*>(P.weight.p) + first * P.weight.stride * E::ESZ;
         LogitGrads G{};
         G.weight = Operand{w, P.weight.stride * E::ESZ, columns};
-        G.rows = rows;
+        G.rows = Operand{ws + s.rows, panel, P.tokens};
         G.count = count;
         G.coef = reinterpret_cast<const float4*>(ws + s.coef);
         G.inner = P.width;
@@ -516,14 +505,14 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
         G.columns = int(columns);
         G.c = P.scale * LOG2E;
         G.piece = ws + s.piece;
-        G.stride = pitch;
+        G.panel = panel;
         if (const onecomp_status st =
                 with_tiles(P.tokens, columns, [&](auto shape) { return run_logit_grads<E, decltype(shape)>(G, P.tokens, stream); }))
             return st;
         if (P.dh.p) {
             GradRows R{};
             R.weight = Operand{w, P.weight.stride * E::ESZ, P.width};
-            R.piece = Operand{ws + s.piece, pitch, P.tokens};
+            R.piece = Operand{ws + s.piece, panel, P.tokens};
             R.count = count;
             R.columns = int(columns);
             R.full = int(s.columns);
@@ -532,12 +521,14 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             R.out = reinterpret_cast<float*>(ws + s.dh);
             R.tokens = P.tokens;
             R.width = int(P.width);
-            if (const onecomp_status st = with_tiles(P.tokens, P.width, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); })) return st;
+            if (const onecomp_status st =
+                    with_tiles(P.tokens, P.width, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); }))
+                return st;
         }
         if (P.dweight.p) {
             GradWeight W{};
-            W.rows = Operand{ws + s.rows, P.width * E::ESZ, P.width};
-            W.piece = Operand{ws + s.piece, pitch, s.columns};
+            W.rows = Operand{ws + s.rows, panel, P.width};
+            W.piece = Operand{ws + s.piece, panel, s.columns};
             W.count = count;
             W.columns = int(columns);
             W.width = int(P.width);

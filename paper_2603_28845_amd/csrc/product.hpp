@@ -15,6 +15,10 @@
 //   ACROSS  rows of k as they are; in bf16 their chunks lie permuted by fours (Side::swizzle) and fragments are transposed
 //           reads; in fp32 a fragment is four plain reads.
 // What lies behind the operands' ends becomes zeros by the loads' bounds check.
+//
+// The loss's operands come in panels where they are written here: 64 bytes of the columns of all rows, [panel][row][64 bytes].  A
+// wave's load is then 1 KB of memory instead of 64 bytes in each of 16 rows (16384 x 32000 logits, k 4096, bf16: 1.22 PFLOP/s from
+// rows, 1.34 from panels).  The same panels serve products along the columns (PANELS_ALONG) and along the rows (PANELS_ACROSS).
 #pragma once
 #include "common.hpp"
 #include "token_plan.hpp"
@@ -60,10 +64,12 @@ struct Int8 {
     }
 };
 
-enum Layout { ALONG, ACROSS };
+enum Layout { ALONG, ACROSS, PANELS_ALONG, PANELS_ACROSS };
+constexpr bool across(Layout l) { return l == ACROSS || l == PANELS_ACROSS; }
+constexpr bool panels(Layout l) { return l == PANELS_ALONG || l == PANELS_ACROSS; }
 
-// rows: how many n (m) there are; stride: bytes between rows of n (ALONG) or of k (ACROSS), below 2^23 and, like the address, a
-// multiple of 16
+// rows: how many n (m) there are; stride: bytes between rows of n (ALONG) or of k (ACROSS), below 2^23, or between panels; like the
+// address, a multiple of 16
 struct Operand {
     const char* data;
     int64_t stride, rows;
@@ -86,86 +92,105 @@ constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
 // One operand's tile: how a wave brings its part of a step to LDS, and how a lane reads fragments from there.
 template <class E, Layout L, int T, int WAVES, int STEP>
 struct Side {
-    static constexpr int LOADS = T * STEP / 1024 / WAVES, ROW_CHUNKS = STEP / 16;                   // of 1 KB, per wave and step
+    static constexpr int LOADS = T * STEP / 1024 / WAVES, ROW_CHUNKS = STEP / 16;   // loads of 1 KB, per wave and step
     static_assert(T * STEP % (1024 * WAVES) == 0, "whole loads per wave");
-    // ALONG: where the chunks of row r of the tile go
-    static __device__ __forceinline__ int turn(int r) { return STEP == 64 ? (r >> 1) & 3 : r & 7; }
+    static_assert(!panels(L) || STEP == 64, "a panel is a step along the columns");
+    static_assert(!across(L) || E::ESZ != 1, "no transposed reads of bytes here");
     static constexpr int ROWB = T * E::ESZ, CHUNKS = ROWB / 16;   // ACROSS: a row of k
+    static constexpr int PER_PANEL = E::ESZ == 2 ? 2 : 1;         // PANELS_ACROSS: loads of a step's rows of one panel
+    // along k: where the chunks of row r of the tile go
+    static __device__ __forceinline__ int turn(int r) { return STEP == 64 ? (r >> 1) & 3 : r & 7; }
     // ACROSS, bf16: which group of four chunks goes where in row r of k; the same for r + 4.  Four rows of a read lie 64 bytes
     // apart in the banks (rows of 128 bytes: two and two).
     static __device__ __forceinline__ int swizzle(int r) { return CHUNKS >= 16 ? r & 3 : (r >> 1) & 1; }
-    static_assert(L == ALONG || E::ESZ != 2 || CHUNKS == 8 || CHUNKS % 16 == 0, "the swizzle stays inside a row");
-    uint32_t off[LOADS], chunk;
+    static_assert(L != ACROSS || E::ESZ != 2 || CHUNKS == 8 || CHUNKS % 16 == 0, "the swizzle stays inside a row");
+    uint32_t off[LOADS], lane_at;                                 // lane_at: where the lane's 16 bytes lie in a step of a row or panel
     const char* p;
-    int64_t left, step;                                           // bytes: what is left of the operand (ALONG: of a row), one step
+    int64_t left, step, taken;                                    // bytes: what is left of the operand (of a row, of a panel); a step's in memory, of `left`
     int read0;
     // group: of `split` that take the steps in turn
     __device__ __forceinline__ void init(const Operand& o, int64_t first, int64_t inner, int wave, int lane, int group, int split) {
-        if constexpr (L == ALONG) {
-            p = o.data + first * o.stride + group * STEP;
+        const int i16 = lane & 15, kq = i16 >> 2, half = lane >> 5, r32 = lane & 31;
+        if constexpr (!across(L)) {
+            const int64_t row = L == ALONG ? o.stride : 64, one = L == ALONG ? STEP : o.stride;
+            p = o.data + first * row + group * one;
             left = inner * E::ESZ - group * STEP;
-            step = STEP * split;
-            chunk = uint32_t((lane % ROW_CHUNKS) ^ turn(lane / ROW_CHUNKS)) * 16u;
+            step = one * split;
+            taken = STEP * split;
+            lane_at = uint32_t((lane % ROW_CHUNKS) ^ turn(lane / ROW_CHUNKS)) * 16u;
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
                 const int r = ((wave * LOADS + q) * 64 + lane) / ROW_CHUNKS;
-                off[q] = first + r < o.rows ? uint32_t(r) * uint32_t(o.stride) + chunk : NOWHERE;
+                off[q] = first + r < o.rows ? uint32_t(r) * uint32_t(row) + lane_at : NOWHERE;
             }
-            const int r = lane & 31;
-            read0 = r * STEP + (((lane >> 5) ^ turn(r)) << 4);
-        } else {
+            read0 = r32 * STEP + ((half ^ turn(r32)) << 4);
+        } else if constexpr (L == ACROSS) {
             const int64_t one = int64_t(STEP / E::ESZ) * o.stride;
             p = o.data + first * E::ESZ + group * one;
             left = inner * o.stride - first * E::ESZ - group * one;
-            step = one * split;
-            chunk = 0;
+            step = taken = one * split;
+            lane_at = 0;
 #pragma unroll
             for (int q = 0; q < LOADS; ++q) {
                 const int at = (wave * LOADS + q) * 64 + lane, r = at / CHUNKS;
                 const int c = (at % CHUNKS) ^ (E::ESZ == 2 ? swizzle(r) << 2 : 0);
                 off[q] = first + c * (16 / E::ESZ) < o.rows ? uint32_t(r) * uint32_t(o.stride) + uint32_t(c) * 16u : NOWHERE;
             }
-            if constexpr (E::ESZ == 2) {
-                // inside 16 lanes, lane 4 k + c points at four columns of row k and lane i receives column i of rows 0 .. 3
-                const int i16 = lane & 15, kq = i16 >> 2;
-                read0 = ((lane >> 5) * 8 + kq) * ROWB + (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
-            } else {
-                read0 = (lane >> 5) * 4 * ROWB + (lane & 31) * 4;
+            // bf16: inside 16 lanes, lane 4 k + c points at four columns of row k and lane i receives column i of rows 0 .. 3
+            if constexpr (E::ESZ == 2) read0 = (half * 8 + kq) * ROWB + (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+            else read0 = half * 4 * ROWB + r32 * 4;
+        } else {
+            constexpr int ROWS = 64 / E::ESZ;                     // of k, per step
+            p = o.data + first * E::ESZ / 64 * o.stride + group * (ROWS * 64);
+            left = inner * 64 - group * (ROWS * 64);
+            step = taken = int64_t(ROWS * 64) * split;
+            lane_at = uint32_t(lane) * 16u;
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) {
+                const int j = wave * LOADS + q, panel = j / PER_PANEL;
+                off[q] = first + panel * (64 / E::ESZ) < o.rows ? uint32_t(panel) * uint32_t(o.stride) + uint32_t(j % PER_PANEL) * 1024u + lane_at : NOWHERE;
             }
+            // a fragment's 32 columns: a panel of 64 bytes a row (bf16), two panels (fp32)
+            if constexpr (E::ESZ == 2) read0 = (half * 8 + kq) * 64 + (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+            else read0 = (r32 >> 4) * 1024 + half * 4 * 64 + (r32 & 15) * 4;
         }
     }
     struct Step {
         __amdgpu_buffer_rsrc_t rsrc;
-        uint32_t mask;
+        uint32_t mask[PER_PANEL];
     };
-    // the next step: an empty range (or mask) behind the last one
+    // the next step: an empty range, or masks, behind the last one
     __device__ __forceinline__ Step next() {
         Step s;
-        const int64_t range = L == ALONG ? 0x7FFFFFFF : left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
+        const int64_t range = L != ACROSS ? 0x7FFFFFFF : left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
         s.rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, int(range), 0x00020000);
-        const int here = left > STEP ? STEP : int(left);
-        s.mask = L == ALONG ? (int(chunk) < here ? 0u : NOWHERE) : 0u;
+        const int here = left > 4096 ? 4096 : left < 0 ? 0 : int(left);
+#pragma unroll
+        for (int i = 0; i < PER_PANEL; ++i) s.mask[i] = L == ACROSS || int(lane_at) + i * 1024 < here ? 0u : NOWHERE;
         p += step;
-        left -= step;
+        left -= taken;
         return s;
     }
     __device__ __forceinline__ void load(const Step& s, uint32_t lds, int wave, int q) const {
-        lds_load16(lds + uint32_t(wave * LOADS + q) * 1024u, L == ALONG ? off[q] | s.mask : off[q], s.rsrc);
+        const uint32_t mask = PER_PANEL == 2 && L == PANELS_ACROSS && ((wave * LOADS + q) & 1) ? s.mask[PER_PANEL - 1] : s.mask[0];
+        lds_load16(lds + uint32_t(wave * LOADS + q) * 1024u, L == ACROSS ? off[q] : off[q] | mask, s.rsrc);
     }
-    // fragment f of the tile (32 of n or m), half step s
+    // fragment f of the tile (32 of n or m), 32 bytes s of the step
     __device__ __forceinline__ uint4v read(const char* tile, int f, int s, int lane) const {
-        if constexpr (L == ALONG) {
+        if constexpr (!across(L)) {
             return *reinterpret_cast<const uint4v*>(tile + f * 32 * STEP + (read0 ^ (s << 5)));
         } else if constexpr (E::ESZ == 2) {
-            const char* a = tile + s * 16 * ROWB + read0 + ((f ^ swizzle((lane & 15) >> 2)) << 6);
+            constexpr int ROW = L == ACROSS ? ROWB : 64;
+            const char* a = tile + s * 16 * ROW + read0 + (L == ACROSS ? (f ^ swizzle((lane & 15) >> 2)) << 6 : f * 2048);
             const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a));
-            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 4 * ROWB));
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ONECOMP_LDS short4v*)(a + 4 * ROW));
             return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const char* a = tile + s * 8 * ROWB + read0 + f * 128;
+            constexpr int ROW = L == ACROSS ? ROWB : 64;
+            const char* a = tile + s * 8 * ROW + read0 + f * (L == ACROSS ? 128 : 2048);
             uint4v v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(a + i * ROWB);
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(a + i * ROW);
             return v;
         }
     }
@@ -331,6 +356,29 @@ auto with_shape(token::Tiles t, F&& f) {
     }
 }
 
+// Rows to panels: row r of the result is row(r) of the source (nullptr: nothing is there), row_bytes long (a multiple of 16); what is
+// behind a row's end in its last panel becomes zeros.  A wave takes 16 rows of eight panels at a time: 512 bytes a row in, 1 KB
+// out per panel.  `units` of these are shared out over the workgroups from `unit` on in steps of `stride`.
+template <class R>
+__device__ __forceinline__ void rows_to_panels(R&& row, int rows, int64_t row_bytes, char* to, int64_t panel, int unit, int stride) {
+    const int lane = threadIdx.x & 63, c = lane & 3;
+    const int n_panels = int((row_bytes + 63) >> 6), eights = (n_panels + 7) / 8, units = (rows + 15) / 16 * eights;
+    for (; unit < units; unit += stride) {
+        const int r = unit / eights * 16 + (lane >> 2), first = unit % eights * 8;
+        const char* const from = r < rows ? row(r) : nullptr;
+        uint4v v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t at = int64_t(first + u) * 64 + c * 16;
+            v[u] = uint4v{0u, 0u, 0u, 0u};
+            if (from && at < row_bytes) v[u] = *reinterpret_cast<const uint4v*>(from + at);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (r < rows && first + u < n_panels) *reinterpret_cast<uint4v*>(to + (first + u) * panel + r * 64 + c * 16) = v[u];
+    }
+}
+
 // tile_of for a workgroup of this launch, in scalar registers
 __device__ __forceinline__ bool my_tile(int m_tiles, int n_tiles, int& tm, int& tn) {
     if (!tile_of(blockIdx.x, m_tiles, n_tiles, tm, tn)) return false;
@@ -344,12 +392,14 @@ __device__ __forceinline__ bool my_tile(int m_tiles, int n_tiles, int& tm, int& 
 //   value(x, i, j, q, n, m)   four neighbours of n from acc[i][j][4 q ..]; n and m inside the tile
 //   row(m)                    address of n = 0 of the tile in row m of the tile, or nullptr: no such row
 //   left                      how many n there are from the tile's first on
-// ADD: added to what is there (fp32).  lds: the tile's, behind a barrier; OUT_LDS bytes of it are used.
+//   panel                     0: rows are dense; else rows are 64 bytes of the tile's panels, which are so many bytes apart (all of them
+//                             are written)
+// ADD: added to what is there (fp32).  lds: the tile's, behind a barrier; out_lds() bytes of it are used.
 template <class T, class S>
 constexpr int out_lds() { return S::WAVES * 32 * (32 * S::FR * int(sizeof(T)) + 16); }
 
 template <class T, class S, bool ADD, class V, class R>
-__device__ __forceinline__ void store_tile(char* lds, V&& value, R&& row, int64_t left) {
+__device__ __forceinline__ void store_tile(char* lds, V&& value, R&& row, int64_t left, int64_t panel = 0) {
     constexpr int NW = 32 * S::FR, PITCH = NW * int(sizeof(T)) + 16, CHUNKS = NW * int(sizeof(T)) / 16, N = 16 / int(sizeof(T));
     static_assert(out_lds<T, S>() <= S::LDS, "room in the tile's LDS");
     static_assert(!ADD || sizeof(T) == 4, "added in 32 bits");
@@ -382,7 +432,14 @@ __device__ __forceinline__ void store_tile(char* lds, V&& value, R&& row, int64_
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int it = 0; it < CHUNKS / 2; ++it) {
-            const int id = it * 64 + lane, r = id / CHUNKS, c = id % CHUNKS, n = wr * NW + c * N;
+            const int id = it * 64 + lane;
+            if (panel) {
+                const int r = id % 128 / 4, c = id / 128 * 4 + id % 4;
+                T* const to = row((wc * S::FC + j) * 32 + r);
+                if (to) *reinterpret_cast<uint4v*>(reinterpret_cast<char*>(to) + (wr * (CHUNKS / 4) + id / 128) * panel + id % 4 * 16) = *reinterpret_cast<const uint4v*>(mine + r * PITCH + c * 16);
+                continue;
+            }
+            const int r = id / CHUNKS, c = id % CHUNKS, n = wr * NW + c * N;
             uint4v v = *reinterpret_cast<const uint4v*>(mine + r * PITCH + c * 16);
             T* const to = row((wc * S::FC + j) * 32 + r);
             if (!to || n >= left) continue;
@@ -433,7 +490,8 @@ template <int RF, int TF>
 constexpr int few_lds() { return FEW_WAVES * 16 * RF * 16 * TF * 4; }
 
 // sums[n + 16 RF m] in the first 1024 RF TF bytes of lds, behind a barrier
-template <class E, int RF, int TF>
+// (B: ALONG or PANELS_ALONG)
+template <class E, int RF, int TF, Layout LB>
 __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t inner) {
     typedef typename Few<E>::Acc Acc;
     constexpr int AHEAD = RF + TF >= 5 ? 2 : 4;                   // steps on their way at a time
@@ -449,7 +507,7 @@ __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const 
 #pragma unroll
     for (int j = 0; j < TF; ++j) {
         const int r = j * 16 + (lane & 15);
-        bt[j] = r < B.rows ? uint32_t(r) * uint32_t(B.stride) + chunk : NOWHERE;
+        bt[j] = r < B.rows ? uint32_t(r) * uint32_t(LB == ALONG ? B.stride : 64) + chunk : NOWHERE;
     }
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(A.data + n0 * A.stride), 0, 0x7FFFFFFF, 0x00020000);
     const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(B.data), 0, 0x7FFFFFFF, 0x00020000);
@@ -472,7 +530,8 @@ __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const 
 #pragma unroll
             for (int i = 0; i < RF; ++i) x.a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, there && at[i] != NOWHERE ? at[i] + k : NOWHERE, 0, 0);
 #pragma unroll
-            for (int j = 0; j < TF; ++j) x.b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, there && bt[j] != NOWHERE ? bt[j] + k : NOWHERE, 0, 0);
+            for (int j = 0; j < TF; ++j)
+                x.b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, there && bt[j] != NOWHERE ? bt[j] + uint32_t(LB == ALONG ? k : (s0 + u) * int(B.stride)) : NOWHERE, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };

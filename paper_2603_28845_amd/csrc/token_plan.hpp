@@ -90,8 +90,8 @@ inline Tiles choose_tiles(int64_t m, int64_t n) {
 // ---- loss ----
 // Columns of the vocabulary that leave one maximum and sum per token.
 inline int64_t part_columns(int64_t tokens, int64_t vocab) { return tokens <= FEW ? 32 : shape_of(choose_tiles(tokens, vocab)).n; }
-// Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns.
-constexpr int64_t PIECE_BYTES = int64_t(512) << 20;
+// Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns: 1 GB of them.
+constexpr int64_t PIECE_BYTES = int64_t(1) << 30;
 inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
     const int64_t rows = ceil_of(tokens < 1 ? 1 : tokens, 256) * 256, all = ceil_of(vocab, 256) * 256;
     int64_t c = PIECE_BYTES / (rows * esz) / 256 * 256;
@@ -120,10 +120,14 @@ ONECOMP_TOKEN_FN int shares_of(int tiles, int columns, int slots, int most) {
     return best;
 }
 
+inline int64_t round_up(int64_t x, int64_t to) { return ceil_of(x, to) * to; }
+
 struct LossSpace {
     size_t index, place, count, coef, rows, parts, hit, piece, dh, all;
     int64_t columns, shares;
 };
+// Rows in panels.
+inline size_t panel_bytes(int64_t rows, int64_t width, int esz) { return size_t(rows) * size_t(round_up(width * esz, 64)); }
 // n_parts: tiles of the vocabulary that leave a maximum and a sum per token
 inline LossSpace loss_space(int64_t tokens, int64_t width, int64_t vocab, int esz, int64_t n_parts, bool gradient) {
     LossSpace s{};
@@ -138,13 +142,13 @@ inline LossSpace loss_space(int64_t tokens, int64_t width, int64_t vocab, int es
     s.index = take(t * 4);
     s.place = take(gradient ? t * 4 : 0);
     s.coef = take(t * (gradient ? 16 : 4));
-    s.rows = take(t * size_t(width) * esz);
+    s.rows = take(panel_bytes(tokens, width, esz));
     s.parts = take(gradient ? 0 : t * size_t(n_parts) * 8);
     s.hit = take(gradient ? 0 : t * 4);
     if (gradient) {
         s.columns = piece_columns(tokens, vocab, esz);
         s.shares = most_shares(tokens, width);
-        s.piece = take(t * size_t(s.columns) * esz);
+        s.piece = take(panel_bytes(tokens, s.columns, esz));
         s.dh = take(t * size_t(width) * 4 * size_t(s.shares));
     }
     s.all = at;

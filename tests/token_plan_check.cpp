@@ -50,34 +50,34 @@ static void check_embedding() {
 
 static void check_loss() {
     for (int esz : {2, 4})
-        for (int64_t tokens : {0, 1, 100, 4096, 16384, 100000, 1 << 24})
-            for (int64_t vocab : {1, 255, 256, 257, 5000, 128000, 1 << 20, 1 << 24}) {
-                const int64_t c = piece_columns(tokens, vocab, esz);
-                REQUIRE(c > 0 && c % 256 == 0 && c < vocab + 256 + 2048, "%ld %ld", long(tokens), long(vocab));
-                REQUIRE(c <= 2048 || tokens * c * esz <= PIECE_BYTES, "%ld %ld", long(tokens), long(vocab));
-                for (int64_t width : {4, 64, 4096}) {
-                    const int64_t shares = most_shares(tokens, width);
-                    REQUIRE(shares >= 1 && shares <= 16, "%ld", long(shares));
-                    for (int tiles : {0, 1, 20, 255, 256, 257, 320, 5000}) {
-                        const int taken = shares_of(tiles, int(c), 256, int(shares));
-                        REQUIRE(taken >= 1 && taken <= shares, "%d of %ld", taken, long(shares));
-                    }
+        for (int64_t tokens : {0, 1, 64, 65, 100, 1535, 1536, 4096, 16384, 100000, 1 << 20})
+            for (int64_t vocab : {1, 255, 256, 257, 5000, 128000, 1 << 20, 1 << 24})
+                for (int64_t width : {8, 64, 1000, 4096, 8192}) {
+                    const size_t t = size_t(tokens), row = size_t(ceil_of(width * esz, 64) * 64);
+                    const int64_t parts = ceil_of(vocab, part_columns(tokens, vocab));
                     for (bool gradient : {false, true}) {
-                        const LossSpace s = loss_space(tokens, width, vocab, esz, ceil_of(vocab, 128), gradient);
-                        const size_t t = size_t(tokens);
+                        const LossSpace s = loss_space(tokens, width, vocab, esz, parts, gradient);
+                        const int64_t c = s.columns, shares = s.shares;
                         REQUIRE(s.index >= s.count + 4 && s.coef >= s.index + 4 * t && s.rows >= s.coef + (gradient ? 16 : 4) * t, "%ld", long(tokens));
                         if (gradient) {
+                            REQUIRE(c > 0 && c % 256 == 0 && c < vocab + 256 + 2048, "%ld %ld", long(tokens), long(vocab));
+                            REQUIRE(c <= 2048 || tokens * c * esz <= PIECE_BYTES, "%ld %ld", long(tokens), long(vocab));
                             REQUIRE(s.place >= s.index + 4 * t && s.coef >= s.place + 4 * t, "%ld", long(tokens));
-                            REQUIRE(s.piece >= s.rows + t * size_t(width) * esz && s.dh >= s.piece + t * size_t(s.columns) * esz, "%ld", long(tokens));
-                            REQUIRE(s.all >= s.dh + t * size_t(width) * 4 * size_t(s.shares), "%ld", long(tokens));
+                            REQUIRE(s.piece >= s.rows + t * row && s.dh >= s.piece + t * size_t(c) * esz, "%ld", long(tokens));
+                            REQUIRE(s.all >= s.dh + t * size_t(width) * 4 * size_t(shares), "%ld", long(tokens));
+                            REQUIRE(shares >= 1 && shares <= 16, "%ld", long(shares));
+                            for (int tiles : {0, 1, 20, 255, 256, 257, 320, 5000}) {
+                                const int taken = shares_of(tiles, int(c), 256, int(shares));
+                                REQUIRE(taken >= 1 && taken <= shares, "%d of %ld", taken, long(shares));
+                            }
                         } else {
-                            REQUIRE(s.parts >= s.rows + t * size_t(width) * esz && s.hit >= s.parts + t * size_t(ceil_of(vocab, 128)) * 8 && s.all >= s.hit + 4 * t, "%ld",
-                                    long(tokens));
+                            REQUIRE(s.parts >= s.rows + t * row && s.hit >= s.parts + t * size_t(parts) * 8 && s.all >= s.hit + 4 * t, "%ld", long(tokens));
                         }
+                        // offsets of the loads of a tile stay below 2^31: up to sixteen panels
+                        REQUIRE(tokens * 64 * 16 < (int64_t(1) << 31), "%ld", long(tokens));
                         for (size_t at : {s.count, s.index, s.place, s.coef, s.rows, s.parts, s.hit, s.piece, s.dh}) REQUIRE(at % 256 == 0, "%ld", long(tokens));
                     }
                 }
-            }
 }
 
 int main() {
