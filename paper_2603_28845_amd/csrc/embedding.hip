@@ -32,13 +32,23 @@ __device__ __forceinline__ void store_some(T* p, const float (&x)[N], int n) {
 }
 template <class T, int N>
 __device__ __forceinline__ void load_any(float (&x)[N], const T* p, int n) {
-    if (n >= N) load_vector(x, p);
-    else load_some(x, p, n);
+    constexpr int V = 16 / int(sizeof(T));
+    if (n >= N) {
+#pragma unroll
+        for (int i = 0; i < N / V; ++i) load_vector(reinterpret_cast<float (&)[V]>(x[i * V]), p + i * V);
+    } else {
+        load_some(x, p, n);
+    }
 }
 template <class T, int N>
 __device__ __forceinline__ void store_any(T* p, const float (&x)[N], int n) {
-    if (n >= N) store_vector(p, x);
-    else store_some(p, x, n);
+    constexpr int V = 16 / int(sizeof(T));
+    if (n >= N) {
+#pragma unroll
+        for (int i = 0; i < N / V; ++i) store_vector(p + i * V, reinterpret_cast<const float (&)[V]>(x[i * V]));
+    } else {
+        store_some(p, x, n);
+    }
 }
 
 struct Lookup {
@@ -76,6 +86,7 @@ struct Sort {
     int vocab, rows;                         // rows of the vocabulary per workgroup
     int32_t *order, *starts;
 };
+constexpr int HELD = 16;
 __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
     extern __shared__ int32_t at[];          // [wave][row]
     __shared__ int32_t s_wave[SORT_WAVES], s_below;
@@ -88,12 +99,19 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
     __syncthreads();
     int32_t* const mine = at + wave * P.rows;
     int below = 0;
-#pragma unroll 4
-    for (int64_t t = begin + lane; t < end; t += 64) {
-        const int token = P.tokens[t], row = token - lo;
+    auto count = [&](int token) __attribute__((always_inline)) {
+        const int row = token - lo;
         below += token >= 0 && row < 0;
-        if (row >= 0 && row < rows) atomicAdd(&mine[row], 1);      // whole numbers: any order
-    }
+        if (token >= 0 && row >= 0 && row < rows) atomicAdd(&mine[row], 1);   // whole numbers: any order
+    };
+    // the wave's first tokens stay in registers for the second pass (all of them up to 16384)
+    int held[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) held[h] = begin + h * 64 + lane < end ? P.tokens[begin + h * 64 + lane] : -1;
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) count(held[h]);
+#pragma unroll 8
+    for (int64_t t = begin + HELD * 64 + lane; t < end; t += 64) count(P.tokens[t]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
     if (lane == 0 && below) atomicAdd(&s_below, below);
@@ -123,9 +141,8 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
         }
     }
     __syncthreads();
-    for (int64_t t0 = begin; t0 < end; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const int row = t < end ? P.tokens[t] - lo : -1;
+    auto put = [&](int token, int64_t t) __attribute__((always_inline)) {
+        const int row = token < 0 ? -1 : token - lo;
         unsigned long long left = __ballot(row >= 0 && row < rows);
         while (left) {                                             // one token of the 64 after the other, all its places at a time
             const int same_row = __builtin_amdgcn_readlane(row, __ffsll(left) - 1);
@@ -136,6 +153,15 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
             __builtin_amdgcn_wave_barrier();
             left &= ~same;
         }
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) put(held[h], begin + h * 64 + lane);
+    for (int64_t t0 = begin + HELD * 64; t0 < end; t0 += 256) {
+        int token[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) token[u] = t0 + u * 64 + lane < end ? P.tokens[t0 + u * 64 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) put(token[u], t0 + u * 64 + lane);
     }
 }
 
@@ -210,10 +236,7 @@ __device__ void add_up(const Sums& P, int64_t unit) {
                 if (end && here) {
                     finish_row<T>(P, __builtin_amdgcn_readlane(token, i), c, n, sum);
                 } else {
-                    float* to = P.parts + (segment * 2 + (here ? 1 : 0)) * P.width + c;
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e < n) to[e] = sum[e];
+                    store_any(P.parts + (segment * 2 + (here ? 1 : 0)) * P.width + c, sum, n);
                 }
             }
             here = false;
@@ -251,11 +274,20 @@ __global__ __launch_bounds__(256) void join_kernel(Sums P) {
     float sum[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = 0.f;
-    for (int64_t s = segment; s * P.segment < end; ++s) {
-        const float* from = P.parts + (s * 2 + (s == segment ? 1 : 0)) * P.width + c;
+    const float* from = P.parts + (segment * 2 + 1) * P.width + c;   // begun here; then the parts begun before, one after the other
+    load_any(sum, from, n);
+    from += P.width;
+    const int64_t more = (end - 1) / P.segment - segment;
+    for (int64_t s = 0; s < more; s += 8) {
+        float x[8][N];
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e < n) sum[e] += from[e];
+        for (int u = 0; u < 8; ++u)
+            if (s + u < more) load_any(x[u], from + (s + u) * 2 * P.width, n);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s + u < more)
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] += x[u][e];
     }
     finish_row<T>(P, token, c, n, sum);
 }
