@@ -211,7 +211,7 @@ onecomp_status dispatch(const Args& P, hipStream_t stream) {
         if (P.tokens <= 32) return wide ? run_few<T, 2, 2>(P, stream) : run_few<T, 1, 2>(P, stream);
         return wide ? run_few<T, 2, 4>(P, stream) : run_few<T, 1, 4>(P, stream);
     }
-    return product::with_shape<128>(choose_tiles(P.tokens, P.d_out), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
+    return product::with_shape<128>(choose_tiles(P.tokens, P.d_out, steps_of(P.inner, 1), false), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
 }
 
 }  // namespace

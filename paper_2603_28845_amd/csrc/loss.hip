@@ -287,8 +287,9 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kerne
 struct GradRows {
     Operand weight, piece;                   // ACROSS, PANELS_ALONG
     const int32_t* count;
-    int columns, full;                       // of this piece; of the largest
-    int most, add;                           // shares that there is room for; whether there is something to add to
+    int columns, add;                        // of this piece; whether there is something to add to
+    unsigned steps, fixed, step;             // of the largest piece: what decides on the shares
+    int most;                                // shares that there is room for
     float* out;                              // [share][token][width]
     int64_t tokens;
     int width;
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(
     const int count = *P.count;
     int tm, tn;
     const int m_tiles = (count + S::TM - 1) / S::TM, n_tiles = (P.width + S::TN - 1) / S::TN;
-    const int shares = __builtin_amdgcn_readfirstlane(shares_of(m_tiles * n_tiles, P.full, 256 * S::PER_CU, P.most)), share = blockIdx.y;
+    const int shares = __builtin_amdgcn_readfirstlane(shares_of(m_tiles * n_tiles, P.steps, P.fixed, P.step, P.most)), share = blockIdx.y;
     if (share >= shares || !product::my_tile(m_tiles, n_tiles, tm, tn)) return;
     const int each = __builtin_amdgcn_readfirstlane((int(unsigned(P.columns + shares - 1) / unsigned(shares)) + 63) & ~63), begin = share * each;
     const int inner = P.columns - begin < each ? P.columns - begin : each;
@@ -353,24 +354,34 @@ struct Finish {
     const float* parts;
     const int32_t *place, *count;
     int64_t tokens;
-    int full, width, tile_m, tile_n, slots, most;            // as grad_rows_kernel had them
+    int width, tile_m, tile_n, most;         // as grad_rows_kernel had them
+    unsigned steps, fixed, step;
     float scale;
     Rows dh;
 };
-// dh of every token from the shares' sums: a wave per token, zeros where it was left out
+// dh of every token from the shares' sums, zeros where it was left out.  A wave per token and `gridDim.y`-th part of its columns.
 template <class T>
 __global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
     const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (t >= P.tokens) return;
     const int at = P.place[t];
     const int tiles = (*P.count + P.tile_m - 1) / P.tile_m * ((P.width + P.tile_n - 1) / P.tile_n);
-    const int shares = shares_of(tiles, P.full, P.slots, P.most);
+    const int shares = shares_of(tiles, P.steps, P.fixed, P.step, P.most);
     T* to = static_cast<T*>(P.dh.p) + t * P.dh.stride;
-#pragma unroll 2
-    for (int c = (threadIdx.x & 63) * 4; c < P.width; c += 256) {
+    for (int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 4; c < P.width; c += gridDim.y * 256) {
         float4v x = {0.f, 0.f, 0.f, 0.f};
-        if (at >= 0)
-            for (int s = 0; s < shares; ++s) x += *reinterpret_cast<const float4v*>(P.parts + (s * P.tokens + at) * P.width + c);
+        if (at >= 0) {
+            const float* const from = P.parts + int64_t(at) * P.width + c;
+            for (int s0 = 0; s0 < shares; s0 += 8) {               // eight on their way, added in their order
+                float4v v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (s0 + u < shares) v[u] = *reinterpret_cast<const float4v*>(from + (s0 + u) * P.tokens * P.width);
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (s0 + u < shares) x += v[u];
+            }
+        }
         const float y[4] = {x[0] * P.scale, x[1] * P.scale, x[2] * P.scale, x[3] * P.scale};
         store_four(to + c, y);
     }
@@ -386,10 +397,10 @@ onecomp_status launch(K kernel, int lds, int threads, int64_t blocks, int64_t sh
     return ONECOMP_OK;
 }
 
-// f(shape) for the tiles that a product of m x n results takes
-template <class F>
-onecomp_status with_tiles(int64_t m, int64_t n, F&& f) {
-    return product::with_shape<64>(choose_tiles(m, n), f);
+// f(shape) for the tiles that a product of m x n results over `inner` values takes
+template <class E, class F>
+onecomp_status with_tiles(int64_t m, int64_t n, int64_t inner, F&& f) {
+    return product::with_shape<64>(choose_tiles(m, n, steps_of(inner, E::ESZ), E::ESZ == 4), f);
 }
 
 template <class E, class S>
@@ -423,7 +434,7 @@ onecomp_status run_few_logits(const Logits& P, hipStream_t stream) {
     return ONECOMP_OK;
 }
 
-int64_t n_parts(int64_t tokens, int64_t vocab) { return ceil_div(vocab, part_columns(tokens, vocab)); }
+int64_t n_parts(int64_t tokens, int64_t width, int64_t vocab, int esz) { return ceil_div(vocab, part_columns(tokens, width, vocab, esz)); }
 
 onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient, hipStream_t stream) {
     char* ws = static_cast<char*>(P.workspace);
@@ -460,7 +471,7 @@ onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient,
 
 template <class E>
 onecomp_status forward(const Loss& P, hipStream_t stream) {
-    const LossSpace s = loss_space(P.tokens, P.width, P.vocab, E::ESZ, n_parts(P.tokens, P.vocab), false);
+    const LossSpace s = loss_space(P.tokens, P.width, P.vocab, E::ESZ, n_parts(P.tokens, P.width, P.vocab, E::ESZ), false);
     char* ws = static_cast<char*>(P.workspace);
     if (const onecomp_status st = gather(P, s, E::ESZ, false, stream)) return st;
     Logits L{};
@@ -472,11 +483,11 @@ onecomp_status forward(const Loss& P, hipStream_t stream) {
     L.parts = reinterpret_cast<float2*>(ws + s.parts);
     L.hit = reinterpret_cast<float*>(ws + s.hit);
     L.tokens = P.tokens;
-    L.n_parts = n_parts(P.tokens, P.vocab);
+    L.n_parts = n_parts(P.tokens, P.width, P.vocab, E::ESZ);
     L.weight = Operand{static_cast<const char*>(P.weight.p), P.weight.stride * E::ESZ, P.vocab};
     L.columns = int(P.vocab);
     const onecomp_status st = P.tokens <= FEW ? run_few_logits<E>(L, stream)
-                                              : with_tiles(P.tokens, P.vocab, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); });
+                                              : with_tiles<E>(P.tokens, P.vocab, P.width, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); });
     if (st) return st;
     const Join J{L.count, reinterpret_cast<const int32_t*>(ws + s.index), L.parts, L.hit, int(L.n_parts), P.loss, P.lse};
     if (P.tokens <= 1024) join_kernel<256><<<dim3(unsigned(P.tokens)), dim3(256), 0, stream>>>(J);
@@ -492,6 +503,9 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
     if (const onecomp_status st = gather(P, s, E::ESZ, true, stream)) return st;
     const int32_t* count = reinterpret_cast<const int32_t*>(ws + s.count);
     const int64_t panel = P.tokens * 64;     // of what has tokens for rows
+    const Tiles rows_tiles = choose_rows(P.tokens, P.width, s.columns, E::ESZ);
+    const TileShape tile = rows_shape(rows_tiles, E::ESZ == 4);
+    const unsigned rows_steps = unsigned(steps_of(s.columns, E::ESZ));
     for (int64_t first = 0; first < P.vocab; first += s.columns) {
         const int64_t columns = P.vocab - first < s.columns ? P.vocab - first : s.columns;
         const char* const w = static_cast<const char*>(P.weight.p) + first * P.weight.stride * E::ESZ;
@@ -507,7 +521,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
         G.piece = ws + s.piece;
         G.panel = panel;
         if (const onecomp_status st =
-                with_tiles(P.tokens, columns, [&](auto shape) { return run_logit_grads<E, decltype(shape)>(G, P.tokens, stream); }))
+                with_tiles<E>(P.tokens, columns, P.width, [&](auto shape) { return run_logit_grads<E, decltype(shape)>(G, P.tokens, stream); }))
             return st;
         if (P.dh.p) {
             GradRows R{};
@@ -515,14 +529,16 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             R.piece = Operand{ws + s.piece, panel, P.tokens};
             R.count = count;
             R.columns = int(columns);
-            R.full = int(s.columns);
+            R.steps = rows_steps;
+            R.fixed = unsigned(tile.fixed);
+            R.step = unsigned(tile.step);
             R.most = int(s.shares);
             R.add = first > 0;
             R.out = reinterpret_cast<float*>(ws + s.dh);
             R.tokens = P.tokens;
             R.width = int(P.width);
             if (const onecomp_status st =
-                    with_tiles(P.tokens, P.width, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); }))
+                    product::with_shape<64>(rows_tiles, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); }))
                 return st;
         }
         if (P.dweight.p) {
@@ -535,14 +551,14 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             W.scale = P.scale;
             W.out = static_cast<char*>(P.dweight.p) + first * P.dweight.stride * E::ESZ;
             W.stride = P.dweight.stride * E::ESZ;
-            if (const onecomp_status st = with_tiles(columns, P.width, [&](auto shape) { return run_grad_weight<E, decltype(shape)>(W, stream); })) return st;
+            if (const onecomp_status st = with_tiles<E>(columns, P.width, P.tokens, [&](auto shape) { return run_grad_weight<E, decltype(shape)>(W, stream); })) return st;
         }
     }
     if (P.dh.p && P.tokens) {
-        const TileShape tile = shape_of(choose_tiles(P.tokens, P.width));
-        const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(s.columns), int(P.width),
-                       tile.m, tile.n, 256 * tile.per_cu, int(s.shares), P.scale, P.dh};
-        finish_rows_kernel<typename E::T><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(F);
+        const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(P.width), tile.m, tile.n,
+                       int(s.shares), rows_steps, unsigned(tile.fixed), unsigned(tile.step), P.scale, P.dh};
+        const int64_t groups = ceil_div(P.tokens, 4), parts = ceil_div(1024, groups), most = ceil_div(P.width, 256);
+        finish_rows_kernel<typename E::T><<<dim3(unsigned(groups), unsigned(parts < most ? parts : most)), dim3(256), 0, stream>>>(F);
         ONECOMP_CHECK_LAUNCH();
     }
     return ONECOMP_OK;
@@ -551,7 +567,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
 }  // namespace
 
 size_t loss_workspace_bytes(onecomp_dtype dtype, int64_t tokens, int64_t width, int64_t vocab, bool gradient) {
-    return loss_space(tokens, width, vocab, dtype == ONECOMP_BF16 ? 2 : 4, gradient ? 0 : n_parts(tokens, vocab), gradient).all;
+    return loss_space(tokens, width, vocab, dtype == ONECOMP_BF16 ? 2 : 4, gradient ? 0 : n_parts(tokens, width, vocab, dtype == ONECOMP_BF16 ? 2 : 4), gradient).all;
 }
 onecomp_status loss_forward_run(onecomp_dtype dtype, const Loss& P, hipStream_t stream) {
     return dtype == ONECOMP_BF16 ? forward<product::Bf16>(P, stream) : forward<product::F32>(P, stream);

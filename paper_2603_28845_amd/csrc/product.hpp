@@ -348,9 +348,7 @@ auto with_shape(token::Tiles t, F&& f) {
     switch (t) {
         case token::BIG: return f(Shape<2, 2, 4, 4, STEP, 1, 1>{});          // 256 x 256
         case token::MID: return f(Shape<2, 2, 2, 2, STEP, 1, 2>{});          // 128 x 128
-        case token::MID_SPLIT: return f(Shape<2, 2, 2, 2, STEP, 2, 1>{});
         case token::HALF: return f(Shape<2, 2, 2, 1, STEP, 1, 3>{});         // 128 x 64
-        case token::HALF_SPLIT: return f(Shape<2, 2, 2, 1, STEP, 3, 1>{});
         case token::SMALL: return f(Shape<2, 2, 1, 1, STEP, 1, 4>{});        // 64 x 64
         default: return f(Shape<2, 2, 1, 1, STEP, 4, 1>{});
     }

@@ -3,6 +3,7 @@
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
+#include <initializer_list>
 
 #if defined(__HIPCC__)
 #define ONECOMP_TOKEN_FN __host__ __device__ inline
@@ -61,35 +62,49 @@ inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t wid
 // ---- tiles of products ----
 // Up to FEW rows of m are multiplied without tiles.
 constexpr int64_t FEW = 64;
-enum Tiles { BIG, MID, MID_SPLIT, HALF, HALF_SPLIT, SMALL, SMALL_SPLIT };
+enum Tiles { BIG, MID, HALF, SMALL, SMALL_SPLIT };
+// fixed, step: ns that a compute unit takes for a tile's beginning and end and for 64 bytes of k, all units at work (several small
+// tiles overlap, so that they cost less than one alone): logits of 8192 tokens over 32000 entries, widths 64 to 4096, bf16 and
+// fp32.  8-bit layers go by bf16.
 struct TileShape {
-    int n, m, per_cu;
+    int n, m, fixed, step;
 };
-inline TileShape shape_of(Tiles t) {
+inline TileShape shape_of(Tiles t, bool f32) {
     switch (t) {
-        case BIG: return {256, 256, 1};
-        case MID: return {128, 128, 2};
-        case MID_SPLIT: return {128, 128, 1};
-        case HALF: return {128, 64, 3};
-        case HALF_SPLIT: return {128, 64, 1};
-        case SMALL: return {64, 64, 4};
-        default: return {64, 64, 1};
+        case BIG: return {256, 256, 7100, f32 ? 3740 : 770};
+        case MID: return {128, 128, 1600, f32 ? 933 : 255};
+        case HALF: return {128, 64, 800, f32 ? 473 : 185};
+        default: return {64, 64, 500, f32 ? 244 : 125};
     }
 }
-inline int64_t tiles_of(Tiles t, int64_t m, int64_t n) { return ceil_of(m, shape_of(t).m) * ceil_of(n, shape_of(t).n); }
-// The largest tiles that are many enough for the chip.
-inline Tiles choose_tiles(int64_t m, int64_t n) {
-    if (tiles_of(BIG, m, n) >= 192) return BIG;
-    if (tiles_of(MID, m, n) > 256) return MID;
-    if (tiles_of(MID, m, n) > 192) return MID_SPLIT;
-    if (tiles_of(HALF, m, n) > 256) return HALF;
-    if (tiles_of(HALF, m, n) > 192) return HALF_SPLIT;
-    return tiles_of(SMALL, m, n) > 256 ? SMALL : SMALL_SPLIT;
+// what the fullest compute unit takes for `tiles` of a shape
+ONECOMP_TOKEN_FN uint64_t tile_cost(unsigned tiles, unsigned steps, unsigned fixed, unsigned step) {
+    return uint64_t((tiles + 255u) / 256u) * (fixed + uint64_t(steps) * step);
 }
+inline unsigned tiles_of(const TileShape& t, int64_t m, int64_t n) { return unsigned(ceil_of(m, t.m) * ceil_of(n, t.n)); }
+// Tiles for m x n results of `steps` times 64 bytes of k.  us, chosen : largest tiles : smallest: 512 x 8000, k 4096 bf16 46 : 87 : 74; 2048 x
+// 8000 122 : 122 : 244; 128 x 32000, k 1024 fp32 83 : 256 : 83; 512 x 32000, k 64 bf16 18 : 20 : 22.  Where a unit has one small
+// tile of many steps, four groups of waves share these out (512 x 1000, k 4096: 31.6 -> 29.1 bf16, 94 -> 84 fp32).
+inline Tiles choose_tiles(int64_t m, int64_t n, int64_t steps, bool f32) {
+    Tiles best = BIG;
+    uint64_t least = uint64_t(1) << 62;
+    for (Tiles t : {BIG, MID, HALF, SMALL}) {
+        const TileShape s = shape_of(t, f32);
+        const uint64_t cost = tile_cost(tiles_of(s, m, n), unsigned(steps), unsigned(s.fixed), unsigned(s.step));
+        if (cost < least + least / 20) {                          // smaller ones at about the same cost: tokens may be left out
+            best = t;
+            least = cost;
+        }
+    }
+    return best == SMALL && steps >= 64 && tiles_of(shape_of(SMALL, f32), m, n) <= 256 ? SMALL_SPLIT : best;
+}
+inline int64_t steps_of(int64_t inner, int esz) { return ceil_of(inner * esz, 64); }
 
 // ---- loss ----
 // Columns of the vocabulary that leave one maximum and sum per token.
-inline int64_t part_columns(int64_t tokens, int64_t vocab) { return tokens <= FEW ? 32 : shape_of(choose_tiles(tokens, vocab)).n; }
+inline int64_t part_columns(int64_t tokens, int64_t width, int64_t vocab, int esz) {
+    return tokens <= FEW ? 32 : shape_of(choose_tiles(tokens, vocab, steps_of(width, esz), esz == 4), esz == 4).n;
+}
 // Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns: 1 GB of them.
 constexpr int64_t PIECE_BYTES = int64_t(1) << 30;
 inline int64_t piece_columns(int64_t tokens, int64_t vocab, int esz) {
@@ -104,16 +119,40 @@ inline int64_t most_shares(int64_t tokens, int64_t width) {
     const int64_t s = (int64_t(1) << 30) / ((tokens < 1 ? 1 : tokens) * width * 4);
     return s < 1 ? 1 : s > 16 ? 16 : s;
 }
-// How many are taken, from the number of kept tokens: the fewest rounds of the chip's `slots` tiles, by the columns that a
-// workgroup goes through one after the other and 256 for the beginning and end of each tile.
-ONECOMP_TOKEN_FN int shares_of(int tiles, int columns, int slots, int most) {
+// How many are taken, from the number of kept tokens (of whose tiles there are `tiles`): more only where they save a twelfth, since
+// a second small tile for every compute unit is not dealt out evenly (231 x 832 over 76393 fp32: 297 us in 8 shares of
+// 28 tiles, 484 in 16).
+ONECOMP_TOKEN_FN int shares_of(unsigned tiles, unsigned steps, unsigned fixed, unsigned step, int most) {
     int best = 1;
-    uint64_t least = 0;
+    uint64_t least = ~uint64_t(0);
     for (int s = 1; s <= most; ++s) {
-        const unsigned rounds = (unsigned(tiles) * unsigned(s) + unsigned(slots) - 1) / unsigned(slots);
-        const uint64_t cost = uint64_t(rounds) * ((unsigned(columns) + unsigned(s) - 1) / unsigned(s) + 256u);
-        if (s == 1 || cost < least) {
+        const uint64_t cost = tile_cost(tiles * unsigned(s), (steps + unsigned(s) - 1) / unsigned(s), fixed, step);
+        if (s == 1 || cost < least - least / 12) {
             best = s;
+            least = cost;
+        }
+    }
+    return best;
+}
+// The shape of dh's tiles, if all tokens are kept: with the shares that it would take.  Each share's sums go to memory in 32 bits
+// and are read again (by the next piece of the vocabulary, by the kernel that adds the shares up): 13 us for a quarter MB of every
+// compute unit at 5 TB/s, three times.
+inline TileShape rows_shape(Tiles t, bool f32) {
+    TileShape s = shape_of(t, f32);
+    s.fixed += int(int64_t(39000) * s.n * s.m / 65536);
+    return s;
+}
+inline Tiles choose_rows(int64_t tokens, int64_t width, int64_t columns, int esz) {
+    Tiles best = BIG;
+    uint64_t least = ~uint64_t(0);
+    const unsigned steps = unsigned(steps_of(columns, esz));
+    for (Tiles t : {BIG, MID, HALF, SMALL}) {
+        const TileShape s = rows_shape(t, esz == 4);
+        const unsigned tiles = tiles_of(s, tokens, width);
+        const unsigned shares = unsigned(shares_of(tiles, steps, unsigned(s.fixed), unsigned(s.step), int(most_shares(tokens, width))));
+        const uint64_t cost = tile_cost(tiles * shares, (steps + shares - 1) / shares, unsigned(s.fixed), unsigned(s.step));
+        if (cost < least) {
+            best = t;
             least = cost;
         }
     }

@@ -54,7 +54,7 @@ static void check_loss() {
             for (int64_t vocab : {1, 255, 256, 257, 5000, 128000, 1 << 20, 1 << 24})
                 for (int64_t width : {8, 64, 1000, 4096, 8192}) {
                     const size_t t = size_t(tokens), row = size_t(ceil_of(width * esz, 64) * 64);
-                    const int64_t parts = ceil_of(vocab, part_columns(tokens, vocab));
+                    const int64_t parts = ceil_of(vocab, part_columns(tokens, width, vocab, esz));
                     for (bool gradient : {false, true}) {
                         const LossSpace s = loss_space(tokens, width, vocab, esz, parts, gradient);
                         const int64_t c = s.columns, shares = s.shares;
@@ -66,8 +66,9 @@ static void check_loss() {
                             REQUIRE(s.piece >= s.rows + t * row && s.dh >= s.piece + t * size_t(c) * esz, "%ld", long(tokens));
                             REQUIRE(s.all >= s.dh + t * size_t(width) * 4 * size_t(shares), "%ld", long(tokens));
                             REQUIRE(shares >= 1 && shares <= 16, "%ld", long(shares));
-                            for (int tiles : {0, 1, 20, 255, 256, 257, 320, 5000}) {
-                                const int taken = shares_of(tiles, int(c), 256, int(shares));
+                            const TileShape tile = rows_shape(choose_rows(tokens, width, c, esz), esz == 4);
+                            for (unsigned tiles : {0u, 1u, 20u, 255u, 256u, 257u, 320u, 5000u}) {
+                                const int taken = shares_of(tiles, unsigned(steps_of(c, esz)), unsigned(tile.fixed), unsigned(tile.step), int(shares));
                                 REQUIRE(taken >= 1 && taken <= shares, "%d of %ld", taken, long(shares));
                             }
                         } else {
