@@ -179,7 +179,7 @@ __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_tokens_kernel(Arg
     __shared__ Columns c;
     const int64_t n0 = int64_t(blockIdx.x) * 16 * RF;
     load_columns<T>(c, P, n0, 16 * RF, 64 * product::FEW_WAVES);
-    product::multiply_few<Int8, RF, TF, ALONG>(lds, P.q, P.codes, n0, P.inner);
+    product::multiply_few<Int8, RF, TF>(lds, P.q, P.codes, [&](int m) __attribute__((always_inline)) { return m < P.tokens ? m : -1; }, n0, P.inner);
     for (int e = threadIdx.x; e < 256 * RF * TF; e += 64 * product::FEW_WAVES) {
         const int n = e % (16 * RF), m = e / (16 * RF);
         if (n0 + n < P.d_out && m < P.tokens)

@@ -91,7 +91,7 @@ __device__ __forceinline__ void join_two(float2& x, float2 y) {
 struct Logits {
     Operand weight, rows;                    // rows.rows: all tokens' room; what counts is *count
     const int32_t* count;
-    const int32_t* target;
+    const int32_t* target;                   // of the kept tokens; few tokens: of all
     int64_t inner;
     int columns;                             // of the vocabulary
     float c;                                 // scale log2(e)
@@ -164,15 +164,29 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Log
     }
 }
 
-// Few tokens: 32 entries of the vocabulary per workgroup, a half wave per token.
+// Which of up to 64 tokens are kept: every wave finds out by itself.  Returns their number; index, target: of the kept ones.
+__device__ __forceinline__ int kept_of(const int32_t* targets, int tokens, int vocab, int* index, int* target) {
+    const int lane = threadIdx.x & 63, t = lane < tokens ? targets[lane] : -1;
+    const bool kept = uint32_t(t) < uint32_t(vocab);
+    const unsigned long long mask = __ballot(kept);
+    if (kept && threadIdx.x < 64) {
+        const int rank = __popcll(mask & ((1ull << lane) - 1));
+        index[rank] = lane;
+        target[rank] = t;
+    }
+    __syncthreads();
+    return __popcll(mask);
+}
+
+// Few tokens, taken where they lie: 32 entries of the vocabulary per workgroup, a half wave per token.
 template <class E, int TF>
 __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Logits P) {
     __shared__ __align__(16) char lds[product::few_lds<2, TF>()];
-    const int count = *P.count;
+    __shared__ int s_index[64], s_target[64];
+    const int count = kept_of(P.target, int(P.tokens), P.columns, s_index, s_target);
     const int64_t n0 = int64_t(blockIdx.x) * 32;
     if (count == 0) return;
-    P.rows.rows = count;
-    product::multiply_few<E, 2, TF, PANELS_ALONG>(lds, P.weight, P.rows, n0, P.inner);
+    product::multiply_few<E, 2, TF>(lds, P.weight, P.rows, [&](int m) __attribute__((always_inline)) { return m < count ? s_index[m] : -1; }, n0, P.inner);
     const int n = threadIdx.x & 31;
     for (int m = threadIdx.x >> 5; m < count; m += 2 * product::FEW_WAVES) {
         const float x = n0 + n < P.columns ? reinterpret_cast<const float*>(lds)[m * 32 + n] : -__builtin_inff();
@@ -184,25 +198,27 @@ __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Log
         float sum = __builtin_amdgcn_exp2f(fmaf(x, P.c, -from));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (n == 0) P.parts[m * P.n_parts + blockIdx.x] = make_float2(top, sum);
-        if (P.target[m] == n0 + n) P.hit[m] = x * P.c;
+        const int64_t t = s_index[m];
+        if (n == 0) P.parts[t * P.n_parts + blockIdx.x] = make_float2(top, sum);
+        if (s_target[m] == n0 + n) P.hit[t] = x * P.c;
     }
 }
 
 struct Join {
-    const int32_t *count, *index;
+    const int32_t *count, *index;            // FEW_TOKENS: null; parts and hit go by token then
+    const int32_t* targets;
     const float2* parts;
     const float* hit;
-    int n_parts;
+    int n_parts, vocab;
     float *loss, *lse;
 };
 // LANES threads per token: each takes every LANES-th part, then they join in a tree.
-template <int LANES>
+template <int LANES, bool FEW_TOKENS>
 __global__ __launch_bounds__(256) void join_kernel(Join P) {
     __shared__ float2 red[4];
     const int m = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, l = threadIdx.x % LANES;
     float2 x = make_float2(-__builtin_inff(), 0.f);
-    const bool there = m < *P.count;
+    const bool there = FEW_TOKENS ? uint32_t(P.targets[m]) < uint32_t(P.vocab) : m < *P.count;
     if (there) {
         const float2* const from = P.parts + int64_t(m) * P.n_parts;
 #pragma unroll 4
@@ -216,11 +232,11 @@ __global__ __launch_bounds__(256) void join_kernel(Join P) {
         x = red[0];
         for (int w = 1; w < 4; ++w) join_two(x, red[w]);
     }
-    if (!there || l != 0) return;
+    if (l != 0 || (!there && !FEW_TOKENS)) return;
     const float lse2 = x.x + __builtin_amdgcn_logf(x.y);           // of two
-    const int t = P.index[m];
-    if (P.loss) P.loss[t] = (lse2 - P.hit[m]) * LN2;
-    if (P.lse) P.lse[t] = lse2 * LN2;
+    const int t = FEW_TOKENS ? m : P.index[m];
+    if (P.loss) P.loss[t] = there ? (lse2 - P.hit[m]) * LN2 : 0.f;
+    if (P.lse) P.lse[t] = there ? lse2 * LN2 : 0.f;
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------------------
@@ -473,25 +489,32 @@ template <class E>
 onecomp_status forward(const Loss& P, hipStream_t stream) {
     const LossSpace s = loss_space(P.tokens, P.width, P.vocab, E::ESZ, n_parts(P.tokens, P.width, P.vocab, E::ESZ), false);
     char* ws = static_cast<char*>(P.workspace);
-    if (const onecomp_status st = gather(P, s, E::ESZ, false, stream)) return st;
     Logits L{};
-    L.rows = Operand{ws + s.rows, P.tokens * 64, P.tokens};
-    L.count = reinterpret_cast<const int32_t*>(ws + s.count);
-    L.target = reinterpret_cast<const int32_t*>(ws + s.coef);
+    L.weight = Operand{static_cast<const char*>(P.weight.p), P.weight.stride * E::ESZ, P.vocab};
     L.inner = P.width;
+    L.columns = int(P.vocab);
     L.c = P.scale * LOG2E;
     L.parts = reinterpret_cast<float2*>(ws + s.parts);
     L.hit = reinterpret_cast<float*>(ws + s.hit);
     L.tokens = P.tokens;
     L.n_parts = n_parts(P.tokens, P.width, P.vocab, E::ESZ);
-    L.weight = Operand{static_cast<const char*>(P.weight.p), P.weight.stride * E::ESZ, P.vocab};
-    L.columns = int(P.vocab);
-    const onecomp_status st = P.tokens <= FEW ? run_few_logits<E>(L, stream)
-                                              : with_tiles<E>(P.tokens, P.vocab, P.width, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); });
-    if (st) return st;
-    const Join J{L.count, reinterpret_cast<const int32_t*>(ws + s.index), L.parts, L.hit, int(L.n_parts), P.loss, P.lse};
-    if (P.tokens <= 1024) join_kernel<256><<<dim3(unsigned(P.tokens)), dim3(256), 0, stream>>>(J);
-    else join_kernel<64><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(J);
+    Join J{nullptr, nullptr, P.targets, L.parts, L.hit, int(L.n_parts), int(P.vocab), P.loss, P.lse};
+    if (P.tokens <= FEW) {
+        L.rows = Operand{static_cast<const char*>(P.h.p), P.h.stride * E::ESZ, P.tokens};
+        L.target = P.targets;
+        if (const onecomp_status st = run_few_logits<E>(L, stream)) return st;
+        join_kernel<256, true><<<dim3(unsigned(P.tokens)), dim3(256), 0, stream>>>(J);
+        ONECOMP_CHECK_LAUNCH();
+        return ONECOMP_OK;
+    }
+    if (const onecomp_status st = gather(P, s, E::ESZ, false, stream)) return st;
+    L.rows = Operand{ws + s.rows, P.tokens * 64, P.tokens};
+    L.count = J.count = reinterpret_cast<const int32_t*>(ws + s.count);
+    L.target = reinterpret_cast<const int32_t*>(ws + s.coef);
+    J.index = reinterpret_cast<const int32_t*>(ws + s.index);
+    if (const onecomp_status st = with_tiles<E>(P.tokens, P.vocab, P.width, [&](auto shape) { return run_logits<E, decltype(shape)>(L, stream); })) return st;
+    if (P.tokens <= 1024) join_kernel<256, false><<<dim3(unsigned(P.tokens)), dim3(256), 0, stream>>>(J);
+    else join_kernel<64, false><<<dim3(unsigned(ceil_div(P.tokens, 4))), dim3(256), 0, stream>>>(J);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }

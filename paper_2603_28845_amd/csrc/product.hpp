@@ -488,9 +488,9 @@ template <int RF, int TF>
 constexpr int few_lds() { return FEW_WAVES * 16 * RF * 16 * TF * 4; }
 
 // sums[n + 16 RF m] in the first 1024 RF TF bytes of lds, behind a barrier
-// (B: ALONG or PANELS_ALONG)
-template <class E, int RF, int TF, Layout LB>
-__device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const Operand& B, int64_t n0, int64_t inner) {
+// row(m): the row of B that is row m of the product, or -1 (B.rows is not looked at)
+template <class E, int RF, int TF, class R>
+__device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const Operand& B, R&& row, int64_t n0, int64_t inner) {
     typedef typename Few<E>::Acc Acc;
     constexpr int AHEAD = RF + TF >= 5 ? 2 : 4;                   // steps on their way at a time
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -504,8 +504,8 @@ __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const 
     }
 #pragma unroll
     for (int j = 0; j < TF; ++j) {
-        const int r = j * 16 + (lane & 15);
-        bt[j] = r < B.rows ? uint32_t(r) * uint32_t(LB == ALONG ? B.stride : 64) + chunk : NOWHERE;
+        const int r = row(j * 16 + (lane & 15));
+        bt[j] = r >= 0 ? uint32_t(r) * uint32_t(B.stride) + chunk : NOWHERE;
     }
     const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(A.data + n0 * A.stride), 0, 0x7FFFFFFF, 0x00020000);
     const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(B.data), 0, 0x7FFFFFFF, 0x00020000);
@@ -529,7 +529,7 @@ __device__ __forceinline__ void multiply_few(char* lds, const Operand& A, const 
             for (int i = 0; i < RF; ++i) x.a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(ra, there && at[i] != NOWHERE ? at[i] + k : NOWHERE, 0, 0);
 #pragma unroll
             for (int j = 0; j < TF; ++j)
-                x.b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, there && bt[j] != NOWHERE ? bt[j] + uint32_t(LB == ALONG ? k : (s0 + u) * int(B.stride)) : NOWHERE, 0, 0);
+                x.b[u][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, there && bt[j] != NOWHERE ? bt[j] + k : NOWHERE, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
