@@ -205,11 +205,10 @@ onecomp_status run_few(const Args& P, hipStream_t stream) {
 }
 template <class T>
 onecomp_status dispatch(const Args& P, hipStream_t stream) {
-    if (P.tokens <= FEW) {
-        const bool wide = P.d_out > 8192;
-        if (P.tokens <= 16) return wide ? run_few<T, 2, 1>(P, stream) : run_few<T, 1, 1>(P, stream);
-        if (P.tokens <= 32) return wide ? run_few<T, 2, 2>(P, stream) : run_few<T, 1, 2>(P, stream);
-        return wide ? run_few<T, 2, 4>(P, stream) : run_few<T, 1, 4>(P, stream);
+    if (few_rows(P.tokens, P.d_out, false)) {
+        // 32 outputs a workgroup where these still fill the chip: the tokens' codes are read half as often
+        if (P.d_out > 8192) return run_few<T, 2, 1>(P, stream);
+        return P.tokens <= 16 ? run_few<T, 1, 1>(P, stream) : P.tokens <= 32 ? run_few<T, 1, 2>(P, stream) : run_few<T, 1, 4>(P, stream);
     }
     return product::with_shape<128>(choose_tiles(P.tokens, P.d_out, steps_of(P.inner, 1), false), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
 }

@@ -499,7 +499,7 @@ onecomp_status forward(const Loss& P, hipStream_t stream) {
     L.tokens = P.tokens;
     L.n_parts = n_parts(P.tokens, P.width, P.vocab, E::ESZ);
     Join J{nullptr, nullptr, P.targets, L.parts, L.hit, int(L.n_parts), int(P.vocab), P.loss, P.lse};
-    if (P.tokens <= FEW) {
+    if (few_rows(P.tokens, P.vocab, E::ESZ == 4)) {
         L.rows = Operand{static_cast<const char*>(P.h.p), P.h.stride * E::ESZ, P.tokens};
         L.target = P.targets;
         if (const onecomp_status st = run_few_logits<E>(L, stream)) return st;

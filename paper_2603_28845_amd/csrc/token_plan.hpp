@@ -60,8 +60,11 @@ inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t wid
 }
 
 // ---- tiles of products ----
-// Up to FEW rows of m are multiplied without tiles.
-constexpr int64_t FEW = 64;
+// Whether m rows are multiplied without tiles, straight from memory: up to 64, and where n alone fills the chip with tiles as long as
+// the rows' own bytes, which every workgroup reads, do not count.  us without tiles : with them: k 4096 bf16, 64 x 4000 31 : 25,
+// 32 x 4000 22 : 23, 16 x 32000 58 : 52, 24 x 32000 77 : 55; fp32 64 x 4000 55 : 77, 32 x 32000 173 : 166; 8 bits 64 x 4096, k 14336 40 : 47,
+// 16 x 14336 19 : 21, 64 x 14336 35 : 23.
+inline bool few_rows(int64_t m, int64_t n, bool f32) { return m <= (n <= 8192 ? 64 : f32 ? 32 : 16); }
 enum Tiles { BIG, MID, HALF, SMALL, SMALL_SPLIT };
 // fixed, step: ns that a compute unit takes for a tile's beginning and end and for 64 bytes of k, all units at work (several small
 // tiles overlap, so that they cost less than one alone): logits of 8192 tokens over 32000 entries, widths 64 to 4096, bf16 and
@@ -103,7 +106,7 @@ inline int64_t steps_of(int64_t inner, int esz) { return ceil_of(inner * esz, 64
 // ---- loss ----
 // Columns of the vocabulary that leave one maximum and sum per token.
 inline int64_t part_columns(int64_t tokens, int64_t width, int64_t vocab, int esz) {
-    return tokens <= FEW ? 32 : shape_of(choose_tiles(tokens, vocab, steps_of(width, esz), esz == 4), esz == 4).n;
+    return few_rows(tokens, vocab, esz == 4) ? 32 : shape_of(choose_tiles(tokens, vocab, steps_of(width, esz), esz == 4), esz == 4).n;
 }
 // Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns: 1 GB of them.
 constexpr int64_t PIECE_BYTES = int64_t(1) << 30;
