@@ -10,8 +10,8 @@
 // the first, lanes 32 .. 63 the second 16 bytes of 32 (8 bf16, 16 int8, 4 fp32 values).  Tiles reach LDS by direct loads through a
 // ring of four or two steps; the fragments of 32 bytes are read while those before are multiplied, reads and loads one by one
 // behind the matrix instructions.
-//   ALONG   a row's bytes of a step are chunks of 16, permuted per row (Side::turn) so that eight rows' same chunk fall into
-//           different banks.
+//   ALONG   a row's bytes of a step are chunks of 16, permuted per row (Side::turn) so that rows' same chunk fall into different
+//           banks.
 //   ACROSS  rows of k as they are; in bf16 their chunks lie permuted by fours (Side::swizzle) and fragments are transposed
 //           reads; in fp32 a fragment is four plain reads.
 // What lies behind the operands' ends becomes zeros by the loads' bounds check.
@@ -98,8 +98,10 @@ struct Side {
     static_assert(!across(L) || E::ESZ != 1, "no transposed reads of bytes here");
     static constexpr int ROWB = T * E::ESZ, CHUNKS = ROWB / 16;   // ACROSS: a row of k
     static constexpr int PER_PANEL = E::ESZ == 2 ? 2 : 1;         // PANELS_ACROSS: loads of a step's rows of one panel
-    // along k: where the chunks of row r of the tile go
-    static __device__ __forceinline__ int turn(int r) { return STEP == 64 ? (r >> 1) & 3 : r & 7; }
+    // along k: chunk c of row r of the tile lies at c ^ turn(r).  LDS serves 16 lanes together, 16 rows of one chunk: with 64 bytes a row
+    // they lie in different banks, with 128 two and two share theirs (a turn that repeats after eight rows, those of one load;
+    // without these conflicts the 8-bit products take as long: 501 and 503 us for 8192 x 4096 x 14336).
+    static __device__ __forceinline__ int turn(int r) { return STEP == 64 ? (r >> 2) & 3 : r & 7; }
     // ACROSS, bf16: which group of four chunks goes where in row r of k; the same for r + 4.  Four rows of a read lie 64 bytes
     // apart in the banks (rows of 128 bytes: two and two).
     static __device__ __forceinline__ int swizzle(int r) { return CHUNKS >= 16 ? r & 3 : (r >> 1) & 1; }
