@@ -611,7 +611,7 @@ ONECOMP_API onecomp_status onecomp_embedding_forward(const int32_t* tokens, int6
 
 ONECOMP_API size_t onecomp_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width) {
     if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24)) return 0;
-    return token::embedding_space(n, vocab, width).all;
+    return token::embedding_workspace_bytes(n, vocab, width);
 }
 
 ONECOMP_API onecomp_status onecomp_embedding_backward(const int32_t* tokens, int64_t n, onecomp_dtype dtype, const onecomp_rows* d_out, int64_t vocab,
@@ -624,7 +624,7 @@ ONECOMP_API onecomp_status onecomp_embedding_backward(const int32_t* tokens, int
     if ((n > 0 && !tokens) || !aligned(tokens, 4) || !check_plain(d_out, dtype, n, width) || !check_plain(d_table, dtype, vocab, width) ||
         (base && !check_plain(base, dtype, vocab, width)))
         return ONECOMP_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < token::embedding_space(n, vocab, width).all) return ONECOMP_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < token::embedding_workspace_bytes(n, vocab, width)) return ONECOMP_ERR_WORKSPACE;
     if (n > 0 && d_table->data == d_out->data) return ONECOMP_ERR_INVALID_ARG;
     if (base && base->data == d_table->data && base->row_stride != d_table->row_stride && vocab > 1) return ONECOMP_ERR_INVALID_ARG;
     return token::embedding_backward_run(dtype, tokens, n, rows_of(d_out), vocab, width, scale, rows_of(base), rows_of(d_table), workspace,

@@ -27,6 +27,7 @@ onecomp_status linear_run(onecomp_dtype dtype, const Linear& P, hipStream_t stre
 
 onecomp_status embedding_forward_run(onecomp_dtype dtype, const int32_t* tokens, int64_t n, const Rows& table, int64_t vocab, int64_t width, float scale,
                                      const Rows& out, hipStream_t stream);
+size_t embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width);
 // base: p == nullptr: none
 onecomp_status embedding_backward_run(onecomp_dtype dtype, const int32_t* tokens, int64_t n, const Rows& d_out, int64_t vocab, int64_t width, float scale,
                                       const Rows& base, const Rows& d_table, void* workspace, hipStream_t stream);

@@ -40,7 +40,7 @@ static void check_embedding() {
         for (int64_t n : {0, 1, 15, 16, 17, 16383, 16384, 100000, 1 << 30})
             for (int64_t width : {1, 64, 4097}) {
                 const EmbeddingSpace s = embedding_space(n, vocab, width);
-                REQUIRE(s.segments * segment_of(n) >= n && (s.segments - 1) * segment_of(n) < n, "%ld", long(n));
+                REQUIRE(s.segments * segment_of(n, width) >= n && (s.segments - 1) * segment_of(n, width) < n, "%ld", long(n));
                 REQUIRE(s.starts >= s.order + size_t(n) * 4 && s.parts >= s.starts + (size_t(vocab) + 1) * 4 && s.all >= s.parts + size_t(s.segments) * 2 * size_t(width) * 4,
                         "%ld %ld %ld", long(n), long(vocab), long(width));
                 REQUIRE(s.order % 256 == 0 && s.starts % 256 == 0 && s.parts % 256 == 0, "%ld", long(n));
