@@ -563,7 +563,9 @@ size_t onecomp_clip_workspace_bytes(void);
 /* ---- From tokens to the loss --------------------------------------------------------------------------------------
  * What a quantized model needs besides its blocks to be scored (perplexity), run and tuned: the embedding in front of them,
  * linear layers on the codes of onecomp_quantize_layer, and the loss over the vocabulary behind them, with gradients.
- * Tokens and targets are int32; one outside 0 .. vocab - 1 (a negative one, say) marks a token that takes no part.
+ * Tokens and targets are int32; one outside 0 .. vocab - 1 (a negative one, say) marks a token that takes no part.  A call takes
+ * less than 2^24 tokens (the loss 2^20 at most), a vocabulary of 2^24 at most, and products of less than 2^24 tiles of 64 x 64 results
+ * (tokens x d_out, tokens x vocab, tokens x width and vocab x width of the loss); more is ONECOMP_ERR_UNSUPPORTED.
  */
 
 /*
@@ -616,7 +618,7 @@ onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scale
 size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
 
 /* The loss of a model's last layer.  h and weight: base addresses and strides of whole 16 bytes, width a multiple of 8 (bf16) or
- * 4 (fp32), row strides below 2^23 bytes; at most 2^20 tokens and a vocabulary of 2^24. */
+ * 4 (fp32), row strides below 2^23 bytes. */
 typedef struct {
     onecomp_dtype dtype;       /* of h, weight and their gradients */
     int64_t tokens, width, vocab;
@@ -626,7 +628,7 @@ typedef struct {
 /*
  * With the logits z_tv = scale h_t . weight_v: lse_t = log sum_v exp(z_tv), loss_t = lse_t - z_t,targets_t (the token's negative log
  * likelihood); both 0 where the target is outside the vocabulary.  Logits are formed in tiles and not kept: the workspace
- * grows with tokens (width + vocab / 16), not tokens x vocab.  bf16 products are exact and added in fp32, fp32 inputs are multiplied
+ * holds tokens x width elements and 8 bytes per token and 64 to 256 entries of the vocabulary (32 for few tokens).  bf16 products are exact and added in fp32, fp32 inputs are multiplied
  * in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.
  *   h          [tokens, width], weight [vocab, width], targets device int32 [tokens]
  *   loss, lse  device fp32 [tokens]; either may be NULL (lse is wanted for onecomp_token_loss_backward)

@@ -181,8 +181,8 @@ onecomp_status check_loss(const onecomp_loss_shape* s) {
     const int64_t most = int64_t(1) << 24;
     if (s->tokens > (int64_t(1) << 20) || s->width > most || s->vocab > most || s->scale < 0x1p-100f || s->scale > 0x1p100f) return ONECOMP_ERR_UNSUPPORTED;
     if (s->width * int64_t(size_of(s->dtype)) % 16 != 0 || s->width * int64_t(size_of(s->dtype)) >= (int64_t(1) << 23)) return ONECOMP_ERR_UNSUPPORTED;
-    // workgroups of a launch: tiles of 128 x 128
-    if (ceil_div(s->tokens, 128) * ceil_div(s->vocab, 128) > (int64_t(1) << 30)) return ONECOMP_ERR_UNSUPPORTED;
+    if (!product::product_fits(s->tokens, s->vocab) || !product::product_fits(s->tokens, s->width) || !product::product_fits(s->vocab, s->width))
+        return ONECOMP_ERR_UNSUPPORTED;
     return ONECOMP_OK;
 }
 bool check_operand(const onecomp_loss_shape* s, const onecomp_rows* r, int64_t rows) {
@@ -601,7 +601,7 @@ ONECOMP_API onecomp_status onecomp_embedding_forward(const int32_t* tokens, int6
                                                      int64_t width, float scale, const onecomp_rows* out, void* hip_stream) {
     const ApiRange range("onecomp_embedding_forward");
     if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
-    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
+    if (n < 0 || n >= (int64_t(1) << 24) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
         return ONECOMP_ERR_INVALID_ARG;
     if ((n > 0 && !tokens) || !aligned(tokens, 4) || !check_plain(table, dtype, vocab, width) || !check_plain(out, dtype, n, width)) return ONECOMP_ERR_INVALID_ARG;
     if (n == 0) return ONECOMP_OK;
@@ -610,7 +610,7 @@ ONECOMP_API onecomp_status onecomp_embedding_forward(const int32_t* tokens, int6
 }
 
 ONECOMP_API size_t onecomp_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t width) {
-    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24)) return 0;
+    if (n < 0 || n >= (int64_t(1) << 24) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24)) return 0;
     return token::embedding_workspace_bytes(n, vocab, width);
 }
 
@@ -619,7 +619,7 @@ ONECOMP_API onecomp_status onecomp_embedding_backward(const int32_t* tokens, int
                                                       void* workspace, size_t workspace_bytes, void* hip_stream) {
     const ApiRange range("onecomp_embedding_backward");
     if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
-    if (n < 0 || n > (int64_t(1) << 30) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
+    if (n < 0 || n >= (int64_t(1) << 24) || vocab <= 0 || vocab > (int64_t(1) << 24) || width <= 0 || width > (int64_t(1) << 24) || !std::isfinite(scale))
         return ONECOMP_ERR_INVALID_ARG;
     if ((n > 0 && !tokens) || !aligned(tokens, 4) || !check_plain(d_out, dtype, n, width) || !check_plain(d_table, dtype, vocab, width) ||
         (base && !check_plain(base, dtype, vocab, width)))
@@ -635,16 +635,17 @@ ONECOMP_API onecomp_status onecomp_quantize_tokens(const onecomp_rows* x, onecom
                                                    int32_t* sums, void* hip_stream) {
     const ApiRange range("onecomp_quantize_tokens");
     if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
-    if (tokens < 0 || tokens > (int64_t(1) << 30) || width <= 0 || !check_plain(x, dtype, tokens, width)) return ONECOMP_ERR_INVALID_ARG;
+    if (tokens < 0 || tokens >= (int64_t(1) << 24) || width <= 0 || !check_plain(x, dtype, tokens, width)) return ONECOMP_ERR_INVALID_ARG;
     if (width % 16 != 0 || width > 65520) return ONECOMP_ERR_UNSUPPORTED;
     if (tokens == 0) return ONECOMP_OK;
-    if (!codes || !scales || !sums || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(sums, 4) || static_cast<const void*>(codes) == x->data)
+    if (!codes || !scales || !sums || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(sums, 4) || static_cast<const void*>(codes) == x->data ||
+        static_cast<const void*>(scales) == static_cast<const void*>(sums))
         return ONECOMP_ERR_INVALID_ARG;
     return token::quantize_tokens_run(dtype, rows_of(x), tokens, width, codes, scales, sums, static_cast<hipStream_t>(hip_stream));
 }
 
 ONECOMP_API size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in) {
-    if (tokens <= 0 || tokens > (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || d_in % 16 != 0 || d_in > 65520) return 0;
+    if (tokens <= 0 || tokens >= (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || d_in % 16 != 0 || d_in > 65520) return 0;
     return token::linear_workspace_bytes(tokens, d_out, d_in);
 }
 
@@ -654,9 +655,9 @@ ONECOMP_API onecomp_status onecomp_linear_int8(const int8_t* codes, const float*
                                                void* hip_stream) {
     const ApiRange range("onecomp_linear_int8");
     if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
-    if (tokens < 0 || tokens > (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || !check_plain(y, dtype, tokens, d_out))
+    if (tokens < 0 || tokens >= (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || !check_plain(y, dtype, tokens, d_out))
         return ONECOMP_ERR_INVALID_ARG;
-    if (d_in % 16 != 0 || d_in > 65520 || ceil_div(tokens, 128) * ceil_div(d_out, 128) > (int64_t(1) << 30)) return ONECOMP_ERR_UNSUPPORTED;
+    if (d_in % 16 != 0 || d_in > 65520 || !product::product_fits(tokens, d_out)) return ONECOMP_ERR_UNSUPPORTED;
     if (!Q_codes || !scales || !zeros || !aligned(Q_codes, 16) || !aligned(scales, 4) || !aligned(zeros, 4) || !aligned(bias, size_of(dtype)))
         return ONECOMP_ERR_INVALID_ARG;
     if (tokens == 0) return ONECOMP_OK;

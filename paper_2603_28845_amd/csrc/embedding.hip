@@ -378,6 +378,7 @@ onecomp_status embedding_backward_run(onecomp_dtype dtype, const int32_t* tokens
     P.in_place = base.p == d_table.p;
     P.units = s.segments * P.strips;
     P.sum_blocks = ceil_div(P.units, 4);
+    if (P.sum_blocks + ceil_div(vocab, 4) >= int64_t(1) << 24) return ONECOMP_ERR_UNSUPPORTED;   // a launch has less than 2^32 threads
     P.scale = scale;
     P.parts = reinterpret_cast<float*>(ws + s.parts);
     return dtype == ONECOMP_BF16 ? backward<uint16_t>(P, S, stream) : backward<float>(P, S, stream);

@@ -26,6 +26,8 @@ ONECOMP_TOKEN_FN bool tile_of(unsigned block, int m_tiles, int n_tiles, int& tm,
     tm = int(band * BAND + rest % high);
     return true;
 }
+// A launch has less than 2^32 threads along x: tiles of 64 x 64 with 256 threads, the smallest, have room for m x n results.
+inline bool product_fits(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + 63) / 64) < int64_t(1) << 24; }
 // workgroups that reach every tile
 inline int64_t tile_blocks(int64_t m_tiles, int64_t n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
 

@@ -34,7 +34,7 @@ def test_embedding_forward_refusals(lib):
         return lib.onecomp_embedding_forward(tokens, n, dtype, rows(*table) if table else None, vocab, width, scale, rows(*out) if out else None, None)
 
     assert call(dtype=2) == UNSUPPORTED
-    for bad in ({"tokens": None}, {"tokens": A + 2}, {"n": -1}, {"n": (1 << 30) + 1}, {"table": None}, {"out": None}, {"table": (0, 64)}, {"out": (0, 64)},
+    for bad in ({"tokens": None}, {"tokens": A + 2}, {"n": -1}, {"n": 1 << 24}, {"table": None}, {"out": None}, {"table": (0, 64)}, {"out": (0, 64)},
                 {"vocab": 0}, {"vocab": (1 << 24) + 1}, {"width": 0}, {"table": (B, 63)}, {"out": (C, 63)}, {"table": (B + 1, 64)}, {"out": (C + 1, 64)},
                 {"out": (B, 64)}, {"scale": float("nan")}, {"scale": float("inf")}, {"dtype": 0, "table": (B + 2, 64)}):
         assert call(**bad) == INVALID, bad
@@ -50,6 +50,8 @@ def test_embedding_backward_refusals(lib):
     for bad in ({"tokens": None}, {"n": -1}, {"d_out": None}, {"d_table": None}, {"vocab": 0}, {"width": 0}, {"d_out": (B, 60)}, {"d_table": (C, 60)},
                 {"d_table": (B, 64)}, {"base": (C, 65)}, {"base": (0, 64)}, {"base": (B + 1, 64)}, {"scale": float("nan")}):
         assert call(**bad) == INVALID, bad
+    # more workgroups than a launch has: refused before anything is launched
+    assert call(n=(1 << 24) - 1, width=1 << 23, d_out=(B, 1 << 23), d_table=(C, 1 << 23)) == UNSUPPORTED
     need = lib.onecomp_embedding_workspace_bytes(8, 100, 64)
     for bad in ({"ws": None}, {"ws": D + 16}, {"size": need - 1}):
         assert call(**bad) == WORKSPACE, bad
@@ -62,7 +64,7 @@ def test_quantize_tokens_refusals(lib):
 
     assert call(dtype=3) == UNSUPPORTED and call(width=72, x=(A, 72)) == UNSUPPORTED and call(width=65536, x=(A, 65536)) == UNSUPPORTED
     for bad in ({"x": None}, {"x": (0, 64)}, {"x": (A + 1, 64)}, {"x": (A, 63)}, {"tokens": -1}, {"width": 0}, {"codes": None}, {"codes": B + 8}, {"scales": None},
-                {"scales": C + 2}, {"sums": None}, {"codes": A}):
+                {"scales": C + 2}, {"sums": None}, {"codes": A}, {"tokens": 1 << 24}, {"scales": D}):
         assert call(**bad) == INVALID, bad
     assert call(tokens=0, x=(0, 64), codes=None, scales=None, sums=None) == OK
 
@@ -72,6 +74,7 @@ def test_linear_refusals(lib):
         return lib.onecomp_linear_int8(codes, ts, sums, q, scales, zeros, bias, dtype, tokens, d_out, d_in, rows(*y) if y else None, ws, size, None)
 
     assert call(dtype=9) == UNSUPPORTED and call(d_in=72) == UNSUPPORTED and call(d_in=65536) == UNSUPPORTED
+    assert call(tokens=1 << 20, d_out=1 << 16, y=(D, 1 << 16)) == UNSUPPORTED
     for bad in ({"codes": None}, {"ts": None}, {"sums": None}, {"q": None}, {"scales": None}, {"zeros": None}, {"codes": A + 8}, {"q": C + 8}, {"bias": B + 1},
                 {"tokens": -1}, {"d_out": 0}, {"d_in": 0}, {"y": None}, {"y": (0, 32)}, {"y": (D, 31)}, {"y": (D + 1, 32)}, {"y": (A, 32)}, {"y": (C, 32)}):
         assert call(**bad) == INVALID, bad
@@ -86,7 +89,8 @@ def loss_shape(dtype=1, tokens=10, width=64, vocab=1000, scale=1.0):
 SHAPES = [({"dtype": 4}, UNSUPPORTED), ({"tokens": -1}, INVALID), ({"width": 0}, INVALID), ({"vocab": 0}, INVALID), ({"width": 60}, UNSUPPORTED),
           ({"width": 62, "dtype": 0}, UNSUPPORTED), ({"scale": 0.0}, INVALID), ({"scale": -1.0}, INVALID), ({"scale": float("nan")}, INVALID),
           ({"scale": float("inf")}, INVALID), ({"scale": 2.0 ** 101}, UNSUPPORTED), ({"scale": 2.0 ** -101}, UNSUPPORTED), ({"tokens": (1 << 20) + 1}, UNSUPPORTED),
-          ({"vocab": (1 << 24) + 1}, UNSUPPORTED), ({"width": 1 << 22}, UNSUPPORTED)]
+          ({"vocab": (1 << 24) + 1}, UNSUPPORTED), ({"width": 1 << 22}, UNSUPPORTED),
+          ({"tokens": 1 << 20, "vocab": 1 << 16}, UNSUPPORTED), ({"vocab": 1 << 20, "width": 1 << 16}, UNSUPPORTED)]
 
 
 def test_loss_forward_refusals(lib):
