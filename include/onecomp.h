@@ -610,12 +610,10 @@ onecomp_status onecomp_quantize_tokens(const onecomp_rows* x, onecomp_dtype dtyp
  *   scales, zeros  device fp32 [d_out]; zeros are whole numbers of 0 .. 255
  *   bias      [d_out] of dtype, or NULL
  *   y         [tokens, d_out] of dtype, any address and stride of whole elements
- *   workspace >= onecomp_linear_int8_workspace_bytes(tokens, d_out, d_in), 256-byte aligned (0 bytes: may be NULL)
  */
 onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scales, const int32_t* token_sums, const uint8_t* Q_codes,
                                    const float* scales, const float* zeros, const void* bias, onecomp_dtype dtype, int64_t tokens, int64_t d_out,
-                                   int64_t d_in, const onecomp_rows* y, void* workspace, size_t workspace_bytes, void* hip_stream);
-size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
+                                   int64_t d_in, const onecomp_rows* y, void* hip_stream);
 
 /* The loss of a model's last layer.  h and weight: base addresses and strides of whole 16 bytes, width a multiple of 8 (bf16) or
  * 4 (fp32), row strides below 2^23 bytes. */

@@ -65,7 +65,6 @@ EXPORTED_SYMBOLS = (
     "onecomp_embedding_workspace_bytes",
     "onecomp_quantize_tokens",
     "onecomp_linear_int8",
-    "onecomp_linear_int8_workspace_bytes",
     "onecomp_token_loss_forward",
     "onecomp_token_loss_workspace_bytes",
     "onecomp_token_loss_backward",
@@ -206,10 +205,8 @@ def load_library() -> ctypes.CDLL:
     lib.onecomp_embedding_workspace_bytes.restype = sz
     lib.onecomp_quantize_tokens.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp]
     lib.onecomp_quantize_tokens.restype = i32
-    lib.onecomp_linear_int8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, vp, sz, vp]
+    lib.onecomp_linear_int8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, vp]
     lib.onecomp_linear_int8.restype = i32
-    lib.onecomp_linear_int8_workspace_bytes.argtypes = [i64, i64, i64]
-    lib.onecomp_linear_int8_workspace_bytes.restype = sz
     lib.onecomp_token_loss_forward.argtypes = [vp] * 7 + [sz, vp]
     lib.onecomp_token_loss_forward.restype = i32
     lib.onecomp_token_loss_workspace_bytes.argtypes = [vp]
@@ -941,7 +938,7 @@ def onecomp_quantize_tokens(x: torch.Tensor, codes: Optional[torch.Tensor] = Non
 
 def onecomp_linear_int8(codes: torch.Tensor, token_scales: torch.Tensor, token_sums: torch.Tensor, Q_codes: torch.Tensor, scales: torch.Tensor,
                         zeros: torch.Tensor, bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
-                        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A quantized layer on quantized tokens: [tokens, d_out] of dtype.  codes, token_scales, token_sums: onecomp_quantize_tokens;
     Q_codes [d_out, d_in], scales, zeros: onecomp_quantize_layer with group_size = d_in; bias: [d_out] of dtype."""
     lib = _lib or load_library()
@@ -956,13 +953,11 @@ def onecomp_linear_int8(codes: torch.Tensor, token_scales: torch.Tensor, token_s
     if out is None:
         out = codes.new_empty((tokens, d_out), dtype=dtype)
     struct.pack_into("Pq", _buffer.data, 0, *_plain_rows(out, "out", dtype, device, tokens, d_out))
-    need = lib.onecomp_linear_int8_workspace_bytes(tokens, d_out, d_in)
-    ws, ws_bytes, _keep = _scratch(workspace, need, codes.device)
     rc = lib.onecomp_linear_int8(_vector(codes, "codes", torch.int8, device, tokens * d_in), _vector(token_scales, "token_scales", torch.float32, device, tokens),
                                  _vector(token_sums, "token_sums", torch.int32, device, tokens),
                                  _vector(Q_codes, "Q_codes", torch.uint8, device, d_out * d_in), _vector(scales, "scales", torch.float32, device, d_out),
                                  _vector(zeros, "zeros", torch.float32, device, d_out), _vector(bias, "bias", dtype, device, d_out), code, tokens, d_out, d_in,
-                                 _buffer.at, ws, ws_bytes, _raw_stream())
+                                 _buffer.at, _raw_stream())
     if rc != ONECOMP_OK:
         raise OnecompError(rc, "onecomp_linear_int8")
     return out

@@ -644,15 +644,9 @@ ONECOMP_API onecomp_status onecomp_quantize_tokens(const onecomp_rows* x, onecom
     return token::quantize_tokens_run(dtype, rows_of(x), tokens, width, codes, scales, sums, static_cast<hipStream_t>(hip_stream));
 }
 
-ONECOMP_API size_t onecomp_linear_int8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in) {
-    if (tokens <= 0 || tokens >= (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || d_in % 16 != 0 || d_in > 65520) return 0;
-    return token::linear_workspace_bytes(tokens, d_out, d_in);
-}
-
 ONECOMP_API onecomp_status onecomp_linear_int8(const int8_t* codes, const float* token_scales, const int32_t* token_sums, const uint8_t* Q_codes,
                                                const float* scales, const float* zeros, const void* bias, onecomp_dtype dtype, int64_t tokens,
-                                               int64_t d_out, int64_t d_in, const onecomp_rows* y, void* workspace, size_t workspace_bytes,
-                                               void* hip_stream) {
+                                               int64_t d_out, int64_t d_in, const onecomp_rows* y, void* hip_stream) {
     const ApiRange range("onecomp_linear_int8");
     if (!known(dtype)) return ONECOMP_ERR_UNSUPPORTED;
     if (tokens < 0 || tokens >= (int64_t(1) << 24) || d_out <= 0 || d_out > (int64_t(1) << 24) || d_in <= 0 || !check_plain(y, dtype, tokens, d_out))
@@ -663,9 +657,7 @@ ONECOMP_API onecomp_status onecomp_linear_int8(const int8_t* codes, const float*
     if (tokens == 0) return ONECOMP_OK;
     if (!codes || !token_scales || !token_sums || !aligned(codes, 16) || !aligned(token_scales, 4) || !aligned(token_sums, 4)) return ONECOMP_ERR_INVALID_ARG;
     if (y->data == static_cast<const void*>(codes) || y->data == static_cast<const void*>(Q_codes)) return ONECOMP_ERR_INVALID_ARG;
-    const size_t need = token::linear_workspace_bytes(tokens, d_out, d_in);
-    if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ONECOMP_ERR_WORKSPACE;
-    const token::Linear P{codes, token_scales, token_sums, Q_codes, scales, zeros, bias, rows_of(y), tokens, d_out, d_in, workspace};
+    const token::Linear P{codes, token_scales, token_sums, Q_codes, scales, zeros, bias, rows_of(y), tokens, d_out, d_in};
     return token::linear_run(dtype, P, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -220,8 +220,6 @@ onecomp_status quantize_tokens_run(onecomp_dtype dtype, const Rows& x, int64_t t
     return dtype == ONECOMP_BF16 ? quantize<uint16_t>(x, tokens, width, codes, scales, sums, stream) : quantize<float>(x, tokens, width, codes, scales, sums, stream);
 }
 
-size_t linear_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
-
 onecomp_status linear_run(onecomp_dtype dtype, const Linear& L, hipStream_t stream) {
     Args P{};
     P.q = Operand{reinterpret_cast<const char*>(L.q), L.d_in, L.d_out};

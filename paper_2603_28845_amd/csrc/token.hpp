@@ -20,9 +20,7 @@ struct Linear {
     const void* bias;
     Rows y;
     int64_t tokens, d_out, d_in;
-    void* workspace;
 };
-size_t linear_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
 onecomp_status linear_run(onecomp_dtype dtype, const Linear& P, hipStream_t stream);
 
 onecomp_status embedding_forward_run(onecomp_dtype dtype, const int32_t* tokens, int64_t n, const Rows& table, int64_t vocab, int64_t width, float scale,

@@ -70,8 +70,8 @@ def test_quantize_tokens_refusals(lib):
 
 
 def test_linear_refusals(lib):
-    def call(codes=A, ts=B, sums=B, q=C, scales=B, zeros=B, bias=None, dtype=1, tokens=4, d_out=32, d_in=64, y=(D, 32), ws=D, size=BIG):
-        return lib.onecomp_linear_int8(codes, ts, sums, q, scales, zeros, bias, dtype, tokens, d_out, d_in, rows(*y) if y else None, ws, size, None)
+    def call(codes=A, ts=B, sums=B, q=C, scales=B, zeros=B, bias=None, dtype=1, tokens=4, d_out=32, d_in=64, y=(D, 32)):
+        return lib.onecomp_linear_int8(codes, ts, sums, q, scales, zeros, bias, dtype, tokens, d_out, d_in, rows(*y) if y else None, None)
 
     assert call(dtype=9) == UNSUPPORTED and call(d_in=72) == UNSUPPORTED and call(d_in=65536) == UNSUPPORTED
     assert call(tokens=1 << 20, d_out=1 << 16, y=(D, 1 << 16)) == UNSUPPORTED
@@ -79,7 +79,6 @@ def test_linear_refusals(lib):
                 {"tokens": -1}, {"d_out": 0}, {"d_in": 0}, {"y": None}, {"y": (0, 32)}, {"y": (D, 31)}, {"y": (D + 1, 32)}, {"y": (A, 32)}, {"y": (C, 32)}):
         assert call(**bad) == INVALID, bad
     assert call(tokens=0, codes=None, ts=None, sums=None, y=(0, 32)) == OK
-    assert lib.onecomp_linear_int8_workspace_bytes(0, 32, 64) == 0 and lib.onecomp_linear_int8_workspace_bytes(4, 32, 72) == 0
 
 
 def loss_shape(dtype=1, tokens=10, width=64, vocab=1000, scale=1.0):
