@@ -137,3 +137,15 @@ def test_no_tokens():
     codes = og.onecomp_quantize_tokens(empty)
     q, s, z = _layer(_gen(1), 8, 64)
     assert codes[0].shape == (0, 64) and og.onecomp_linear_int8(*codes, q, s, z).shape == (0, 8)
+
+
+@pytest.mark.parametrize("tokens", [3, 90])
+def test_codes_past_32_bits(tokens):
+    gen = _gen(tokens)
+    d_out, d_in = 66000, 65520                                     # 4.3e9 codes
+    q, s, z = _layer(gen, d_out, d_in)
+    codes = og.onecomp_quantize_tokens(torch.randn(tokens, d_in, generator=gen, device=DEV).to(BF16))
+    y = og.onecomp_linear_int8(*codes, q, s, z, dtype=F32)
+    for part in (slice(0, 300), slice(d_out - 300, d_out)):
+        want, off = linear(codes[0], codes[1], q[part], s[part], z[part], None, F32)
+        assert bool(((y[:, part].double() - want).abs() <= off).all())

@@ -174,3 +174,21 @@ def test_strided_rows_side_stream_and_used_workspace():
     _check("dh", dh_room[:, 8:80], want[0], off[0])
     _check("dweight", dw_room[:, :72], want[1], off[1])
     assert bool((dh_room[:, :8] == 5).all()) and bool((dh_room[:, 80:] == 5).all()) and bool((dw_room[:, 72:] == 5).all())
+
+
+@pytest.mark.parametrize("n,width,vocab", [(20000, 16, 30000), (3, 4104, 530000), (70, 4104, 530000)])
+def test_pieces_and_weights_past_32_bits(n, width, vocab):
+    """Two pieces of logit gradients; weights of 2.2e9 entries, with a target in the last row."""
+    gen = _gen(vocab)
+    h, w, targets = _inputs(gen, n, width, vocab, BF16, 0.1 if n > 100 else 0.0)
+    targets[-1] = vocab - 1
+    ref = Loss(h, w, targets)
+    loss, lse = og.onecomp_token_loss_forward(h, w, targets)
+    want, off = ref.forward()
+    _check("loss", loss, want[0], off[0])
+    _check("lse", lse, want[1], off[1])
+    d_loss = torch.rand(n, generator=gen, device=DEV) / n
+    dh, dw = og.onecomp_token_loss_backward(d_loss, h, w, targets, lse)
+    want, off = ref.backward(d_loss)
+    _check("dh", dh, want[0], off[0])
+    _check("dweight", dw, want[1], off[1])
