@@ -143,7 +143,7 @@ __device__ __forceinline__ float value(int sum, int token_sum, float token_scale
 
 // 8192 x 4096 x 14336: 495 to 550 us, 1.75 to 1.94 POP/s, against 2.06 of a large library product; matrix pipes 45 % busy at 2.02 GHz, L2 hits
 // 78 %.  Its 1792 tiles of 256 x 256 are seven for every compute unit, each only 32 steps of k long, with a beginning and an end that
-// nothing of the same unit covers.
+// nothing of the same unit covers (tiles of 128 x 128, two a unit: 588 us where these take 538, both with the tokens' quantization).
 template <class T, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void linear_kernel(Args P) {
     extern __shared__ __align__(1024) char lds[];
