@@ -40,6 +40,7 @@ struct Gather {
     // gradients: (dloss + dlse, dloss, lse log2(e), target) per kept token
     float4* coef;
     const float *d_loss, *d_lse, *lse;
+    float* unit;                             // bf16: what the logits' gradients are counted in
 };
 
 // Bound by HBM (16384 rows of 4096 bf16: 268 MB read and written in 51 us, 5.3 TB/s).
@@ -47,6 +48,7 @@ struct Gather {
 // L2 for the last of 65536 tokens), numbers its own and copies a part of their rows.
 __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
     __shared__ int s_before[4], s_index[64];
+    __shared__ float s_top[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * 64;
     int n = 0;
 #pragma unroll 4
@@ -81,6 +83,19 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
     __syncthreads();
     product::rows_to_panels([&](int r) __attribute__((always_inline)) { return g.h + s_index[r] * g.h_stride; }, many, g.width_bytes,
                             g.rows + int64_t(before) * 64, g.panel, blockIdx.y * 4 + wave, gridDim.y * 4);
+    if (!g.unit || blockIdx.y != 0 || first + 64 < g.tokens) return;
+    // The last workgroup: the digits of the largest |d_loss| of a kept token, a number from 1 up to 2.
+    float top = 0.f;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < g.tokens; t += 256) {
+        const float d = fabsf(g.d_loss[t]);
+        if (uint32_t(g.targets[t]) < uint32_t(g.vocab) && d < __builtin_inff()) top = fmaxf(top, d);
+    }
+    top = wave_max(top);
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    if (threadIdx.x == 0) *g.unit = top < 0x1p-126f ? 1.f : __uint_as_float((__float_as_uint(top) & 0x007FFFFFu) | 0x3F800000u);
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
@@ -253,6 +268,7 @@ struct LogitGrads {
     float c;
     char* piece;                             // the gradients, tokens as rows, in panels
     int64_t panel;
+    const float* unit;                       // bf16
 };
 
 __device__ __forceinline__ void store_four(uint16_t* p, const float (&x)[4]) {
@@ -270,8 +286,11 @@ __device__ __forceinline__ void store_four(float* p, const float (&x)[4]) {
 }
 
 // The logits again and, in place of their sums, their gradients: rounded to the operands' type, since the two products that follow take
-// them so.  In bf16 that moves dh and dweight by about as much as their own rounding does (error against 64 bits 0.0019 to 0.0028
-// instead of 0.0017 with 32-bit gradients, whose products would cost eight times as much).  4915 kept
+// them so (32-bit gradients' products would cost eight times as much).  In bf16 they are counted in units of the largest weight's
+// digits: where all kept tokens have one weight d, as in a mean, the targets' -d (1 - p), which are most of the gradient, are then off
+// by p or a 512th at most and not all by the same up to 1/256 that d itself is rounded by.  Errors of dh and dweight against
+// 64 bits, where their own rounding alone is 0.00166: one weight 0.00166 to 0.0017 (700 tokens over 4000 entries of 1024 and 8192 over 128000 of
+// 4096; counted in ones 0.00167 to 0.00207, and up to 0.0030 by the weight), weights all different 0.0022. 4915 kept
 // tokens over 64000 entries of 4096: 2.2 ms, 1.16 to 1.18 PFLOP/s, pipes 66 % busy at 1.73 GHz, the stores of a tile between its products
 // and the next tile's.
 template <class E, class S>
@@ -290,6 +309,10 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kerne
     for (int j = 0; j < S::FC; ++j) {
         const int64_t m = m0 + (wc * S::FC + j) * 32 + (lane & 31);
         coef[j] = m < count ? P.coef[m] : make_float4(0.f, 0.f, 0.f, 0.f);
+        if constexpr (E::ESZ == 2) {
+            coef[j].x /= *P.unit;
+            coef[j].y /= *P.unit;
+        }
     }
     __syncthreads();
     product::store_tile<typename E::T, S, false>(
@@ -355,6 +378,7 @@ struct GradWeight {
     float scale;
     char* out;                               // the piece's first row of the gradient
     int64_t stride;
+    const float* unit;                       // bf16
 };
 // dweight of a piece's rows, over the kept tokens.  64000 x 4096 over 4915 bf16: 1.95 to 1.98 ms, 1.3 PFLOP/s, pipes 72 % busy at 1.68 GHz;
 // fp32 32003 x 500 over 901: 253 to 264 us, 114 TFLOP/s.
@@ -366,12 +390,13 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_weight_kerne
     const int64_t n0 = int64_t(tn) * S::TN, m0 = int64_t(tm) * S::TM;
     float16v acc[S::FR][S::FC];
     if (!product::multiply<E, PANELS_ACROSS, PANELS_ACROSS, S>(lds, P.rows, P.piece, n0, m0, *P.count, acc)) return;
+    const float scale = E::ESZ == 2 ? P.scale * *P.unit : P.scale;
     __syncthreads();
     product::store_tile<typename E::T, S, false>(
         lds,
         [&](float (&x)[4], int i, int j, int q, int, int) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e] * P.scale;
+            for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * q + e] * scale;
         },
         [&](int m) __attribute__((always_inline)) {
             return m0 + m < P.columns ? reinterpret_cast<typename E::T*>(P.out + (m0 + m) * P.stride) + n0 : nullptr;
@@ -387,6 +412,7 @@ struct Finish {
     unsigned steps, fixed, step;
     float scale;
     Rows dh;
+    const float* unit;                       // bf16
 };
 // dh of every token from the shares' sums, zeros where it was left out.  Bound by HBM (8192 x 4096, three fifths kept: 68 us).  A wave per token and `gridDim.y`-th part of its columns.
 template <class T>
@@ -396,6 +422,7 @@ __global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
     const int at = P.place[t];
     const int tiles = (*P.count + P.tile_m - 1) / P.tile_m * ((P.width + P.tile_n - 1) / P.tile_n);
     const int shares = shares_of(tiles, P.steps, P.fixed, P.step, P.most);
+    const float scale = sizeof(T) == 2 ? P.scale * *P.unit : P.scale;
     T* to = static_cast<T*>(P.dh.p) + t * P.dh.stride;
     for (int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 4; c < P.width; c += gridDim.y * 256) {
         float4v x = {0.f, 0.f, 0.f, 0.f};
@@ -411,7 +438,7 @@ __global__ __launch_bounds__(256) void finish_rows_kernel(Finish P) {
                     if (s0 + u < shares) x += v[u];
             }
         }
-        const float y[4] = {x[0] * P.scale, x[1] * P.scale, x[2] * P.scale, x[3] * P.scale};
+        const float y[4] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
         store_four(to + c, y);
     }
 }
@@ -484,6 +511,7 @@ onecomp_status gather(const Loss& P, const LossSpace& s, int esz, bool gradient,
         g.d_loss = P.d_loss;
         g.d_lse = P.d_lse;
         g.lse = P.lse;
+        if (esz == 2) g.unit = reinterpret_cast<float*>(ws + s.unit);
     } else {
         g.target = reinterpret_cast<int32_t*>(ws + s.coef);
         g.loss = P.loss;
@@ -538,6 +566,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
     char* ws = static_cast<char*>(P.workspace);
     if (const onecomp_status st = gather(P, s, E::ESZ, true, stream)) return st;
     const int32_t* count = reinterpret_cast<const int32_t*>(ws + s.count);
+    const float* unit = reinterpret_cast<const float*>(ws + s.unit);
     const int64_t panel = P.tokens * 64;     // of what has tokens for rows
     const Tiles rows_tiles = choose_rows(P.tokens, P.width, s.columns, E::ESZ);
     const TileShape tile = rows_shape(rows_tiles, E::ESZ == 4);
@@ -556,6 +585,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
         G.c = P.scale * LOG2E;
         G.piece = ws + s.piece;
         G.panel = panel;
+        G.unit = unit;
         if (const onecomp_status st =
                 with_tiles<E>(P.tokens, columns, P.width, [&](auto shape) { return run_logit_grads<E, decltype(shape)>(G, P.tokens, stream); }))
             return st;
@@ -585,6 +615,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             W.columns = int(columns);
             W.width = int(P.width);
             W.scale = P.scale;
+            W.unit = unit;
             W.out = static_cast<char*>(P.dweight.p) + first * P.dweight.stride * E::ESZ;
             W.stride = P.dweight.stride * E::ESZ;
             if (const onecomp_status st = with_tiles<E>(columns, P.width, P.tokens, [&](auto shape) { return run_grad_weight<E, decltype(shape)>(W, stream); })) return st;
@@ -592,7 +623,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
     }
     if (P.dh.p && P.tokens) {
         const Finish F{reinterpret_cast<const float*>(ws + s.dh), reinterpret_cast<const int32_t*>(ws + s.place), count, P.tokens, int(P.width), tile.m, tile.n,
-                       int(s.shares), rows_steps, unsigned(tile.fixed), unsigned(tile.step), P.scale, P.dh};
+                       int(s.shares), rows_steps, unsigned(tile.fixed), unsigned(tile.step), P.scale, P.dh, unit};
         const int64_t groups = ceil_div(P.tokens, 4), parts = ceil_div(1024, groups), most = ceil_div(P.width, 256);
         finish_rows_kernel<typename E::T><<<dim3(unsigned(groups), unsigned(parts < most ? parts : most)), dim3(256), 0, stream>>>(F);
         ONECOMP_CHECK_LAUNCH();

@@ -173,7 +173,7 @@ inline Tiles choose_rows(int64_t tokens, int64_t width, int64_t columns, int esz
 inline int64_t round_up(int64_t x, int64_t to) { return ceil_of(x, to) * to; }
 
 struct LossSpace {
-    size_t index, place, count, coef, rows, parts, hit, piece, dh, all;
+    size_t index, place, count, unit, coef, rows, parts, hit, piece, dh, all;
     int64_t columns, shares;
 };
 // Rows in panels.
@@ -189,6 +189,7 @@ inline LossSpace loss_space(int64_t tokens, int64_t width, int64_t vocab, int es
         return here;
     };
     s.count = take(4);
+    s.unit = take(gradient ? 4 : 0);
     s.index = take(t * 4);
     s.place = take(gradient ? t * 4 : 0);
     s.coef = take(t * (gradient ? 16 : 4));
