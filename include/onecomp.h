@@ -627,7 +627,8 @@ typedef struct {
  * With the logits z_tv = scale h_t . weight_v: lse_t = log sum_v exp(z_tv), loss_t = lse_t - z_t,targets_t (the token's negative log
  * likelihood); both 0 where the target is outside the vocabulary.  Logits are formed in tiles and not kept: the workspace
  * holds tokens x width elements and 8 bytes per token and 64 to 256 entries of the vocabulary (32 for few tokens).  bf16 products are exact and added in fp32, fp32 inputs are multiplied
- * in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.
+ * in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.  With a
+ * logit of +inf (and no NaN) lse is +inf, and the loss too, but NaN where that logit is the target's.
  *   h          [tokens, width], weight [vocab, width], targets device int32 [tokens]
  *   loss, lse  device fp32 [tokens]; either may be NULL (lse is wanted for onecomp_token_loss_backward)
  *   workspace  >= onecomp_token_loss_workspace_bytes(shape), 256-byte aligned

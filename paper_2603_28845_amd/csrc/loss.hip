@@ -99,8 +99,10 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather g) {
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
+// What powers are taken relative to: the maximum; with one that is infinite nothing, so that a logit of +inf gives a sum of +inf.
+__device__ __forceinline__ float base_of(float top) { return fabsf(top) < __builtin_inff() ? top : 0.f; }
 __device__ __forceinline__ void join_two(float2& x, float2 y) {
-    const float top = fmaxf(x.x, y.x), from = top == -__builtin_inff() ? 0.f : top;
+    const float top = fmaxf(x.x, y.x), from = base_of(top);
     x = make_float2(top, x.y * __builtin_amdgcn_exp2f(x.x - from) + y.y * __builtin_amdgcn_exp2f(y.x - from));
 }
 
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Log
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
         top = fmaxf(top, __shfl_xor(top, 32, 64)) * P.c;
-        const float from = top == -__builtin_inff() ? 0.f : top;
+        const float from = base_of(top);
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < S::FR; ++i)
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Log
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
         top *= P.c;
-        const float from = top == -__builtin_inff() ? 0.f : top;
+        const float from = base_of(top);
         float sum = __builtin_amdgcn_exp2f(fmaf(x, P.c, -from));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
@@ -290,7 +292,7 @@ __device__ __forceinline__ void store_four(float* p, const float (&x)[4]) {
 // digits: where all kept tokens have one weight d, as in a mean, the targets' -d (1 - p), which are most of the gradient, are then off
 // by p or a 512th at most and not all by the same up to 1/256 that d itself is rounded by.  Errors of dh and dweight against
 // 64 bits, where their own rounding alone is 0.00166: one weight 0.00166 to 0.0017 (700 tokens over 4000 entries of 1024 and 8192 over 128000 of
-// 4096; counted in ones 0.00167 to 0.00207, and up to 0.0030 by the weight), weights all different 0.0022. 4915 kept
+// 4096; counted in ones 0.00167 to 0.00207, and a weight of 1.0039 made all results 0.0037 too small), weights all different 0.0022.  4915 kept
 // tokens over 64000 entries of 4096: 2.2 ms, 1.16 to 1.18 PFLOP/s, pipes 66 % busy at 1.73 GHz, the stores of a tile between its products
 // and the next tile's.
 template <class E, class S>
