@@ -138,9 +138,9 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
     int32_t* const mine = at + wave * P.rows;
     int below = 0;
     auto count = [&](int token) __attribute__((always_inline)) {
-        const int row = token - lo;
-        below += token >= 0 && row < 0;
-        if (token >= 0 && row >= 0 && row < rows) atomicAdd(&mine[row], 1);   // whole numbers: any order
+        const int row = row_of(token, lo, rows);
+        below += token >= 0 && token < lo;
+        if (row >= 0) atomicAdd(&mine[row], 1);                    // whole numbers: any order
     };
     // the wave's first tokens stay in registers for the second pass (all of them up to 16384)
     int held[HELD];
@@ -180,8 +180,8 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
     }
     __syncthreads();
     auto put = [&](int token, int64_t t) __attribute__((always_inline)) {
-        const int row = token < 0 ? -1 : token - lo;
-        unsigned long long left = __ballot(row >= 0 && row < rows);
+        const int row = row_of(token, lo, rows);
+        unsigned long long left = __ballot(row >= 0);
         while (left) {                                             // one token of the 64 after the other, all its places at a time
             const int same_row = __builtin_amdgcn_readlane(row, __ffsll(left) - 1);
             const unsigned long long same = __ballot(row == same_row);

@@ -44,6 +44,8 @@ inline int sort_rows(int64_t vocab) {
     const int64_t r = ceil_of(ceil_of(vocab, 256), 64) * 64;
     return int(r > SORT_MOST ? SORT_MOST : r);
 }
+// A token's row among the `rows` from lo on, or -1, for tokens of any 32 bits.
+ONECOMP_TOKEN_FN int row_of(int32_t token, int lo, int rows) { return token >= lo && token - lo < rows ? token - lo : -1; }
 // Sorted tokens that a wave adds up: more where there is enough to read that fewer waves still fill the chip, since each segment
 // may leave two partial sums to be joined.  us in segments of 16 : 32 : 64, tokens x width: 1392 x 80 17.9 : 23.2 : 34.6;
 // 8000 x 2048 38.7 : 36.1 : 43.9; 25915 x 144 32.3 : 34.6 : 44.2; 23215 x 891 fp32 53.5 : 50.6 : 52.0; 65536 x 512 88.9 : 76.7 : 74.5;
