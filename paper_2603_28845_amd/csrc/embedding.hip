@@ -86,7 +86,6 @@ struct Lookup {
     int width;
     float scale;
 };
-// A wave per token.
 // A wave per token, four loads on their way a lane.  Bound by HBM: 65536 tokens of 4096 bf16, drawn log-uniformly, 157 us, of which 537 MB
 // are written; repeated rows come out of the caches (174 MB are fetched).  8 tokens: 3.5 us, a launch's latency.
 template <class T>
@@ -188,6 +187,7 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void sort_kernel(Sort P) {
             const int from = mine[same_row];
             if (row == same_row) P.order[from + __popcll(same & ((1ull << lane) - 1))] = int32_t(t);
             if (lane == 0) mine[same_row] = from + __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the other lanes read it in a later turn
             __builtin_amdgcn_wave_barrier();
             left &= ~same;
         }
