@@ -211,7 +211,7 @@ onecomp_status run_few(const Args& P, hipStream_t stream) {
 }
 template <class T>
 onecomp_status dispatch(const Args& P, hipStream_t stream) {
-    if (few_rows(P.tokens, P.d_out, false)) {
+    if (few_rows(P.tokens, P.d_out, 1)) {
         // 32 outputs a workgroup where these still fill the chip: the tokens' codes are read half as often
         if (P.d_out > 8192) return run_few<T, 2, 1>(P, stream);
         return P.tokens <= 16 ? run_few<T, 1, 1>(P, stream) : P.tokens <= 32 ? run_few<T, 1, 2>(P, stream) : run_few<T, 1, 4>(P, stream);

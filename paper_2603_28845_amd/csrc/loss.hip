@@ -199,7 +199,7 @@ __device__ __forceinline__ int kept_of(const int32_t* targets, int tokens, int v
 }
 
 // Few tokens, taken where they lie: 32 entries of the vocabulary per workgroup, a half wave per token.  Bound by reading the weight
-// once: 16 tokens over 128000 entries of 4096 bf16 230 us, 4.6 TB/s.
+// once: 16 tokens over 64000 entries of 4096 bf16 114 us, 4.6 TB/s; over 128000 fp32 435 us, 4.8 TB/s.
 template <class E, int TF>
 __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_logits_kernel(Logits P) {
     __shared__ __align__(16) char lds[product::few_lds<2, TF>()];
@@ -486,8 +486,8 @@ template <class E>
 onecomp_status run_few_logits(const Logits& P, hipStream_t stream) {
     const dim3 grid(unsigned(P.n_parts)), threads(64 * product::FEW_WAVES);
     if (P.tokens <= 16) few_logits_kernel<E, 1><<<grid, threads, 0, stream>>>(P);
-    else if (P.tokens <= 32) few_logits_kernel<E, 2><<<grid, threads, 0, stream>>>(P);
-    else few_logits_kernel<E, 4><<<grid, threads, 0, stream>>>(P);
+    else if (E::ESZ == 2 || P.tokens <= 32) few_logits_kernel<E, 2><<<grid, threads, 0, stream>>>(P);
+    else if constexpr (E::ESZ == 4) few_logits_kernel<E, 4><<<grid, threads, 0, stream>>>(P);
     ONECOMP_CHECK_LAUNCH();
     return ONECOMP_OK;
 }
@@ -542,7 +542,7 @@ onecomp_status forward(const Loss& P, hipStream_t stream) {
     L.tokens = P.tokens;
     L.n_parts = n_parts(P.tokens, P.width, P.vocab, E::ESZ);
     Join J{nullptr, nullptr, P.targets, L.parts, L.hit, int(L.n_parts), int(P.vocab), P.loss, P.lse};
-    if (few_rows(P.tokens, P.vocab, E::ESZ == 4)) {
+    if (few_rows(P.tokens, P.vocab, E::ESZ)) {
         L.rows = Operand{static_cast<const char*>(P.h.p), P.h.stride * E::ESZ, P.tokens};
         L.target = P.targets;
         if (const onecomp_status st = run_few_logits<E>(L, stream)) return st;

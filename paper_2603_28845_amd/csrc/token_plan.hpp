@@ -70,11 +70,18 @@ inline EmbeddingSpace embedding_space(int64_t tokens, int64_t vocab, int64_t wid
 }
 
 // ---- tiles of products ----
-// Whether m rows are multiplied without tiles, straight from memory: up to 64, and where n alone fills the chip with tiles as long as
-// the rows' own bytes, which every workgroup reads, do not count.  us without tiles : with them: k 4096 bf16, 64 x 4000 31 : 25,
-// 32 x 4000 22 : 23, 16 x 32000 58 : 52, 24 x 32000 77 : 55; fp32 64 x 4000 55 : 77, 32 x 32000 173 : 166; 8 bits 64 x 4096, k 14336 40 : 47,
-// 16 x 14336 19 : 21, 64 x 14336 35 : 23.
-inline bool few_rows(int64_t m, int64_t n, bool f32) { return m <= (n <= 8192 ? 64 : f32 ? 32 : 16); }
+// Whether m rows are multiplied without tiles, straight from memory: up to 64, the fewer the more n there are, since tiles of enough n
+// fill the chip and read the rows once for 64 to 256 of n instead of 16 or 32.  esz: bytes of an element; 1: the 8-bit layers.
+// us without tiles : with them.  bf16, k 4096: 16 x 4000 19 : 27, 32 x 8000 28 : 33, 48 x 4000 30 : 30, 64 x 1000 30 : 24, 16 x 32000 64 : 71, 24 x 12000
+// 43 : 34, 16 x 64000 114 : 114, 16 x 128000 215 : 186, 1 x 128000 193 : 201; k 512: 48 x 4000 11 : 12, 16 x 64000 28 : 25, 1 x 200000 60 : 48.  fp32,
+// k 4096: 64 x 8000 65 : 79, 48 x 12000 108 : 82, 32 x 12000 81 : 82, 32 x 32000 172 : 152, 16 x 128000 435 : 567; k 512: 32 x 16000 19 : 21, 24 x 64000
+// 59 : 48.  8 bits: 64 x 4096, k 14336 40 : 46, k 4096 12.6 : 12.2; k 4096, 32 x 8192 15.0 : 15.1, 48 x 8192 21 : 16, 16 x 14336 17.2 : 19.4.  The bounds
+// lie where both are about equal; close to them either is faster by up to a tenth, after k.
+inline bool few_rows(int64_t m, int64_t n, int esz) {
+    if (esz == 1) return m <= (n <= 4096 ? 64 : n <= 8192 ? 32 : 16);
+    if (esz == 2) return m <= (n <= 8192 ? 32 : n <= 65536 ? 16 : 0);
+    return m <= (n <= 8192 ? 64 : n <= 16384 ? 32 : 16);
+}
 enum Tiles { BIG, MID, HALF, SMALL, SMALL_SPLIT };
 // fixed, step: ns that a compute unit takes for a tile's beginning and end and for 64 bytes of k, all units at work (several small
 // tiles overlap, so that they cost less than one alone): logits of 8192 tokens over 32000 entries, widths 64 to 4096, bf16 and
@@ -116,7 +123,7 @@ inline int64_t steps_of(int64_t inner, int esz) { return ceil_of(inner * esz, 64
 // ---- loss ----
 // Columns of the vocabulary that leave one maximum and sum per token.
 inline int64_t part_columns(int64_t tokens, int64_t width, int64_t vocab, int esz) {
-    return few_rows(tokens, vocab, esz == 4) ? 32 : shape_of(choose_tiles(tokens, vocab, steps_of(width, esz), esz == 4), esz == 4).n;
+    return few_rows(tokens, vocab, esz) ? 32 : shape_of(choose_tiles(tokens, vocab, steps_of(width, esz), esz == 4), esz == 4).n;
 }
 // Gradients of logits are formed for a piece of the vocabulary at a time, a multiple of 256 columns: 1 GB of them.
 constexpr int64_t PIECE_BYTES = int64_t(1) << 30;
