@@ -216,7 +216,7 @@ onecomp_status dispatch(const Args& P, hipStream_t stream) {
         if (P.d_out > 8192) return run_few<T, 2, 1>(P, stream);
         return P.tokens <= 16 ? run_few<T, 1, 1>(P, stream) : P.tokens <= 32 ? run_few<T, 1, 2>(P, stream) : run_few<T, 1, 4>(P, stream);
     }
-    return product::with_shape<128>(choose_tiles(P.tokens, P.d_out, steps_of(P.inner, 1), false), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
+    return product::with_shape<128, true, true>(choose_tiles(P.tokens, P.d_out, steps_of(P.inner, 1), false), [&](auto shape) { return run<T, decltype(shape)>(P, stream); });
 }
 
 }  // namespace

@@ -458,7 +458,7 @@ onecomp_status launch(K kernel, int lds, int threads, int64_t blocks, int64_t sh
 // f(shape) for the tiles that a product of m x n results over `inner` values takes
 template <class E, class F>
 onecomp_status with_tiles(int64_t m, int64_t n, int64_t inner, F&& f) {
-    return product::with_shape<64>(choose_tiles(m, n, steps_of(inner, E::ESZ), E::ESZ == 4), f);
+    return product::with_shape<64, E::ESZ == 2, true>(choose_tiles(m, n, steps_of(inner, E::ESZ), E::ESZ == 4), f);
 }
 
 template <class E, class S>
@@ -606,7 +606,7 @@ onecomp_status backward(const Loss& P, hipStream_t stream) {
             R.tokens = P.tokens;
             R.width = int(P.width);
             if (const onecomp_status st =
-                    product::with_shape<64>(rows_tiles, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); }))
+                    product::with_shape<64, true, false>(rows_tiles, [&](auto shape) { return run_grad_rows<E, decltype(shape)>(R, stream); }))
                 return st;
         }
         if (P.dweight.p) {

@@ -344,16 +344,18 @@ __device__ __forceinline__ bool multiply(char* lds, const Operand& A, const Oper
     return true;
 }
 
-// f(shape) for a choice of tiles
-template <int STEP, class F>
+// f(shape) for a choice of tiles; LARGE, SPLIT: whether the choice may be of 128 x 128 and more, of waves that share k
+template <int STEP, bool LARGE, bool SPLIT, class F>
 auto with_shape(token::Tiles t, F&& f) {
-    switch (t) {
-        case token::BIG: return f(Shape<2, 2, 4, 4, STEP, 1, 1>{});          // 256 x 256
-        case token::MID: return f(Shape<2, 2, 2, 2, STEP, 1, 2>{});          // 128 x 128
-        case token::HALF: return f(Shape<2, 2, 2, 1, STEP, 1, 3>{});         // 128 x 64
-        case token::SMALL: return f(Shape<2, 2, 1, 1, STEP, 1, 4>{});        // 64 x 64
-        default: return f(Shape<2, 2, 1, 1, STEP, 4, 1>{});
+    if constexpr (LARGE) {
+        if (t == token::BIG) return f(Shape<2, 2, 4, 4, STEP, 1, 1>{});      // 256 x 256
+        if (t == token::MID) return f(Shape<2, 2, 2, 2, STEP, 1, 2>{});      // 128 x 128
     }
+    if constexpr (SPLIT) {
+        if (t == token::SMALL_SPLIT) return f(Shape<2, 2, 1, 1, STEP, 4, 1>{});
+    }
+    return t == token::HALF ? f(Shape<2, 2, 2, 1, STEP, 1, 3>{})             // 128 x 64
+                            : f(Shape<2, 2, 1, 1, STEP, 1, 4>{});            // 64 x 64
 }
 
 // Rows to panels: row r of the result is row(r) of the source (nullptr: nothing is there), row_bytes long (a multiple of 16); what is

@@ -102,16 +102,22 @@ ONECOMP_TOKEN_FN uint64_t tile_cost(unsigned tiles, unsigned steps, unsigned fix
     return uint64_t((tiles + 255u) / 256u) * (fixed + uint64_t(steps) * step);
 }
 inline unsigned tiles_of(const TileShape& t, int64_t m, int64_t n) { return unsigned(ceil_of(m, t.m) * ceil_of(n, t.n)); }
-// Tiles for m x n results of `steps` times 64 bytes of k.  us, chosen : largest tiles : smallest: 512 x 8000, k 4096 bf16 46 : 87 : 74; 2048 x
-// 8000 122 : 122 : 244; 128 x 32000, k 1024 fp32 83 : 256 : 83; 512 x 32000, k 64 bf16 18 : 20 : 22.  Where a unit has one small
-// tile of many steps, four groups of waves share these out (512 x 1000, k 4096: 31.6 -> 29.1 bf16, 94 -> 84 fp32).
+// Tiles for m x n results of `steps` times 64 bytes of k: from the largest on, the next smaller shape as long as its cost is at most a
+// twentieth above that of the last one taken.  us, chosen : largest tiles : smallest: 512 x 8000, k 4096 bf16 46 : 87 : 74; 2048 x 8000 122 : 122 : 244;
+// 128 x 32000, k 1024 fp32 83 : 256 : 83; 512 x 32000, k 64 bf16 18 : 20 : 22.  Chosen : the least cost: logits (within a twentieth of it) 884 x 149623,
+// k 544 fp32 1135 : 1092, 1745 x 8049, k 112 bf16 21.0 : 20.2; the weight's gradient 18946 x 3360 over 5351 bf16 1297 : 1283, 46547 x 5976 over 253 529 : 584;
+// 8-bit layers, whose steps are others than the table's, 8965 x 12250, k 448 124 : 147, 8447 x 955, k 352 15.6 : 18.2, but 542 x 8373, k 2576 34.8 : 28.3.
+// In fp32 128 x 64 is never dearer than the two larger shapes by a twentieth: four tiles of 128 x 128 cost less than one of 256 x 256,
+// two of 128 x 64 less than 1.02 of 128 x 128, for any number of steps.  Where a unit has one small tile of many steps, four groups of
+// waves share these out (512 x 1000, k 4096: 31.6 -> 29.1 bf16, 94 -> 84 fp32).
 inline Tiles choose_tiles(int64_t m, int64_t n, int64_t steps, bool f32) {
     Tiles best = BIG;
     uint64_t least = uint64_t(1) << 62;
     for (Tiles t : {BIG, MID, HALF, SMALL}) {
+        if (f32 && (t == BIG || t == MID)) continue;
         const TileShape s = shape_of(t, f32);
         const uint64_t cost = tile_cost(tiles_of(s, m, n), unsigned(steps), unsigned(s.fixed), unsigned(s.step));
-        if (cost < least + least / 20) {                          // smaller ones at about the same cost: tokens may be left out
+        if (cost < least + least / 20) {
             best = t;
             least = cost;
         }
