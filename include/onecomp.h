@@ -564,8 +564,9 @@ size_t onecomp_clip_workspace_bytes(void);
  * What a quantized model needs besides its blocks to be scored (perplexity), run and tuned: the embedding in front of them,
  * linear layers on the codes of onecomp_quantize_layer, and the loss over the vocabulary behind them, with gradients.
  * Tokens and targets are int32; one outside 0 .. vocab - 1 (a negative one, say) marks a token that takes no part.  A call takes
- * less than 2^24 tokens (the loss 2^20 at most), a vocabulary of 2^24 at most, and products of less than 2^24 tiles of 64 x 64 results
- * (tokens x d_out, tokens x vocab, tokens x width and vocab x width of the loss); more is ONECOMP_ERR_UNSUPPORTED.
+ * less than 2^24 tokens (the loss 2^20 at most) and a vocabulary, width and d_out of 2^24 at most: the loss answers more with
+ * ONECOMP_ERR_UNSUPPORTED, the others with ONECOMP_ERR_INVALID_ARG.  Products have less than 2^24 tiles of 64 x 64 results (tokens x d_out;
+ * tokens x vocab, tokens x width and vocab x width of the loss), a table's gradient as many workgroups; more is ONECOMP_ERR_UNSUPPORTED.
  */
 
 /*
@@ -626,8 +627,8 @@ typedef struct {
 /*
  * With the logits z_tv = scale h_t . weight_v: lse_t = log sum_v exp(z_tv), loss_t = lse_t - z_t,targets_t (the token's negative log
  * likelihood); both 0 where the target is outside the vocabulary.  Logits are formed in tiles and not kept: the workspace
- * holds tokens x width elements and 8 bytes per token and 64 to 256 entries of the vocabulary (32 for few tokens).  bf16 products are exact and added in fp32, fp32 inputs are multiplied
- * in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.  With a
+ * holds tokens x width elements and 8 bytes per token and 64 to 256 entries of the vocabulary (32 for few tokens).  bf16 products are
+ * exact and added in fp32, fp32 inputs are multiplied in fp32.  What is not finite in a token's row reaches that token's results alone; left-out tokens' rows are not used.  With a
  * logit of +inf (and no NaN) lse is +inf, and the loss too, but NaN where that logit is the target's.
  *   h          [tokens, width], weight [vocab, width], targets device int32 [tokens]
  *   loss, lse  device fp32 [tokens]; either may be NULL (lse is wanted for onecomp_token_loss_backward)
@@ -641,8 +642,10 @@ size_t onecomp_token_loss_workspace_bytes(const onecomp_loss_shape* shape);
  * Gradients from those of the losses (d_loss) and of the log-sum-exps (d_lse, NULL if there are none), with lse as the forward call
  * left it:  g_tv = (d_loss_t + d_lse_t) exp(z_tv - lse_t) - d_loss_t [v = targets_t],
  *   dh_t = scale sum_v g_tv weight_v,  dweight_v = scale sum_t g_tv h_t.
- * Left-out tokens have dh 0 and no part in dweight.  The vocabulary is taken in pieces whose g (in dtype, 1 GB at most, or 2048
- * columns) lies in the workspace.  Sums in fp32, no atomics: the same inputs give the same bits.
+ * Left-out tokens have dh 0 and no part in dweight.  The vocabulary is taken in pieces whose g lies in the workspace (in dtype; in bf16
+ * counted in units of the digits of the largest |d_loss| of a kept token).  The workspace holds, whichever gradient is wanted: the tokens'
+ * rows, g of a piece (1 GB at most, or 2048 columns), and sums of dh in fp32, up to 16 times tokens x width (1 GB at most, or one).
+ * Sums in fp32, no atomics: the same inputs give the same bits.
  *   d_loss, d_lse  device fp32 [tokens]
  *   dh, dweight    like h and weight, overwritten, over none of the inputs; either may be NULL
  *   workspace      >= onecomp_token_loss_backward_workspace_bytes(shape), 256-byte aligned
