@@ -141,7 +141,7 @@ __device__ __forceinline__ float value(int sum, int token_sum, float token_scale
     return fmaf(float(sum + zero * token_sum) * token_scale, scale, bias);
 }
 
-// 8192 x 4096 x 14336: 495 to 550 us, 1.75 to 1.94 POP/s, against 2.06 of a large library product; matrix pipes 45 % busy at 2.02 GHz, L2 hits
+// 8192 x 4096 x 14336: 490 to 533 us, 1.80 to 1.96 POP/s, against 2.06 of a large library product; matrix pipes 45 % busy at 2.05 GHz, L2 hits
 // 78 %.  Its 1792 tiles of 256 x 256 are seven for every compute unit, each only 32 steps of k long, with a beginning and an end that
 // nothing of the same unit covers (tiles of 128 x 128, two a unit: 588 us where these take 538, both with the tokens' quantization).
 template <class T, class S>
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void linear_kernel(Arg
         [&](int m) __attribute__((always_inline)) { return m0 + m < P.tokens ? static_cast<T*>(P.y) + (m0 + m) * P.y_stride + n0 : nullptr; }, P.d_out - n0);
 }
 
-// Few tokens: bound by reading the layer's codes once.  16 x 4096 x 14336 15.1 us (59 MB, 3.9 TB/s), 1 x 4096 x 4096 4.8 us (17 MB, in
+// Few tokens: bound by reading the layer's codes once.  16 x 4096 x 14336 14.8 us (59 MB, 4.0 TB/s), 1 x 4096 x 4096 4.7 us (17 MB, in
 // a launch that takes about three by itself).
 template <class T, int RF, int TF>
 __global__ __launch_bounds__(64 * product::FEW_WAVES) void few_tokens_kernel(Args P) {

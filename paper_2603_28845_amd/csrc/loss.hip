@@ -118,8 +118,8 @@ struct Logits {
     int64_t tokens, n_parts;
 };
 
-// 16384 tokens over 128000 entries of 4096 bf16: 12.6 ms, 1.36 PFLOP/s, matrix pipes 76 % busy at 1.60 GHz: bound by power (L2 hits 87 %).  fp32, 901
-// over 32003 of 500: 267 us, 108 TFLOP/s, pipes 71 to 79 % busy at 2.15 GHz.
+// 16384 tokens over 128000 entries of 4096 bf16: 12.4 to 13.2 ms, 1.30 to 1.39 PFLOP/s, matrix pipes 75 % busy at 1.67 GHz: bound by power (L2 hits 87 %).
+// 16 tokens: by reading the weight, 185 us.  fp32, 901 over 32003 of 500: 271 to 283 us, 102 to 107 TFLOP/s, pipes 78 % busy at 2.13 GHz.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logits_kernel(Logits P) {
     extern __shared__ __align__(1024) char lds[];
@@ -293,7 +293,7 @@ __device__ __forceinline__ void store_four(float* p, const float (&x)[4]) {
 // by p or a 512th at most and not all by the same up to 1/256 that d itself is rounded by.  Errors of dh and dweight against
 // 64 bits, where their own rounding alone is 0.00166: one weight 0.00166 to 0.0017 (700 tokens over 4000 entries of 1024 and 8192 over 128000 of
 // 4096; counted in ones 0.00167 to 0.00207, and a weight of 1.0039 made all results 0.0037 too small), weights all different 0.0022.  4915 kept
-// tokens over 64000 entries of 4096: 2.2 ms, 1.16 to 1.18 PFLOP/s, pipes 66 % busy at 1.73 GHz, the stores of a tile between its products
+// tokens over 64000 entries of 4096: 2.2 ms, 1.16 to 1.18 PFLOP/s, pipes 63 % busy at 1.79 GHz, the stores of a tile between its products
 // and the next tile's.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void logit_grads_kernel(LogitGrads P) {
@@ -345,7 +345,7 @@ struct GradRows {
     int width;
 };
 // dh of the kept tokens, a piece of the vocabulary added to those before; few tiles share out the piece's columns (shares_of).  4915 x 4096
-// over 64000 bf16: 2.0 to 2.1 ms, 1.22 to 1.31 PFLOP/s, pipes 68 % busy at 1.76 GHz, L2 hits 72 %; fp32 901 x 500 over 32003: 285 to 299 us.
+// over 64000 bf16: 2.0 to 2.1 ms, 1.22 to 1.31 PFLOP/s, pipes 67 % busy at 1.80 GHz, L2 hits 72 %; fp32 901 x 500 over 32003: 288 to 301 us.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_rows_kernel(GradRows P) {
     extern __shared__ __align__(1024) char lds[];
@@ -382,8 +382,8 @@ struct GradWeight {
     int64_t stride;
     const float* unit;                       // bf16
 };
-// dweight of a piece's rows, over the kept tokens.  64000 x 4096 over 4915 bf16: 1.95 to 1.98 ms, 1.3 PFLOP/s, pipes 72 % busy at 1.68 GHz;
-// fp32 32003 x 500 over 901: 253 to 264 us, 114 TFLOP/s.
+// dweight of a piece's rows, over the kept tokens.  64000 x 4096 over 4915 bf16: 1.92 to 1.98 ms, 1.3 PFLOP/s, pipes 73 % busy at 1.70 GHz;
+// fp32 32003 x 500 over 901: 257 to 265 us, 109 to 112 TFLOP/s.
 template <class E, class S>
 __global__ __launch_bounds__(S::ALL_THREADS, S::PER_SIMD) void grad_weight_kernel(GradWeight P) {
     extern __shared__ __align__(1024) char lds[];

@@ -85,7 +85,8 @@ inline bool few_rows(int64_t m, int64_t n, int esz) {
 enum Tiles { BIG, MID, HALF, SMALL, SMALL_SPLIT };
 // fixed, step: ns that a compute unit takes for a tile's beginning and end and for 64 bytes of k, all units at work (several small
 // tiles overlap, so that they cost less than one alone): logits of 8192 tokens over 32000 entries, widths 64 to 4096, bf16 and
-// fp32.  8-bit layers go by bf16.
+// fp32.  8-bit layers go by bf16, which puts the shapes in about the right order but is no time of theirs: 1999 x 777, k 2000 would
+// take 6.7 us and takes 16.
 struct TileShape {
     int n, m, fixed, step;
 };
